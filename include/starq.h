@@ -74,7 +74,8 @@ enum starq_status {
     STARQ_ERR_ALIGN = -3,    /* pointer not aligned as the call requires       */
     STARQ_ERR_BITS = -4,     /* bit-width other than 4 on the GPU path         */
     STARQ_ERR_CUDA = -5,     /* a CUDA runtime call or launch failed           */
-    STARQ_ERR_TIMEOUT = -6   /* a kernel gave up a bounded wait (see status)   */
+    STARQ_ERR_TIMEOUT = -6,  /* a kernel gave up a bounded wait (see status)   */
+    STARQ_ERR_RANGE = -7     /* a kernel met an index outside its array (see status) */
 };
 
 /* Library version (major * 10000 + minor * 100 + patch). */
@@ -85,9 +86,11 @@ const char* starq_last_error(void);
 
 /*
  * Synchronise `stream`, then read and clear the device status word that the
- * kernels set when a bounded wait inside them runs out. Returns STARQ_OK,
- * STARQ_ERR_TIMEOUT (the kernel returned early; its outputs are undefined)
- * or STARQ_ERR_CUDA.
+ * kernels set when a bounded wait inside them runs out, or when an index that
+ * they read from device memory (a position, a page, a length) lies outside
+ * its array. Returns STARQ_OK, STARQ_ERR_TIMEOUT (the kernel returned early;
+ * its outputs are undefined), STARQ_ERR_RANGE (the access was skipped; the
+ * outputs that depend on it are undefined) or STARQ_ERR_CUDA.
  *
  * Scope: there is ONE status word per device, shared by every stream and
  * host thread that launches this library's kernels on it. The call waits
@@ -746,6 +749,159 @@ int sgat_linear_noalloc(const void* X, int x_dtype, int L, int K, const uint8_t*
 int glue_add_rmsnorm(const void* X, const void* R, int dtype, int L, int K, const float* w, float eps,
                      void* h_out, void* Y, void* stream);
 int glue_rope(void* QK, int dtype, int L, int ld, int heads, const int32_t* pos, double theta, void* stream);
+
+/*
+ * Cached decoding: the operators of a step that computes a few new tokens of
+ * each sequence (one token, a drafted run, or a block of positions under
+ * denoising) against a paged cache of the keys and values before them. Not
+ * part of the paper's method; the quantised stacks recompute every position
+ * in every step, and this is the way to keep a finished prefix.
+ *
+ * Sequences. Row arrays of the new tokens are packed: sequence b owns rows
+ * seq_start[b] .. seq_start[b + 1] - 1 (device int32 [B + 1], from 0, not
+ * decreasing), at most max_new of them; T is the number of rows of the
+ * arrays. page_table [B][table_ld] (device int32) names the page that holds
+ * slots page * i .. page * i + page - 1 of a sequence. Lengths, page numbers
+ * and positions are read on the device: one outside its array is skipped
+ * and reported by starq_check_status as STARQ_ERR_RANGE.
+ * Row strides ld* are in elements.
+ */
+
+/*
+ * The paged 8-bit cache, caller-owned. A block is one page of one key/value
+ * head; a value is scale * (byte - 128), with byte - 128 in [-127, 127].
+ *   K, V              [pages][Hkv][page][D] bytes, 16-byte aligned
+ *   k_scale, v_scale  [pages][Hkv] float32: one scale per block
+ *   page              16, 32, 64 or 128 tokens; D (head size) 64 or 128
+ */
+typedef struct {
+    uint8_t* K;
+    uint8_t* V;
+    float* k_scale;
+    float* v_scale;
+    int pages;
+    int page;
+    int Hkv;
+    int D;
+} starq_kv_cache;
+
+/*
+ * glue_rope_table -- cosines and sines of rotary positions: entry (p, i) of
+ * table [positions][rot / 2][2] is m (cos(p f_i), sin(p f_i)), computed in
+ * float64 and rounded once. f_i = theta^(-2 i / rot), changed for contexts
+ * longer than the trained one by `scaling`:
+ *   STARQ_ROPE_NONE    as it is (factor is ignored)
+ *   STARQ_ROPE_LINEAR  f_i / factor (interpolated positions)
+ *   STARQ_ROPE_NTK     theta replaced by theta factor^(rot / (rot - 2))
+ *   STARQ_ROPE_PARTS   f_i for pairs that turn more than beta_fast times
+ *                      within `original` positions, f_i / factor below
+ *                      beta_slow turns, a linear ramp over i between
+ *                      (usual: beta_fast 32, beta_slow 1)
+ *   mscale  m; 0 = 1, or 0.1 ln(factor) + 1 with STARQ_ROPE_PARTS.
+ * table 16-byte aligned. Shapes: positions >= 0, rot even, 2 <= rot <= 1024;
+ * theta > 1, factor >= 1, with PARTS original > 0 and beta_fast > beta_slow
+ * > 0.
+ *
+ * glue_rope_apply -- the rotation by such a table of the first `heads` heads
+ * (D channels each) of every row of X [L][ldx] into Y [L][ldy], both of
+ * dtype (F16, BF16 or F32): of a head's first rot channels, the pairs
+ * (x_i, x_{i + rot/2}), or (x_2i, x_{2i+1}) with interleaved != 0, become
+ * (a c - b s, b c + a s) with float32 products and one rounding; the other
+ * channels are copied. inverse != 0 negates the sine: the transposed map,
+ * i.e. the gradient with respect to X of a gradient with respect to Y (and
+ * the inverse rotation when m = 1). pos [L] device int32, 0 <= pos <
+ * positions. Y may be X (with ldy = ldx); otherwise they must not overlap.
+ * Shapes: L >= 0, heads >= 1, D >= 1, rot even, 0 <= rot <= D; ldx, ldy >=
+ * heads D. Wide accesses are used when D and rot are multiples of 16 and
+ * rows, X, Y and table are 16-byte aligned.
+ */
+enum starq_rope_scaling { STARQ_ROPE_NONE = 0, STARQ_ROPE_LINEAR = 1, STARQ_ROPE_NTK = 2, STARQ_ROPE_PARTS = 3 };
+int glue_rope_table(float* table, int positions, int rot, double theta, int scaling, double factor, double original,
+                    double beta_fast, double beta_slow, double mscale, void* stream);
+int glue_rope_apply(const void* X, int ldx, int dtype, int L, int heads, int D, int rot, int interleaved, int inverse,
+                    const int32_t* pos, const float* table, int positions, void* Y, int ldy, void* stream);
+
+/*
+ * kv_cache_append -- stores the new tokens' keys (rotated on the way) and
+ * values into the cache, and rotates their queries.
+ *
+ * Row r of sequence b goes to slot past[b] + r - seq_start[b]. past [B]:
+ * the tokens that the sequence keeps; what the cache held behind them is
+ * replaced (a block under denoising is written again in every step with the
+ * same past). In a block that keeps n rows, with top the largest magnitude
+ * of the new rows (float32, rotated keys):
+ *   s' = max(s if n > 0, top / 127, 2^-100)
+ *   kept codes c -> rne(c (s / s')) when s' > s
+ *   new codes    -> clamp(rne(x (1 / s')), -127, 127)
+ * A row that is not finite makes its block's scale NaN and the block's codes
+ * 0; every later read of the block gives NaN until it is begun anew (n = 0).
+ *
+ *   K, V   rows of Hkv D channels (strides ldk, ldv), dtype F16 or BF16.
+ *   Q, Qo  rows of H D channels and their rotation out (Qo may be Q, with
+ *          ldqo = ldq), or both NULL.
+ *   pos [T], table, positions, rot, interleaved: as glue_rope_apply (rot 0:
+ *          no rotation, pos and table may be NULL).
+ * All pointers and row strides 16-byte aligned; rot % 16 == 0. A page that
+ * is written must belong to one sequence of the call.
+ *
+ * kv_cache_read -- rows of the cache as numbers: slot first[b] + r -
+ * out_start[b] of sequence b into row r of K and V (either may be NULL),
+ * [T][ld] of dtype F16, BF16 or F32, r in out_start[b] .. out_start[b + 1]
+ * - 1 (at most max_rows rows a sequence): fl(scale * code), one more
+ * rounding for the 16-bit types.
+ */
+int kv_cache_append(const starq_kv_cache* cache, const void* K, int ldk, const void* V, int ldv, const void* Q,
+                    int ldq, void* Qo, int ldqo, int H, int dtype, int T, const int32_t* seq_start,
+                    const int32_t* past, int B, int max_new, const int32_t* page_table, int table_ld,
+                    const int32_t* pos, const float* table, int positions, int rot, int interleaved, void* stream);
+int kv_cache_read(const starq_kv_cache* cache, const int32_t* page_table, int table_ld, const int32_t* first,
+                  const int32_t* out_start, int B, int max_rows, int T, void* K, void* V, int ld, int dtype,
+                  void* stream);
+
+/*
+ * kv_cache_attention -- attention of the new tokens' queries over the cache:
+ *   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(scale q_i . k_j)
+ * over the slots j < kv_len[b] that row i of sequence b sees:
+ *   causal != 0: j <= kv_len[b] - n + i, n the sequence's new tokens (they
+ *     are its last n slots), i counted from 0; causal = 0: all (a block
+ *     under denoising sees itself in both directions).
+ *   key_mask [B][mask_ld] bytes or NULL: slots with a 0 byte are not seen.
+ * A row that sees no slot gives 0 and a log-sum-exp of -inf. Blocks of
+ * which no row sees a slot may hold anything (scales NaN included).
+ *
+ *   Q    [T][ldq], Out [T][ldo]: H heads of D channels, dtype F16 or BF16;
+ *        query head h reads key/value head h / (H / Hkv). 16-byte aligned
+ *        rows.
+ *   lse  [T][H] float32 out, ln sum_j p_ij, or NULL: joins this result with
+ *        attention over other keys.
+ *   kv_len [B], at most max_len each; mask_ld >= max_len.
+ *   workspace: kv_cache_attention_workspace_size bytes, 256-byte aligned;
+ *        its contents do not matter.
+ * Products on 16-bit tensor cores with float32 sums; the softmax weights
+ * are rounded to fp16 once before they meet the values.
+ */
+size_t kv_cache_attention_workspace_size(int B, int max_new, int H, int Hkv, int D);
+int kv_cache_attention(const void* Q, int ldq, int dtype, int T, const int32_t* seq_start, int B, int max_new, int H,
+                       const starq_kv_cache* cache, const int32_t* page_table, int table_ld, const int32_t* kv_len,
+                       int max_len, int causal, const uint8_t* key_mask, int mask_ld, float scale, void* Out, int ldo,
+                       float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * w4g_linear -- a linear layer of a few rows with 4-bit weights that carry
+ * one scale per group of input channels (weight-only: activations stay
+ * 16-bit):
+ *   Y[i][n] = sum_k X[i][k] scales[n][k / group] q[n][k] (+ bias[n])
+ *   X [L][ldx] F16 or BF16; Wq [N][K/2] packed int4 (low nibble = even k,
+ *     two's complement), 16-byte aligned; scales [N][K / group] float32;
+ *     bias [N] float32 or NULL; Y [L][ldy] F16, BF16 or F32.
+ *   sgat_prepare_weight on the weight seen as [N K / group][group] rows with
+ *   hb = 1 gives exactly these codes and scales.
+ * Float32 accumulation; a group's sum is scaled after it is complete.
+ * Shapes: 0 <= L <= 32, N >= 1, group 32, 64 or 128, K >= group with
+ * K % group == 0; ldx >= K, rows of X 16-byte aligned.
+ */
+int w4g_linear(const void* X, int ldx, int dtype, int L, int K, const uint8_t* Wq, const float* scales, int group,
+               int N, const float* bias, void* Y, int ldy, int y_dtype, void* stream);
 
 #ifdef __cplusplus
 }

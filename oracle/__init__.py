@@ -23,6 +23,10 @@ Every function is a plain, slow restatement of the paper:
   embedding, SwiGLU), standard definitions of the model family, not the
   paper's method.
 
+* ``decode``: the cached-decoding operators (rotary tables, the paged 8-bit
+  key/value cache, attention over it, group-scaled 4-bit linears), standard
+  definitions with the float32 steps that fix the cache's codes.
+
 Floating point: the transform and the quantiser decision run in float32, the
 precision the CUDA kernels take the integer decision in (a quantised code is
 an integer decided by floating point, so both sides decide it in the same
@@ -35,4 +39,4 @@ closed forms, brute force on tiny inputs, hand-worked fixtures in
 "parity unpinned".
 """
 
-from . import attention, glue, sgat, tac  # noqa: F401
+from . import attention, decode, glue, sgat, tac  # noqa: F401

@@ -14,7 +14,7 @@ import torch
 from .build import LIB
 
 F16, BF16, F32 = 0, 1, 2
-OK, ERR_ARG, ERR_SHAPE, ERR_ALIGN, ERR_BITS, ERR_CUDA, ERR_TIMEOUT = 0, -1, -2, -3, -4, -5, -6
+OK, ERR_ARG, ERR_SHAPE, ERR_ALIGN, ERR_BITS, ERR_CUDA, ERR_TIMEOUT, ERR_RANGE = 0, -1, -2, -3, -4, -5, -6, -7
 
 EXPORTED = (
     "starq_version", "starq_last_error", "starq_check_status",
@@ -28,6 +28,8 @@ EXPORTED = (
     "sgat_linear_dense_workspace_size", "sgat_linear_dense", "sgat_linear_noalloc",
     "starq_selftest_wait_timeout", "starq_probe_mma", "attention_pv_tac_gqa", "glue_add_rmsnorm", "glue_rope",
     "w4a4_gemm_mma_sync", "starq_set_gemm_pair_limit", "w4a4_gemm_grouped", "sgat_quantize_act_grouped",
+    "glue_rope_table", "glue_rope_apply", "kv_cache_append", "kv_cache_read",
+    "kv_cache_attention_workspace_size", "kv_cache_attention", "w4g_linear",
 )
 
 
@@ -44,6 +46,13 @@ class StarqTac(ctypes.Structure):
     w4a4_gemm."""
     _fields_ = [("g", ctypes.c_int), ("M", ctypes.c_void_p), ("d", ctypes.c_void_p), ("Mp", ctypes.c_void_p),
                 ("scratch", ctypes.c_void_p)]
+
+
+class StarqKvCache(ctypes.Structure):
+    """starq_kv_cache: the paged 8-bit key/value cache."""
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("pages", ctypes.c_int), ("page", ctypes.c_int),
+                ("Hkv", ctypes.c_int), ("D", ctypes.c_int)]
 
 
 def _tac_struct(M, d, g, Mp, scratch):
@@ -127,6 +136,15 @@ def _load():
                                          vp]
     lib.sgat_linear_noalloc.argtypes = [vp, i, i, i, u8p, f_p, f_p, i, i, i, i, f_p, f_p, i, vp,
                                         u8p, u8p, f_p, f_p, i, i, vp, i, vp]
+    lib.glue_rope_table.argtypes = [f_p, i, i, dbl, i, dbl, dbl, dbl, dbl, dbl, vp]
+    lib.glue_rope_apply.argtypes = [vp, i, i, i, i, i, i, i, i, vp, f_p, i, vp, i, vp]
+    lib.kv_cache_append.argtypes = [vp, vp, i, vp, i, vp, i, vp, i, i, i, i, vp, vp, i, i, vp, i, vp, f_p, i, i, i, vp]
+    lib.kv_cache_read.argtypes = [vp, vp, i, vp, vp, i, i, i, vp, vp, i, i, vp]
+    lib.kv_cache_attention_workspace_size.argtypes = [i, i, i, i, i]
+    lib.kv_cache_attention_workspace_size.restype = ctypes.c_size_t
+    lib.kv_cache_attention.argtypes = [vp, i, i, i, vp, i, i, i, vp, vp, i, vp, i, i, vp, i, ctypes.c_float, vp, i, f_p,
+                                       vp, ctypes.c_size_t, vp]
+    lib.w4g_linear.argtypes = [vp, i, i, i, i, u8p, f_p, i, i, f_p, vp, i, i, vp]
     return lib
 
 
@@ -524,3 +542,198 @@ def sgat_linear_noalloc(X, mask, a_m, a_u, hb, d_sh, d_m, d_u, Wq, s_w, Y, bias=
     _check(lib.sgat_linear_noalloc(_p(X), dtype_code(X), L, K, _p(mask), _p(a_m), _p(a_u), hb, d_sh,
                                    d_m, d_u, _p(tac_M), _p(tac_d), tac_g, _p(tac_Mp), _p(Wq), _p(We), _p(s_w), _p(bias), N,
                                    bits, _p(Y), dtype_code(Y), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# Cached decoding (include/starq.h, "Cached decoding"). These calls run once
+# per layer for a handful of tokens, so the marshalling is kept short.
+# ---------------------------------------------------------------------------
+_CODES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+ROPE_SCALING = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
+
+
+def _rows(t, name):
+    """A matrix with unit column stride: (pointer, row stride)."""
+    if t is None:
+        return None, 0
+    st = t.stride()
+    if len(st) != 2 or (st[1] != 1 and t.shape[1] != 1):
+        raise ValueError(f"starq expects {name} as rows with unit column stride")
+    return t.data_ptr(), st[0]
+
+
+def _ints(name, t, n):
+    """A contiguous int32 vector of n entries."""
+    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"starq expects {name} as {n} contiguous int32 entries")
+    return t.data_ptr()
+
+
+def _f32(name, t, shape):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"starq expects {name} as contiguous float32 {list(shape)}")
+    return t.data_ptr()
+
+
+def _same(dtype, **ts):
+    for name, t in ts.items():
+        if t is not None and t.dtype != dtype:
+            raise ValueError(f"starq expects {name} of type {dtype}")
+
+
+class KVCache:
+    """The paged 8-bit cache: K, V uint8 [pages][Hkv][page][D] (a byte is a
+    code + 128), k_scale, v_scale float32 [pages][Hkv] (one scale per block
+    of a page and a head). Holds the tensors."""
+    __slots__ = ("K", "V", "k_scale", "v_scale", "Hkv", "D", "c")
+
+    def __init__(self, K, V, k_scale, v_scale):
+        pages, Hkv, page, D = K.shape
+        if K.dtype != torch.uint8 or V.dtype != torch.uint8 or V.shape != K.shape:
+            raise ValueError("starq expects the cache's K and V as uint8 of one shape [pages][Hkv][page][D]")
+        _contig(K, V)
+        self.K, self.V, self.k_scale, self.v_scale, self.Hkv, self.D = K, V, k_scale, v_scale, Hkv, D
+        self.c = StarqKvCache(K.data_ptr(), V.data_ptr(), _f32("k_scale", k_scale, (pages, Hkv)),
+                              _f32("v_scale", v_scale, (pages, Hkv)), pages, page, Hkv, D)
+
+    @classmethod
+    def empty(cls, pages, Hkv, page, D, device="cuda"):
+        code = lambda: torch.full((pages, Hkv, page, D), 128, dtype=torch.uint8, device=device)
+        scale = lambda: torch.zeros(pages, Hkv, dtype=torch.float32, device=device)
+        return cls(code(), code(), scale(), scale())
+
+
+def _pages(t, B):
+    if t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != B or not t.is_contiguous():
+        raise ValueError(f"starq expects the page table as contiguous int32 [{B}][pages per sequence]")
+    return t.data_ptr(), t.shape[1]
+
+
+def rope_table(table, theta, scaling="none", factor=1.0, original=0.0, beta_fast=32.0, beta_slow=1.0, mscale=0.0,
+               stream=None):
+    """Fills table [positions][rot / 2][2] (float32) with the cosines and
+    sines of the rotary positions; scaling: "none", "linear", "ntk" or
+    "parts" (see include/starq.h)."""
+    positions, half, two = table.shape
+    assert two == 2
+    _f32("table", table, (positions, half, 2))
+    _check(lib.glue_rope_table(table.data_ptr(), positions, 2 * half, float(theta), ROPE_SCALING[scaling],
+                               float(factor), float(original), float(beta_fast), float(beta_slow), float(mscale),
+                               _stream(stream)))
+
+
+def rope_apply(X, heads, pos, table, Y=None, D=None, interleaved=False, inverse=False, stream=None):
+    """Rotates the first `heads` heads of D channels (default: X's columns
+    over heads) of each row of X by table[pos] into Y (default: in place);
+    inverse: the transposed map (the gradient)."""
+    Y = X if Y is None else Y
+    L = X.shape[0]
+    D = X.shape[1] // heads if D is None else D
+    if X.shape[1] < heads * D or Y.shape[0] != L or Y.shape[1] < heads * D:
+        raise ValueError("starq expects X and Y as rows of at least heads * D channels")
+    _same(X.dtype, Y=Y)
+    x, ldx = _rows(X, "X")
+    y, ldy = _rows(Y, "Y")
+    positions, half, _ = table.shape
+    _check(lib.glue_rope_apply(x, ldx, _CODES[X.dtype], L, heads, D, 2 * half, interleaved, inverse,
+                               _ints("pos", pos, L), _f32("table", table, (positions, half, 2)), positions, y, ldy,
+                               _stream(stream)))
+
+
+def kv_cache_append(cache, K, V, seq_start, past, page_table, pos, table, max_new, Q=None, Q_out=None,
+                    interleaved=False, stream=None):
+    """Stores the rows of K (rotated by table[pos]; table None: as they are)
+    and V [T][Hkv D] behind the past[b] tokens that sequence b keeps, and
+    rotates Q [T][H D] into Q_out. seq_start [B + 1]: each sequence's rows,
+    at most max_new."""
+    T, B, w = K.shape[0], past.shape[0], cache.Hkv * cache.D
+    if K.shape[1] != w or V.shape[0] != T or V.shape[1] != w:
+        raise ValueError(f"starq expects K and V as rows of Hkv * D = {w} channels")
+    _same(K.dtype, V=V, Q=Q, Q_out=Q_out)
+    k, ldk = _rows(K, "K")
+    v, ldv = _rows(V, "V")
+    q, ldq = _rows(Q, "Q")
+    qo, ldqo = _rows(Q_out, "Q_out")
+    H = 0
+    if Q is not None:
+        H = Q.shape[1] // cache.D
+        if Q_out is None or Q.shape != Q_out.shape or Q.shape[0] != T or Q.shape[1] != H * cache.D:
+            raise ValueError("starq expects Q and Q_out as T rows of H * D channels")
+    tab, positions, half = None, 0, 0
+    if table is not None:
+        positions, half, _ = table.shape
+        tab = _f32("table", table, (positions, half, 2))
+    pt, pld = _pages(page_table, B)
+    _check(lib.kv_cache_append(ctypes.byref(cache.c), k, ldk, v, ldv, q, ldq, qo, ldqo, H, _CODES[K.dtype], T,
+                               _ints("seq_start", seq_start, B + 1), _ints("past", past, B), B, max_new, pt, pld,
+                               None if pos is None else _ints("pos", pos, T), tab, positions, 2 * half, interleaved,
+                               _stream(stream)))
+
+
+def kv_cache_read(cache, page_table, first, out_start, K, V, max_rows, stream=None):
+    """Rows of the cache as numbers: slots from first[b] on of sequence b
+    into rows out_start[b] .. out_start[b + 1] - 1 (at most max_rows) of K
+    and V [T][Hkv D] (either may be None)."""
+    B, w = first.shape[0], cache.Hkv * cache.D
+    one = K if K is not None else V
+    for t in (K, V):
+        if t is not None and (t.shape != one.shape or t.shape[1] != w or t.stride() != one.stride()):
+            raise ValueError(f"starq expects K and V as rows of Hkv * D = {w} channels with one stride")
+    _same(one.dtype, K=K, V=V)
+    k, ldk = _rows(K, "K")
+    v, ldv = _rows(V, "V")
+    pt, pld = _pages(page_table, B)
+    _check(lib.kv_cache_read(ctypes.byref(cache.c), pt, pld, _ints("first", first, B),
+                             _ints("out_start", out_start, B + 1), B, max_rows, one.shape[0], k, v, ldk or ldv,
+                             _CODES[one.dtype], _stream(stream)))
+
+
+def kv_cache_attention_workspace_size(B, max_new, H, Hkv, D):
+    return int(lib.kv_cache_attention_workspace_size(B, max_new, H, Hkv, D))
+
+
+def kv_cache_attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, causal=False, key_mask=None,
+                       scale=None, lse=None, workspace=None, stream=None):
+    """Attention of the rows of Q [T][H D] (sequence b: rows seq_start[b] ..,
+    at most max_new) over the kv_len[b] (at most max_len) cached tokens into
+    Out [T][H D]; lse [T][H] receives the log-sum-exp. key_mask uint8
+    [B][>= max_len]: 0 = not seen. scale: default 1 / sqrt(D)."""
+    T, B, D = Q.shape[0], kv_len.shape[0], cache.D
+    H = Q.shape[1] // D
+    if Q.shape[1] != H * D or Out.shape != Q.shape:
+        raise ValueError("starq expects Q and Out as T rows of H * D channels")
+    _same(Q.dtype, Out=Out)
+    q, ldq = _rows(Q, "Q")
+    o, ldo = _rows(Out, "Out")
+    pt, pld = _pages(page_table, B)
+    mk, mld = None, 0
+    if key_mask is not None:
+        if key_mask.dtype != torch.uint8 or key_mask.shape[0] != B:
+            raise ValueError(f"starq expects key_mask as uint8 [{B}][slots]")
+        mk, mld = _rows(key_mask, "key_mask")
+        if key_mask.shape[1] < max_len:
+            raise ValueError(f"starq expects key_mask rows of at least max_len = {max_len} bytes")
+    if workspace is None:
+        workspace = torch.empty(lib.kv_cache_attention_workspace_size(B, max_new, H, cache.Hkv, D), dtype=torch.uint8,
+                                device=Q.device)
+    _check(lib.kv_cache_attention(q, ldq, _CODES[Q.dtype], T, _ints("seq_start", seq_start, B + 1), B, max_new, H,
+                                  ctypes.byref(cache.c), pt, pld, _ints("kv_len", kv_len, B), max_len, causal, mk, mld,
+                                  D ** -0.5 if scale is None else scale, o, ldo, _f32("lse", lse, (T, H)),
+                                  workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                  _stream(stream)))
+
+
+def w4g_linear(X, Wq, scales, Y, bias=None, stream=None):
+    """Y [L][N] = X [L][K] W^T (+ bias) for at most 32 rows; Wq uint8
+    [N][K/2] packed int4, scales float32 [N][K / group]."""
+    L, K = X.shape
+    N, groups = scales.shape
+    if Wq.dtype != torch.uint8 or tuple(Wq.shape) != (N, K // 2) or tuple(Y.shape) != (L, N) or K % max(groups, 1):
+        raise ValueError("starq expects X [L][K], Wq [N][K/2] uint8, scales [N][K / group] and Y [L][N]")
+    _contig(Wq)
+    x, ldx = _rows(X, "X")
+    y, ldy = _rows(Y, "Y")
+    _check(lib.w4g_linear(x, ldx, _CODES[X.dtype], L, K, Wq.data_ptr(), _f32("scales", scales, (N, groups)),
+                          K // max(groups, 1), N, _f32("bias", bias, (N,)), y, ldy, _CODES[Y.dtype], _stream(stream)))

@@ -12,6 +12,7 @@
 #include "w8a8.cuh"
 #include "asym.cuh"
 #include "dense.cuh"
+#include "decode.cuh"
 
 namespace starq {
 
@@ -184,6 +185,7 @@ int check_w8a8(const uint8_t* Xe, const float* s_a, const uint8_t* We, const flo
 }  // namespace
 
 int report_error(int code, const char* msg) { return fail(code, "%s", msg); }
+unsigned* device_status(int* err) { return status_ptr(err); }
 
 namespace {
 // Failure-detection self-test: one thread waits on an mbarrier that nothing
@@ -250,6 +252,8 @@ int starq_check_status(void* stream) {
     if (v != 0) {
         e = cudaMemcpyToSymbol(g_status_word, &zero, sizeof(zero));
         if (e != cudaSuccess) return cuda_fail(e, "clear status word");
+        if (v == STATUS_RANGE)
+            return fail(STARQ_ERR_RANGE, "a kernel met an index outside its array (status bits 0x%x)", v);
         return fail(STARQ_ERR_TIMEOUT, "a kernel gave up a bounded wait (status bits 0x%x)", v);
     }
     return STARQ_OK;

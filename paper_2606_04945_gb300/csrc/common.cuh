@@ -126,6 +126,7 @@ cudaError_t launch_rope(void* QK, int dtype, int L, int ld, int heads, const int
 cudaError_t launch_probe_mma(int kind, int iters, unsigned long long* cycles, int* errors, unsigned* status,
                              int* ctas, double* macs_per_cta, cudaStream_t stream);
 int report_error(int code, const char* msg);  // record msg for starq_last_error(), return code
+unsigned* device_status(int* err);            // the device's status word (NULL and *err on failure)
 
 // sgat_linear with a workspace that the library owns (the device scratch
 // array of sgat_linear_noalloc), which the device-memory check skips.

@@ -1,0 +1,639 @@
+// Attention of new query tokens over the paged 8-bit key/value cache.
+//
+//   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(scale q_i . k_j),
+//   k_j = s_k(j) c_j,  v_j = s_v(j) e_j     (one scale per block and head)
+// over the keys j that row i sees; a row that sees none gives 0 and a
+// log-sum-exp of -inf.
+//
+// Arithmetic. The codes c, e are integers of magnitude <= 127, exact in
+// fp16, so both products run on the 16-bit MMA with float32 accumulators.
+// A bf16 query row is scaled by a power of two into fp16's range: its eight
+// significand bits fit, so only values below 2^-28 of the row's largest
+// lose bits. s_k and the softmax scale multiply the float32 score. s_v
+// enters through the exponent: with
+//   x_ij = log2(e) scale q_i . k_j + log2 s_v(j),  P_ij = 2^(x_ij - m_i + 7)
+// the weights P_ij already carry the value's scale and are at most 2^15, so
+// rounding them to fp16 (2^-11 relative, as a 16-bit attention does) loses
+// only weights 2^-32 below the row's largest, which is at least 2^7; the sum of the plain weights is
+// sum_j P_ij / s_v(j) in float32 from the unrounded P. m_i is a running
+// maximum that moves only when a score passes it by 8 (2^8 of headroom), so
+// most tiles do not rescale the accumulators.
+//
+// Work. For one query token the cache is read once and the rest is small:
+// bound by memory. The G query heads of a key/value head and the new tokens
+// share a unit's rows (16 of an MMA tile), so a key is loaded once for all
+// of them. The 64-key tiles of all units are cut into equal runs, one per
+// CTA: a long sequence is spread over the whole GPU and short ones are
+// packed, whatever the lengths are. A run that covers a unit writes its
+// rows; partial runs leave (sum, maximum, accumulators) in the workspace and
+// a second kernel joins them in run order (results do not depend on timing).
+//
+// In a CTA each of four warps owns 16 keys of a tile and a private ring of
+// cp.async stages, so warps meet only at the end of a unit. 16-byte chunks
+// are XOR-swizzled by row so that both fragments read without bank
+// conflicts. The MMA's k order is free: a key's fragment takes 4 consecutive
+// channels per thread, and value columns are taken in the order that makes a
+// thread's 16 bytes one row's 16 columns, so no transposition is needed.
+#include <type_traits>
+
+#include "decode.cuh"
+
+namespace starq {
+namespace {
+
+constexpr int WARPS = 4;
+constexpr int THREADS = WARPS * 32;
+constexpr int ROWS = 16;               // query rows of a unit
+constexpr int WKEYS = 16;              // keys of a warp in a tile
+constexpr int TILE = WARPS * WKEYS;    // 64 keys
+constexpr int STAGES = 4;
+constexpr float HEAD = 7.f;            // P = 2^(x - m + HEAD)
+constexpr float LAZY = 8.f;            // m moves when x > m + LAZY
+constexpr float NEG_INF = -__builtin_huge_valf();
+
+// Workspace: prefix [B] (tiles before each sequence), then two partial
+// slots per CTA: D accumulators, m and l for each of 16 rows.
+constexpr size_t prefix_bytes(int B) { return ((size_t)(B + 1) * 8 + 255) / 256 * 256; }
+template <int D> struct Slot {
+    static constexpr int FLOATS = ROWS * (D + 2);
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() {
+    asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory");
+}
+
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+                 "{%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Two bytes u (code + 128) in the low bytes of 0x64uu halves (1024 + u) to
+// the two codes in fp16, exactly.
+__device__ __forceinline__ uint32_t codes_half2(uint32_t biased) {
+    const __half2 k = __half2half2(__ushort_as_half((unsigned short)0x6480));       // 1152
+    __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&biased), k);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+
+// Byte offset of 16-byte chunk c of row r (of 16) in a warp's stage.
+template <int D> __device__ __forceinline__ uint32_t stage_offset(int r, int c) {
+    if (D == 128) return r * 128 + ((c ^ (r & 7) ^ ((r & 1) << 2)) << 4);
+    return (r >> 1) * 128 + (((r & 1) ^ ((r >> 2) & 1)) << 6) + ((c ^ (((r >> 1) & 1) << 1)) << 4);
+}
+
+struct SeqShape { int len, n, row0, nt, rt; };       // cached tokens, new tokens, first row, key tiles, row tiles
+
+// The lengths of sequence b; a sequence whose numbers do not fit their
+// bounds counts as having no rows.
+__device__ __forceinline__ SeqShape seq_shape(const KvAttnArgs& a, int G, int b, bool report) {
+    SeqShape s;
+    s.row0 = __ldg(a.seq_start + b);
+    s.n = __ldg(a.seq_start + b + 1) - s.row0;
+    s.len = __ldg(a.kv_len + b);
+    const bool bad = s.n < 0 || s.n > a.max_new || s.row0 < 0 || s.row0 > a.T - s.n || s.len < 0 || s.len > a.max_len;
+    if (bad) {
+        if (report) atomicOr(a.status, STATUS_RANGE);
+        s.n = 0; s.len = 0; s.row0 = 0;
+    }
+    s.nt = s.n > 0 ? (s.len + TILE - 1) / TILE : 0;
+    s.rt = (s.n * G + ROWS - 1) / ROWS;
+    return s;
+}
+
+// Position in the flat list of tiles: sequence, head, row tile, key tile.
+struct Cursor {
+    int b, h, rt, kt;
+    SeqShape s;
+    __device__ __forceinline__ void next_unit(const KvAttnArgs& a, int G) {
+        kt = 0;
+        if (++rt < s.rt) return;
+        rt = 0;
+        if (++h < a.c.Hkv) return;
+        h = 0;
+        do {
+            if (++b >= a.B) return;
+            s = seq_shape(a, G, b, false);
+        } while (s.nt == 0);
+    }
+};
+
+// Fragments of one query row (half of the A operand's registers): channels
+// 64 h + 16 t + 4 s + {0, 1} in q[h][s][0], {2, 3} in q[h][s][1], and the
+// power of two that undoes the row's scaling.
+template <typename T, int D>
+__device__ __forceinline__ float load_row(const T* row, int t, uint32_t (&q)[D / 64][4][2]) {
+    float v[D / 64][16], top = 0.f;
+    #pragma unroll
+    for (int h = 0; h < D / 64; ++h) {
+        float x[8];
+        #pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            #pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+            if (row != nullptr) Eight<T>::load(row + 64 * h + 16 * t + 8 * k, x);
+            #pragma unroll
+            for (int i = 0; i < 8; ++i) { v[h][8 * k + i] = x[i]; top = fmaxf(top, fabsf(x[i])); }
+        }
+    }
+    float up = 1.f, down = 1.f;
+    if (std::is_same<T, __nv_bfloat16>::value) {
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // 2^(14 - e), e the exponent of the row's largest value (at least -112)
+        int e = (int)(__float_as_uint(top) >> 23) - 127;
+        e = max(e, -112);
+        up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
+        down = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
+    }
+    #pragma unroll
+    for (int h = 0; h < D / 64; ++h)
+        #pragma unroll
+        for (int s = 0; s < 4; ++s)
+            #pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const __half2 p = __floats2half2_rn(v[h][4 * s + 2 * k] * up, v[h][4 * s + 2 * k + 1] * up);
+                q[h][s][k] = *reinterpret_cast<const uint32_t*>(&p);
+            }
+    return down;
+}
+
+template <typename T, int D>
+struct AttnSmem {
+    static constexpr int STAGE = 2 * WKEYS * D;                 // bytes of a warp's stage: keys, then values
+    static constexpr int RING = WARPS * STAGES * STAGE;
+    static constexpr int MERGE = ROWS * D * 4 + WARPS * ROWS * 8;
+    static constexpr int BYTES = RING + MERGE;
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(THREADS, 2) kv_attention_kernel(const KvAttnArgs a, int G, long long* prefix_out,
+                                                                 float* slots) {
+    using SM = AttnSmem<T, D>;
+    constexpr int KH = D / 64;               // 64-channel halves of a key
+    constexpr int DN = D / 8;                // value columns per thread, and column tiles
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ long long s_total, s_part[WARPS], s_tau;
+    __shared__ int s_b;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+
+    // --- how many tiles there are, and where this CTA's run begins --------
+    long long mine = 0;
+    for (int b = tid; b < a.B; b += THREADS) {
+        const SeqShape s = seq_shape(a, G, b, blockIdx.x == 0);
+        mine += (long long)s.nt * s.rt * a.c.Hkv;
+    }
+    #pragma unroll
+    for (int m = 16; m > 0; m >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, m);
+    if (lane == 0) s_part[warp] = mine;
+    if (tid == 0) s_b = -1;
+    __syncthreads();
+    long long total = 0;
+    #pragma unroll
+    for (int w = 0; w < WARPS; ++w) total += s_part[w];
+    const long long share = (total + gridDim.x - 1) / gridDim.x;
+    const long long tau0 = share * blockIdx.x;
+    const long long tau1 = min(total, tau0 + share);
+    if (tau0 >= total && blockIdx.x != 0) return;
+    long long before = 0;                                     // tiles before the current chunk of sequences
+    for (int b0 = 0; b0 < a.B; b0 += THREADS) {
+        const int b = b0 + tid;
+        long long cnt = 0;
+        if (b < a.B) {
+            const SeqShape s = seq_shape(a, G, b, false);
+            cnt = (long long)s.nt * s.rt * a.c.Hkv;
+        }
+        long long inc = cnt;
+        #pragma unroll
+        for (int m = 1; m < 32; m <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, inc, m);
+            if (lane >= m) inc += v;
+        }
+        __syncthreads();
+        if (lane == 31) s_part[warp] = inc;
+        __syncthreads();
+        long long base = before;
+        for (int w = 0; w < warp; ++w) base += s_part[w];
+        const long long at = base + inc - cnt;
+        if (b < a.B) {
+            if (blockIdx.x == 0) prefix_out[b] = at;
+            if (cnt > 0 && tau0 >= at && tau0 < at + cnt) { s_b = b; s_tau = at; }
+        }
+        for (int w = 0; w < WARPS; ++w) before += s_part[w];
+    }
+    if (tid == 0) {
+        s_total = total;
+        if (blockIdx.x == 0) prefix_out[a.B] = total;
+    }
+    __syncthreads();
+    if (tau0 >= total) return;
+
+    Cursor cur;
+    cur.b = s_b;
+    cur.s = seq_shape(a, G, cur.b, false);
+    {
+        const long long off = tau0 - s_tau;
+        const long long unit = off / cur.s.nt;
+        cur.kt = (int)(off - unit * cur.s.nt);
+        cur.h = (int)(unit / cur.s.rt);
+        cur.rt = (int)(unit - (long long)cur.h * cur.s.rt);
+    }
+    Cursor pre = cur;
+    long long pre_left = tau1 - tau0;        // tiles still to be fetched
+
+    const uint32_t ring = smem_addr(smem) + warp * (STAGES * SM::STAGE);
+    const size_t block_bytes = (size_t)a.c.page * D;
+
+    // Scales of the stages in flight: x = log2(e) scale s_k, y = s_v of the
+    // warp's 16 keys (a page holds a multiple of 16).
+    float sk[STAGES], sv[STAGES];
+    auto fetch = [&](int slot, float& k_out, float& v_out) {
+        k_out = 0.f; v_out = 1.f;
+        if (pre_left > 0) {
+            const int key0 = pre.kt * TILE + warp * WKEYS;
+            if (key0 < pre.s.len) {
+                const int page_i = key0 / a.c.page;
+                int page = -1;
+                if (page_i < a.table_ld) page = __ldg(a.page_table + (size_t)pre.b * a.table_ld + page_i);
+                if (page < 0 || page >= a.c.pages) {
+                    if (lane == 0) atomicOr(a.status, STATUS_RANGE);
+                    k_out = __uint_as_float(0x7fffffffu);      // the rows that see these keys become NaN
+                } else {
+                    const size_t blk = (size_t)page * a.c.Hkv + pre.h;
+                    const size_t off = blk * block_bytes + (size_t)(key0 - page_i * a.c.page) * D;
+                    const uint32_t dst = ring + slot * SM::STAGE;
+                    #pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        const int id = lane + 32 * i, r = id / (D / 16), c = id % (D / 16);
+                        cp_async16(dst + stage_offset<D>(r, c), a.c.K + off + id * 16);
+                    }
+                    #pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        const int id = lane + 32 * i, r = id / (D / 16), c = id % (D / 16);
+                        cp_async16(dst + WKEYS * D + stage_offset<D>(r, c), a.c.V + off + id * 16);
+                    }
+                    k_out = __ldg(a.c.k_scale + blk);
+                    v_out = __ldg(a.c.v_scale + blk);
+                }
+            }
+            --pre_left;
+            if (++pre.kt == pre.s.nt && pre_left > 0) pre.next_unit(a, G);
+        }
+        cp_async_commit();
+    };
+    #pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) fetch(i, sk[i], sv[i]);
+
+    uint32_t qf[KH][4][4];
+    float o[DN][4], m[2], l[2], rs[2];
+    int lim[2];                              // keys [0, lim) are visible to the rows (causal limit and length)
+    const float unit_scale = a.scale * 1.4426950408889634f;
+    bool fresh = true;
+    int seg_kt0 = cur.kt;
+    long long left = tau1 - tau0;
+    long long tau = tau0;
+
+    while (left > 0) {
+        #pragma unroll
+        for (int st = 0; st < STAGES; ++st) {
+            if (left <= 0) break;
+            if (fresh) {                     // a new unit: its query rows
+                #pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int r = cur.rt * ROWS + g + 8 * k, i = r / G, j = r - i * G;
+                    const T* row = nullptr;
+                    lim[k] = 0;
+                    if (i < cur.s.n) {
+                        row = static_cast<const T*>(a.Q) + (size_t)(cur.s.row0 + i) * a.ldq +
+                              (size_t)(cur.h * G + j) * D;
+                        lim[k] = a.causal ? max(0, cur.s.len - cur.s.n + i + 1) : cur.s.len;
+                    }
+                    uint32_t q2[KH][4][2];
+                    rs[k] = load_row<T, D>(row, t, q2);
+                    #pragma unroll
+                    for (int h = 0; h < KH; ++h)
+                        #pragma unroll
+                        for (int s = 0; s < 4; ++s) { qf[h][s][k] = q2[h][s][0]; qf[h][s][2 + k] = q2[h][s][1]; }
+                    m[k] = NEG_INF; l[k] = 0.f;
+                }
+                #pragma unroll
+                for (int j = 0; j < DN; ++j)
+                    #pragma unroll
+                    for (int k = 0; k < 4; ++k) o[j][k] = 0.f;
+                fresh = false;
+                seg_kt0 = cur.kt;
+            }
+            fetch((st + STAGES - 1) % STAGES, sk[(st + STAGES - 1) % STAGES], sv[(st + STAGES - 1) % STAGES]);
+            cp_async_wait<STAGES - 1>();
+            __syncwarp();
+            const int key0 = cur.kt * TILE + warp * WKEYS;
+            if (key0 < cur.s.len) {
+                const uint8_t* stage = smem + warp * (STAGES * SM::STAGE) + st * SM::STAGE;
+                // --- scores of 16 keys: two column tiles ---------------------
+                float x[2][4];
+                #pragma unroll
+                for (int nt = 0; nt < 2; ++nt) {
+                    #pragma unroll
+                    for (int k = 0; k < 4; ++k) x[nt][k] = 0.f;
+                    #pragma unroll
+                    for (int h = 0; h < KH; ++h) {
+                        const uint4 w = *reinterpret_cast<const uint4*>(stage + stage_offset<D>(nt * 8 + g, 4 * h + t));
+                        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+                        #pragma unroll
+                        for (int s = 0; s < 4; ++s)
+                            mma_16816(x[nt], qf[h][s], codes_half2(prmt(ws[s], 0x64646464u, 0x4140u)),
+                                      codes_half2(prmt(ws[s], 0x64646464u, 0x4342u)));
+                    }
+                }
+                const float ks = sk[st] * unit_scale;
+                // a value scale below the floor counts as the floor (an empty block's codes are 0)
+                const float vs = sv[st] < KV_SCALE_FLOOR ? KV_SCALE_FLOOR : sv[st];
+                const float lv = __log2f(vs), iv = __fdividef(1.f, vs);
+                const float k0 = ks * rs[0], k1 = ks * rs[1];
+                #pragma unroll
+                for (int nt = 0; nt < 2; ++nt) {
+                    x[nt][0] = fmaf(x[nt][0], k0, lv);
+                    x[nt][1] = fmaf(x[nt][1], k0, lv);
+                    x[nt][2] = fmaf(x[nt][2], k1, lv);
+                    x[nt][3] = fmaf(x[nt][3], k1, lv);
+                }
+                const bool edge = key0 + WKEYS > cur.s.len || a.key_mask != nullptr ||
+                                  (a.causal && key0 + WKEYS > cur.s.len - cur.s.n + 1);
+                unsigned seen = 0xff;        // bit 4 nt + k: x[nt][k] counts
+                if (edge) {
+                    seen = 0;
+                    #pragma unroll
+                    for (int nt = 0; nt < 2; ++nt)
+                        #pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int key = key0 + nt * 8 + 2 * t + (k & 1);
+                            bool ok = key < lim[k >> 1];
+                            if (ok && a.key_mask != nullptr)
+                                ok = __ldg(a.key_mask + (size_t)cur.b * a.mask_ld + key) != 0;
+                            if (ok) seen |= 1u << (4 * nt + k);
+                            else x[nt][k] = NEG_INF;
+                        }
+                }
+                // --- running maximum, moved only when it is passed by LAZY ---
+                float top0 = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
+                float top1 = fmaxf(fmaxf(x[0][2], x[0][3]), fmaxf(x[1][2], x[1][3]));
+                if (__any_sync(0xffffffffu, top0 > m[0] + LAZY || top1 > m[1] + LAZY)) {
+                    #pragma unroll
+                    for (int d = 1; d < 4; d <<= 1) {
+                        top0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, d));
+                        top1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, d));
+                    }
+                    const float n0 = fmaxf(m[0], top0), n1 = fmaxf(m[1], top1);
+                    const float f0 = m[0] == n0 ? 1.f : ex2(m[0] - n0), f1 = m[1] == n1 ? 1.f : ex2(m[1] - n1);
+                    m[0] = n0; m[1] = n1;
+                    l[0] *= f0; l[1] *= f1;
+                    #pragma unroll
+                    for (int j = 0; j < DN; ++j) { o[j][0] *= f0; o[j][1] *= f0; o[j][2] *= f1; o[j][3] *= f1; }
+                }
+                const float s0 = m[0] == NEG_INF ? 0.f : m[0] - HEAD, s1 = m[1] == NEG_INF ? 0.f : m[1] - HEAD;
+                uint32_t p[4];
+                #pragma unroll
+                for (int nt = 0; nt < 2; ++nt) {
+                    float e[4];
+                    #pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        e[k] = ex2(x[nt][k] - (k < 2 ? s0 : s1));
+                        // a masked weight is 0 whatever its block's scale is
+                        const float add = !edge || (seen >> (4 * nt + k) & 1) ? e[k] * iv : 0.f;
+                        l[k >> 1] += add;
+                    }
+                    const __half2 pa = __floats2half2_rn(e[0], e[1]), pb = __floats2half2_rn(e[2], e[3]);
+                    p[2 * nt] = *reinterpret_cast<const uint32_t*>(&pa);
+                    p[2 * nt + 1] = *reinterpret_cast<const uint32_t*>(&pb);
+                }
+                // --- values: keys 2t, 2t+1, 2t+8, 2t+9, columns DN g .. ------
+                const uint8_t* vst = stage + WKEYS * D;
+                #pragma unroll
+                for (int c = 0; c < D / 64; ++c) {           // 8 columns at a time
+                    uint2 r[4];
+                    #pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int key = 2 * t + (k & 1) + 8 * (k >> 1);
+                        if (D == 128)
+                            r[k] = *reinterpret_cast<const uint2*>(vst + stage_offset<D>(key, g) + 8 * c);
+                        else
+                            r[k] = *reinterpret_cast<const uint2*>(vst + stage_offset<D>(key, g >> 1) + 8 * (g & 1));
+                    }
+                    #pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        const uint32_t k0w = w ? r[0].y : r[0].x, k1w = w ? r[1].y : r[1].x;
+                        const uint32_t k8w = w ? r[2].y : r[2].x, k9w = w ? r[3].y : r[3].x;
+                        const uint32_t lo01 = prmt(k0w, k1w, 0x5140u), hi01 = prmt(k0w, k1w, 0x7362u);
+                        const uint32_t lo89 = prmt(k8w, k9w, 0x5140u), hi89 = prmt(k8w, k9w, 0x7362u);
+                        const int j = 8 * c + 4 * w;
+                        mma_16816(o[j], p, codes_half2(prmt(lo01, 0x64646464u, 0x4140u)),
+                                  codes_half2(prmt(lo89, 0x64646464u, 0x4140u)));
+                        mma_16816(o[j + 1], p, codes_half2(prmt(lo01, 0x64646464u, 0x4342u)),
+                                  codes_half2(prmt(lo89, 0x64646464u, 0x4342u)));
+                        mma_16816(o[j + 2], p, codes_half2(prmt(hi01, 0x64646464u, 0x4140u)),
+                                  codes_half2(prmt(hi89, 0x64646464u, 0x4140u)));
+                        mma_16816(o[j + 3], p, codes_half2(prmt(hi01, 0x64646464u, 0x4342u)),
+                                  codes_half2(prmt(hi89, 0x64646464u, 0x4342u)));
+                    }
+                }
+            }
+            __syncwarp();
+            --left;
+            ++tau;
+            if (++cur.kt == cur.s.nt || left == 0) {
+                // --- end of the unit in this CTA: join the four warps --------
+                float* buf = reinterpret_cast<float*>(smem + SM::RING);            // [16][D]
+                float2* ml = reinterpret_cast<float2*>(smem + SM::RING + ROWS * D * 4);   // [warp][16]
+                #pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    #pragma unroll
+                    for (int d = 1; d < 4; d <<= 1) l[k] += __shfl_xor_sync(0xffffffffu, l[k], d);
+                if (t == 0) {
+                    ml[warp * ROWS + g] = make_float2(m[0], l[0]);
+                    ml[warp * ROWS + g + 8] = make_float2(m[1], l[1]);
+                }
+                __syncthreads();
+                float mm[2], ll[2];
+                #pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float top = NEG_INF;
+                    #pragma unroll
+                    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, ml[w * ROWS + g + 8 * k].x);
+                    float sum = 0.f;
+                    #pragma unroll
+                    for (int w = 0; w < WARPS; ++w) {
+                        const float2 v = ml[w * ROWS + g + 8 * k];
+                        if (v.x != NEG_INF || v.y != 0.f) sum += v.y * (v.x == top ? 1.f : ex2(v.x - top));
+                    }
+                    mm[k] = top; ll[k] = sum;
+                    const float f = m[k] == top ? 1.f : ex2(m[k] - top);           // 0 for a warp that saw nothing
+                    #pragma unroll
+                    for (int j = 0; j < DN; ++j) { o[j][2 * k] *= f; o[j][2 * k + 1] *= f; }
+                }
+                for (int w = 0; w < WARPS; ++w) {
+                    if (warp == w) {
+                        #pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            float4* dst = reinterpret_cast<float4*>(buf + (g + 8 * (k >> 1)) * D + DN * (2 * t + (k & 1)));
+                            #pragma unroll
+                            for (int j = 0; j < DN; j += 4) {
+                                float4 v = make_float4(o[j][k], o[j + 1][k], o[j + 2][k], o[j + 3][k]);
+                                if (w > 0) {
+                                    const float4 u = dst[j / 4];
+                                    v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+                                }
+                                dst[j / 4] = v;
+                            }
+                        }
+                    }
+                    __syncthreads();
+                }
+                if (warp == 0 && t == 0) {
+                    ml[g] = make_float2(mm[0], ll[0]);
+                    ml[g + 8] = make_float2(mm[1], ll[1]);
+                }
+                __syncthreads();
+                const bool whole = seg_kt0 == 0 && cur.kt == cur.s.nt;
+                if (whole) {
+                    for (int e = tid; e < ROWS * (D / 8); e += THREADS) {
+                        const int r = e / (D / 8), c = e % (D / 8);
+                        const int rr = cur.rt * ROWS + r, i = rr / G, j = rr - i * G;
+                        if (i >= cur.s.n) continue;
+                        const float2 v = ml[r];
+                        const float inv = v.y == 0.f ? 0.f : __fdiv_rn(1.f, v.y);
+                        float f[8];
+                        #pragma unroll
+                        for (int k = 0; k < 8; ++k) f[k] = v.y == 0.f ? 0.f : buf[r * D + 8 * c + k] * inv;
+                        const size_t row = (size_t)(cur.s.row0 + i);
+                        Eight<T>::store(static_cast<T*>(a.Out) + row * a.ldo + (size_t)(cur.h * G + j) * D + 8 * c, f);
+                        if (c == 0 && a.lse != nullptr)
+                            a.lse[row * a.H + cur.h * G + j] =
+                                v.y == 0.f ? NEG_INF : (log2f(v.y) + (v.x - HEAD)) * 0.6931471805599453f;
+                    }
+                } else {
+                    // slot 0: the run begins with (or inside) this unit; slot 1: it ends in it
+                    const bool first = tau - (cur.kt - seg_kt0) == tau0;
+                    float* dst = slots + ((size_t)blockIdx.x * 2 + (first ? 0 : 1)) * Slot<D>::FLOATS;
+                    for (int e = tid; e < ROWS * D / 4; e += THREADS)
+                        reinterpret_cast<float4*>(dst)[e] = reinterpret_cast<const float4*>(buf)[e];
+                    if (tid < ROWS) reinterpret_cast<float2*>(dst + ROWS * D)[tid] = ml[tid];
+                }
+                __syncthreads();
+                if (left > 0) cur.next_unit(a, G);
+                fresh = true;
+            }
+        }
+    }
+    cp_async_wait<0>();
+}
+
+// One warp per query row: joins the partial runs of the row's unit in run
+// order, and writes the rows that no key reaches.
+template <typename T, int D>
+__global__ void __launch_bounds__(THREADS) kv_attention_join_kernel(const KvAttnArgs a, int G, int ctas,
+                                                                   const long long* __restrict__ prefix,
+                                                                   const float* __restrict__ slots) {
+    constexpr int PER = D / 32;
+    grid_dependency_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int b = blockIdx.y;
+    const SeqShape s = seq_shape(a, G, b, false);
+    const int idx = blockIdx.x * WARPS + warp;            // token * H + head
+    const int i = idx / a.H, head = idx - i * a.H;
+    if (i >= s.n) return;
+    const size_t row = (size_t)(s.row0 + i);
+    T* out = static_cast<T*>(a.Out) + row * a.ldo + (size_t)head * D + lane * PER;
+    if (s.nt == 0) {
+        #pragma unroll
+        for (int k = 0; k < PER; ++k) out[k] = (T)0.f;
+        if (lane == 0 && a.lse != nullptr) a.lse[row * a.H + head] = NEG_INF;
+        return;
+    }
+    const int h = head / G, r = i * G + (head - h * G);
+    const int rt = r / ROWS, rr = r - rt * ROWS;
+    const long long total = prefix[a.B];
+    const long long share = (total + ctas - 1) / ctas;
+    const long long u0 = prefix[b] + ((long long)h * s.rt + rt) * s.nt;
+    const int c0 = (int)(u0 / share), c1 = (int)((u0 + s.nt - 1) / share);
+    if (c0 == c1) return;                                 // one run covered the unit
+    auto slot = [&](int c) {
+        return slots + ((size_t)c * 2 + (u0 > (long long)c * share ? 1 : 0)) * Slot<D>::FLOATS;
+    };
+    // maximum over the runs, lanes side by side
+    float top = NEG_INF;
+    for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, slot(c)[ROWS * D + 2 * rr]);
+    #pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    float l = 0.f, acc[PER];
+    #pragma unroll
+    for (int k = 0; k < PER; ++k) acc[k] = 0.f;
+    #pragma unroll 4
+    for (int c = c0; c <= c1; ++c) {
+        const float* p = slot(c);
+        const float2 ml = *reinterpret_cast<const float2*>(p + ROWS * D + 2 * rr);
+        const float f = ml.x == top ? 1.f : ex2(ml.x - top);
+        l = fmaf(ml.y, f, l);
+        #pragma unroll
+        for (int k = 0; k < PER; ++k) acc[k] = fmaf(p[rr * D + lane * PER + k], f, acc[k]);
+    }
+    const float inv = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
+    #pragma unroll
+    for (int k = 0; k < PER; ++k) out[k] = (T)(l == 0.f ? 0.f : acc[k] * inv);
+    if (lane == 0 && a.lse != nullptr)
+        a.lse[row * a.H + head] = l == 0.f ? NEG_INF : (log2f(l) + (top - HEAD)) * 0.6931471805599453f;
+}
+
+constexpr int CTAS_PER_SM = 2;
+
+template <typename T, int D>
+cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
+    const int G = a.H / a.c.Hkv;
+    static DeviceCache<int> ready;
+    int dummy = 0;
+    cudaError_t e = ready.get(&dummy, [](int, int* v) {
+        *v = 1;
+        return cudaFuncSetAttribute(kv_attention_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    AttnSmem<T, D>::BYTES);
+    });
+    if (e != cudaSuccess) return e;
+    const int ctas = num_sms() * CTAS_PER_SM;
+    long long* prefix = static_cast<long long*>(a.workspace);
+    float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + prefix_bytes(a.B));
+    kv_attention_kernel<T, D><<<ctas, THREADS, AttnSmem<T, D>::BYTES, s>>>(a, G, prefix, slots);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(((size_t)a.max_new * a.H + WARPS - 1) / WARPS), (unsigned)a.B);
+    cfg.blockDim = dim3(THREADS);
+    cfg.stream = s;
+    cudaLaunchAttribute at = pdl_attribute();
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kv_attention_join_kernel<T, D>, a, G, ctas, (const long long*)prefix,
+                              (const float*)slots);
+}
+
+}  // namespace
+
+size_t kv_attention_workspace_bytes(int B, int max_new, int H, int Hkv, int D) {
+    (void)max_new; (void)H; (void)Hkv;
+    return prefix_bytes(B) + (size_t)num_sms() * CTAS_PER_SM * 2 * ROWS * (D + 2) * 4;
+}
+
+cudaError_t launch_kv_attention(const KvAttnArgs& a, cudaStream_t s) {
+    if (a.dtype == STARQ_BF16)
+        return a.c.D == 64 ? launch_typed<__nv_bfloat16, 64>(a, s) : launch_typed<__nv_bfloat16, 128>(a, s);
+    return a.c.D == 64 ? launch_typed<__half, 64>(a, s) : launch_typed<__half, 128>(a, s);
+}
+
+}  // namespace starq
