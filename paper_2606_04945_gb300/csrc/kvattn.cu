@@ -36,7 +36,7 @@
 // thread's 16 bytes one row's 16 columns, so no transposition is needed.
 #include <type_traits>
 
-#include "decode.cuh"
+#include "kvattn.cuh"
 
 namespace starq {
 namespace {
@@ -47,17 +47,6 @@ constexpr int ROWS = 16;               // query rows of a unit
 constexpr int WKEYS = 16;              // keys of a warp in a tile
 constexpr int TILE = WARPS * WKEYS;    // 64 keys
 constexpr int STAGES = 4;
-constexpr float HEAD = 7.f;            // P = 2^(x - m + HEAD)
-constexpr float LAZY = 8.f;            // m moves when x > m + LAZY
-constexpr float NEG_INF = -__builtin_huge_valf();
-
-// Workspace: prefix [B] (tiles before each sequence), then two partial
-// slots per CTA: D accumulators, m and l for each of 16 rows.
-constexpr size_t prefix_bytes(int B) { return ((size_t)(B + 1) * 8 + 255) / 256 * 256; }
-template <int D> struct Slot {
-    static constexpr int FLOATS = ROWS * (D + 2);
-};
-
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
 }
@@ -73,61 +62,11 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// Two bytes u (code + 128) in the low bytes of 0x64uu halves (1024 + u) to
-// the two codes in fp16, exactly.
-__device__ __forceinline__ uint32_t codes_half2(uint32_t biased) {
-    const __half2 k = __half2half2(__ushort_as_half((unsigned short)0x6480));       // 1152
-    __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&biased), k);
-    return *reinterpret_cast<uint32_t*>(&v);
-}
-
 // Byte offset of 16-byte chunk c of row r (of 16) in a warp's stage.
 template <int D> __device__ __forceinline__ uint32_t stage_offset(int r, int c) {
     if (D == 128) return r * 128 + ((c ^ (r & 7) ^ ((r & 1) << 2)) << 4);
     return (r >> 1) * 128 + (((r & 1) ^ ((r >> 2) & 1)) << 6) + ((c ^ (((r >> 1) & 1) << 1)) << 4);
 }
-
-struct SeqShape { int len, n, row0, nt, rt; };       // cached tokens, new tokens, first row, key tiles, row tiles
-
-// The lengths of sequence b; a sequence whose numbers do not fit their
-// bounds counts as having no rows.
-__device__ __forceinline__ SeqShape seq_shape(const KvAttnArgs& a, int G, int b, bool report) {
-    SeqShape s;
-    s.row0 = __ldg(a.seq_start + b);
-    s.n = __ldg(a.seq_start + b + 1) - s.row0;
-    s.len = __ldg(a.kv_len + b);
-    const bool bad = s.n < 0 || s.n > a.max_new || s.row0 < 0 || s.row0 > a.T - s.n || s.len < 0 || s.len > a.max_len;
-    if (bad) {
-        if (report) atomicOr(a.status, STATUS_RANGE);
-        s.n = 0; s.len = 0; s.row0 = 0;
-    }
-    s.nt = s.n > 0 ? (s.len + TILE - 1) / TILE : 0;
-    s.rt = (s.n * G + ROWS - 1) / ROWS;
-    return s;
-}
-
-// Position in the flat list of tiles: sequence, head, row tile, key tile.
-struct Cursor {
-    int b, h, rt, kt;
-    SeqShape s;
-    __device__ __forceinline__ void next_unit(const KvAttnArgs& a, int G) {
-        kt = 0;
-        if (++rt < s.rt) return;
-        rt = 0;
-        if (++h < a.c.Hkv) return;
-        h = 0;
-        do {
-            if (++b >= a.B) return;
-            s = seq_shape(a, G, b, false);
-        } while (s.nt == 0);
-    }
-};
 
 // Fragments of one query row (half of the A operand's registers): channels
 // 64 h + 16 t + 4 s + {0, 1} in q[h][s][0], {2, 3} in q[h][s][1], and the
@@ -151,11 +90,7 @@ __device__ __forceinline__ float load_row(const T* row, int t, uint32_t (&q)[D /
     if (std::is_same<T, __nv_bfloat16>::value) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // 2^(14 - e), e the exponent of the row's largest value (at least -112)
-        int e = (int)(__float_as_uint(top) >> 23) - 127;
-        e = max(e, -112);
-        up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
-        down = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
+        row_power(top, up, down);
     }
     #pragma unroll
     for (int h = 0; h < D / 64; ++h)
@@ -184,73 +119,15 @@ __global__ void __launch_bounds__(THREADS, 2) kv_attention_kernel(const KvAttnAr
     constexpr int KH = D / 64;               // 64-channel halves of a key
     constexpr int DN = D / 8;                // value columns per thread, and column tiles
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ long long s_total, s_part[WARPS], s_tau;
-    __shared__ int s_b;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
 
-    // --- how many tiles there are, and where this CTA's run begins --------
-    long long mine = 0;
-    for (int b = tid; b < a.B; b += THREADS) {
-        const SeqShape s = seq_shape(a, G, b, blockIdx.x == 0);
-        mine += (long long)s.nt * s.rt * a.c.Hkv;
-    }
-    #pragma unroll
-    for (int m = 16; m > 0; m >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, m);
-    if (lane == 0) s_part[warp] = mine;
-    if (tid == 0) s_b = -1;
-    __syncthreads();
-    long long total = 0;
-    #pragma unroll
-    for (int w = 0; w < WARPS; ++w) total += s_part[w];
-    const long long share = (total + gridDim.x - 1) / gridDim.x;
-    const long long tau0 = share * blockIdx.x;
-    const long long tau1 = min(total, tau0 + share);
-    if (tau0 >= total && blockIdx.x != 0) return;
-    long long before = 0;                                     // tiles before the current chunk of sequences
-    for (int b0 = 0; b0 < a.B; b0 += THREADS) {
-        const int b = b0 + tid;
-        long long cnt = 0;
-        if (b < a.B) {
-            const SeqShape s = seq_shape(a, G, b, false);
-            cnt = (long long)s.nt * s.rt * a.c.Hkv;
-        }
-        long long inc = cnt;
-        #pragma unroll
-        for (int m = 1; m < 32; m <<= 1) {
-            const long long v = __shfl_up_sync(0xffffffffu, inc, m);
-            if (lane >= m) inc += v;
-        }
-        __syncthreads();
-        if (lane == 31) s_part[warp] = inc;
-        __syncthreads();
-        long long base = before;
-        for (int w = 0; w < warp; ++w) base += s_part[w];
-        const long long at = base + inc - cnt;
-        if (b < a.B) {
-            if (blockIdx.x == 0) prefix_out[b] = at;
-            if (cnt > 0 && tau0 >= at && tau0 < at + cnt) { s_b = b; s_tau = at; }
-        }
-        for (int w = 0; w < WARPS; ++w) before += s_part[w];
-    }
-    if (tid == 0) {
-        s_total = total;
-        if (blockIdx.x == 0) prefix_out[a.B] = total;
-    }
-    __syncthreads();
-    if (tau0 >= total) return;
-
-    Cursor cur;
-    cur.b = s_b;
-    cur.s = seq_shape(a, G, cur.b, false);
-    {
-        const long long off = tau0 - s_tau;
-        const long long unit = off / cur.s.nt;
-        cur.kt = (int)(off - unit * cur.s.nt);
-        cur.h = (int)(unit / cur.s.rt);
-        cur.rt = (int)(unit - (long long)cur.h * cur.s.rt);
-    }
-    Cursor pre = cur;
-    long long pre_left = tau1 - tau0;        // tiles still to be fetched
+    const Run run = find_run<ROWS, TILE, THREADS>(a, G, prefix_out);
+    if (run.tau0 >= run.tau1) return;
+    Cursor<ROWS, TILE> cur;
+    cur.start(a, G, run);
+    Cursor<ROWS, TILE> pre = cur;
+    int left = (int)(run.tau1 - run.tau0);   // tiles of the run
+    int pre_left = left;                     // tiles still to be fetched
 
     const uint32_t ring = smem_addr(smem) + warp * (STAGES * SM::STAGE);
     const size_t block_bytes = (size_t)a.c.page * D;
@@ -301,8 +178,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_attention_kernel(const KvAttnAr
     const float unit_scale = a.scale * 1.4426950408889634f;
     bool fresh = true;
     int seg_kt0 = cur.kt;
-    long long left = tau1 - tau0;
-    long long tau = tau0;
+    int tau = 0;                             // tiles done
 
     while (left > 0) {
         #pragma unroll
@@ -523,8 +399,8 @@ __global__ void __launch_bounds__(THREADS, 2) kv_attention_kernel(const KvAttnAr
                     }
                 } else {
                     // slot 0: the run begins with (or inside) this unit; slot 1: it ends in it
-                    const bool first = tau - (cur.kt - seg_kt0) == tau0;
-                    float* dst = slots + ((size_t)blockIdx.x * 2 + (first ? 0 : 1)) * Slot<D>::FLOATS;
+                    const bool first = tau == cur.kt - seg_kt0;
+                    float* dst = slots + ((size_t)blockIdx.x * 2 + (first ? 0 : 1)) * slot_floats(ROWS, D);
                     for (int e = tid; e < ROWS * D / 4; e += THREADS)
                         reinterpret_cast<float4*>(dst)[e] = reinterpret_cast<const float4*>(buf)[e];
                     if (tid < ROWS) reinterpret_cast<float2*>(dst + ROWS * D)[tid] = ml[tid];
@@ -536,62 +412,6 @@ __global__ void __launch_bounds__(THREADS, 2) kv_attention_kernel(const KvAttnAr
         }
     }
     cp_async_wait<0>();
-}
-
-// One warp per query row: joins the partial runs of the row's unit in run
-// order, and writes the rows that no key reaches.
-template <typename T, int D>
-__global__ void __launch_bounds__(THREADS) kv_attention_join_kernel(const KvAttnArgs a, int G, int ctas,
-                                                                   const long long* __restrict__ prefix,
-                                                                   const float* __restrict__ slots) {
-    constexpr int PER = D / 32;
-    grid_dependency_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int b = blockIdx.y;
-    const SeqShape s = seq_shape(a, G, b, false);
-    const int idx = blockIdx.x * WARPS + warp;            // token * H + head
-    const int i = idx / a.H, head = idx - i * a.H;
-    if (i >= s.n) return;
-    const size_t row = (size_t)(s.row0 + i);
-    T* out = static_cast<T*>(a.Out) + row * a.ldo + (size_t)head * D + lane * PER;
-    if (s.nt == 0) {
-        #pragma unroll
-        for (int k = 0; k < PER; ++k) out[k] = (T)0.f;
-        if (lane == 0 && a.lse != nullptr) a.lse[row * a.H + head] = NEG_INF;
-        return;
-    }
-    const int h = head / G, r = i * G + (head - h * G);
-    const int rt = r / ROWS, rr = r - rt * ROWS;
-    const long long total = prefix[a.B];
-    const long long share = (total + ctas - 1) / ctas;
-    const long long u0 = prefix[b] + ((long long)h * s.rt + rt) * s.nt;
-    const int c0 = (int)(u0 / share), c1 = (int)((u0 + s.nt - 1) / share);
-    if (c0 == c1) return;                                 // one run covered the unit
-    auto slot = [&](int c) {
-        return slots + ((size_t)c * 2 + (u0 > (long long)c * share ? 1 : 0)) * Slot<D>::FLOATS;
-    };
-    // maximum over the runs, lanes side by side
-    float top = NEG_INF;
-    for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, slot(c)[ROWS * D + 2 * rr]);
-    #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    float l = 0.f, acc[PER];
-    #pragma unroll
-    for (int k = 0; k < PER; ++k) acc[k] = 0.f;
-    #pragma unroll 4
-    for (int c = c0; c <= c1; ++c) {
-        const float* p = slot(c);
-        const float2 ml = *reinterpret_cast<const float2*>(p + ROWS * D + 2 * rr);
-        const float f = ml.x == top ? 1.f : ex2(ml.x - top);
-        l = fmaf(ml.y, f, l);
-        #pragma unroll
-        for (int k = 0; k < PER; ++k) acc[k] = fmaf(p[rr * D + lane * PER + k], f, acc[k]);
-    }
-    const float inv = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
-    #pragma unroll
-    for (int k = 0; k < PER; ++k) out[k] = (T)(l == 0.f ? 0.f : acc[k] * inv);
-    if (lane == 0 && a.lse != nullptr)
-        a.lse[row * a.H + head] = l == 0.f ? NEG_INF : (log2f(l) + (top - HEAD)) * 0.6931471805599453f;
 }
 
 constexpr int CTAS_PER_SM = 2;
@@ -612,25 +432,22 @@ cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
     float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + prefix_bytes(a.B));
     kv_attention_kernel<T, D><<<ctas, THREADS, AttnSmem<T, D>::BYTES, s>>>(a, G, prefix, slots);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(((size_t)a.max_new * a.H + WARPS - 1) / WARPS), (unsigned)a.B);
-    cfg.blockDim = dim3(THREADS);
-    cfg.stream = s;
-    cudaLaunchAttribute at = pdl_attribute();
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kv_attention_join_kernel<T, D>, a, G, ctas, (const long long*)prefix,
-                              (const float*)slots);
+    return launch_join<T, D, ROWS, TILE>(a, G, ctas, ROWS, prefix, slots, s);
 }
 
 }  // namespace
 
+// More than 16 rows of a key/value head go to the tcgen05 kernel.
+static bool many_rows(const KvAttnArgs& a) { return (long long)a.max_new * (a.H / a.c.Hkv) > ROWS; }
+
 size_t kv_attention_workspace_bytes(int B, int max_new, int H, int Hkv, int D) {
-    (void)max_new; (void)H; (void)Hkv;
-    return prefix_bytes(B) + (size_t)num_sms() * CTAS_PER_SM * 2 * ROWS * (D + 2) * 4;
+    const long long rows = (long long)max_new * (H / Hkv);
+    return prefix_bytes(B) + (rows > ROWS ? kv_attention_tc_slot_bytes((int)(rows < 256 ? rows : 256), D)
+                                          : (size_t)num_sms() * CTAS_PER_SM * 2 * slot_floats(ROWS, D) * 4);
 }
 
 cudaError_t launch_kv_attention(const KvAttnArgs& a, cudaStream_t s) {
+    if (many_rows(a)) return launch_kv_attention_tc(a, s);
     if (a.dtype == STARQ_BF16)
         return a.c.D == 64 ? launch_typed<__nv_bfloat16, 64>(a, s) : launch_typed<__nv_bfloat16, 128>(a, s);
     return a.c.D == 64 ? launch_typed<__half, 64>(a, s) : launch_typed<__half, 128>(a, s);

@@ -1,0 +1,236 @@
+// What the two attention kernels over the 8-bit cache share (kvattn.cu: up
+// to 16 query rows of a key/value head; kvattn_tc.cu: more): the cutting of
+// all units' key tiles into one run per CTA, and the kernel that joins the
+// partial runs of a unit.
+//
+// A unit is a sequence, a key/value head and up to ROWS query rows (new
+// tokens x query heads of the group); its work is a list of key tiles of
+// TILE keys. The tiles of all units, in order, are cut into gridDim.x runs
+// of equal length. A unit inside one run is written at once; otherwise each
+// of its runs leaves, in slot 2 c (the run of CTA c begins with or inside the
+// unit) or 2 c + 1 (it ends in it), the rows' accumulators, maxima and sums.
+#pragma once
+
+#include <type_traits>
+
+#include "decode.cuh"
+
+namespace starq {
+namespace {
+
+constexpr float HEAD = 7.f;            // weights are 2^(x - m + HEAD)
+constexpr float LAZY = 8.f;            // m moves when x > m + LAZY
+constexpr float NEG_INF = -__builtin_huge_valf();
+
+// Workspace: prefix [B + 1] (tiles before each sequence), then the slots:
+// [rows][D] accumulators, then (m, l) for each row.
+constexpr size_t prefix_bytes(int B) { return ((size_t)(B + 1) * 8 + 255) / 256 * 256; }
+constexpr size_t slot_floats(int rows, int D) { return (size_t)rows * (D + 2); }
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Two bytes u (code + 128) in the low bytes of 0x64uu halves (1024 + u) to
+// the two codes in fp16, exactly.
+__device__ __forceinline__ uint32_t codes_half2(uint32_t biased) {
+    const __half2 k = __half2half2(__ushort_as_half((unsigned short)0x6480));       // 1152
+    __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&biased), k);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+
+// The power of two that brings a bf16 row with largest magnitude `top` into
+// fp16's range (its largest value to [2^14, 2^15)), and the one that undoes it.
+__device__ __forceinline__ void row_power(float top, float& up, float& down) {
+    const int e = max((int)(__float_as_uint(top) >> 23) - 127, -112);
+    up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
+    down = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
+}
+
+struct SeqShape { int len, n, row0, nt, rt; };       // cached tokens, new tokens, first row, key tiles, row tiles
+
+// The lengths of sequence b; a sequence whose numbers do not fit their
+// bounds counts as having no rows.
+template <int ROWS, int TILE>
+__device__ __forceinline__ SeqShape seq_shape(const KvAttnArgs& a, int G, int b, bool report) {
+    SeqShape s;
+    s.row0 = __ldg(a.seq_start + b);
+    s.n = __ldg(a.seq_start + b + 1) - s.row0;
+    s.len = __ldg(a.kv_len + b);
+    const bool bad = s.n < 0 || s.n > a.max_new || s.row0 < 0 || s.row0 > a.T - s.n || s.len < 0 || s.len > a.max_len;
+    if (bad) {
+        if (report) atomicOr(a.status, STATUS_RANGE);
+        s.n = 0; s.len = 0; s.row0 = 0;
+    }
+    s.nt = s.n > 0 ? (s.len + TILE - 1) / TILE : 0;
+    s.rt = (s.n * G + ROWS - 1) / ROWS;
+    return s;
+}
+
+// This CTA's run [tau0, tau1) of the flat list of tiles, the sequence that
+// tau0 falls into and the tiles before that sequence. CTA 0 writes `prefix`.
+struct Run { long long tau0, tau1, before; int b; };
+template <int ROWS, int TILE, int THREADS>
+__device__ __forceinline__ Run find_run(const KvAttnArgs& a, int G, long long* prefix) {
+    constexpr int WARPS = THREADS / 32;
+    __shared__ long long s_part[WARPS], s_before;
+    __shared__ int s_b;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    long long mine = 0;
+    for (int b = tid; b < a.B; b += THREADS) {
+        const SeqShape s = seq_shape<ROWS, TILE>(a, G, b, blockIdx.x == 0);
+        mine += (long long)s.nt * s.rt * a.c.Hkv;
+    }
+    #pragma unroll
+    for (int m = 16; m > 0; m >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, m);
+    if (lane == 0) s_part[warp] = mine;
+    if (tid == 0) { s_b = -1; s_before = 0; }
+    __syncthreads();
+    long long total = 0;
+    #pragma unroll
+    for (int w = 0; w < WARPS; ++w) total += s_part[w];
+    const long long share = (total + gridDim.x - 1) / gridDim.x;
+    Run r;
+    r.tau0 = share * blockIdx.x;
+    r.tau1 = min(total, r.tau0 + share);
+    r.b = -1;
+    r.before = 0;
+    if (r.tau0 >= total && blockIdx.x != 0) return r;
+    long long done = 0;                                       // tiles before the current chunk of sequences
+    for (int b0 = 0; b0 < a.B; b0 += THREADS) {
+        const int b = b0 + tid;
+        long long cnt = 0;
+        if (b < a.B) {
+            const SeqShape s = seq_shape<ROWS, TILE>(a, G, b, false);
+            cnt = (long long)s.nt * s.rt * a.c.Hkv;
+        }
+        long long inc = cnt;
+        #pragma unroll
+        for (int m = 1; m < 32; m <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, inc, m);
+            if (lane >= m) inc += v;
+        }
+        __syncthreads();
+        if (lane == 31) s_part[warp] = inc;
+        __syncthreads();
+        long long base = done;
+        for (int w = 0; w < warp; ++w) base += s_part[w];
+        const long long at = base + inc - cnt;
+        if (b < a.B) {
+            if (blockIdx.x == 0) prefix[b] = at;
+            if (cnt > 0 && r.tau0 >= at && r.tau0 < at + cnt) { s_b = b; s_before = at; }
+        }
+        for (int w = 0; w < WARPS; ++w) done += s_part[w];
+    }
+    if (tid == 0 && blockIdx.x == 0) prefix[a.B] = total;
+    __syncthreads();
+    r.b = s_b;
+    r.before = s_before;
+    return r;
+}
+
+// Position in the flat list of tiles: sequence, head, row tile, key tile.
+template <int ROWS, int TILE>
+struct Cursor {
+    int b, h, rt, kt;
+    SeqShape s;
+    __device__ __forceinline__ void start(const KvAttnArgs& a, int G, const Run& r) {
+        b = r.b;
+        s = seq_shape<ROWS, TILE>(a, G, b, false);
+        const long long off = r.tau0 - r.before, unit = off / s.nt;
+        kt = (int)(off - unit * s.nt);
+        h = (int)(unit / s.rt);
+        rt = (int)(unit - (long long)h * s.rt);
+    }
+    __device__ __forceinline__ void next_unit(const KvAttnArgs& a, int G) {
+        kt = 0;
+        if (++rt < s.rt) return;
+        rt = 0;
+        if (++h < a.c.Hkv) return;
+        h = 0;
+        do {
+            if (++b >= a.B) return;
+            s = seq_shape<ROWS, TILE>(a, G, b, false);
+        } while (s.nt == 0);
+    }
+};
+
+// One warp per query row: joins the partial runs of the row's unit in run
+// order, and writes the rows that no key reaches.
+constexpr int JOIN_WARPS = 4;
+template <typename T, int D, int ROWS, int TILE>
+__global__ void __launch_bounds__(JOIN_WARPS * 32)
+kv_attention_join_kernel(const KvAttnArgs a, int G, int ctas, int slot_rows, const long long* __restrict__ prefix,
+                         const float* __restrict__ slots) {
+    constexpr int PER = D / 32;
+    grid_dependency_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int b = blockIdx.y;
+    const SeqShape s = seq_shape<ROWS, TILE>(a, G, b, false);
+    const int idx = blockIdx.x * JOIN_WARPS + warp;            // token * H + head
+    const int i = idx / a.H, head = idx - i * a.H;
+    if (i >= s.n) return;
+    const size_t row = (size_t)(s.row0 + i);
+    T* out = static_cast<T*>(a.Out) + row * a.ldo + (size_t)head * D + lane * PER;
+    if (s.nt == 0) {
+        #pragma unroll
+        for (int k = 0; k < PER; ++k) out[k] = (T)0.f;
+        if (lane == 0 && a.lse != nullptr) a.lse[row * a.H + head] = NEG_INF;
+        return;
+    }
+    const int h = head / G, r = i * G + (head - h * G);
+    const int rt = r / ROWS, rr = r - rt * ROWS;
+    const long long total = prefix[a.B];
+    const long long share = (total + ctas - 1) / ctas;
+    const long long u0 = prefix[b] + ((long long)h * s.rt + rt) * s.nt;
+    const int c0 = (int)(u0 / share), c1 = (int)((u0 + s.nt - 1) / share);
+    if (c0 == c1) return;                                 // one run covered the unit
+    auto slot = [&](int c) {
+        return slots + ((size_t)c * 2 + (u0 > (long long)c * share ? 1 : 0)) * slot_floats(slot_rows, D);
+    };
+    // maximum over the runs, lanes side by side
+    float top = NEG_INF;
+    for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, slot(c)[(size_t)slot_rows * D + 2 * rr]);
+    #pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    float l = 0.f, acc[PER];
+    #pragma unroll
+    for (int k = 0; k < PER; ++k) acc[k] = 0.f;
+    #pragma unroll 4
+    for (int c = c0; c <= c1; ++c) {
+        const float* p = slot(c);
+        const float2 ml = *reinterpret_cast<const float2*>(p + (size_t)slot_rows * D + 2 * rr);
+        const float f = ml.x == top ? 1.f : ex2(ml.x - top);
+        l = fmaf(ml.y, f, l);
+        #pragma unroll
+        for (int k = 0; k < PER; ++k) acc[k] = fmaf(p[rr * D + lane * PER + k], f, acc[k]);
+    }
+    const float inv = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
+    #pragma unroll
+    for (int k = 0; k < PER; ++k) out[k] = (T)(l == 0.f ? 0.f : acc[k] * inv);
+    if (lane == 0 && a.lse != nullptr)
+        a.lse[row * a.H + head] = l == 0.f ? NEG_INF : (log2f(l) + (top - HEAD)) * 0.6931471805599453f;
+}
+
+template <typename T, int D, int ROWS, int TILE>
+cudaError_t launch_join(const KvAttnArgs& a, int G, int ctas, int slot_rows, const long long* prefix,
+                        const float* slots, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(((size_t)a.max_new * a.H + JOIN_WARPS - 1) / JOIN_WARPS), (unsigned)a.B);
+    cfg.blockDim = dim3(JOIN_WARPS * 32);
+    cfg.stream = s;
+    cudaLaunchAttribute at = pdl_attribute();
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kv_attention_join_kernel<T, D, ROWS, TILE>, a, G, ctas, slot_rows, prefix, slots);
+}
+
+}  // namespace
+
+// kvattn_tc.cu
+size_t kv_attention_tc_slot_bytes(int max_rows, int D);
+cudaError_t launch_kv_attention_tc(const KvAttnArgs& a, cudaStream_t s);
+
+}  // namespace starq
