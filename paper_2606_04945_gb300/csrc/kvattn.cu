@@ -47,8 +47,12 @@ constexpr int ROWS = 16;               // query rows of a unit
 constexpr int WKEYS = 16;              // keys of a warp in a tile
 constexpr int TILE = WARPS * WKEYS;    // 64 keys
 constexpr int STAGES = 4;
+constexpr int CTAS_PER_SM = 3;
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() {
@@ -106,14 +110,14 @@ __device__ __forceinline__ float load_row(const T* row, int t, uint32_t (&q)[D /
 
 template <typename T, int D>
 struct AttnSmem {
-    static constexpr int STAGE = 2 * WKEYS * D;                 // bytes of a warp's stage: keys, then values
+    static constexpr int STAGE = 2 * WKEYS * D + 16;            // bytes of a warp's stage: keys, values, their two scales
     static constexpr int RING = WARPS * STAGES * STAGE;
     static constexpr int MERGE = ROWS * D * 4 + WARPS * ROWS * 8;
     static constexpr int BYTES = RING + MERGE;
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(THREADS, 2) kv_attention_kernel(const KvAttnArgs a, int G, long long* prefix_out,
+__global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(const KvAttnArgs a, int G, long long* prefix_out,
                                                                  float* slots) {
     using SM = AttnSmem<T, D>;
     constexpr int KH = D / 64;               // 64-channel halves of a key
@@ -130,38 +134,39 @@ __global__ void __launch_bounds__(THREADS, 2) kv_attention_kernel(const KvAttnAr
     int pre_left = left;                     // tiles still to be fetched
 
     const uint32_t ring = smem_addr(smem) + warp * (STAGES * SM::STAGE);
+    const int shift = __ffs(a.c.page) - 1;
     const size_t block_bytes = (size_t)a.c.page * D;
+    // where this lane's 16-byte chunks go in a stage (rows D / 16 lanes apart repeat the pattern every 8 rows)
+    uint32_t dst_at[D / 32];
+    #pragma unroll
+    for (int i = 0; i < D / 32; ++i) dst_at[i] = stage_offset<D>((lane + 32 * i) / (D / 16), (lane + 32 * i) % (D / 16));
 
-    // Scales of the stages in flight: x = log2(e) scale s_k, y = s_v of the
-    // warp's 16 keys (a page holds a multiple of 16).
-    float sk[STAGES], sv[STAGES];
-    auto fetch = [&](int slot, float& k_out, float& v_out) {
-        k_out = 0.f; v_out = 1.f;
+    // One warp's 16 keys of the next tile (a page holds a multiple of 16, so they lie in one block).
+    auto fetch = [&](int slot) {
         if (pre_left > 0) {
             const int key0 = pre.kt * TILE + warp * WKEYS;
             if (key0 < pre.s.len) {
-                const int page_i = key0 / a.c.page;
+                const int page_i = key0 >> shift;
                 int page = -1;
                 if (page_i < a.table_ld) page = __ldg(a.page_table + (size_t)pre.b * a.table_ld + page_i);
+                const uint32_t dst = ring + slot * SM::STAGE;
                 if (page < 0 || page >= a.c.pages) {
-                    if (lane == 0) atomicOr(a.status, STATUS_RANGE);
-                    k_out = __uint_as_float(0x7fffffffu);      // the rows that see these keys become NaN
+                    if (lane == 0) {
+                        atomicOr(a.status, STATUS_RANGE);
+                        // the rows that see these keys become NaN
+                        asm volatile("st.shared.v2.b32 [%0], {%1, %2};"
+                                     :: "r"(dst + 2 * WKEYS * D), "r"(0x7fffffffu), "r"(0x3f800000u) : "memory");
+                    }
                 } else {
                     const size_t blk = (size_t)page * a.c.Hkv + pre.h;
-                    const size_t off = blk * block_bytes + (size_t)(key0 - page_i * a.c.page) * D;
-                    const uint32_t dst = ring + slot * SM::STAGE;
+                    const size_t off = blk * block_bytes + (size_t)(key0 & (a.c.page - 1)) * D + lane * 16;
+                    const uint8_t* k = a.c.K + off;
+                    const uint8_t* v = a.c.V + off;
                     #pragma unroll
-                    for (int i = 0; i < D / 32; ++i) {
-                        const int id = lane + 32 * i, r = id / (D / 16), c = id % (D / 16);
-                        cp_async16(dst + stage_offset<D>(r, c), a.c.K + off + id * 16);
-                    }
+                    for (int i = 0; i < D / 32; ++i) cp_async16(dst + dst_at[i], k + 512 * i);
                     #pragma unroll
-                    for (int i = 0; i < D / 32; ++i) {
-                        const int id = lane + 32 * i, r = id / (D / 16), c = id % (D / 16);
-                        cp_async16(dst + WKEYS * D + stage_offset<D>(r, c), a.c.V + off + id * 16);
-                    }
-                    k_out = __ldg(a.c.k_scale + blk);
-                    v_out = __ldg(a.c.v_scale + blk);
+                    for (int i = 0; i < D / 32; ++i) cp_async16(dst + WKEYS * D + dst_at[i], v + 512 * i);
+                    if (lane < 2) cp_async4(dst + 2 * WKEYS * D + 4 * lane, (lane ? a.c.v_scale : a.c.k_scale) + blk);
                 }
             }
             --pre_left;
@@ -170,7 +175,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_attention_kernel(const KvAttnAr
         cp_async_commit();
     };
     #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) fetch(i, sk[i], sv[i]);
+    for (int i = 0; i < STAGES - 1; ++i) fetch(i);
 
     uint32_t qf[KH][4][4];
     float o[DN][4], m[2], l[2], rs[2];
@@ -180,10 +185,10 @@ __global__ void __launch_bounds__(THREADS, 2) kv_attention_kernel(const KvAttnAr
     int seg_kt0 = cur.kt;
     int tau = 0;                             // tiles done
 
+    int st = 0;
+    #pragma unroll 1
     while (left > 0) {
-        #pragma unroll
-        for (int st = 0; st < STAGES; ++st) {
-            if (left <= 0) break;
+        {
             if (fresh) {                     // a new unit: its query rows
                 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
@@ -210,7 +215,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_attention_kernel(const KvAttnAr
                 fresh = false;
                 seg_kt0 = cur.kt;
             }
-            fetch((st + STAGES - 1) % STAGES, sk[(st + STAGES - 1) % STAGES], sv[(st + STAGES - 1) % STAGES]);
+            fetch((st + STAGES - 1) % STAGES);
             cp_async_wait<STAGES - 1>();
             __syncwarp();
             const int key0 = cur.kt * TILE + warp * WKEYS;
@@ -220,21 +225,25 @@ __global__ void __launch_bounds__(THREADS, 2) kv_attention_kernel(const KvAttnAr
                 float x[2][4];
                 #pragma unroll
                 for (int nt = 0; nt < 2; ++nt) {
-                    #pragma unroll
-                    for (int k = 0; k < 4; ++k) x[nt][k] = 0.f;
+                    float part[KH][4];               // a chain for each half of the channels
                     #pragma unroll
                     for (int h = 0; h < KH; ++h) {
+                        #pragma unroll
+                        for (int k = 0; k < 4; ++k) part[h][k] = 0.f;
                         const uint4 w = *reinterpret_cast<const uint4*>(stage + stage_offset<D>(nt * 8 + g, 4 * h + t));
                         const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
                         #pragma unroll
                         for (int s = 0; s < 4; ++s)
-                            mma_16816(x[nt], qf[h][s], codes_half2(prmt(ws[s], 0x64646464u, 0x4140u)),
+                            mma_16816(part[h], qf[h][s], codes_half2(prmt(ws[s], 0x64646464u, 0x4140u)),
                                       codes_half2(prmt(ws[s], 0x64646464u, 0x4342u)));
                     }
+                    #pragma unroll
+                    for (int k = 0; k < 4; ++k) x[nt][k] = KH == 2 ? part[0][k] + part[KH - 1][k] : part[0][k];
                 }
-                const float ks = sk[st] * unit_scale;
+                const float2 scales = *reinterpret_cast<const float2*>(stage + 2 * WKEYS * D);
+                const float ks = scales.x * unit_scale;
                 // a value scale below the floor counts as the floor (an empty block's codes are 0)
-                const float vs = sv[st] < KV_SCALE_FLOOR ? KV_SCALE_FLOOR : sv[st];
+                const float vs = scales.y < KV_SCALE_FLOOR ? KV_SCALE_FLOOR : scales.y;
                 const float lv = __log2f(vs), iv = __fdividef(1.f, vs);
                 const float k0 = ks * rs[0], k1 = ks * rs[1];
                 #pragma unroll
@@ -325,6 +334,7 @@ __global__ void __launch_bounds__(THREADS, 2) kv_attention_kernel(const KvAttnAr
                 }
             }
             __syncwarp();
+            st = (st + 1) % STAGES;
             --left;
             ++tau;
             if (++cur.kt == cur.s.nt || left == 0) {
@@ -413,8 +423,6 @@ __global__ void __launch_bounds__(THREADS, 2) kv_attention_kernel(const KvAttnAr
     }
     cp_async_wait<0>();
 }
-
-constexpr int CTAS_PER_SM = 2;
 
 template <typename T, int D>
 cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {

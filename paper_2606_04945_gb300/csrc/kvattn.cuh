@@ -78,51 +78,56 @@ __device__ __forceinline__ Run find_run(const KvAttnArgs& a, int G, long long* p
     __shared__ long long s_part[WARPS], s_before;
     __shared__ int s_b;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    long long mine = 0;
-    for (int b = tid; b < a.B; b += THREADS) {
-        const SeqShape s = seq_shape<ROWS, TILE>(a, G, b, blockIdx.x == 0);
-        mine += (long long)s.nt * s.rt * a.c.Hkv;
-    }
-    #pragma unroll
-    for (int m = 16; m > 0; m >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, m);
-    if (lane == 0) s_part[warp] = mine;
+    auto tiles_of = [&](int b, bool report) {
+        if (b >= a.B) return 0ll;
+        const SeqShape s = seq_shape<ROWS, TILE>(a, G, b, report);
+        return (long long)s.nt * s.rt * a.c.Hkv;
+    };
+    // inclusive sums over the CTA's threads; part sums of the warps in s_part
+    auto scan = [&](long long v) {
+        #pragma unroll
+        for (int m = 1; m < 32; m <<= 1) {
+            const long long u = __shfl_up_sync(0xffffffffu, v, m);
+            if (lane >= m) v += u;
+        }
+        __syncthreads();
+        if (lane == 31) s_part[warp] = v;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) v += s_part[w];
+        return v;
+    };
     if (tid == 0) { s_b = -1; s_before = 0; }
-    __syncthreads();
+    const long long first = tiles_of(tid, blockIdx.x == 0);   // the first THREADS sequences: read once
+    const long long first_sum = scan(first);
     long long total = 0;
-    #pragma unroll
     for (int w = 0; w < WARPS; ++w) total += s_part[w];
+    long long rest = 0;
+    for (int b = tid + THREADS; b < a.B; b += THREADS) rest += tiles_of(b, blockIdx.x == 0);
+    if (a.B > THREADS) {
+        scan(rest);
+        for (int w = 0; w < WARPS; ++w) total += s_part[w];
+    }
     const long long share = (total + gridDim.x - 1) / gridDim.x;
     Run r;
     r.tau0 = share * blockIdx.x;
     r.tau1 = min(total, r.tau0 + share);
     r.b = -1;
     r.before = 0;
-    if (r.tau0 >= total && blockIdx.x != 0) return r;
     long long done = 0;                                       // tiles before the current chunk of sequences
     for (int b0 = 0; b0 < a.B; b0 += THREADS) {
         const int b = b0 + tid;
-        long long cnt = 0;
-        if (b < a.B) {
-            const SeqShape s = seq_shape<ROWS, TILE>(a, G, b, false);
-            cnt = (long long)s.nt * s.rt * a.c.Hkv;
-        }
-        long long inc = cnt;
-        #pragma unroll
-        for (int m = 1; m < 32; m <<= 1) {
-            const long long v = __shfl_up_sync(0xffffffffu, inc, m);
-            if (lane >= m) inc += v;
-        }
-        __syncthreads();
-        if (lane == 31) s_part[warp] = inc;
-        __syncthreads();
-        long long base = done;
-        for (int w = 0; w < warp; ++w) base += s_part[w];
-        const long long at = base + inc - cnt;
+        const long long cnt = b0 == 0 ? first : tiles_of(b, false);
+        const long long at = done + (b0 == 0 ? first_sum : scan(cnt)) - cnt;
         if (b < a.B) {
             if (blockIdx.x == 0) prefix[b] = at;
             if (cnt > 0 && r.tau0 >= at && r.tau0 < at + cnt) { s_b = b; s_before = at; }
         }
-        for (int w = 0; w < WARPS; ++w) done += s_part[w];
+        if (b0 + THREADS < a.B) {                             // the chunk's sum: its last thread's
+            __shared__ long long s_done;
+            if (tid == THREADS - 1) s_done = at + cnt;
+            __syncthreads();
+            done = s_done;
+        }
     }
     if (tid == 0 && blockIdx.x == 0) prefix[a.B] = total;
     __syncthreads();
@@ -183,29 +188,61 @@ kv_attention_join_kernel(const KvAttnArgs a, int G, int ctas, int slot_rows, con
     const int h = head / G, r = i * G + (head - h * G);
     const int rt = r / ROWS, rr = r - rt * ROWS;
     const long long total = prefix[a.B];
-    const long long share = (total + ctas - 1) / ctas;
-    const long long u0 = prefix[b] + ((long long)h * s.rt + rt) * s.nt;
-    const int c0 = (int)(u0 / share), c1 = (int)((u0 + s.nt - 1) / share);
+    const long long u0 = prefix[b] + (long long)(h * s.rt + rt) * s.nt;
+    // (64-bit divisions take a hundred instructions each; few lists need them)
+    long long share;
+    int c0, c1;
+    if (total < (1ll << 31)) {
+        const unsigned sh = ((unsigned)total + ctas - 1) / (unsigned)ctas;
+        share = sh;
+        c0 = (int)((unsigned)u0 / sh);
+        c1 = (int)((unsigned)(u0 + s.nt - 1) / sh);
+    } else {
+        share = (total + ctas - 1) / ctas;
+        c0 = (int)(u0 / share);
+        c1 = (int)((u0 + s.nt - 1) / share);
+    }
     if (c0 == c1) return;                                 // one run covered the unit
     auto slot = [&](int c) {
         return slots + ((size_t)c * 2 + (u0 > (long long)c * share ? 1 : 0)) * slot_floats(slot_rows, D);
     };
-    // maximum over the runs, lanes side by side
-    float top = NEG_INF;
-    for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, slot(c)[(size_t)slot_rows * D + 2 * rr]);
-    #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    float l = 0.f, acc[PER];
+    // AT_ONCE runs' loads in flight together; the running maximum moves between batches
+    constexpr int AT_ONCE = 8;
+    float top = NEG_INF, l = 0.f, acc[PER];
     #pragma unroll
     for (int k = 0; k < PER; ++k) acc[k] = 0.f;
-    #pragma unroll 4
-    for (int c = c0; c <= c1; ++c) {
-        const float* p = slot(c);
-        const float2 ml = *reinterpret_cast<const float2*>(p + (size_t)slot_rows * D + 2 * rr);
-        const float f = ml.x == top ? 1.f : ex2(ml.x - top);
-        l = fmaf(ml.y, f, l);
+    for (int c = c0; c <= c1; c += AT_ONCE) {
+        float2 ml[AT_ONCE];
+        float v[AT_ONCE][PER];
         #pragma unroll
-        for (int k = 0; k < PER; ++k) acc[k] = fmaf(p[rr * D + lane * PER + k], f, acc[k]);
+        for (int q = 0; q < AT_ONCE; ++q) {
+            ml[q] = make_float2(NEG_INF, 0.f);
+            if (c + q <= c1) {
+                const float* p = slot(c + q);
+                ml[q] = *reinterpret_cast<const float2*>(p + (size_t)slot_rows * D + 2 * rr);
+                #pragma unroll
+                for (int k = 0; k < PER; k += 2) {
+                    const float2 w = *reinterpret_cast<const float2*>(p + rr * D + lane * PER + k);
+                    v[q][k] = w.x; v[q][k + 1] = w.y;
+                }
+            }
+        }
+        float to = top;
+        #pragma unroll
+        for (int q = 0; q < AT_ONCE; ++q) to = fmaxf(to, ml[q].x);
+        const float f0 = top == to ? 1.f : ex2(top - to);
+        top = to;
+        l *= f0;
+        #pragma unroll
+        for (int k = 0; k < PER; ++k) acc[k] *= f0;
+        #pragma unroll
+        for (int q = 0; q < AT_ONCE; ++q) {
+            if (c + q > c1) break;
+            const float f = ml[q].x == top ? 1.f : ex2(ml[q].x - top);
+            l = fmaf(ml[q].y, f, l);
+            #pragma unroll
+            for (int k = 0; k < PER; ++k) acc[k] = fmaf(v[q][k], f, acc[k]);
+        }
     }
     const float inv = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
     #pragma unroll

@@ -5,10 +5,12 @@
 // With R rows a cached key costs 4 R D operations for 2 D bytes, so from
 // about 100 rows on the tensor cores' work outweighs the cache's bytes; the
 // warp-level MMA would be the bound from 24 rows on. What has to be fed is
-// fp16 tiles: four warps read a tile's codes (128 keys) straight from their
-// pages, turn them into fp16 and store them as 128-byte-swizzled tiles, keys
-// and values alike; the value product takes its tile as an MN-major operand,
-// so no transposition is needed.
+// fp16 tiles: one warp brings a tile's codes (128 keys) from their pages by
+// bulk copies, three warps for the keys and three for the values turn them
+// into fp16 and store them as 128-byte-swizzled tiles; the value product
+// takes its tile as an MN-major operand, so no transposition is needed.
+// (Loads into the converting warps' registers had to wait for the proxy fence
+// of the last hand-over, and it for them.)
 //
 // A unit is up to 256 rows. Two streams, each with 128 TMEM lanes of rows,
 // its own scores, weights and accumulators, and four softmax warps (one
@@ -18,6 +20,12 @@
 // key tiles in turn, with the same rows, and their results are joined in
 // shared memory at the end. Weights replace the scores they came from in
 // TMEM (A operand from tensor memory). Warps without rows skip the softmax.
+//
+// A key that no row sees (masked out, or past the length) costs the softmax
+// nothing: its place in the tile takes the codes of another key of its
+// 16-key block that is seen (so no score is above those that count), values
+// of 0, and a factor of 0 in the sum. A block without such a key has scores
+// of -inf. Only the causal boundary is tested score by score.
 #include <algorithm>
 
 #include "kvattn.cuh"
@@ -28,33 +36,41 @@ namespace {
 constexpr unsigned STATUS_TIMEOUT_KVATTN = 1u << 5;
 constexpr int ROWS = 256;                          // rows of a unit
 constexpr int TILE = 128;                          // keys of a tile, rows of a stream
-constexpr int SOFT_WARPS = 8, CONV_WARPS = 4;
-constexpr int MMA_WARP = SOFT_WARPS + CONV_WARPS;
+constexpr int SOFT_WARPS = 8, CONV_WARPS = 3;      // CONV_WARPS for the keys, as many for the values
+constexpr int INFO_WARP = SOFT_WARPS + 2 * CONV_WARPS, MMA_WARP = INFO_WARP + 1;
 constexpr int THREADS = (MMA_WARP + 1) * 32;
 constexpr int CONV_THREADS = CONV_WARPS * 32;
-constexpr int STAGES = 2;
+// fp16 tiles (the keys' scores are taken soon after a tile is there, the
+// values wait for the softmax), and tiles of codes
+constexpr int K_STAGES = 1, V_STAGES = 1, CK_STAGES = 3, CV_STAGES = 2;
+constexpr int INFOS = 4;                           // descriptions of tiles
 constexpr uint32_t TM_S = 0, TM_O = 256;           // TMEM columns: two score tiles, two accumulators
 constexpr int BLOCKS = TILE / 16;                  // 16-key blocks of a tile (each inside one page)
 
-struct TileInfo {                                  // what the softmax needs of a key tile
+struct TileInfo {                                  // what the other warps need of a key tile
     float4 blk[BLOCKS];                            // log2(e) scale s_k, log2 s_v, 1 / s_v
-    float bias[TILE];                              // with a key mask: 0, or -inf for a key that is not seen
-    int key0, edge;                                // first key; whether keys past the length or a mask concern it
+    float inv[TILE];                               // 1 / s_v for each key, 0 for one that is not seen
+    uint32_t seen[4];                              // bit b of word j: key 4 b + j is seen
+    uint32_t met;                                  // bit b: some key of block b is seen
+    int key0, edge;                                // first key; whether the causal boundary is inside
 };
 
 struct Shared {
-    uint64_t k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES], info[STAGES];
-    uint64_t q_full, s_full[2], p_full[2], pv_done[2], meet;
+    uint64_t k_full[K_STAGES], k_empty[K_STAGES], v_full[V_STAGES], v_empty[V_STAGES], info[INFOS], info_empty[INFOS];
+    uint64_t ck_full[CK_STAGES], ck_empty[CK_STAGES], cv_full[CV_STAGES], cv_empty[CV_STAGES];
+    uint64_t q_full, meet, s_full[2], p_full[2], pv_done[2];
     uint32_t tmem_base;
     int abort;
-    alignas(16) TileInfo tile[STAGES];
+    alignas(16) TileInfo tile[INFOS];
     float2 ml[TILE];                               // the odd stream's (m, l) for the join of the two
 };
 
 template <int D> struct Layout {
     static constexpr int TILE_BYTES = TILE * D * 2;                  // fp16, 64-channel halves of 16 KB
     static constexpr int HALF = TILE * 128;
-    static constexpr int Q = 0, K = 2 * TILE_BYTES, V = K + STAGES * TILE_BYTES, END = V + STAGES * TILE_BYTES;
+    static constexpr int CODES = TILE * D;                           // bytes of a tile's codes (keys or values)
+    static constexpr int Q = 0, K = 2 * TILE_BYTES, V = K + K_STAGES * TILE_BYTES, CK = V + V_STAGES * TILE_BYTES;
+    static constexpr int CV = CK + CK_STAGES * CODES, END = CV + CV_STAGES * CODES;
     // the join of the two streams uses a 128 x D float32 area over Q (and, for
     // D = 64, exactly Q's two tiles)
     static constexpr int SMEM = END + 1024 + (int)sizeof(Shared);
@@ -95,6 +111,26 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 
+// Whole-warp wait of the roles that run ahead: polls 40 ns apart, so that they
+// leave the issue slots to the softmax.
+__device__ __forceinline__ bool wait_idle(uint32_t bar, uint32_t parity, volatile int* abort) {
+    const bool ok = mbar_try_wait(bar, parity) || mbar_wait_bounded_sleepy(bar, parity, abort, 40);
+    return __all_sync(0xffffffffu, ok);
+}
+
+// Whether the phase is complete, without waiting (try_wait may suspend the thread).
+__device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+
+// max(a, b), NaN if a is.
+__device__ __forceinline__ float fmaxf_nan(float a, float b) { return a < b ? b : a; }
+
 // 16 codes of a row, channels 16 c .. 16 c + 15, as fp16 into row r of a
 // tile. Threads whose channels lie in the upper half store their two chunks
 // in the other order, so that a quarter warp covers all banks.
@@ -131,17 +167,26 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
     volatile int* abort = &sh->abort;
     auto B = [](const uint64_t& bar) { return smem_addr(&bar); };
 
-    const Run run = find_run<ROWS, TILE, THREADS>(a, G, prefix);
-    if (run.tau0 >= run.tau1) return;
-    const int count = (int)(run.tau1 - run.tau0);
-
     if (threadIdx.x == 0) {
-        for (int i = 0; i < STAGES; ++i) {
+        for (int i = 0; i < K_STAGES; ++i) {
             mbar_init(B(sh->k_full[i]), CONV_WARPS);
-            mbar_init(B(sh->v_full[i]), CONV_WARPS);
-            mbar_init(B(sh->info[i]), 1);
             mbar_init(B(sh->k_empty[i]), 1);
+        }
+        for (int i = 0; i < V_STAGES; ++i) {
+            mbar_init(B(sh->v_full[i]), CONV_WARPS);
             mbar_init(B(sh->v_empty[i]), 1);
+        }
+        for (int i = 0; i < CK_STAGES; ++i) {
+            mbar_init(B(sh->ck_full[i]), 1);
+            mbar_init(B(sh->ck_empty[i]), CONV_WARPS);
+        }
+        for (int i = 0; i < CV_STAGES; ++i) {
+            mbar_init(B(sh->cv_full[i]), 1);
+            mbar_init(B(sh->cv_empty[i]), CONV_WARPS);
+        }
+        for (int i = 0; i < INFOS; ++i) {
+            mbar_init(B(sh->info[i]), 1);
+            mbar_init(B(sh->info_empty[i]), 1);
         }
         mbar_init(B(sh->q_full), SOFT_WARPS);
         mbar_init(B(sh->meet), SOFT_WARPS);
@@ -161,120 +206,185 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sh->tmem_base;
-    bool ok = true;
+    const Run run = find_run<ROWS, TILE, THREADS>(a, G, prefix);
+    const int count = (int)(run.tau1 - run.tau0);
+    bool ok = count > 0;
 
     // Every role walks the run segment by segment (a segment is the run's
     // part of one unit). In a segment of n key tiles the streams' steps are
     // items: shared = 1 (more than 128 rows): item u is key tile u / 2 for
-    // stream u & 1; shared = 0: key tile u for stream u & 1.
+    // stream u & 1; shared = 0: key tile u for stream u & 1. Either way it is
+    // the stream's step u / 2 of the segment.
     Cur cur;
-    cur.start(a, G, run);
+    if (count > 0) cur.start(a, G, run);
     auto unit_rows = [&](const Cur& c) { return min(ROWS, c.s.n * G - c.rt * ROWS); };
     auto segment = [&](const Cur& c, int left) { return min(left, c.s.nt - c.kt); };
 
-    if (warp >= SOFT_WARPS && warp < MMA_WARP) {
-        // --- codes to fp16 tiles ------------------------------------------------
-        const int ct = threadIdx.x - SOFT_WARPS * 32, cw = warp - SOFT_WARPS;
-        constexpr int CPR = D / 16;                          // 16-code chunks of a row
-        constexpr int PER = TILE * CPR / CONV_THREADS;       // chunks of a thread
-        const int c = ct % CPR, r0 = ct / CPR;               // its channels, its rows r0 + RSTEP i
-        constexpr int RSTEP = CONV_THREADS / CPR;
-        uint4 kreg[PER], vreg[PER];
-        const int shift = __ffs(a.c.page) - 1;
-        const size_t row_of_head = (size_t)a.c.page * D;
-        // page number of a key of the cursor's tile, -1 past the length or outside the cache
-        auto page_of = [&](const Cur& q, int key) {
-            if (key >= q.s.len) return -1;
-            const int i = key >> shift;
-            if (i >= a.table_ld) return -2;
-            const int p = __ldg(a.page_table + (size_t)q.b * a.table_ld + i);
-            return p < 0 || p >= a.c.pages ? -2 : p;
+    if (count <= 0) {
+        // nothing but the release of TMEM
+    } else if (warp == INFO_WARP) {
+        // --- the tiles' descriptions and codes; lane b < 8 looks after block b -----------
+        // A tile's page numbers are loaded two tiles ahead, its scales and mask
+        // bytes one ahead (in a row they were 3 of 5 thousand cycles a tile).
+        const int shift = __ffs(a.c.page) - 1, b = lane & (BLOCKS - 1);
+        auto advance = [&](Cur& q, int& left) {
+            if (--left > 0 && ++q.kt == q.s.nt) q.next_unit(a, G);
         };
-        auto load = [&](const Cur& q, const uint8_t* src, uint4 (&reg)[PER]) {
+        auto page_of = [&](const Cur& q) {
+            const int key = q.kt * TILE + 16 * b, i = key >> shift;
+            int p = -1;
+            if (key < q.s.len && i < a.table_ld) p = __ldg(a.page_table + (size_t)q.b * a.table_ld + i);
+            return p;
+        };
+        struct Raw { int page; float sk, sv; uint8_t mask[4]; };
+        auto raw_of = [&](const Cur& q, int page) {
+            Raw r;
+            r.page = page < a.c.pages ? page : -1;
+            r.sk = r.sv = 0.f;
+            if (r.page >= 0) {
+                const size_t blk = (size_t)r.page * a.c.Hkv + q.h;
+                r.sk = __ldg(a.c.k_scale + blk);
+                r.sv = __ldg(a.c.v_scale + blk);
+            }
+            #pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int key = q.kt * TILE + 4 * lane + j;
+                r.mask[j] = key < q.s.len;
+                if (r.mask[j] && a.key_mask != nullptr) r.mask[j] = __ldg(a.key_mask + (size_t)q.b * a.mask_ld + key);
+            }
+            return r;
+        };
+        Cur ahead = cur;                                     // two tiles ahead of `cur`, then one
+        int left_ahead = count;
+        Raw raw = raw_of(cur, page_of(cur));
+        advance(ahead, left_ahead);
+        Cur nxt = ahead;
+        int next_page = left_ahead > 0 ? page_of(nxt) : -1;
+        for (int it = 0; it < count; ++it) {
+            const int key0 = cur.kt * TILE, slot = it % INFOS;
+            Raw raw_next = raw;
+            if (left_ahead > 0) raw_next = raw_of(nxt, next_page);
+            advance(ahead, left_ahead);
+            if (left_ahead > 0) next_page = page_of(ahead);
+            // which keys are seen: bit lane of word j is key 4 lane + j
+            uint32_t seen[4];
+            #pragma unroll
+            for (int j = 0; j < 4; ++j) seen[j] = __ballot_sync(0xffffffffu, raw.mask[j] != 0);
+            const int page = raw.page;
+            const bool any = ((seen[0] | seen[1] | seen[2] | seen[3]) >> (4 * b) & 0xf) != 0;
+            const size_t blk = (size_t)(page < 0 ? 0 : page) * a.c.Hkv + cur.h;
+            const unsigned met = __ballot_sync(0xffffffffu, any) & 0xff;
+            const bool fetch = any && page >= 0 && lane < BLOCKS;
+            const unsigned fetched = __popc(__ballot_sync(0xffffffffu, fetch));
+            const size_t at = blk * ((size_t)a.c.page * D) + (size_t)((key0 + 16 * b) & (a.c.page - 1)) * D;
+            float4 d = make_float4(0.f, NEG_INF, 0.f, 0.f);
+            if (any && page >= 0) {
+                const float vs = raw.sv < KV_SCALE_FLOOR ? KV_SCALE_FLOOR : raw.sv;
+                d = make_float4(fmaxf_nan(raw.sk, 1e-37f) * (a.scale * 1.4426950408889634f), __log2f(vs),
+                                __fdividef(1.f, vs), 0.f);
+            } else if (any) {
+                if (lane < BLOCKS) atomicOr(a.status, STATUS_RANGE);
+                d = make_float4(__uint_as_float(0x7fffffffu), 0.f, 1.f, 0.f);      // the rows that see it become NaN
+            }
+            const int edge = a.causal && key0 + TILE > cur.s.len - cur.s.n + 1;
+            cur = nxt;
+            nxt = ahead;
+            raw = raw_next;
+            ok = wait_idle(B(sh->info_empty[slot]), ((uint32_t)(it / INFOS) & 1u) ^ 1u, abort);
+            if (!ok) break;
+            TileInfo& ti = sh->tile[slot];
+            if (lane < BLOCKS) ti.blk[lane] = d;
+            const float iv = __shfl_sync(0xffffffffu, d.z, lane >> 2);
+            *reinterpret_cast<float4*>(ti.inv + 4 * lane) =
+                make_float4(seen[0] >> lane & 1 ? iv : 0.f, seen[1] >> lane & 1 ? iv : 0.f,
+                            seen[2] >> lane & 1 ? iv : 0.f, seen[3] >> lane & 1 ? iv : 0.f);
+            if (lane == 0) {
+                ti.met = met;
+                ti.seen[0] = seen[0]; ti.seen[1] = seen[1]; ti.seen[2] = seen[2]; ti.seen[3] = seen[3];
+                ti.key0 = key0;
+                ti.edge = edge;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(B(sh->info[slot]));
+            // the codes: one bulk copy a block
+            auto bring = [&](int st, int stages, uint64_t* full, uint64_t* empty, uint32_t area, const uint8_t* codes) {
+                if (!wait_idle(B(empty[st]), ((uint32_t)(it / stages) & 1u) ^ 1u, abort)) return false;
+                const uint32_t bar = B(full[st]);
+                if (lane == 0) mbar_arrive_expect_tx(bar, fetched * (16 * D));
+                __syncwarp();
+                if (fetch) bulk_load(base + area + st * L::CODES + b * (16 * D), codes + at, 16 * D, bar);
+                return true;
+            };
+            ok = bring(it % CK_STAGES, CK_STAGES, sh->ck_full, sh->ck_empty, L::CK, a.c.K) &&
+                 bring(it % CV_STAGES, CV_STAGES, sh->cv_full, sh->cv_empty, L::CV, a.c.V);
+            if (!ok) break;
+        }
+        // no commit lands after this CTA has exited
+        for (int st = 0; st < INFOS && ok; ++st) {
+            const int uses = (count - st + INFOS - 1) / INFOS;
+            if (uses > 0) ok = wait_idle(B(sh->info_empty[st]), (uint32_t)(uses - 1) & 1u, abort);
+        }
+        if (!ok && lane == 0) { sh->abort = 1; atomicOr(a.status, STATUS_TIMEOUT_KVATTN); }
+    } else if (warp >= SOFT_WARPS && warp < INFO_WARP) {
+        // --- codes to fp16 tiles: keys or values ------------------------------------
+        const bool keys = warp < SOFT_WARPS + CONV_WARPS;
+        const int ct = threadIdx.x - SOFT_WARPS * 32 - (keys ? 0 : CONV_THREADS);
+        constexpr int CPR = D / 16;                          // 16-code chunks of a row
+        constexpr int RSTEP = CONV_THREADS / CPR;            // 12 or 24 rows
+        constexpr int PER = (TILE + RSTEP - 1) / RSTEP;      // chunks of a thread
+        const int c = ct % CPR, r0 = ct / CPR;               // its channels, its rows r0 + RSTEP i
+        const int stages = keys ? K_STAGES : V_STAGES, cstages = keys ? CK_STAGES : CV_STAGES;
+        const uint32_t tiles = base + (keys ? L::K : L::V);
+        const uint8_t* const codes = smem + (keys ? L::CK : L::CV) + 16 * c;
+        uint64_t* const full_bar = keys ? sh->k_full : sh->v_full;
+        uint64_t* const empty_bar = keys ? sh->k_empty : sh->v_empty;
+        uint64_t* const cfull_bar = keys ? sh->ck_full : sh->cv_full;
+        uint64_t* const cempty_bar = keys ? sh->ck_empty : sh->cv_empty;
+        for (int it = 0; it < count && ok; ++it) {
+            const int st = it % stages, cs = it % cstages;
+            ok = wait_idle(B(sh->info[it % INFOS]), (uint32_t)(it / INFOS) & 1u, abort) &&
+                 wait_idle(B(cfull_bar[cs]), (uint32_t)(it / cstages) & 1u, abort);
+            if (!ok) break;
+            const TileInfo& ti = sh->tile[it % INFOS];
+            const uint32_t w0 = ti.seen[0], w1 = ti.seen[1], w2 = ti.seen[2], w3 = ti.seen[3];
+            const bool full = (w0 & w1 & w2 & w3) == 0xffffffffu;
+            // this thread's rows are r0 modulo 4
+            const uint32_t mine = (r0 & 2) ? ((r0 & 1) ? w3 : w2) : ((r0 & 1) ? w1 : w0);
+            uint4 v[PER];                                    // all loads before the first store
             #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int key = q.kt * TILE + r0 + RSTEP * i, p = page_of(q, key);
-                reg[i] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);   // codes 0
-                if (p >= 0)
-                    reg[i] = ld_global_nc_v4(src + ((size_t)p * a.c.Hkv + q.h) * row_of_head +
-                                             (size_t)(key & (a.c.page - 1)) * D + 16 * c);
-            }
-        };
-        Cur nxt = cur;
-        int left = count;
-        load(nxt, a.c.K, kreg);
-        load(nxt, a.c.V, vreg);
-        for (int it = 0; it < count && ok; ++it) {
-            const int st = it % STAGES;
-            const uint32_t parity = (uint32_t)(it / STAGES) & 1u;
-            cur = nxt;
-            --left;
-            if (++nxt.kt == nxt.s.nt && left > 0) nxt.next_unit(a, G);
-            ok = mbar_wait_bounded_warp(B(sh->k_empty[st]), parity ^ 1u, abort);
-            if (!ok) break;
-            #pragma unroll
-            for (int i = 0; i < PER; ++i) store_codes<D>(base + L::K + st * L::TILE_BYTES, r0 + RSTEP * i, c, kreg[i]);
-            if (left > 0) load(nxt, a.c.K, kreg);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(B(sh->k_full[st]));
-            ok = mbar_wait_bounded_warp(B(sh->v_empty[st]), parity ^ 1u, abort);
-            if (!ok) break;
-            if (cw == 0) {
-                // the tile's scales and mask (the values' stage is free, so the softmax is done with the last ones)
-                TileInfo& ti = sh->tile[st];
-                const int key0 = cur.kt * TILE;
-                bool none = true;                            // this lane's 4 keys are all masked or past the length
-                if (a.key_mask != nullptr) {
-                    #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = key0 + 4 * lane + i;
-                        const bool see = key < cur.s.len &&
-                                         __ldg(a.key_mask + (size_t)cur.b * a.mask_ld + key) != 0;
-                        ti.bias[4 * lane + i] = see ? 0.f : NEG_INF;
-                        none = none && !see;
-                    }
-                } else {
-                    none = key0 + (lane & ~3) * 4 >= cur.s.len;
-                }
-                const unsigned hidden = __ballot_sync(0xffffffffu, none);
-                if (lane < BLOCKS) {
-                    float4 b = make_float4(0.f, 0.f, 1.f, 0.f);
-                    if ((hidden >> (4 * lane) & 0xf) != 0xf) {   // some key counts
-                        const int p = page_of(cur, key0 + 16 * lane);
-                        if (p >= 0) {
-                            const size_t blk = (size_t)p * a.c.Hkv + cur.h;
-                            const float sv = __ldg(a.c.v_scale + blk), vs = sv < KV_SCALE_FLOOR ? KV_SCALE_FLOOR : sv;
-                            b = make_float4(__ldg(a.c.k_scale + blk) * (a.scale * 1.4426950408889634f), __log2f(vs),
-                                            __fdividef(1.f, vs), 0.f);
-                        } else {
-                            atomicOr(a.status, STATUS_RANGE);
-                            b.x = __uint_as_float(0x7fffffffu);
+                const int r = min(r0 + RSTEP * i, TILE - 1);
+                int from = r;                                // the row whose codes stand here, -1: zeros
+                if (!full && !(mine >> (r >> 2) & 1)) {
+                    from = -1;
+                    if (keys) {                              // some key of the block that is seen
+                        const int q = 4 * (r >> 4);
+                        const unsigned n0 = w0 >> q & 0xf, n1 = w1 >> q & 0xf, n2 = w2 >> q & 0xf, n3 = w3 >> q & 0xf;
+                        if (n0 | n1 | n2 | n3) {
+                            const unsigned n = n0 ? n0 : n1 ? n1 : n2 ? n2 : n3;
+                            from = (r & ~15) + 4 * (__ffs(n) - 1) + (n0 ? 0 : n1 ? 1 : n2 ? 2 : 3);
                         }
                     }
-                    ti.blk[lane] = b;
                 }
-                if (lane == 0) {
-                    ti.key0 = key0;
-                    ti.edge = a.key_mask != nullptr || key0 + TILE > cur.s.len ||
-                              (a.causal && key0 + TILE > cur.s.len - cur.s.n + 1);
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(B(sh->info[st]));
+                v[i] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);      // codes 0
+                if (from >= 0) v[i] = *reinterpret_cast<const uint4*>(codes + cs * L::CODES + from * D);
             }
+            ok = wait_idle(B(empty_bar[st]), ((uint32_t)(it / stages) & 1u) ^ 1u, abort);
+            if (!ok) break;
             #pragma unroll
-            for (int i = 0; i < PER; ++i) store_codes<D>(base + L::V + st * L::TILE_BYTES, r0 + RSTEP * i, c, vreg[i]);
-            if (left > 0) load(nxt, a.c.V, vreg);
+            for (int i = 0; i < PER; ++i)
+                if (r0 + RSTEP * i < TILE) store_codes<D>(tiles + st * L::TILE_BYTES, r0 + RSTEP * i, c, v[i]);
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(B(sh->v_full[st]));
+            if (lane == 0) {
+                mbar_arrive(B(cempty_bar[cs]));
+                mbar_arrive(B(full_bar[st]));
+            }
         }
         // the last use of every stage has been given back, so no commit lands after this CTA has exited
-        for (int st = 0; st < STAGES && ok; ++st) {
-            const int uses = (count - st + STAGES - 1) / STAGES;
-            if (uses > 0)
-                ok = mbar_wait_bounded_warp(B(sh->k_empty[st]), (uint32_t)(uses - 1) & 1u, abort) &&
-                     mbar_wait_bounded_warp(B(sh->v_empty[st]), (uint32_t)(uses - 1) & 1u, abort);
+        for (int st = 0; st < stages && ok; ++st) {
+            const int uses = (count - st + stages - 1) / stages;
+            if (uses > 0) ok = wait_idle(B(empty_bar[st]), (uint32_t)(uses - 1) & 1u, abort);
         }
         if (!ok && lane == 0) { sh->abort = 1; atomicOr(a.status, STATUS_TIMEOUT_KVATTN); }
     } else if (warp == MMA_WARP) {
@@ -288,9 +398,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
             const int shared = unit_rows(cur) > TILE;
             const int items = shared ? 2 * n : n;
             ok = mbar_wait_bounded_warp(B(sh->q_full), (uint32_t)seg & 1u, abort);
-            auto qk = [&](int u) {
-                const int kt = tile0 + (shared ? u >> 1 : u), st = kt % STAGES, s = u & 1;
-                if (!mbar_wait_bounded_warp(B(sh->k_full[st]), (uint32_t)(kt / STAGES) & 1u, abort)) return false;
+            auto qk = [&](int u, bool seen_k) {
+                const int kt = tile0 + (shared ? u >> 1 : u), st = kt % K_STAGES, s = u & 1;
+                if (!seen_k && !mbar_wait_bounded_warp(B(sh->k_full[st]), (uint32_t)(kt / K_STAGES) & 1u, abort))
+                    return false;
                 tc_fence_after();
                 if (elect_one()) {
                     const uint64_t qd = smem_desc_sw128(base + L::Q + (shared ? s : 0) * L::TILE_BYTES);
@@ -306,24 +417,30 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                 __syncwarp();
                 return true;
             };
-            for (int u = 0; u < 2 && u < items && ok; ++u) ok = qk(u);
+            for (int u = 0; u < 2 && u < items && ok; ++u) ok = qk(u, false);
             for (int u = 0; u < items && ok; ++u) {
-                const int kt = tile0 + (shared ? u >> 1 : u), st = kt % STAGES, s = u & 1, step = u >> 1;
-                ok = mbar_wait_bounded_warp(B(sh->p_full[s]), (uint32_t)(steps[s] + step) & 1u, abort) &&
-                     mbar_wait_bounded_warp(B(sh->v_full[st]), (uint32_t)(kt / STAGES) & 1u, abort);
+                const int kt = tile0 + (shared ? u >> 1 : u), st = kt % V_STAGES, s = u & 1, step = u >> 1;
+                const int kn = tile0 + (shared ? (u + 2) >> 1 : u + 2);
+                ok = mbar_wait_bounded_warp(B(sh->v_full[st]), (uint32_t)(kt / V_STAGES) & 1u, abort) &&
+                     mbar_wait_bounded_warp(B(sh->p_full[s]), (uint32_t)(steps[s] + step) & 1u, abort);
                 if (!ok) break;
+                const bool k_there = u + 2 < items &&
+                                     mbar_test_wait(B(sh->k_full[kn % K_STAGES]), (uint32_t)(kn / K_STAGES) & 1u);
                 tc_fence_after();
                 if (elect_one()) {
                     const uint64_t vd = smem_desc_mn(base + L::V + st * L::TILE_BYTES, L::HALF);
                     #pragma unroll
                     for (int k = 0; k < TILE / 16; ++k)
-                        mma_f16_ts(tmem + TM_O + s * TILE, tmem + TM_S + s * TILE + 8 * k, vd + (uint64_t)(k * 2048 >> 4),
-                                   IDESC_PV, step > 0 || k > 0);
-                    if (!shared || s == 1) tc_commit(B(sh->v_empty[st]));
+                        mma_f16_ts(tmem + TM_O + s * TILE, tmem + TM_S + s * TILE + 8 * k,
+                                   vd + (uint64_t)(k * 2048 >> 4), IDESC_PV, step > 0 || k > 0);
+                    if (!shared || s == 1) {
+                        tc_commit(B(sh->v_empty[st]));
+                        tc_commit(B(sh->info_empty[kt % INFOS]));
+                    }
                     tc_commit(B(sh->pv_done[s]));
                 }
                 __syncwarp();
-                if (u + 2 < items) ok = qk(u + 2);
+                if (u + 2 < items) ok = qk(u + 2, __all_sync(0xffffffffu, k_there));
             }
             steps[0] += (items + 1) / 2;
             steps[1] += items / 2;
@@ -359,35 +476,38 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
             const int lim = !valid ? 0 : a.causal ? max(0, cur.s.len - cur.s.n + i + 1) : cur.s.len;
             // the unit's query rows, as the A operand (with few rows both streams use the first tile)
             float down = 1.f;
-            if (shared || s == 0 || !std::is_same<T, __half>::value) {
-                uint4 raw4[D / 8];
-                const T* src = static_cast<const T*>(a.Q) + (size_t)(cur.s.row0 + (valid ? i : 0)) * a.ldq +
-                               (size_t)(valid ? head : 0) * D;
+            const T* src = static_cast<const T*>(a.Q) + (size_t)(cur.s.row0 + (valid ? i : 0)) * a.ldq +
+                           (size_t)(valid ? head : 0) * D;
+            float up = 1.f;
+            if (shared || s == 0 || std::is_same<T, __nv_bfloat16>::value) {
+                uint4 q[D / 8];                                                 // the whole row on its way at once
                 #pragma unroll
-                for (int k = 0; k < D / 8; ++k)
-                    raw4[k] = valid ? *reinterpret_cast<const uint4*>(src + 8 * k) : make_uint4(0, 0, 0, 0);
-                float up = 1.f;
+                for (int k = 0; k < D / 8; ++k) q[k] = ld_global_nc_v4(src + 8 * k);
                 if (std::is_same<T, __nv_bfloat16>::value) {
-                    float top = 0.f;
+                    // the largest magnitude: bf16 numbers without their sign are ordered as integers
+                    uint32_t top = 0;
                     #pragma unroll
                     for (int k = 0; k < D / 8; ++k) {
-                        float f[8];
-                        Eight<T>::load(reinterpret_cast<const T*>(&raw4[k]), f);
+                        const uint32_t w[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
                         #pragma unroll
-                        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[e]));
+                        for (int e = 0; e < 4; ++e) top = max(top, max(w[e] << 16 & 0x7fff0000u, w[e] & 0x7fff0000u));
                     }
-                    row_power(top, up, down);
+                    row_power(__uint_as_float(top), up, down);
                 }
                 if (shared || s == 0) {
                     #pragma unroll
                     for (int k = 0; k < D / 8; ++k) {
-                        uint4 v = raw4[k];
+                        uint4 v = valid ? q[k] : make_uint4(0, 0, 0, 0);
                         if (std::is_same<T, __nv_bfloat16>::value) {
-                            float f[8];
-                            Eight<T>::load(reinterpret_cast<const T*>(&raw4[k]), f);
+                            const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+                            uint32_t o[4];
                             #pragma unroll
-                            for (int e = 0; e < 8; ++e) f[e] *= up;
-                            Eight<__half>::store(reinterpret_cast<__half*>(&v), f);
+                            for (int e = 0; e < 4; ++e) {
+                                const float2 f = __bfloat1622float2(h[e]);
+                                const __half2 p = __floats2half2_rn(f.x * up, f.y * up);
+                                o[e] = *reinterpret_cast<const uint32_t*>(&p);
+                            }
+                            v = make_uint4(o[0], o[1], o[2], o[3]);
                         }
                         st_shared_v4(base + L::Q + s * L::TILE_BYTES + (k >> 3) * L::HALF + sw128_offset(row, k & 7), v.x,
                                      v.y, v.z, v.w);
@@ -400,40 +520,53 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
 
             float m = NEG_INF, l = 0.f;
             for (int step = 0; step < mine && ok; ++step) {
-                const int kt = tile0 + (shared ? step : 2 * step + s), st = kt % STAGES;
+                const int kt = tile0 + (shared ? step : 2 * step + s), st = kt % INFOS;
                 ok = mbar_wait_bounded_warp(B(sh->s_full[s]), (uint32_t)(steps + step) & 1u, abort) &&
-                     mbar_wait_bounded_warp(B(sh->info[st]), (uint32_t)(kt / STAGES) & 1u, abort);
+                     mbar_wait_bounded_warp(B(sh->info[st]), (uint32_t)(kt / INFOS) & 1u, abort);
                 if (!ok) break;
                 if (active) {
                     tc_fence_after();
                     const TileInfo& ti = sh->tile[st];
-                    const bool edge = ti.edge != 0, masked = a.key_mask != nullptr;
-                    const int see = lim - ti.key0;                              // keys [0, see) of the tile
+                    const bool edge = ti.edge != 0;  // the causal boundary is in the tile
                     float top = NEG_INF;
-                    #pragma unroll
+                    unsigned met = edge ? 0u : ti.met;                          // blocks of which the row sees a key
+                    #pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
                         uint32_t x[32];
                         tmem_ld_32x32b_x32(t_s + 32 * c, x);
                         tmem_ld_wait();
                         if (edge) {
+                            const int see = lim - ti.key0 - 32 * c;
                             #pragma unroll
-                            for (int k = 0; k < 32; ++k) {
-                                const float bias = masked ? ti.bias[32 * c + k] : 0.f;
-                                if (32 * c + k >= see || bias != 0.f) x[k] = 0xff800000u;
+                            for (int k = 0; k < 32; ++k)
+                                if (k >= see || ti.inv[32 * c + k] == 0.f) x[k] = 0xff800000u;
+                            #pragma unroll
+                            for (int q = 0; q < 2; ++q) {                       // for the second pass
+                                uint32_t y[16];
+                                #pragma unroll
+                                for (int k = 0; k < 16; ++k) y[k] = x[16 * q + k];
+                                tmem_st_32x32b_x16(t_s + 32 * c + 16 * q, y);
                             }
                         }
                         #pragma unroll
                         for (int q = 0; q < 2; ++q) {
-                            float t = __uint_as_float(x[16 * q]);
+                            const uint32_t* y = &x[16 * q];
+                            float t = __uint_as_float(y[0]);
                             #pragma unroll
-                            for (int k = 1; k < 15; k += 2)
-                                t = max3(t, __uint_as_float(x[16 * q + k]), __uint_as_float(x[16 * q + k + 1]));
-                            t = fmaxf(t, __uint_as_float(x[16 * q + 15]));
+                            for (int k = 1; k < 15; k += 2) t = max3(t, __uint_as_float(y[k]), __uint_as_float(y[k + 1]));
+                            t = fmaxf(t, __uint_as_float(y[15]));
                             const float4 b = ti.blk[2 * c + q];
-                            // a maximum of -inf: no key of the block is seen (its scale may be anything)
-                            if (t != NEG_INF) top = fmaxf(top, fmaf(t, b.x * down, b.y));
+                            if (edge) {
+                                if (b.y != NEG_INF && t != NEG_INF) {
+                                    met |= 1u << (2 * c + q);
+                                    top = fmaxf(top, fmaf(t, b.x * down, b.y));
+                                }
+                            } else {
+                                top = fmaxf(top, fmaf(t, b.x * down, b.y));
+                            }
                         }
                     }
+                    if (edge) tmem_st_wait();
                     if (__any_sync(0xffffffffu, top > m + LAZY)) {
                         const float to = fmaxf(m, top), f = m == to ? 1.f : ex2(m - to);
                         m = to;
@@ -442,7 +575,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                             ok = mbar_wait_bounded_warp(B(sh->pv_done[s]), (uint32_t)(steps + step - 1) & 1u, abort);
                             if (!ok) break;
                             tc_fence_after();
-                            #pragma unroll
+                            #pragma unroll 1
                             for (int c = 0; c < D / 16; ++c) {
                                 uint32_t o[16];
                                 tmem_ld_32x32b_x16(t_o + 16 * c, o);
@@ -455,38 +588,46 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                         }
                     }
                     const float sub = m == NEG_INF ? 0.f : m - HEAD;
-                    float2 sum = make_float2(0.f, 0.f);
-                    #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t x[32], p[16];
-                        tmem_ld_32x32b_x32(t_s + 32 * c, x);
-                        tmem_ld_wait();
-                        #pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            const float4 b = ti.blk[2 * c + q];
-                            const float ax = b.x * down, cx = b.y - sub;
+                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    // `all`: every row sees a key of every block. Else a block without one weighs nothing,
+                    // whatever its scales are.
+                    auto weights = [&](auto all) {
+                        #pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t x[32], p[16];
+                            tmem_ld_32x32b_x32(t_s + 32 * c, x);
+                            tmem_ld_wait();
                             #pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                const int e = 16 * q + 2 * k;
-                                float2 v = fma2(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])),
-                                                make_float2(ax, ax), make_float2(cx, cx));
-                                v.x = ex2(v.x);
-                                v.y = ex2(v.y);
-                                float2 add = make_float2(b.z, b.z);
-                                if (edge) {
-                                    // a weight that does not count is 0 whatever its block's scale is
-                                    const int key = 32 * c + e;
-                                    if (key >= see || (masked && ti.bias[key] != 0.f)) v.x = add.x = 0.f;
-                                    if (key + 1 >= see || (masked && ti.bias[key + 1] != 0.f)) v.y = add.y = 0.f;
+                            for (int q = 0; q < 2; ++q) {
+                                const float4 b = ti.blk[2 * c + q];
+                                const float ax = b.x * down, cx = b.y - sub;
+                                const bool any = decltype(all)::value || (met >> (2 * c + q) & 1);
+                                #pragma unroll
+                                for (int k = 0; k < 16; k += 4) {
+                                    const float4 f = *reinterpret_cast<const float4*>(ti.inv + 32 * c + 16 * q + k);
+                                    float2 v[2];
+                                    #pragma unroll
+                                    for (int h = 0; h < 2; ++h) {
+                                        v[h] = fma2(make_float2(__uint_as_float(x[16 * q + k + 2 * h]),
+                                                                __uint_as_float(x[16 * q + k + 2 * h + 1])),
+                                                    make_float2(ax, ax), make_float2(cx, cx));
+                                        v[h].x = ex2(v[h].x);
+                                        v[h].y = ex2(v[h].y);
+                                        const __half2 w = __floats2half2_rn(v[h].x, v[h].y);
+                                        p[8 * q + k / 2 + h] = any ? *reinterpret_cast<const uint32_t*>(&w) : 0u;
+                                    }
+                                    if (any) {
+                                        sum[0] = fma2(v[0], make_float2(f.x, f.y), sum[0]);
+                                        sum[1] = fma2(v[1], make_float2(f.z, f.w), sum[1]);
+                                    }
                                 }
-                                sum = fma2(v, add, sum);
-                                const __half2 h = __floats2half2_rn(v.x, v.y);
-                                p[8 * q + k] = *reinterpret_cast<const uint32_t*>(&h);
                             }
+                            tmem_st_32x32b_x16(t_s + 16 * c, p);                // over scores of chunks up to c / 2
                         }
-                        tmem_st_32x32b_x16(t_s + 16 * c, p);
-                    }
-                    l += sum.x + sum.y;
+                    };
+                    if (__all_sync(0xffffffffu, met == 0xffu)) weights(std::true_type{});
+                    else weights(std::false_type{});
+                    l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
                     tmem_st_wait();
                     tc_fence_before();
                 }
@@ -534,41 +675,57 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                     l = l * f0 + o.y * f1;
                     m = top;
                 }
+                // Half of the columns at a time through this warp's part of the Q area (its rows of the join
+                // area, or its quarter of the stream's Q tile), so that the stores run along the rows.
+                constexpr int C4 = D / 8, RPW = 32 / C4;                        // float4s of half a row, rows a warp store
                 const float inv = whole ? (l == 0.f ? 0.f : __fdiv_rn(1.f, l)) : 1.f;
                 float* slot = slots + ((size_t)blockIdx.x * 2 + (tile0 == 0 ? 0 : 1)) * slot_floats(slot_rows, D);
                 const int srow = (shared ? s * TILE : 0) + row;
-                T* out = static_cast<T*>(a.Out) + (size_t)(cur.s.row0 + i) * a.ldo + (size_t)head * D;
-                #pragma unroll
-                for (int c = 0; c < D / 16; ++c) {
-                    uint32_t o[16];
-                    tmem_ld_32x32b_x16(t_o + 16 * c, o);
-                    tmem_ld_wait();
-                    float f[16];
-                    #pragma unroll
-                    for (int k = 0; k < 16; ++k) f[k] = __uint_as_float(o[k]);
-                    if (!shared) {
+                const long long at = whole ? (long long)(cur.s.row0 + i) * a.ldo + (long long)head * D
+                                           : (long long)srow * D;
+                float* stage = reinterpret_cast<float*>(smem + L::Q + s * L::TILE_BYTES + (warp & 3) * (64 * D));
+                auto stage_at = [&](int r, int c) { return stage + r * (D / 2) + ((c ^ (r & (C4 - 1))) << 2); };
+                #pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+                    #pragma unroll 2
+                    for (int c = half * (D / 32); c < (half + 1) * (D / 32); ++c) {
+                        uint32_t o[16];
+                        tmem_ld_32x32b_x16(t_o + 16 * c, o);
+                        tmem_ld_wait();
                         #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const float4 v = *reinterpret_cast<const float4*>(join_at(4 * c + k));
-                            f[4 * k] = f[4 * k] * f0 + v.x * f1;
-                            f[4 * k + 1] = f[4 * k + 1] * f0 + v.y * f1;
-                            f[4 * k + 2] = f[4 * k + 2] * f0 + v.z * f1;
-                            f[4 * k + 3] = f[4 * k + 3] * f0 + v.w * f1;
+                            const float4 v = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]),
+                                                         __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
+                            if (!shared) {
+                                float4* other = reinterpret_cast<float4*>(join_at(4 * c + k));
+                                const float4 w = *other;
+                                *other = make_float4(v.x * f0 + w.x * f1, v.y * f0 + w.y * f1, v.z * f0 + w.z * f1,
+                                                     v.w * f0 + w.w * f1);
+                            } else {
+                                *reinterpret_cast<float4*>(stage_at(lane, 4 * c + k - half * C4)) = v;
+                            }
                         }
                     }
-                    if (!valid) continue;
-                    if (whole) {
-                        float e[2][8];
-                        #pragma unroll
-                        for (int k = 0; k < 16; ++k) e[k >> 3][k & 7] = l == 0.f ? 0.f : f[k] * inv;
-                        Eight<T>::store(out + 16 * c, e[0]);
-                        Eight<T>::store(out + 16 * c + 8, e[1]);
-                    } else {
-                        #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            *reinterpret_cast<float4*>(slot + (size_t)srow * D + 16 * c + 4 * k) =
-                                make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
+                    __syncwarp();
+                    #pragma unroll 4
+                    for (int r0 = 0; r0 < 32; r0 += RPW) {
+                        const int r = r0 + lane / C4, c = lane % C4, c4 = half * C4 + c;
+                        const long long to = __shfl_sync(0xffffffffu, at, r);
+                        const float scale = __shfl_sync(0xffffffffu, inv, r);
+                        const bool put = __shfl_sync(0xffffffffu, (int)valid, r) != 0;
+                        const int jr = row - lane + r;                          // the row in the join area
+                        const float4 v = *reinterpret_cast<const float4*>(
+                            shared ? stage_at(r, c) : join + jr * D + ((c4 ^ (jr & (D / 4 - 1))) << 2));
+                        if (put && whole) {
+                            // (no key seen: accumulators and scale are 0)
+                            const T e[4] = {(T)(v.x * scale), (T)(v.y * scale), (T)(v.z * scale), (T)(v.w * scale)};
+                            *reinterpret_cast<uint2*>(static_cast<T*>(a.Out) + to + 4 * c4) =
+                                *reinterpret_cast<const uint2*>(e);
+                        } else if (put) {
+                            *reinterpret_cast<float4*>(slot + to + 4 * c4) = v;
+                        }
                     }
+                    __syncwarp();
                 }
                 if (valid) {
                     if (!whole)
@@ -579,8 +736,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                 }
             }
             tc_fence_before();
-            // the join area is Q's memory: read before the next unit's rows come in
-            if (!shared && !(ok = meet())) break;
+            // the join and staging areas are Q's memory: read before the next unit's rows come in
+            if (!(ok = meet())) break;
             tile0 += n;
             left -= n;
             cur.kt += n;
