@@ -70,6 +70,23 @@ struct W4gArgs {
 };
 cudaError_t launch_w4g_linear(const W4gArgs& a, cudaStream_t s);
 
+// A launch whose kernel begins with grid_dependency_wait(): its CTAs are
+// brought up while the kernel before it drains. (These kernels do not let
+// their own dependents start early: measured slower, the waiting CTAs take
+// room and issue slots.)
+template <typename... P, typename... A>
+cudaError_t launch_overlapped(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at = pdl_attribute();
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
 // Eight values of an element type to and from float32 (one rounding).
 template <typename T> struct Eight;
 template <> struct Eight<__half> {

@@ -6,7 +6,13 @@
 // log-sum-exp of -inf.
 //
 // Arithmetic. The codes c, e are integers of magnitude <= 127, exact in
-// fp16, so both products run on the 16-bit MMA with float32 accumulators.
+// fp16, so both products run on the 16-bit MMA with float32 accumulators. The
+// keys enter as their bytes u = c + 128: widened to 16 bits a byte reads, as
+// an fp16 subnormal, u 2^-24, and the offset leaves through linearity,
+// sum q c = sum q u - 128 sum q (once a row; it is a few times the codes' size
+// and costs two of float32's 24 bits of the score). The values' codes are
+// made exactly: a channel of which the heavy keys' codes are 0 would show
+// the offset's rounding.
 // A bf16 query row is scaled by a power of two into fp16's range: its eight
 // significand bits fit, so only values below 2^-28 of the row's largest
 // lose bits. s_k and the softmax scale multiply the float32 score. s_v
@@ -28,8 +34,9 @@
 // rows; partial runs leave (sum, maximum, accumulators) in the workspace and
 // a second kernel joins them in run order (results do not depend on timing).
 //
-// In a CTA each of four warps owns 16 keys of a tile and a private ring of
-// cp.async stages, so warps meet only at the end of a unit. 16-byte chunks
+// In a CTA each of four warps owns 32 keys of a tile (two blocks) and a
+// private pair of cp.async stages, so warps meet only at the ends of a unit;
+// the query fragments, alike for all, are in shared memory. 16-byte chunks
 // are XOR-swizzled by row so that both fragments read without bank
 // conflicts. The MMA's k order is free: a key's fragment takes 4 consecutive
 // channels per thread, and value columns are taken in the order that makes a
@@ -44,9 +51,9 @@ namespace {
 constexpr int WARPS = 4;
 constexpr int THREADS = WARPS * 32;
 constexpr int ROWS = 16;               // query rows of a unit
-constexpr int WKEYS = 16;              // keys of a warp in a tile
-constexpr int TILE = WARPS * WKEYS;    // 64 keys
-constexpr int STAGES = 4;
+constexpr int WKEYS = 32;              // keys of a warp in a tile: two 16-key blocks
+constexpr int TILE = WARPS * WKEYS;    // 128 keys
+constexpr int STAGES = 2;
 constexpr int CTAS_PER_SM = 3;
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
@@ -66,6 +73,10 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// Bytes 0 and 1 (2 and 3) of a word as the halves of a register.
+__device__ __forceinline__ uint32_t widen_lo(uint32_t w) { return prmt(w, 0u, 0x4140u); }
+__device__ __forceinline__ uint32_t widen_hi(uint32_t w) { return prmt(w, 0u, 0x4342u); }
+
 // Byte offset of 16-byte chunk c of row r (of 16) in a warp's stage.
 template <int D> __device__ __forceinline__ uint32_t stage_offset(int r, int c) {
     if (D == 128) return r * 128 + ((c ^ (r & 7) ^ ((r & 1) << 2)) << 4);
@@ -73,10 +84,10 @@ template <int D> __device__ __forceinline__ uint32_t stage_offset(int r, int c) 
 }
 
 // Fragments of one query row (half of the A operand's registers): channels
-// 64 h + 16 t + 4 s + {0, 1} in q[h][s][0], {2, 3} in q[h][s][1], and the
-// power of two that undoes the row's scaling.
+// 64 h + 16 t + 4 s + {0, 1} in q[h][s][0], {2, 3} in q[h][s][1], the row's
+// sum, and the power of two that undoes the row's scaling.
 template <typename T, int D>
-__device__ __forceinline__ float load_row(const T* row, int t, uint32_t (&q)[D / 64][4][2]) {
+__device__ __forceinline__ float load_row(const T* row, int t, uint32_t (&q)[D / 64][4][2], float& sum) {
     float v[D / 64][16], top = 0.f;
     #pragma unroll
     for (int h = 0; h < D / 64; ++h) {
@@ -91,6 +102,7 @@ __device__ __forceinline__ float load_row(const T* row, int t, uint32_t (&q)[D /
         }
     }
     float up = 1.f, down = 1.f;
+    sum = 0.f;
     if (std::is_same<T, __nv_bfloat16>::value) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
@@ -104,15 +116,20 @@ __device__ __forceinline__ float load_row(const T* row, int t, uint32_t (&q)[D /
             for (int k = 0; k < 2; ++k) {
                 const __half2 p = __floats2half2_rn(v[h][4 * s + 2 * k] * up, v[h][4 * s + 2 * k + 1] * up);
                 q[h][s][k] = *reinterpret_cast<const uint32_t*>(&p);
+                const float2 back = __half22float2(p);
+                sum += back.x + back.y;
             }
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
     return down;
 }
 
 template <typename T, int D>
 struct AttnSmem {
-    static constexpr int STAGE = 2 * WKEYS * D + 16;            // bytes of a warp's stage: keys, values, their two scales
+    static constexpr int STAGE = 2 * WKEYS * D + 16;            // bytes of a warp's stage: keys, values, the blocks' scales
     static constexpr int RING = WARPS * STAGES * STAGE;
     static constexpr int MERGE = ROWS * D * 4 + WARPS * ROWS * 8;
+    static constexpr int QUERY = RING;                          // fragments [D / 16][32 lanes][4], until the merge
     static constexpr int BYTES = RING + MERGE;
 };
 
@@ -125,6 +142,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
 
+    grid_dependency_wait();
     const Run run = find_run<ROWS, TILE, THREADS>(a, G, prefix_out);
     if (run.tau0 >= run.tau1) return;
     Cursor<ROWS, TILE> cur;
@@ -136,37 +154,41 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
     const uint32_t ring = smem_addr(smem) + warp * (STAGES * SM::STAGE);
     const int shift = __ffs(a.c.page) - 1;
     const size_t block_bytes = (size_t)a.c.page * D;
-    // where this lane's 16-byte chunks go in a stage (rows D / 16 lanes apart repeat the pattern every 8 rows)
+    // where this lane's 16-byte chunks of a 16-key block go
     uint32_t dst_at[D / 32];
     #pragma unroll
     for (int i = 0; i < D / 32; ++i) dst_at[i] = stage_offset<D>((lane + 32 * i) / (D / 16), (lane + 32 * i) % (D / 16));
 
-    // One warp's 16 keys of the next tile (a page holds a multiple of 16, so they lie in one block).
+    // One warp's keys of the next tile, block by block (a page holds whole blocks).
     auto fetch = [&](int slot) {
         if (pre_left > 0) {
-            const int key0 = pre.kt * TILE + warp * WKEYS;
-            if (key0 < pre.s.len) {
-                const int page_i = key0 >> shift;
-                int page = -1;
-                if (page_i < a.table_ld) page = __ldg(a.page_table + (size_t)pre.b * a.table_ld + page_i);
-                const uint32_t dst = ring + slot * SM::STAGE;
-                if (page < 0 || page >= a.c.pages) {
-                    if (lane == 0) {
-                        atomicOr(a.status, STATUS_RANGE);
-                        // the rows that see these keys become NaN
-                        asm volatile("st.shared.v2.b32 [%0], {%1, %2};"
-                                     :: "r"(dst + 2 * WKEYS * D), "r"(0x7fffffffu), "r"(0x3f800000u) : "memory");
+            #pragma unroll
+            for (int blk16 = 0; blk16 < WKEYS / 16; ++blk16) {
+                const int key0 = pre.kt * TILE + warp * WKEYS + 16 * blk16;
+                if (key0 < pre.s.len) {
+                    const int page_i = key0 >> shift;
+                    int page = -1;
+                    if (page_i < a.table_ld) page = __ldg(a.page_table + (size_t)pre.b * a.table_ld + page_i);
+                    const uint32_t dst = ring + slot * SM::STAGE, dst_s = dst + 2 * WKEYS * D + 8 * blk16;
+                    if (page < 0 || page >= a.c.pages) {
+                        if (lane == 0) {
+                            atomicOr(a.status, STATUS_RANGE);
+                            // the rows that see these keys become NaN
+                            asm volatile("st.shared.v2.b32 [%0], {%1, %2};"
+                                         :: "r"(dst_s), "r"(0x7fffffffu), "r"(0x3f800000u) : "memory");
+                        }
+                    } else {
+                        const size_t blk = (size_t)page * a.c.Hkv + pre.h;
+                        const size_t off = blk * block_bytes + (size_t)(key0 & (a.c.page - 1)) * D + lane * 16;
+                        const uint8_t* k = a.c.K + off;
+                        const uint8_t* v = a.c.V + off;
+                        #pragma unroll
+                        for (int i = 0; i < D / 32; ++i) cp_async16(dst + 16 * blk16 * D + dst_at[i], k + 512 * i);
+                        #pragma unroll
+                        for (int i = 0; i < D / 32; ++i)
+                            cp_async16(dst + (WKEYS + 16 * blk16) * D + dst_at[i], v + 512 * i);
+                        if (lane < 2) cp_async4(dst_s + 4 * lane, (lane ? a.c.v_scale : a.c.k_scale) + blk);
                     }
-                } else {
-                    const size_t blk = (size_t)page * a.c.Hkv + pre.h;
-                    const size_t off = blk * block_bytes + (size_t)(key0 & (a.c.page - 1)) * D + lane * 16;
-                    const uint8_t* k = a.c.K + off;
-                    const uint8_t* v = a.c.V + off;
-                    #pragma unroll
-                    for (int i = 0; i < D / 32; ++i) cp_async16(dst + dst_at[i], k + 512 * i);
-                    #pragma unroll
-                    for (int i = 0; i < D / 32; ++i) cp_async16(dst + WKEYS * D + dst_at[i], v + 512 * i);
-                    if (lane < 2) cp_async4(dst + 2 * WKEYS * D + 4 * lane, (lane ? a.c.v_scale : a.c.k_scale) + blk);
                 }
             }
             --pre_left;
@@ -177,8 +199,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
     #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) fetch(i);
 
-    uint32_t qf[KH][4][4];
-    float o[DN][4], m[2], l[2], rs[2];
+    uint4* const query = reinterpret_cast<uint4*>(smem + SM::QUERY) + lane;      // this lane's fragment of k step 0
+    float o[DN][4], m[2], l[2], rs[2], qs[2];
     int lim[2];                              // keys [0, lim) are visible to the rows (causal limit and length)
     const float unit_scale = a.scale * 1.4426950408889634f;
     bool fresh = true;
@@ -190,6 +212,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
     while (left > 0) {
         {
             if (fresh) {                     // a new unit: its query rows
+                uint32_t q2[2][KH][4][2];
                 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int r = cur.rt * ROWS + g + 8 * k, i = r / G, j = r - i * G;
@@ -200,14 +223,18 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                               (size_t)(cur.h * G + j) * D;
                         lim[k] = a.causal ? max(0, cur.s.len - cur.s.n + i + 1) : cur.s.len;
                     }
-                    uint32_t q2[KH][4][2];
-                    rs[k] = load_row<T, D>(row, t, q2);
-                    #pragma unroll
-                    for (int h = 0; h < KH; ++h)
-                        #pragma unroll
-                        for (int s = 0; s < 4; ++s) { qf[h][s][k] = q2[h][s][0]; qf[h][s][2 + k] = q2[h][s][1]; }
+                    rs[k] = load_row<T, D>(row, t, q2[k], qs[k]);
                     m[k] = NEG_INF; l[k] = 0.f;
                 }
+                // every warp has the fragments; each stores its part of them for all
+                #pragma unroll
+                for (int h = 0; h < KH; ++h)
+                    #pragma unroll
+                    for (int s = 0; s < 4; ++s)
+                        if ((4 * h + s) % WARPS == warp)
+                            query[(4 * h + s) * 32] = make_uint4(q2[0][h][s][0], q2[1][h][s][0], q2[0][h][s][1],
+                                                                 q2[1][h][s][1]);
+                __syncthreads();             // (the unit before ended with a barrier: its fragments are done with)
                 #pragma unroll
                 for (int j = 0; j < DN; ++j)
                     #pragma unroll
@@ -221,45 +248,57 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
             const int key0 = cur.kt * TILE + warp * WKEYS;
             if (key0 < cur.s.len) {
                 const uint8_t* stage = smem + warp * (STAGES * SM::STAGE) + st * SM::STAGE;
-                // --- scores of 16 keys: two column tiles ---------------------
-                float x[2][4];
+                // --- scores of 32 keys: four column tiles, a k step for all of them ---
+                float x[4][4];
                 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
-                    float part[KH][4];               // a chain for each half of the channels
+                for (int nt = 0; nt < 4; ++nt)
                     #pragma unroll
-                    for (int h = 0; h < KH; ++h) {
+                    for (int k = 0; k < 4; ++k) x[nt][k] = 0.f;
+                #pragma unroll
+                for (int h = 0; h < KH; ++h) {
+                    uint4 w[4];
+                    #pragma unroll
+                    for (int nt = 0; nt < 4; ++nt)
+                        w[nt] = *reinterpret_cast<const uint4*>(stage + stage_offset<D>(nt * 8 + g, 4 * h + t));
+                    #pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        const uint4 q = query[(4 * h + s) * 32];
+                        const uint32_t qa[4] = {q.x, q.y, q.z, q.w};
                         #pragma unroll
-                        for (int k = 0; k < 4; ++k) part[h][k] = 0.f;
-                        const uint4 w = *reinterpret_cast<const uint4*>(stage + stage_offset<D>(nt * 8 + g, 4 * h + t));
-                        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-                        #pragma unroll
-                        for (int s = 0; s < 4; ++s)
-                            mma_16816(part[h], qf[h][s], codes_half2(prmt(ws[s], 0x64646464u, 0x4140u)),
-                                      codes_half2(prmt(ws[s], 0x64646464u, 0x4342u)));
+                        for (int nt = 0; nt < 4; ++nt) {
+                            const uint32_t ws = s == 0 ? w[nt].x : s == 1 ? w[nt].y : s == 2 ? w[nt].z : w[nt].w;
+                            mma_16816(x[nt], qa, widen_lo(ws), widen_hi(ws));
+                        }
                     }
-                    #pragma unroll
-                    for (int k = 0; k < 4; ++k) x[nt][k] = KH == 2 ? part[0][k] + part[KH - 1][k] : part[0][k];
                 }
-                const float2 scales = *reinterpret_cast<const float2*>(stage + 2 * WKEYS * D);
-                const float ks = scales.x * unit_scale;
-                // a value scale below the floor counts as the floor (an empty block's codes are 0)
-                const float vs = scales.y < KV_SCALE_FLOOR ? KV_SCALE_FLOOR : scales.y;
-                const float lv = __log2f(vs), iv = __fdividef(1.f, vs);
-                const float k0 = ks * rs[0], k1 = ks * rs[1];
+                const float4 scales = *reinterpret_cast<const float4*>(stage + 2 * WKEYS * D);
+                float iv[2];
                 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
-                    x[nt][0] = fmaf(x[nt][0], k0, lv);
-                    x[nt][1] = fmaf(x[nt][1], k0, lv);
-                    x[nt][2] = fmaf(x[nt][2], k1, lv);
-                    x[nt][3] = fmaf(x[nt][3], k1, lv);
+                for (int b = 0; b < 2; ++b) {
+                    const float ks = (b ? scales.z : scales.x) * unit_scale, sv = b ? scales.w : scales.y;
+                    // a value scale below the floor counts as the floor (an empty block's codes are 0)
+                    const float vs = sv < KV_SCALE_FLOOR ? KV_SCALE_FLOOR : sv;
+                    const float lv = __log2f(vs);
+                    iv[b] = __fdividef(1.f, vs);
+                    // x = log2(e) scale s_k (2^24 sum q u 2^-24 - 128 sum q) + log2 s_v
+                    const float k0 = ks * rs[0], k1 = ks * rs[1];
+                    const float b0 = fmaf(-128.f * k0, qs[0], lv), b1 = fmaf(-128.f * k1, qs[1], lv);
+                    const float a0 = k0 * 16777216.f, a1 = k1 * 16777216.f;
+                    #pragma unroll
+                    for (int nt = 2 * b; nt < 2 * b + 2; ++nt) {
+                        x[nt][0] = fmaf(x[nt][0], a0, b0);
+                        x[nt][1] = fmaf(x[nt][1], a0, b0);
+                        x[nt][2] = fmaf(x[nt][2], a1, b1);
+                        x[nt][3] = fmaf(x[nt][3], a1, b1);
+                    }
                 }
                 const bool edge = key0 + WKEYS > cur.s.len || a.key_mask != nullptr ||
                                   (a.causal && key0 + WKEYS > cur.s.len - cur.s.n + 1);
-                unsigned seen = 0xff;        // bit 4 nt + k: x[nt][k] counts
+                unsigned seen = 0xffff;      // bit 4 nt + k: x[nt][k] counts
                 if (edge) {
                     seen = 0;
                     #pragma unroll
-                    for (int nt = 0; nt < 2; ++nt)
+                    for (int nt = 0; nt < 4; ++nt)
                         #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const int key = key0 + nt * 8 + 2 * t + (k & 1);
@@ -271,8 +310,10 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                         }
                 }
                 // --- running maximum, moved only when it is passed by LAZY ---
-                float top0 = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
-                float top1 = fmaxf(fmaxf(x[0][2], x[0][3]), fmaxf(x[1][2], x[1][3]));
+                float top0 = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1])),
+                                   fmaxf(fmaxf(x[2][0], x[2][1]), fmaxf(x[3][0], x[3][1])));
+                float top1 = fmaxf(fmaxf(fmaxf(x[0][2], x[0][3]), fmaxf(x[1][2], x[1][3])),
+                                   fmaxf(fmaxf(x[2][2], x[2][3]), fmaxf(x[3][2], x[3][3])));
                 if (__any_sync(0xffffffffu, top0 > m[0] + LAZY || top1 > m[1] + LAZY)) {
                     #pragma unroll
                     for (int d = 1; d < 4; d <<= 1) {
@@ -287,49 +328,62 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                     for (int j = 0; j < DN; ++j) { o[j][0] *= f0; o[j][1] *= f0; o[j][2] *= f1; o[j][3] *= f1; }
                 }
                 const float s0 = m[0] == NEG_INF ? 0.f : m[0] - HEAD, s1 = m[1] == NEG_INF ? 0.f : m[1] - HEAD;
-                uint32_t p[4];
                 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
-                    float e[4];
+                for (int nt = 0; nt < 4; ++nt)
                     #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        e[k] = ex2(x[nt][k] - (k < 2 ? s0 : s1));
-                        // a masked weight is 0 whatever its block's scale is
-                        const float add = !edge || (seen >> (4 * nt + k) & 1) ? e[k] * iv : 0.f;
-                        l[k >> 1] += add;
-                    }
-                    const __half2 pa = __floats2half2_rn(e[0], e[1]), pb = __floats2half2_rn(e[2], e[3]);
-                    p[2 * nt] = *reinterpret_cast<const uint32_t*>(&pa);
-                    p[2 * nt + 1] = *reinterpret_cast<const uint32_t*>(&pb);
+                    for (int k = 0; k < 4; ++k) x[nt][k] = ex2(x[nt][k] - (k < 2 ? s0 : s1));
+                if (!edge) {
+                    #pragma unroll
+                    for (int nt = 0; nt < 4; ++nt)
+                        #pragma unroll
+                        for (int k = 0; k < 4; ++k) l[k >> 1] = fmaf(x[nt][k], iv[nt >> 1], l[k >> 1]);
+                } else {
+                    // a masked weight is 0 whatever its block's scale is
+                    #pragma unroll
+                    for (int nt = 0; nt < 4; ++nt)
+                        #pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (seen >> (4 * nt + k) & 1) l[k >> 1] = fmaf(x[nt][k], iv[nt >> 1], l[k >> 1]);
                 }
-                // --- values: keys 2t, 2t+1, 2t+8, 2t+9, columns DN g .. ------
-                const uint8_t* vst = stage + WKEYS * D;
                 #pragma unroll
-                for (int c = 0; c < D / 64; ++c) {           // 8 columns at a time
-                    uint2 r[4];
+                for (int b = 0; b < 2; ++b) {
+                    uint32_t p[4];
                     #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int key = 2 * t + (k & 1) + 8 * (k >> 1);
-                        if (D == 128)
-                            r[k] = *reinterpret_cast<const uint2*>(vst + stage_offset<D>(key, g) + 8 * c);
-                        else
-                            r[k] = *reinterpret_cast<const uint2*>(vst + stage_offset<D>(key, g >> 1) + 8 * (g & 1));
+                    for (int nt = 0; nt < 2; ++nt) {
+                        const __half2 pa = __floats2half2_rn(x[2 * b + nt][0], x[2 * b + nt][1]);
+                        const __half2 pb = __floats2half2_rn(x[2 * b + nt][2], x[2 * b + nt][3]);
+                        p[2 * nt] = *reinterpret_cast<const uint32_t*>(&pa);
+                        p[2 * nt + 1] = *reinterpret_cast<const uint32_t*>(&pb);
                     }
+                    // --- values: keys 2t, 2t+1, 2t+8, 2t+9 of the block, columns DN g .. ---
+                    const uint8_t* vst = stage + (WKEYS + 16 * b) * D;
                     #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        const uint32_t k0w = w ? r[0].y : r[0].x, k1w = w ? r[1].y : r[1].x;
-                        const uint32_t k8w = w ? r[2].y : r[2].x, k9w = w ? r[3].y : r[3].x;
-                        const uint32_t lo01 = prmt(k0w, k1w, 0x5140u), hi01 = prmt(k0w, k1w, 0x7362u);
-                        const uint32_t lo89 = prmt(k8w, k9w, 0x5140u), hi89 = prmt(k8w, k9w, 0x7362u);
-                        const int j = 8 * c + 4 * w;
-                        mma_16816(o[j], p, codes_half2(prmt(lo01, 0x64646464u, 0x4140u)),
-                                  codes_half2(prmt(lo89, 0x64646464u, 0x4140u)));
-                        mma_16816(o[j + 1], p, codes_half2(prmt(lo01, 0x64646464u, 0x4342u)),
-                                  codes_half2(prmt(lo89, 0x64646464u, 0x4342u)));
-                        mma_16816(o[j + 2], p, codes_half2(prmt(hi01, 0x64646464u, 0x4140u)),
-                                  codes_half2(prmt(hi89, 0x64646464u, 0x4140u)));
-                        mma_16816(o[j + 3], p, codes_half2(prmt(hi01, 0x64646464u, 0x4342u)),
-                                  codes_half2(prmt(hi89, 0x64646464u, 0x4342u)));
+                    for (int c = 0; c < D / 64; ++c) {       // 8 columns at a time
+                        uint2 r[4];
+                        #pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int key = 2 * t + (k & 1) + 8 * (k >> 1);
+                            if (D == 128)
+                                r[k] = *reinterpret_cast<const uint2*>(vst + stage_offset<D>(key, g) + 8 * c);
+                            else
+                                r[k] = *reinterpret_cast<const uint2*>(vst + stage_offset<D>(key, g >> 1) + 8 * (g & 1));
+                        }
+                        #pragma unroll
+                        for (int w = 0; w < 2; ++w) {
+                            const uint32_t k0w = w ? r[0].y : r[0].x, k1w = w ? r[1].y : r[1].x;
+                            const uint32_t k8w = w ? r[2].y : r[2].x, k9w = w ? r[3].y : r[3].x;
+                            const uint32_t lo01 = prmt(k0w, k1w, 0x5140u), hi01 = prmt(k0w, k1w, 0x7362u);
+                            const uint32_t lo89 = prmt(k8w, k9w, 0x5140u), hi89 = prmt(k8w, k9w, 0x7362u);
+                            const int j = 8 * c + 4 * w;
+                            mma_16816(o[j], p, codes_half2(prmt(lo01, 0x64646464u, 0x4140u)),
+                                      codes_half2(prmt(lo89, 0x64646464u, 0x4140u)));
+                            mma_16816(o[j + 1], p, codes_half2(prmt(lo01, 0x64646464u, 0x4342u)),
+                                      codes_half2(prmt(lo89, 0x64646464u, 0x4342u)));
+                            mma_16816(o[j + 2], p, codes_half2(prmt(hi01, 0x64646464u, 0x4140u)),
+                                      codes_half2(prmt(hi89, 0x64646464u, 0x4140u)));
+                            mma_16816(o[j + 3], p, codes_half2(prmt(hi01, 0x64646464u, 0x4342u)),
+                                      codes_half2(prmt(hi89, 0x64646464u, 0x4342u)));
+                        }
                     }
                 }
             }
@@ -438,8 +492,9 @@ cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
     const int ctas = num_sms() * CTAS_PER_SM;
     long long* prefix = static_cast<long long*>(a.workspace);
     float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + prefix_bytes(a.B));
-    kv_attention_kernel<T, D><<<ctas, THREADS, AttnSmem<T, D>::BYTES, s>>>(a, G, prefix, slots);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = launch_overlapped(kv_attention_kernel<T, D>, dim3(ctas), THREADS, AttnSmem<T, D>::BYTES, s, a, G, prefix,
+                               slots)) != cudaSuccess)
+        return e;
     return launch_join<T, D, ROWS, TILE>(a, G, ctas, ROWS, prefix, slots, s);
 }
 

@@ -162,67 +162,69 @@ struct Cursor {
     }
 };
 
-// One warp per query row: joins the partial runs of the row's unit in run
-// order, and writes the rows that no key reaches.
-constexpr int JOIN_WARPS = 4;
-template <typename T, int D, int ROWS, int TILE>
+// Joins the partial runs of a row's unit, and writes the rows that no key
+// reaches. SHARE warps take a row: one where there are many rows (their units
+// have few runs each), all eight of a CTA where there are few (a long
+// sequence's unit has up to a run per CTA). Every warp takes its runs in run
+// order, AT_ONCE of them on their way together, and the warps' sums are added
+// in warp order.
+constexpr int JOIN_WARPS = 8;
+template <typename T, int D, int ROWS, int TILE, int SHARE>
 __global__ void __launch_bounds__(JOIN_WARPS * 32)
-kv_attention_join_kernel(const KvAttnArgs a, int G, int ctas, int slot_rows, const long long* __restrict__ prefix,
-                         const float* __restrict__ slots) {
-    constexpr int PER = D / 32;
+kv_attention_join_kernel(const KvAttnArgs a, int G, int ctas, int slot_rows, const long long* prefix,
+                         const float* slots) {
+    constexpr int PER = D / 32, AT_ONCE = 8;
+    __shared__ float s_acc[SHARE > 1 ? SHARE : 1][D];
+    __shared__ float2 s_ml[SHARE > 1 ? SHARE : 1];
     grid_dependency_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % SHARE;
     const int b = blockIdx.y;
     const SeqShape s = seq_shape<ROWS, TILE>(a, G, b, false);
-    const int idx = blockIdx.x * JOIN_WARPS + warp;            // token * H + head
+    const long long total = prefix[a.B], before = prefix[b];
+    const int idx = blockIdx.x * (JOIN_WARPS / SHARE) + warp / SHARE;      // token * H + head
     const int i = idx / a.H, head = idx - i * a.H;
     if (i >= s.n) return;
     const size_t row = (size_t)(s.row0 + i);
     T* out = static_cast<T*>(a.Out) + row * a.ldo + (size_t)head * D + lane * PER;
-    if (s.nt == 0) {
-        #pragma unroll
-        for (int k = 0; k < PER; ++k) out[k] = (T)0.f;
-        if (lane == 0 && a.lse != nullptr) a.lse[row * a.H + head] = NEG_INF;
-        return;
-    }
     const int h = head / G, r = i * G + (head - h * G);
     const int rt = r / ROWS, rr = r - rt * ROWS;
-    const long long total = prefix[a.B];
-    const long long u0 = prefix[b] + (long long)(h * s.rt + rt) * s.nt;
-    // (64-bit divisions take a hundred instructions each; few lists need them)
-    long long share;
-    int c0, c1;
-    if (total < (1ll << 31)) {
-        const unsigned sh = ((unsigned)total + ctas - 1) / (unsigned)ctas;
-        share = sh;
-        c0 = (int)((unsigned)u0 / sh);
-        c1 = (int)((unsigned)(u0 + s.nt - 1) / sh);
-    } else {
-        share = (total + ctas - 1) / ctas;
-        c0 = (int)(u0 / share);
-        c1 = (int)((u0 + s.nt - 1) / share);
+    int c0 = 0, c1 = -1;
+    long long u0 = 0, share = 1;
+    if (s.nt > 0) {
+        u0 = before + ((long long)h * s.rt + rt) * s.nt;
+        // (64-bit divisions take a hundred instructions each; few lists need them)
+        if (total < (1ll << 31)) {
+            const unsigned sh = ((unsigned)total + ctas - 1) / (unsigned)ctas;
+            share = sh;
+            c0 = (int)((unsigned)u0 / sh);
+            c1 = (int)((unsigned)(u0 + s.nt - 1) / sh);
+        } else {
+            share = (total + ctas - 1) / ctas;
+            c0 = (int)(u0 / share);
+            c1 = (int)((u0 + s.nt - 1) / share);
+        }
+        if (c0 == c1) return;                             // one run covered the unit
     }
-    if (c0 == c1) return;                                 // one run covered the unit
-    auto slot = [&](int c) {
-        return slots + ((size_t)c * 2 + (u0 > (long long)c * share ? 1 : 0)) * slot_floats(slot_rows, D);
-    };
-    // AT_ONCE runs' loads in flight together; the running maximum moves between batches
-    constexpr int AT_ONCE = 8;
     float top = NEG_INF, l = 0.f, acc[PER];
     #pragma unroll
     for (int k = 0; k < PER; ++k) acc[k] = 0.f;
-    for (int c = c0; c <= c1; c += AT_ONCE) {
+    for (int c = c0 + part; c <= c1; c += AT_ONCE * SHARE) {
         float2 ml[AT_ONCE];
         float v[AT_ONCE][PER];
         #pragma unroll
         for (int q = 0; q < AT_ONCE; ++q) {
+            const int cq = c + q * SHARE;
             ml[q] = make_float2(NEG_INF, 0.f);
-            if (c + q <= c1) {
-                const float* p = slot(c + q);
+            #pragma unroll
+            for (int k = 0; k < PER; ++k) v[q][k] = 0.f;
+            if (cq <= c1) {
+                // the run's first slot, or its second when the unit begins inside the run
+                const float* p = slots + ((size_t)cq * 2 + (cq == c0 && u0 > (long long)c0 * share ? 1 : 0)) *
+                                             slot_floats(slot_rows, D);
                 ml[q] = *reinterpret_cast<const float2*>(p + (size_t)slot_rows * D + 2 * rr);
                 #pragma unroll
                 for (int k = 0; k < PER; k += 2) {
-                    const float2 w = *reinterpret_cast<const float2*>(p + rr * D + lane * PER + k);
+                    const float2 w = *reinterpret_cast<const float2*>(p + (size_t)rr * D + lane * PER + k);
                     v[q][k] = w.x; v[q][k + 1] = w.y;
                 }
             }
@@ -237,11 +239,32 @@ kv_attention_join_kernel(const KvAttnArgs a, int G, int ctas, int slot_rows, con
         for (int k = 0; k < PER; ++k) acc[k] *= f0;
         #pragma unroll
         for (int q = 0; q < AT_ONCE; ++q) {
-            if (c + q > c1) break;
             const float f = ml[q].x == top ? 1.f : ex2(ml[q].x - top);
             l = fmaf(ml[q].y, f, l);
             #pragma unroll
             for (int k = 0; k < PER; ++k) acc[k] = fmaf(v[q][k], f, acc[k]);
+        }
+    }
+    if (SHARE > 1) {                                      // one row a CTA: the warps' results
+        #pragma unroll
+        for (int k = 0; k < PER; ++k) s_acc[part][lane * PER + k] = acc[k];
+        if (lane == 0) s_ml[part] = make_float2(top, l);
+        __syncthreads();
+        if (part != 0) return;
+        float to = NEG_INF;
+        #pragma unroll
+        for (int w = 0; w < SHARE; ++w) to = fmaxf(to, s_ml[w].x);
+        top = to;
+        l = 0.f;
+        #pragma unroll
+        for (int k = 0; k < PER; ++k) acc[k] = 0.f;
+        #pragma unroll
+        for (int w = 0; w < SHARE; ++w) {
+            const float2 ml = s_ml[w];
+            const float f = ml.x == top ? 1.f : ex2(ml.x - top);
+            l = fmaf(ml.y, f, l);
+            #pragma unroll
+            for (int k = 0; k < PER; ++k) acc[k] = fmaf(s_acc[w][lane * PER + k], f, acc[k]);
         }
     }
     const float inv = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
@@ -254,14 +277,14 @@ kv_attention_join_kernel(const KvAttnArgs a, int G, int ctas, int slot_rows, con
 template <typename T, int D, int ROWS, int TILE>
 cudaError_t launch_join(const KvAttnArgs& a, int G, int ctas, int slot_rows, const long long* prefix,
                         const float* slots, cudaStream_t s) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(((size_t)a.max_new * a.H + JOIN_WARPS - 1) / JOIN_WARPS), (unsigned)a.B);
-    cfg.blockDim = dim3(JOIN_WARPS * 32);
-    cfg.stream = s;
-    cudaLaunchAttribute at = pdl_attribute();
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kv_attention_join_kernel<T, D, ROWS, TILE>, a, G, ctas, slot_rows, prefix, slots);
+    const size_t rows = (size_t)a.max_new * a.H;
+    if (rows * a.B <= 4 * (size_t)num_sms())              // up to four CTAs an SM
+        return launch_overlapped(kv_attention_join_kernel<T, D, ROWS, TILE, JOIN_WARPS>,
+                                 dim3((unsigned)rows, (unsigned)a.B), JOIN_WARPS * 32, 0, s, a, G, ctas, slot_rows,
+                                 prefix, slots);
+    return launch_overlapped(kv_attention_join_kernel<T, D, ROWS, TILE, 1>,
+                             dim3((unsigned)((rows + JOIN_WARPS - 1) / JOIN_WARPS), (unsigned)a.B), JOIN_WARPS * 32, 0,
+                             s, a, G, ctas, slot_rows, prefix, slots);
 }
 
 }  // namespace

@@ -206,6 +206,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sh->tmem_base;
+    grid_dependency_wait();
     const Run run = find_run<ROWS, TILE, THREADS>(a, G, prefix);
     const int count = (int)(run.tau1 - run.tau0);
     bool ok = count > 0;
@@ -766,8 +767,9 @@ cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
     const int slot_rows = (int)std::min<long long>(ROWS, most);
     long long* prefix = static_cast<long long*>(a.workspace);
     float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + prefix_bytes(a.B));
-    kv_attention_tc_kernel<T, D><<<ctas, THREADS, Layout<D>::SMEM, s>>>(a, G, slot_rows, prefix, slots);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = launch_overlapped(kv_attention_tc_kernel<T, D>, dim3(ctas), THREADS, Layout<D>::SMEM, s, a, G, slot_rows,
+                               prefix, slots)) != cudaSuccess)
+        return e;
     return launch_join<T, D, ROWS, TILE>(a, G, ctas, slot_rows, prefix, slots, s);
 }
 
