@@ -171,7 +171,7 @@ def _stream(stream):
         return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
     # torch.cuda.current_stream().cuda_stream without building the Stream
     # object (measured on the Grace host: 7 us a call)
-    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _contig(*ts):
@@ -554,13 +554,12 @@ def sgat_linear_noalloc(X, mask, a_m, a_u, hb, d_sh, d_m, d_u, Wq, s_w, Y, bias=
 # per layer for a handful of tokens, so the marshalling is kept short.
 # ---------------------------------------------------------------------------
 _CODES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+_I32, _FP32, _U8 = torch.int32, torch.float32, torch.uint8
 ROPE_SCALING = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
 
 
 def _rows(t, name):
     """A matrix with unit column stride: (pointer, row stride)."""
-    if t is None:
-        return None, 0
     st = t.stride()
     if len(st) != 2 or (st[1] != 1 and t.shape[1] != 1):
         raise ValueError(f"starq expects {name} as rows with unit column stride")
@@ -569,7 +568,7 @@ def _rows(t, name):
 
 def _ints(name, t, n):
     """A contiguous int32 vector of n entries."""
-    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t.dtype is not _I32 or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"starq expects {name} as {n} contiguous int32 entries")
     return t.data_ptr()
 
@@ -577,31 +576,41 @@ def _ints(name, t, n):
 def _f32(name, t, shape):
     if t is None:
         return None
-    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype is not _FP32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"starq expects {name} as contiguous float32 {list(shape)}")
     return t.data_ptr()
 
 
-def _same(dtype, **ts):
-    for name, t in ts.items():
-        if t is not None and t.dtype != dtype:
-            raise ValueError(f"starq expects {name} of type {dtype}")
+def _table(t):
+    """A rotary table: (pointer, positions, rotated channels)."""
+    positions, half, two = t.shape
+    if t.dtype is not _FP32 or two != 2 or not t.is_contiguous():
+        raise ValueError("starq expects the rotary table as contiguous float32 [positions][rot / 2][2]")
+    return t.data_ptr(), positions, 2 * half
+
+
+def _pages(t, B):
+    if t.dtype is not _I32 or t.dim() != 2 or t.shape[0] != B or not t.is_contiguous():
+        raise ValueError(f"starq expects the page table as contiguous int32 [{B}][pages per sequence]")
+    return t.data_ptr(), t.shape[1]
 
 
 class KVCache:
     """The paged 8-bit cache: K, V uint8 [pages][Hkv][page][D] (a byte is a
     code + 128), k_scale, v_scale float32 [pages][Hkv] (one scale per block
     of a page and a head). Holds the tensors."""
-    __slots__ = ("K", "V", "k_scale", "v_scale", "Hkv", "D", "c")
+    __slots__ = ("K", "V", "k_scale", "v_scale", "Hkv", "D", "c", "ref")
 
     def __init__(self, K, V, k_scale, v_scale):
-        pages, Hkv, page, D = K.shape
-        if K.dtype != torch.uint8 or V.dtype != torch.uint8 or V.shape != K.shape:
-            raise ValueError("starq expects the cache's K and V as uint8 of one shape [pages][Hkv][page][D]")
-        _contig(K, V)
+        shape = K.shape
+        pages, Hkv, page, D = shape
+        if K.dtype is not _U8 or V.dtype is not _U8 or V.shape != shape or not (K.is_contiguous() and V.is_contiguous()):
+            raise ValueError("starq expects the cache's K and V as contiguous uint8 of one shape [pages][Hkv][page][D]")
+        scales = (pages, Hkv)
         self.K, self.V, self.k_scale, self.v_scale, self.Hkv, self.D = K, V, k_scale, v_scale, Hkv, D
-        self.c = StarqKvCache(K.data_ptr(), V.data_ptr(), _f32("k_scale", k_scale, (pages, Hkv)),
-                              _f32("v_scale", v_scale, (pages, Hkv)), pages, page, Hkv, D)
+        self.c = StarqKvCache(K.data_ptr(), V.data_ptr(), _f32("k_scale", k_scale, scales),
+                              _f32("v_scale", v_scale, scales), pages, page, Hkv, D)
+        self.ref = ctypes.byref(self.c)
 
     @classmethod
     def empty(cls, pages, Hkv, page, D, device="cuda"):
@@ -610,41 +619,33 @@ class KVCache:
         return cls(code(), code(), scale(), scale())
 
 
-def _pages(t, B):
-    if t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != B or not t.is_contiguous():
-        raise ValueError(f"starq expects the page table as contiguous int32 [{B}][pages per sequence]")
-    return t.data_ptr(), t.shape[1]
-
-
 def rope_table(table, theta, scaling="none", factor=1.0, original=0.0, beta_fast=32.0, beta_slow=1.0, mscale=0.0,
                stream=None):
     """Fills table [positions][rot / 2][2] (float32) with the cosines and
     sines of the rotary positions; scaling: "none", "linear", "ntk" or
     "parts" (see include/starq.h)."""
-    positions, half, two = table.shape
-    assert two == 2
-    _f32("table", table, (positions, half, 2))
-    _check(lib.glue_rope_table(table.data_ptr(), positions, 2 * half, float(theta), ROPE_SCALING[scaling],
-                               float(factor), float(original), float(beta_fast), float(beta_slow), float(mscale),
-                               _stream(stream)))
+    tab, positions, rot = _table(table)
+    _check(lib.glue_rope_table(tab, positions, rot, float(theta), ROPE_SCALING[scaling], float(factor),
+                               float(original), float(beta_fast), float(beta_slow), float(mscale), _stream(stream)))
 
 
 def rope_apply(X, heads, pos, table, Y=None, D=None, interleaved=False, inverse=False, stream=None):
     """Rotates the first `heads` heads of D channels (default: X's columns
     over heads) of each row of X by table[pos] into Y (default: in place);
     inverse: the transposed map (the gradient)."""
-    Y = X if Y is None else Y
-    L = X.shape[0]
-    D = X.shape[1] // heads if D is None else D
-    if X.shape[1] < heads * D or Y.shape[0] != L or Y.shape[1] < heads * D:
-        raise ValueError("starq expects X and Y as rows of at least heads * D channels")
-    _same(X.dtype, Y=Y)
+    if Y is None:
+        Y = X
+    L, width = X.shape
+    if D is None:
+        D = width // heads
+    dtype = X.dtype
+    if width < heads * D or Y.shape[0] != L or Y.shape[1] < heads * D or Y.dtype is not dtype:
+        raise ValueError("starq expects X and Y as rows of at least heads * D channels of one type")
     x, ldx = _rows(X, "X")
     y, ldy = _rows(Y, "Y")
-    positions, half, _ = table.shape
-    _check(lib.glue_rope_apply(x, ldx, _CODES[X.dtype], L, heads, D, 2 * half, interleaved, inverse,
-                               _ints("pos", pos, L), _f32("table", table, (positions, half, 2)), positions, y, ldy,
-                               _stream(stream)))
+    tab, positions, rot = _table(table)
+    _check(lib.glue_rope_apply(x, ldx, _CODES[dtype], L, heads, D, rot, interleaved, inverse, _ints("pos", pos, L), tab,
+                               positions, y, ldy, _stream(stream)))
 
 
 def kv_cache_append(cache, K, V, seq_start, past, page_table, pos, table, max_new, Q=None, Q_out=None,
@@ -653,28 +654,29 @@ def kv_cache_append(cache, K, V, seq_start, past, page_table, pos, table, max_ne
     and V [T][Hkv D] behind the past[b] tokens that sequence b keeps, and
     rotates Q [T][H D] into Q_out. seq_start [B + 1]: each sequence's rows,
     at most max_new."""
-    T, B, w = K.shape[0], past.shape[0], cache.Hkv * cache.D
-    if K.shape[1] != w or V.shape[0] != T or V.shape[1] != w:
-        raise ValueError(f"starq expects K and V as rows of Hkv * D = {w} channels")
-    _same(K.dtype, V=V, Q=Q, Q_out=Q_out)
+    shape, B, D, dtype = K.shape, past.shape[0], cache.D, K.dtype
+    T = shape[0]
+    if shape[1] != cache.Hkv * D or V.shape != shape or V.dtype is not dtype:
+        raise ValueError(f"starq expects K and V as rows of Hkv * D = {cache.Hkv * D} channels of one type")
     k, ldk = _rows(K, "K")
     v, ldv = _rows(V, "V")
-    q, ldq = _rows(Q, "Q")
-    qo, ldqo = _rows(Q_out, "Q_out")
-    H = 0
+    q = qo = tab = at = None
+    ldq = ldqo = H = positions = rot = 0
     if Q is not None:
-        H = Q.shape[1] // cache.D
-        if Q_out is None or Q.shape != Q_out.shape or Q.shape[0] != T or Q.shape[1] != H * cache.D:
-            raise ValueError("starq expects Q and Q_out as T rows of H * D channels")
-    tab, positions, half = None, 0, 0
+        qs = Q.shape
+        H = qs[1] // D
+        if Q_out is None or Q_out.shape != qs or qs != (T, H * D) or Q.dtype is not dtype or Q_out.dtype is not dtype:
+            raise ValueError("starq expects Q and Q_out as T rows of H * D channels of K's type")
+        q, ldq = _rows(Q, "Q")
+        qo, ldqo = _rows(Q_out, "Q_out")
     if table is not None:
-        positions, half, _ = table.shape
-        tab = _f32("table", table, (positions, half, 2))
+        tab, positions, rot = _table(table)
+    if pos is not None:
+        at = _ints("pos", pos, T)
     pt, pld = _pages(page_table, B)
-    _check(lib.kv_cache_append(ctypes.byref(cache.c), k, ldk, v, ldv, q, ldq, qo, ldqo, H, _CODES[K.dtype], T,
-                               _ints("seq_start", seq_start, B + 1), _ints("past", past, B), B, max_new, pt, pld,
-                               None if pos is None else _ints("pos", pos, T), tab, positions, 2 * half, interleaved,
-                               _stream(stream)))
+    _check(lib.kv_cache_append(cache.ref, k, ldk, v, ldv, q, ldq, qo, ldqo, H, _CODES[dtype], T,
+                               _ints("seq_start", seq_start, B + 1), _ints("past", past, B), B, max_new, pt, pld, at,
+                               tab, positions, rot, interleaved, _stream(stream)))
 
 
 def kv_cache_read(cache, page_table, first, out_start, K, V, max_rows, stream=None):
@@ -682,17 +684,20 @@ def kv_cache_read(cache, page_table, first, out_start, K, V, max_rows, stream=No
     into rows out_start[b] .. out_start[b + 1] - 1 (at most max_rows) of K
     and V [T][Hkv D] (either may be None)."""
     B, w = first.shape[0], cache.Hkv * cache.D
-    one = K if K is not None else V
-    for t in (K, V):
-        if t is not None and (t.shape != one.shape or t.shape[1] != w or t.stride() != one.stride()):
-            raise ValueError(f"starq expects K and V as rows of Hkv * D = {w} channels with one stride")
-    _same(one.dtype, K=K, V=V)
-    k, ldk = _rows(K, "K")
-    v, ldv = _rows(V, "V")
+    one = V if K is None else K
+    dtype = one.dtype
+    T, width = one.shape
+    p, ld = _rows(one, "K" if K is not None else "V")
+    k, v = (None, p) if K is None else (p, None)
+    if K is not None and V is not None:
+        v, ldv = _rows(V, "V")
+        if V.shape != one.shape or V.dtype is not dtype or ldv != ld:
+            raise ValueError("starq expects K and V as rows of one shape, type and stride")
+    if width != w:
+        raise ValueError(f"starq expects rows of Hkv * D = {w} channels")
     pt, pld = _pages(page_table, B)
-    _check(lib.kv_cache_read(ctypes.byref(cache.c), pt, pld, _ints("first", first, B),
-                             _ints("out_start", out_start, B + 1), B, max_rows, one.shape[0], k, v, ldk or ldv,
-                             _CODES[one.dtype], _stream(stream)))
+    _check(lib.kv_cache_read(cache.ref, pt, pld, _ints("first", first, B), _ints("out_start", out_start, B + 1), B,
+                             max_rows, T, k, v, ld, _CODES[dtype], _stream(stream)))
 
 
 def kv_cache_attention_workspace_size(B, max_new, H, Hkv, D):
@@ -705,28 +710,30 @@ def kv_cache_attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, ma
     at most max_new) over the kv_len[b] (at most max_len) cached tokens into
     Out [T][H D]; lse [T][H] receives the log-sum-exp. key_mask uint8
     [B][>= max_len]: 0 = not seen. scale: default 1 / sqrt(D)."""
-    T, B, D = Q.shape[0], kv_len.shape[0], cache.D
-    H = Q.shape[1] // D
-    if Q.shape[1] != H * D or Out.shape != Q.shape:
-        raise ValueError("starq expects Q and Out as T rows of H * D channels")
-    _same(Q.dtype, Out=Out)
+    shape, B, D, dtype = Q.shape, kv_len.shape[0], cache.D, Q.dtype
+    T = shape[0]
+    H = shape[1] // D
+    if shape != (T, H * D) or Out.shape != shape or Out.dtype is not dtype:
+        raise ValueError("starq expects Q and Out as T rows of H * D channels of one type")
     q, ldq = _rows(Q, "Q")
     o, ldo = _rows(Out, "Out")
     pt, pld = _pages(page_table, B)
     mk, mld = None, 0
     if key_mask is not None:
-        if key_mask.dtype != torch.uint8 or key_mask.shape[0] != B:
+        if key_mask.dtype is not _U8 or key_mask.shape[0] != B:
             raise ValueError(f"starq expects key_mask as uint8 [{B}][slots]")
         mk, mld = _rows(key_mask, "key_mask")
         if key_mask.shape[1] < max_len:
             raise ValueError(f"starq expects key_mask rows of at least max_len = {max_len} bytes")
     if workspace is None:
-        workspace = torch.empty(lib.kv_cache_attention_workspace_size(B, max_new, H, cache.Hkv, D), dtype=torch.uint8,
-                                device=Q.device)
-    _check(lib.kv_cache_attention(q, ldq, _CODES[Q.dtype], T, _ints("seq_start", seq_start, B + 1), B, max_new, H,
-                                  ctypes.byref(cache.c), pt, pld, _ints("kv_len", kv_len, B), max_len, causal, mk, mld,
-                                  D ** -0.5 if scale is None else scale, o, ldo, _f32("lse", lse, (T, H)),
-                                  workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+        size = lib.kv_cache_attention_workspace_size(B, max_new, H, cache.Hkv, D)
+        workspace = torch.empty(size, dtype=_U8, device=Q.device)
+    else:
+        size = workspace.numel() * workspace.element_size()
+    _check(lib.kv_cache_attention(q, ldq, _CODES[dtype], T, _ints("seq_start", seq_start, B + 1), B, max_new, H,
+                                  cache.ref, pt, pld, _ints("kv_len", kv_len, B), max_len, causal, mk, mld,
+                                  D ** -0.5 if scale is None else scale, o, ldo,
+                                  None if lse is None else _f32("lse", lse, (T, H)), workspace.data_ptr(), size,
                                   _stream(stream)))
 
 
@@ -734,11 +741,13 @@ def w4g_linear(X, Wq, scales, Y, bias=None, stream=None):
     """Y [L][N] = X [L][K] W^T (+ bias) for at most 32 rows; Wq uint8
     [N][K/2] packed int4, scales float32 [N][K / group]."""
     L, K = X.shape
-    N, groups = scales.shape
-    if Wq.dtype != torch.uint8 or tuple(Wq.shape) != (N, K // 2) or tuple(Y.shape) != (L, N) or K % max(groups, 1):
+    sc = scales.shape
+    N, groups = sc
+    if Wq.dtype is not _U8 or Wq.shape != (N, K // 2) or not Wq.is_contiguous() or Y.shape != (L, N) or groups < 1 \
+            or K % groups:
         raise ValueError("starq expects X [L][K], Wq [N][K/2] uint8, scales [N][K / group] and Y [L][N]")
-    _contig(Wq)
     x, ldx = _rows(X, "X")
     y, ldy = _rows(Y, "Y")
-    _check(lib.w4g_linear(x, ldx, _CODES[X.dtype], L, K, Wq.data_ptr(), _f32("scales", scales, (N, groups)),
-                          K // max(groups, 1), N, _f32("bias", bias, (N,)), y, ldy, _CODES[Y.dtype], _stream(stream)))
+    _check(lib.w4g_linear(x, ldx, _CODES[X.dtype], L, K, Wq.data_ptr(), _f32("scales", scales, sc), K // groups, N,
+                          None if bias is None else _f32("bias", bias, (N,)), y, ldy, _CODES[Y.dtype],
+                          _stream(stream)))
