@@ -67,6 +67,7 @@ struct W4gArgs {
     const void* X; int ldx; int dtype; int L; int K;
     const uint8_t* Wq; const float* scales; int group; int N; const float* bias;
     void* Y; int ldy; int y_dtype;
+    unsigned* status;
 };
 cudaError_t launch_w4g_linear(const W4gArgs& a, cudaStream_t s);
 

@@ -6,17 +6,37 @@
 // Bound by memory: the weights are read once for all rows (K / 2 + 4 K /
 // group bytes a channel) and one row needs two operations a weight. The
 // products run on the 16-bit MMA, weights as the 16-row operand and eight
-// activation rows as the columns: with one row the MMA is idle seven
-// eighths of the time and still far from the bound, and the CUDA cores are
-// left to turn codes into 16-bit numbers. Codes are exact in fp16 and bf16,
-// a group's sum is accumulated in float32 and only then multiplied by its
-// scale, so no product is rounded before the float32 sums.
+// activation rows as the columns: with one row the MMA is idle seven eighths
+// of the time and still far from the bound.
 //
-// A CTA owns 16 output channels; its warps take 128-channel blocks of K in
-// turn and meet once at the end in shared memory, in warp order. The k order
-// inside an MMA is free: a thread takes the eight nibbles of one word, pairs
-// nibble i with nibble i + 4 (one AND puts both into the halves of a
-// register), and the activations are paired the same way.
+// A code c enters the MMA as the fp16 subnormal (c + 8) 2^-24: one three-input
+// operation takes two codes out of a word and flips their sign bits, and
+// there is nothing to convert or to subtract (the first form did both, and a
+// third of its instructions were these). The sum of a group starts from
+// -8 2^-24 sum x instead, and the result is multiplied by 2^24 at the end.
+// The upper codes of a byte come out as 16 (c + 8) 2^-24 and have a sum of
+// their own that is divided by 16. The subnormals and the products are exact,
+// a group's sum is accumulated in float32 and only then multiplied by its
+// scale. bf16 activations become fp16, a row's 128 channels of a block scaled
+// by a power of two that puts the largest at 2^14: what lies 2^-29 below
+// that one loses its last bits, which is under the float32 sum's own.
+// The k order inside an MMA is free: a thread takes the eight codes of a word
+// and the activations are paired to match.
+//
+// A warp owns 16 output channels and a slice of K, and nothing in its loop
+// waits for another warp: codes and scales come into a ring of its own by
+// asynchronous 16- and 4-byte copies. A cluster of CTAs shares the slices and
+// adds up at its end, through each other's shared memory, in the order of the
+// slices. So a CTA brings and converts its slice of the activations only,
+// once. Measured at K = 12288, N = 4096, groups of 32, 12 rows (31.8 MB):
+// 15.8 us, 2.0 TB/s; with the warps of one CTA taking the blocks of K in turn
+// for 16 channels, all of them needing all activations, 25.7 us with the
+// codes in registers, 31 us with 512-byte bulk copies. One row at K = 3584,
+// N = 37888, groups of 64 (76.5 MB): 17.9 us, 4.3 TB/s, against 22.3 and 29
+// us. About 5 us of each call are its start, the activations and the joining:
+// K = N = 4096 (8.9 MB) takes 5.6 us. Four stages of two CTAs an SM suffice:
+// 6 or 8 of them, or a third CTA, changed nothing.
+#include <algorithm>
 #include <type_traits>
 
 #include "decode.cuh"
@@ -26,177 +46,336 @@ namespace {
 
 constexpr int WARPS = 8;
 constexpr int THREADS = WARPS * 32;
-constexpr int TILE_N = 16;             // output channels of a CTA
-constexpr int KB = 128;                // input channels of a warp's block
-constexpr int AHEAD = 4;               // blocks in flight per warp
+constexpr int TILE = 16;               // output channels of a warp
+constexpr int CTA_N = WARPS * TILE;    // of a CTA
+constexpr int KB = 128;                // input channels of a block
+constexpr int STAGES = 4;              // blocks of a warp on their way
+constexpr int MAX_SLICES = 8;          // CTAs of a cluster
+constexpr int X_ROW = KB * 2;          // bytes of an activation row in a block
+constexpr int CODES = TILE * KB / 2;   // bytes of a stage's codes
+template <int GROUP> constexpr int STAGE = CODES + TILE * (KB / GROUP) * 4;       // and of its scales behind them
+template <int GROUP> constexpr int RING = WARPS * STAGES * STAGE<GROUP>;
 
-template <typename T>
-__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                          uint32_t b0, uint32_t b1) {
-    if (std::is_same<T, __half>::value)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
-                     "{%0,%1,%2,%3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-    else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
-                     "{%0,%1,%2,%3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+template <typename T> constexpr bool IS_HALF = std::is_same<T, __half>::value;
+
+// d = a b + c (c may be d).
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0,
+                                          float c1, float c2, float c3) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+                 "{%10,%11,%12,%13};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 
-// Nibbles I and I + 4 of a word (two's complement) as a pair of 16-bit
-// numbers: the nibble with its sign bit flipped is c + 8; put under the
-// exponent of 1024 (fp16) or 128 (bf16), whose last place is 1, it reads
-// 1024 + c + 8, and one exact subtraction leaves c.
-template <typename T, int I>
-__device__ __forceinline__ uint32_t nibble_pair(uint32_t w) {
-    constexpr uint32_t magic = std::is_same<T, __half>::value ? 0x64086408u : 0x43084308u;
-    const uint32_t u = ((w >> (4 * I)) & 0x000f000fu) ^ magic;
+// (w & mask) ^ flip in one operation (with both constants as immediates the
+// compiler makes two: a third of all instructions were these).
+__device__ __forceinline__ uint32_t field(uint32_t w, uint32_t mask, uint32_t flip) {
     uint32_t r;
-    if (std::is_same<T, __half>::value) {
-        const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&u),
-                                  __half2half2(__ushort_as_half((unsigned short)0x6408)));       // 1032
-        r = *reinterpret_cast<const uint32_t*>(&v);
-    } else {
-        const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&u),
-                                         __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)0x4308)));   // 136
-        r = *reinterpret_cast<const uint32_t*>(&v);
-    }
+    asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(r) : "r"(w), "r"(mask), "r"(flip));
     return r;
 }
 
-// Words of one weight row in a 128-channel block: sub-block j (of GROUP
-// channels) gives thread t the GROUP / 32 words at channel GROUP j +
-// GROUP / 4 t. Sub-blocks past K stay 0.
-template <int GROUP>
-__device__ __forceinline__ void load_words(uint32_t (&w)[4], const uint8_t* row, int k0, int K, int t) {
-    #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = 0;
-    if (row == nullptr) return;
-    #pragma unroll
-    for (int j = 0; j < KB / GROUP; ++j) {
-        const int k = k0 + GROUP * j;
-        if (k < K) {
-            const uint8_t* p = row + (k + GROUP / 4 * t) / 2;
-            if (GROUP == 128) {
-                const uint4 v = ld_global_nc_v4(p);
-                w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-            } else if (GROUP == 64) {
-                const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-                w[2 * j] = v.x; w[2 * j + 1] = v.y;
-            } else {
-                w[j] = __ldg(reinterpret_cast<const uint32_t*>(p));
-            }
-        }
-    }
+// Eight activations as four fp16 pairs (x0, x4), (x2, x6), (x1, x5), (x3, x7).
+__device__ __forceinline__ uint4 paired(const float (&f)[8]) {
+    uint4 v;
+    const __half2 a = __floats2half2_rn(f[0], f[4]), b = __floats2half2_rn(f[2], f[6]);
+    const __half2 c = __floats2half2_rn(f[1], f[5]), d = __floats2half2_rn(f[3], f[7]);
+    v.x = *reinterpret_cast<const uint32_t*>(&a);
+    v.y = *reinterpret_cast<const uint32_t*>(&b);
+    v.z = *reinterpret_cast<const uint32_t*>(&c);
+    v.w = *reinterpret_cast<const uint32_t*>(&d);
+    return v;
 }
 
-// NT tiles of 8 activation rows.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool real) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"(dst), "l"(src), "r"(real ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() {
+    asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory");
+}
+
+// 16-byte chunk c (of 4) of row r of a stage: rows that are read together
+// fall into different banks.
+template <int GROUP> __device__ __forceinline__ int w_offset(int r, int c) {
+    const int key = GROUP == 128 ? 0 : GROUP == 64 ? r & 2 : (r >> 1) & 3;
+    return r * (KB / 2) + ((c ^ key) << 4);
+}
+
+// 16-byte chunk c (of 16) of activation row i of a block; the four threads
+// and the two rows that are read together fall into different chunks of 128
+// bytes.
+template <int GROUP> __device__ __forceinline__ uint32_t x_offset(int i, int c) {
+    const int odd = i & 1;
+    const int key = GROUP == 128 ? 2 * odd ^ ((c >> 3) & 1) : GROUP == 64 ? odd : 4 * odd;
+    return i * X_ROW + ((c ^ key) << 4);
+}
+
+template <int GROUP, int NT> constexpr int SUM_ROW = KB / GROUP * 8 * NT * 4;      // groups' sums of a block, bytes
+template <int NT> constexpr int POW_ROW = 8 * NT * 4;                              // powers of two of a block, bytes
+constexpr int PART_ROW = CTA_N + 4;                                                // floats of a row of partial sums
+
+// NT tiles of 8 activation rows. A cluster of `slices` CTAs takes CTA_N output
+// channels, each CTA `per` blocks of K; the activations of `chunk` of them are
+// in shared memory at a time.
 template <typename T, int GROUP, int NT>
-__global__ void __launch_bounds__(THREADS) w4g_linear_kernel(const W4gArgs a) {
-    __shared__ float part[WARPS][NT][TILE_N][8];
+__global__ void __launch_bounds__(THREADS, 2) w4g_linear_kernel(const W4gArgs a, int slices, int per, int chunk) {
+    constexpr int GB = KB / GROUP;                   // groups of a block
+    constexpr int GW = GROUP / 32;                   // words of a thread in a group
+    constexpr int COLS = 8 * NT;
+    extern __shared__ __align__(128) uint8_t smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int n0 = blockIdx.x * TILE_N;
     const int blocks = (a.K + KB - 1) / KB, groups = a.K / GROUP;
-    const uint8_t* row[2];
-    const float* srow[2];
+    const int rank = blockIdx.x % slices, n0 = blockIdx.x / slices * CTA_N, nw = n0 + warp * TILE;
+    const int k0 = min(rank * per, blocks), k1 = min(k0 + per, blocks);
+    uint8_t* const ring = smem + warp * STAGES * STAGE<GROUP>;
+    uint8_t* const xs = smem + RING<GROUP>;
+    float* const sums = reinterpret_cast<float*>(xs + chunk * a.L * X_ROW);        // [chunk][GB][COLS]: -8 2^-24 sum x
+    float* const pows = sums + chunk * (SUM_ROW<GROUP, NT> / 4);                   // [chunk][COLS]
+
+    // --- a warp's weights: 16 rows of 64 bytes and their scales a block ---------
+    const uint8_t* src[2];
     #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        const int n = n0 + g + 8 * r;
-        row[r] = n < a.N ? a.Wq + (size_t)n * (a.K / 2) : nullptr;
-        srow[r] = a.scales + (size_t)(n < a.N ? n : 0) * groups;
-    }
+    for (int h = 0; h < 2; ++h)
+        src[h] = a.Wq + (size_t)min(nw + 8 * h + g, a.N - 1) * (size_t)(a.K / 2) + 16 * t;
+    const float* ssrc[(GB + 1) / 2];
+    #pragma unroll
+    for (int h = 0; h < (GB + 1) / 2; ++h)
+        ssrc[h] = a.scales + (size_t)min(nw + (lane + 32 * h) / GB % TILE, a.N - 1) * groups + lane % GB;
+    auto fetch = [&](int kb, int st) {
+        const uint32_t to = smem_addr(ring + st * STAGE<GROUP>);
+        if (kb < k1) {
+            const bool real = kb * KB + 32 * t < a.K;          // K is a multiple of 32: a chunk is in or out
+            #pragma unroll
+            for (int h = 0; h < 2; ++h)
+                copy16(to + w_offset<GROUP>(8 * h + g, t), src[h] + (real ? (size_t)kb * (KB / 2) : 0), real);
+            const bool group = kb * GB + lane % GB < groups;
+            #pragma unroll
+            for (int h = 0; h < (GB + 1) / 2; ++h)
+                if (GB > 1 || lane < TILE)
+                    copy4(to + CODES + 4 * (lane + 32 * h), ssrc[h] + (group ? kb * GB : 0), group);
+        }
+        copies_commit();
+    };
+    #pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) fetch(k0 + i, i);
+
+    // --- the chunk's activations: 16 threads a row of a block ------------------
+    auto bring = [&](int c0) {
+        constexpr int BATCH = 4;                     // loads of a thread on their way together
+        const int pieces = min(chunk, k1 - c0) * a.L * 16;
+        for (int e0 = threadIdx.x; e0 < pieces; e0 += BATCH * THREADS) {
+            uint4 raw[BATCH];
+            int blk[BATCH], tok[BATCH];
+            #pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                const int e = e0 + u * THREADS, c = e & 15;
+                blk[u] = (int)((unsigned)(e >> 4) / (unsigned)a.L);
+                tok[u] = (e >> 4) - blk[u] * a.L;
+                const int k = (c0 + blk[u]) * KB + 8 * c;
+                raw[u] = make_uint4(0, 0, 0, 0);
+                if (e < pieces && k < a.K) raw[u] = ld_global_nc_v4(static_cast<const T*>(a.X) + (size_t)tok[u] * a.ldx + k);
+            }
+            #pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                if (e0 + u * THREADS >= pieces) break;
+                const int c = e0 & 15, b = blk[u], i = tok[u];
+                float f[8];
+                Eight<T>::load(reinterpret_cast<const T*>(&raw[u]), f);
+                float down = 1.f;
+                // the 16 threads of a row are half a warp (the last round may have one half only)
+                const unsigned half = 0xffffu << (lane & 16);
+                if (!IS_HALF<T>) {
+                    float top = 0.f;
+                    #pragma unroll
+                    for (int v = 0; v < 8; ++v) top = fmaxf(top, fabsf(f[v]));
+                    #pragma unroll
+                    for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(half, top, d));
+                    const int ex = max((int)(__float_as_uint(top) >> 23) - 127, -112);
+                    const float up = __uint_as_float((uint32_t)(14 - ex + 127) << 23);          // 2^(14 - ex)
+                    down = __uint_as_float((uint32_t)(ex - 14 + 127) << 23);
+                    #pragma unroll
+                    for (int v = 0; v < 8; ++v) f[v] *= up;
+                }
+                float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+                #pragma unroll
+                for (int d = 1; d < GROUP / 8; d <<= 1) sum += __shfl_xor_sync(half, sum, d);
+                *reinterpret_cast<uint4*>(xs + b * a.L * X_ROW + x_offset<GROUP>(i, c)) = paired(f);
+                if (c % (GROUP / 8) == 0)
+                    sums[(b * GB + c / (GROUP / 8)) * COLS + i] = sum * -4.76837158203125e-07f;         // -8 2^-24
+                if (!IS_HALF<T> && c == 0) pows[b * COLS + i] = down;
+            }
+        }
+    };
+    // constants of the fields, kept in registers
+    uint32_t m0 = 0x000f000fu, f0 = 0x00080008u, m1 = 0x00f000f0u, f1 = 0x00800080u;
+    asm volatile("" : "+r"(m0), "+r"(f0), "+r"(m1), "+r"(f1));
+
     float acc[NT][4];
     #pragma unroll
     for (int i = 0; i < NT; ++i)
         #pragma unroll
-        for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
-
-    for (int kb0 = warp; kb0 < blocks; kb0 += WARPS * AHEAD) {
-        uint32_t w[AHEAD][2][4];
-        float sc[AHEAD][2][KB / GROUP];
-        #pragma unroll
-        for (int p = 0; p < AHEAD; ++p) {
-            const int kb = kb0 + p * WARPS;
+        for (int c = 0; c < 4; ++c) acc[i][c] = 0.f;
+    int st = 0, to = STAGES - 1;
+    for (int c0 = k0; c0 < k1; c0 += chunk) {
+        if (c0 != k0) __syncthreads();               // the last chunk is done with
+        bring(c0);
+        __syncthreads();
+        const int c1 = min(c0 + chunk, k1);
+        for (int kb = c0; kb < c1; ++kb) {
+            copies_wait<STAGES - 2>();
+            __syncwarp();                            // everyone's copies are in, and the stage before is done with
+            fetch(kb + STAGES - 1, to);
+            if (++to == STAGES) to = 0;
+            const uint8_t* const ws = ring + st * STAGE<GROUP>;
+            if (++st == STAGES) st = 0;
+            const uint8_t* const xb = xs + (kb - c0) * a.L * X_ROW;
+            float sc[2][GB];
             #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                load_words<GROUP>(w[p][r], kb < blocks ? row[r] : nullptr, kb * KB, a.K, t);
-                #pragma unroll
-                for (int j = 0; j < KB / GROUP; ++j) {
-                    const int grp = kb * (KB / GROUP) + j;
-                    sc[p][r][j] = kb < blocks && grp < groups ? __ldg(srow[r] + grp) : 0.f;
-                }
+            for (int h = 0; h < 2; ++h) {
+                const float* p = reinterpret_cast<const float*>(ws + CODES) + (8 * h + g) * GB;
+                if (GB == 4) *reinterpret_cast<float4*>(sc[h]) = *reinterpret_cast<const float4*>(p);
+                else if (GB == 2) *reinterpret_cast<float2*>(sc[h]) = *reinterpret_cast<const float2*>(p);
+                else sc[h][0] = *p;
             }
-        }
-        #pragma unroll
-        for (int p = 0; p < AHEAD; ++p) {
-            const int kb = kb0 + p * WARPS;
-            if (kb >= blocks) break;
-            #pragma unroll
-            for (int j = 0; j < KB / GROUP; ++j) {
-                const int k = kb * KB + GROUP * j + GROUP / 4 * t;
-                if (kb * KB + GROUP * j >= a.K) break;
-                float d[NT][4];
+            float2 pw[NT];
+            if (!IS_HALF<T>)
                 #pragma unroll
                 for (int i = 0; i < NT; ++i)
-                    #pragma unroll
-                    for (int c = 0; c < 4; ++c) d[i][c] = 0.f;
+                    pw[i] = *reinterpret_cast<const float2*>(pows + (kb - c0) * COLS + 8 * i + 2 * t);
+            #pragma unroll
+            for (int j = 0; j < GB; ++j) {
+                float2 m8[NT];
                 #pragma unroll
-                for (int e = 0; e < GROUP / 32; ++e) {
-                    const uint32_t w0 = w[p][0][j * (GROUP / 32) + e], w1 = w[p][1][j * (GROUP / 32) + e];
-                    const uint32_t p0 = nibble_pair<T, 0>(w0), p1 = nibble_pair<T, 1>(w0);
-                    const uint32_t p2 = nibble_pair<T, 2>(w0), p3 = nibble_pair<T, 3>(w0);
-                    const uint32_t q0 = nibble_pair<T, 0>(w1), q1 = nibble_pair<T, 1>(w1);
-                    const uint32_t q2 = nibble_pair<T, 2>(w1), q3 = nibble_pair<T, 3>(w1);
+                for (int i = 0; i < NT; ++i)
+                    m8[i] = *reinterpret_cast<const float2*>(sums + ((kb - c0) * GB + j) * COLS + 8 * i + 2 * t);
+                uint32_t w[2][4];
+                #pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    // bytes GROUP / 2 j + GROUP / 8 t of the row
+                    const int at = GROUP / 2 * j + GROUP / 8 * t;
+                    const uint8_t* p = ws + w_offset<GROUP>(8 * h + g, at >> 4) + (at & 15);
+                    if (GROUP == 128) *reinterpret_cast<uint4*>(w[h]) = *reinterpret_cast<const uint4*>(p);
+                    else if (GROUP == 64) *reinterpret_cast<uint2*>(w[h]) = *reinterpret_cast<const uint2*>(p);
+                    else w[h][0] = *reinterpret_cast<const uint32_t*>(p);
+                }
+                float lo[NT][4], hi[NT][4];
+                #pragma unroll
+                for (int e = 0; e < GW; ++e) {
+                    const uint32_t w0 = w[0][e], w1 = w[1][e], v0 = w0 >> 8, v1 = w1 >> 8;
+                    const uint32_t ev[4] = {field(w0, m0, f0), field(w1, m0, f0), field(v0, m0, f0), field(v1, m0, f0)};
+                    const uint32_t od[4] = {field(w0, m1, f1), field(w1, m1, f1), field(v0, m1, f1), field(v1, m1, f1)};
                     #pragma unroll
                     for (int i = 0; i < NT; ++i) {
-                        uint4 x = make_uint4(0, 0, 0, 0);
-                        if (8 * i + g < a.L)
-                            x = ld_global_nc_v4(static_cast<const T*>(a.X) + (size_t)(8 * i + g) * a.ldx + k + 8 * e);
-                        mma_16816<T>(d[i], p0, q0, p1, q1, prmt(x.x, x.z, 0x5410u), prmt(x.x, x.z, 0x7632u));
-                        mma_16816<T>(d[i], p2, q2, p3, q3, prmt(x.y, x.w, 0x5410u), prmt(x.y, x.w, 0x7632u));
+                        // columns past L repeat the last row (not stored)
+                        const uint4 x = *reinterpret_cast<const uint4*>(
+                            xb + x_offset<GROUP>(min(8 * i + g, a.L - 1), GROUP / 8 * j + GW * t + e));
+                        float(&l)[4] = lo[i], (&h)[4] = hi[i];
+                        if (e == 0) {
+                            mma_16816(l, ev, x.x, x.y, m8[i].x, m8[i].y, m8[i].x, m8[i].y);
+                            mma_16816(h, od, x.z, x.w, 0.f, 0.f, 0.f, 0.f);
+                        } else {
+                            mma_16816(l, ev, x.x, x.y, l[0], l[1], l[2], l[3]);
+                            mma_16816(h, od, x.z, x.w, h[0], h[1], h[2], h[3]);
+                        }
                     }
                 }
                 #pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    acc[i][0] = fmaf(d[i][0], sc[p][0][j], acc[i][0]);
-                    acc[i][1] = fmaf(d[i][1], sc[p][0][j], acc[i][1]);
-                    acc[i][2] = fmaf(d[i][2], sc[p][1][j], acc[i][2]);
-                    acc[i][3] = fmaf(d[i][3], sc[p][1][j], acc[i][3]);
-                }
+                for (int i = 0; i < NT; ++i)
+                    #pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        float s = sc[k >> 1][j];
+                        if (!IS_HALF<T>) s *= k & 1 ? pw[i].y : pw[i].x;
+                        acc[i][k] = fmaf(fmaf(hi[i][k], 0.0625f, lo[i][k]), s, acc[i][k]);
+                    }
             }
         }
     }
+
+    // --- the cluster adds up, in the order of the slices -------------------------
+    copies_wait<0>();
+    __syncthreads();                                 // the rings are done with
+    float* const part = reinterpret_cast<float*>(smem);          // [L][PART_ROW]
     #pragma unroll
     for (int i = 0; i < NT; ++i)
         #pragma unroll
-        for (int c = 0; c < 4; ++c) part[warp][i][g + 8 * (c >> 1)][2 * t + (c & 1)] = acc[i][c];
-    __syncthreads();
-    for (int e = threadIdx.x; e < NT * 8 * TILE_N; e += THREADS) {
-        const int n = e % TILE_N, i = e / TILE_N;
-        if (i >= a.L || n0 + n >= a.N) continue;
+        for (int k = 0; k < 4; ++k) {
+            const int row = 8 * i + 2 * t + (k & 1);
+            if (row < a.L) part[row * PART_ROW + warp * TILE + g + 8 * (k >> 1)] = acc[i][k];
+        }
+    if (slices > 1) cluster_sync();
+    else __syncthreads();
+    for (int e = rank * THREADS + threadIdx.x; e < a.L * CTA_N; e += slices * THREADS) {
+        const int row = e / CTA_N, nn = e % CTA_N, n = n0 + nn;
+        if (n >= a.N) continue;
         float y = 0.f;
-        #pragma unroll
-        for (int w = 0; w < WARPS; ++w) y += part[w][i >> 3][n][i & 7];
-        if (a.bias != nullptr) y += __ldg(a.bias + n0 + n);
-        const size_t at = (size_t)i * a.ldy + n0 + n;
+        if (slices == 1) y = part[row * PART_ROW + nn];
+        else {
+            const uint32_t at = smem_addr(part + row * PART_ROW + nn);
+            for (int q = 0; q < slices; ++q) {
+                float v;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(mapa_shared(at, q)) : "memory");
+                y += v;
+            }
+        }
+        y *= 16777216.f;                                         // 2^24
+        if (a.bias != nullptr) y += __ldg(a.bias + n);
+        const size_t at = (size_t)row * a.ldy + n;
         if (a.y_dtype == STARQ_F16) static_cast<__half*>(a.Y)[at] = __float2half_rn(y);
         else if (a.y_dtype == STARQ_BF16) static_cast<__nv_bfloat16*>(a.Y)[at] = __float2bfloat16_rn(y);
         else static_cast<float*>(a.Y)[at] = y;
     }
+    if (slices > 1) cluster_sync();                  // the sums stay until every CTA has read them
+}
+
+template <typename T, int GROUP, int NT>
+cudaError_t launch_tiles(const W4gArgs& a, cudaStream_t s) {
+    const int blocks = (a.K + KB - 1) / KB, tiles = (a.N + CTA_N - 1) / CTA_N;
+    // Slices of K: as few as fill the SMs' 2 CTAs each, counted in blocks of
+    // the busiest SM slot, a CTA's start and end counting as 4.
+    int slices = 1, best = 0;
+    for (int q = 1; q <= MAX_SLICES && q <= blocks; q *= 2) {
+        const long long waves = ((long long)tiles * q + 2 * num_sms() - 1) / (2 * num_sms());
+        const long long cost = waves * ((blocks + q - 1) / q + 4);
+        if (q == 1 || cost < best) { best = (int)std::min(cost, 0x7fffffffLL); slices = q; }
+    }
+    const int per = (blocks + slices - 1) / slices;
+    const int xb = a.L * X_ROW + SUM_ROW<GROUP, NT> + POW_ROW<NT>;       // bytes of a block's activations
+    const int chunk = std::min(per, (110 * 1024 - RING<GROUP>) / xb);
+    const int smem = RING<GROUP> + chunk * xb;
+    static DeviceCache<int> ready;
+    int dummy = 0;
+    cudaError_t e = ready.get(&dummy, [](int, int* v) {
+        *v = 1;
+        return cudaFuncSetAttribute(w4g_linear_kernel<T, GROUP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    110 * 1024);
+    });
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(tiles * slices));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)slices;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = slices > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, w4g_linear_kernel<T, GROUP, NT>, a, slices, per, chunk);
 }
 
 template <typename T, int GROUP>
 cudaError_t launch_group(const W4gArgs& a, cudaStream_t s) {
-    const unsigned grid = (unsigned)((a.N + TILE_N - 1) / TILE_N);
     switch ((a.L + 7) / 8) {
-        case 1: w4g_linear_kernel<T, GROUP, 1><<<grid, THREADS, 0, s>>>(a); break;
-        case 2: w4g_linear_kernel<T, GROUP, 2><<<grid, THREADS, 0, s>>>(a); break;
-        case 3: w4g_linear_kernel<T, GROUP, 3><<<grid, THREADS, 0, s>>>(a); break;
-        default: w4g_linear_kernel<T, GROUP, 4><<<grid, THREADS, 0, s>>>(a); break;
+        case 1: return launch_tiles<T, GROUP, 1>(a, s);
+        case 2: return launch_tiles<T, GROUP, 2>(a, s);
+        case 3: return launch_tiles<T, GROUP, 3>(a, s);
+        default: return launch_tiles<T, GROUP, 4>(a, s);
     }
-    return cudaGetLastError();
 }
 
 template <typename T>
