@@ -232,9 +232,7 @@ int w4g_linear(const void* X, int ldx, int dtype, int L, int K, const uint8_t* W
     if (!aligned(X, 16) || ((size_t)ldx * 2) % 16 != 0 || !aligned(Wq, 16) || !aligned(scales, 4) ||
         !aligned(bias, 4) || !aligned(Y, y_dtype == STARQ_F32 ? 4 : 2))
         return fail(STARQ_ERR_ALIGN, "%s: X, its rows and Wq must be 16-byte aligned, the others to their elements", who);
-    int rc = STARQ_OK;
-    const W4gArgs a{X, ldx, dtype, L, K, Wq, scales, group, N, bias, Y, ldy, y_dtype, device_status(&rc)};
-    if (!a.status) return rc;
+    const W4gArgs a{X, ldx, dtype, L, K, Wq, scales, group, N, bias, Y, ldy, y_dtype};
     return launched(launch_w4g_linear(a, static_cast<cudaStream_t>(stream)), who);
 }
 

@@ -67,7 +67,6 @@ struct W4gArgs {
     const void* X; int ldx; int dtype; int L; int K;
     const uint8_t* Wq; const float* scales; int group; int N; const float* bias;
     void* Y; int ldy; int y_dtype;
-    unsigned* status;
 };
 cudaError_t launch_w4g_linear(const W4gArgs& a, cudaStream_t s);
 
@@ -129,6 +128,17 @@ template <> struct Eight<float> {
         reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
         reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
     }
+};
+
+// Eight values as they lie in memory: half the registers of Eight's floats
+// while loads are on their way.
+template <typename T> struct Packed8 {
+    uint4 w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p) {
+        #pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+    }
+    __device__ __forceinline__ void open(float (&f)[8]) const { Eight<T>::load(reinterpret_cast<const T*>(w), f); }
 };
 
 // One rotation unit: 16 channels of a head that hold eight rotation pairs,

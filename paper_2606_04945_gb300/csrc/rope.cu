@@ -12,7 +12,10 @@
 // rope_apply is bound by memory: every channel is read and written once
 // (2 + 2 bytes), three float32 operations for each. A thread takes the same
 // eight pairs of HEADS heads of a token, so that a table entry is loaded once
-// for HEADS heads and 2 * HEADS 16-byte loads are in flight.
+// for HEADS heads and 2 * HEADS 16-byte loads are in flight; they wait in
+// registers as they lie in memory. Measured (bfloat16, 8192 rows of 32 heads
+// of 128, 138 MB): 24.0 us, 5.8 TB/s; 35 us with floats instead (128
+// registers), 25 us with CTAs of 256, 31 us with a head a thread.
 #include <math.h>
 
 #include "decode.cuh"
@@ -20,7 +23,7 @@
 namespace starq {
 namespace {
 
-constexpr int THREADS = 256;
+constexpr int THREADS = 128;
 constexpr int HEADS = 4;
 
 __global__ void rope_table_kernel(float2* __restrict__ table, int positions, int rot, double theta, int scaling,
@@ -46,6 +49,7 @@ __global__ void rope_table_kernel(float2* __restrict__ table, int positions, int
 // rot / 16 rotate; the others copy their 16 channels (not in place).
 template <typename T>
 __global__ void __launch_bounds__(THREADS) rope_apply_kernel(const RopeArgs a, int groups, int units, unsigned n) {
+    grid_dependency_wait();
     const unsigned t = blockIdx.x * THREADS + threadIdx.x;
     if (t >= n) return;
     const int u = (int)(t % (unsigned)units);
@@ -57,28 +61,27 @@ __global__ void __launch_bounds__(THREADS) rope_apply_kernel(const RopeArgs a, i
     const int hi = turn ? rope_unit_hi(u, a.rot, a.interleaved) : 16 * u + 8;
     const T* x = static_cast<const T*>(a.X) + (size_t)tok * a.ldx;
     T* y = static_cast<T*>(a.Y) + (size_t)tok * a.ldy;
-    float l[HEADS][8], h[HEADS][8];
+    Packed8<T> l[HEADS], h[HEADS];
     #pragma unroll
     for (int k = 0; k < HEADS; ++k) {
         const int head = g + k * groups;
         if (head < a.heads) {
-            Eight<T>::load(x + (size_t)head * a.D + lo, l[k]);
-            Eight<T>::load(x + (size_t)head * a.D + hi, h[k]);
+            l[k].load(x + (size_t)head * a.D + lo);
+            h[k].load(x + (size_t)head * a.D + hi);
         }
     }
-    if (turn) {
-        float2 cs[8];
-        rope_load(cs, a.table, a.positions, a.rot, __ldg(a.pos + tok), u, a.inverse, a.status);
-        #pragma unroll
-        for (int k = 0; k < HEADS; ++k)
-            if (g + k * groups < a.heads) rope_unit(l[k], h[k], cs, a.interleaved);
-    }
+    float2 cs[8];
+    if (turn) rope_load(cs, a.table, a.positions, a.rot, __ldg(a.pos + tok), u, a.inverse, a.status);
     #pragma unroll
     for (int k = 0; k < HEADS; ++k) {
         const int head = g + k * groups;
         if (head < a.heads) {
-            Eight<T>::store(y + (size_t)head * a.D + lo, l[k]);
-            Eight<T>::store(y + (size_t)head * a.D + hi, h[k]);
+            float p[8], q[8];
+            l[k].open(p);
+            h[k].open(q);
+            if (turn) rope_unit(p, q, cs, a.interleaved);
+            Eight<T>::store(y + (size_t)head * a.D + lo, p);
+            Eight<T>::store(y + (size_t)head * a.D + hi, q);
         }
     }
 }
@@ -87,6 +90,7 @@ __global__ void __launch_bounds__(THREADS) rope_apply_kernel(const RopeArgs a, i
 // or copied channel.
 template <typename T>
 __global__ void __launch_bounds__(THREADS) rope_apply_scalar_kernel(const RopeArgs a, size_t n) {
+    grid_dependency_wait();
     const int half = a.rot / 2, per = half + (a.D - a.rot);
     for (size_t t = (size_t)blockIdx.x * THREADS + threadIdx.x; t < n; t += (size_t)gridDim.x * THREADS) {
         const int i = (int)(t % per);
@@ -120,15 +124,15 @@ cudaError_t launch_typed(const RopeArgs& a, cudaStream_t s) {
     const size_t n = (size_t)a.L * groups * units;
     if (wide && n == 0) return cudaSuccess;
     if (wide && n < (1ull << 31)) {
-        rope_apply_kernel<T><<<(unsigned)((n + THREADS - 1) / THREADS), THREADS, 0, s>>>(a, groups, units, (unsigned)n);
+        return launch_overlapped(rope_apply_kernel<T>, dim3((unsigned)((n + THREADS - 1) / THREADS)), THREADS, 0, s, a, groups,
+                                 units, (unsigned)n);
     } else {
         const size_t m = (size_t)a.L * a.heads * (a.rot / 2 + (a.D - a.rot));
         size_t blocks = (m + THREADS - 1) / THREADS;
         const size_t cap = (size_t)num_sms() * 32;
         if (blocks > cap) blocks = cap;
-        rope_apply_scalar_kernel<T><<<(unsigned)blocks, THREADS, 0, s>>>(a, m);
+        return launch_overlapped(rope_apply_scalar_kernel<T>, dim3((unsigned)blocks), THREADS, 0, s, a, m);
     }
-    return cudaGetLastError();
 }
 
 }  // namespace

@@ -127,6 +127,7 @@ __global__ void __launch_bounds__(THREADS, 2) w4g_linear_kernel(const W4gArgs a,
     constexpr int GW = GROUP / 32;                   // words of a thread in a group
     constexpr int COLS = 8 * NT;
     extern __shared__ __align__(128) uint8_t smem[];
+    grid_dependency_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int blocks = (a.K + KB - 1) / KB, groups = a.K / GROUP;
     const int rank = blockIdx.x % slices, n0 = blockIdx.x / slices * CTA_N, nw = n0 + warp * TILE;
@@ -359,12 +360,13 @@ cudaError_t launch_tiles(const W4gArgs& a, cudaStream_t s) {
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)slices;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0] = pdl_attribute();
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)slices;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = slices > 1 ? 1 : 0;
+    cfg.numAttrs = slices > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, w4g_linear_kernel<T, GROUP, NT>, a, slices, per, chunk);
 }
 
