@@ -60,7 +60,7 @@ struct Shared {
     uint64_t ck_full[CK_STAGES], ck_empty[CK_STAGES], cv_full[CV_STAGES], cv_empty[CV_STAGES];
     uint64_t q_full, meet, s_full[2], p_full[2], pv_done[2];
     uint32_t tmem_base;
-    int abort;
+    int abort, never;
     alignas(16) TileInfo tile[INFOS];
     float2 ml[TILE];                               // the odd stream's (m, l) for the join of the two
 };
@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
     uint8_t* smem = smem_raw + (base - raw);
     Shared* sh = reinterpret_cast<Shared*>(smem + L::END);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    volatile int* abort = &sh->abort;
+    volatile int *abort = &sh->abort, *never = &sh->never;       // `never` stays 0: what is in flight lands
     auto B = [](const uint64_t& bar) { return smem_addr(&bar); };
 
     if (threadIdx.x == 0) {
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
             mbar_init(B(sh->p_full[s]), 4);
             mbar_init(B(sh->pv_done[s]), 1);
         }
-        sh->abort = 0;
+        sh->abort = sh->never = 0;
         mbar_fence_init();
     }
     if (warp == MMA_WARP) {
@@ -261,6 +261,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
         advance(ahead, left_ahead);
         Cur nxt = ahead;
         int next_page = left_ahead > 0 ? page_of(nxt) : -1;
+        int k_sent = 0, v_sent = 0;                          // tiles whose codes were asked for
         for (int it = 0; it < count; ++it) {
             const int key0 = cur.kt * TILE, slot = it % INFOS;
             Raw raw_next = raw;
@@ -316,16 +317,25 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                 if (fetch) bulk_load(base + area + st * L::CODES + b * (16 * D), codes + at, 16 * D, bar);
                 return true;
             };
-            ok = bring(it % CK_STAGES, CK_STAGES, sh->ck_full, sh->ck_empty, L::CK, a.c.K) &&
-                 bring(it % CV_STAGES, CV_STAGES, sh->cv_full, sh->cv_empty, L::CV, a.c.V);
+            ok = bring(it % CK_STAGES, CK_STAGES, sh->ck_full, sh->ck_empty, L::CK, a.c.K);
             if (!ok) break;
+            ++k_sent;
+            ok = bring(it % CV_STAGES, CV_STAGES, sh->cv_full, sh->cv_empty, L::CV, a.c.V);
+            if (!ok) break;
+            ++v_sent;
         }
         // no commit lands after this CTA has exited
         for (int st = 0; st < INFOS && ok; ++st) {
             const int uses = (count - st + INFOS - 1) / INFOS;
             if (uses > 0) ok = wait_idle(B(sh->info_empty[st]), (uint32_t)(uses - 1) & 1u, abort);
         }
-        if (!ok && lane == 0) { sh->abort = 1; atomicOr(a.status, STATUS_TIMEOUT_KVATTN); }
+        if (!ok) {
+            if (lane == 0) { sh->abort = 1; atomicOr(a.status, STATUS_TIMEOUT_KVATTN); }
+            for (int it = max(0, k_sent - CK_STAGES); it < k_sent; ++it)
+                wait_idle(B(sh->ck_full[it % CK_STAGES]), (uint32_t)(it / CK_STAGES) & 1u, never);
+            for (int it = max(0, v_sent - CV_STAGES); it < v_sent; ++it)
+                wait_idle(B(sh->cv_full[it % CV_STAGES]), (uint32_t)(it / CV_STAGES) & 1u, never);
+        }
     } else if (warp >= SOFT_WARPS && warp < INFO_WARP) {
         // --- codes to fp16 tiles: keys or values ------------------------------------
         const bool keys = warp < SOFT_WARPS + CONV_WARPS;
@@ -393,6 +403,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
         constexpr uint32_t IDESC_QK = (1u << 4) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
         constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
         int left = count, tile0 = 0, steps[2] = {0, 0};      // key tiles and stream steps before the segment
+        int qks[2] = {0, 0}, pvs[2] = {0, 0};                // products issued, a stream
         int seg = 0;
         while (left > 0 && ok) {
             const int n = segment(cur, left);
@@ -416,6 +427,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                     tc_commit(B(sh->s_full[s]));
                 }
                 __syncwarp();
+                ++qks[s];
                 return true;
             };
             for (int u = 0; u < 2 && u < items && ok; ++u) ok = qk(u, false);
@@ -441,6 +453,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                     tc_commit(B(sh->pv_done[s]));
                 }
                 __syncwarp();
+                ++pvs[s];
                 if (u + 2 < items) ok = qk(u + 2, __all_sync(0xffffffffu, k_there));
             }
             steps[0] += (items + 1) / 2;
@@ -451,7 +464,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
             cur.kt += n;
             if (left > 0) cur.next_unit(a, G);
         }
-        if (!ok && lane == 0) { sh->abort = 1; atomicOr(a.status, STATUS_TIMEOUT_KVATTN); }
+        if (!ok) {
+            if (lane == 0) { sh->abort = 1; atomicOr(a.status, STATUS_TIMEOUT_KVATTN); }
+            for (int s = 0; s < 2; ++s) {
+                if (qks[s] > 0) mbar_wait_bounded_warp(B(sh->s_full[s]), (uint32_t)(qks[s] - 1) & 1u, never);
+                if (pvs[s] > 0) mbar_wait_bounded_warp(B(sh->pv_done[s]), (uint32_t)(pvs[s] - 1) & 1u, never);
+            }
+        }
     } else {
         // --- softmax: one thread a row ----------------------------------------------
         const int s = warp >> 2, row = threadIdx.x & (TILE - 1);
