@@ -29,13 +29,15 @@
 // adds up at its end, through each other's shared memory, in the order of the
 // slices. So a CTA brings and converts its slice of the activations only,
 // once. Measured at K = 12288, N = 4096, groups of 32, 12 rows (31.8 MB):
-// 15.8 us, 2.0 TB/s; with the warps of one CTA taking the blocks of K in turn
+// 16 us, 2.0 TB/s; with the warps of one CTA taking the blocks of K in turn
 // for 16 channels, all of them needing all activations, 25.7 us with the
 // codes in registers, 31 us with 512-byte bulk copies. One row at K = 3584,
-// N = 37888, groups of 64 (76.5 MB): 17.9 us, 4.3 TB/s, against 22.3 and 29
+// N = 37888, groups of 64 (76.5 MB): 17.3 us, 4.4 TB/s, against 22.3 and 29
 // us. About 5 us of each call are its start, the activations and the joining:
 // K = N = 4096 (8.9 MB) takes 5.6 us. Four stages of two CTAs an SM suffice:
-// 6 or 8 of them, or a third CTA, changed nothing.
+// 6 or 8 of them, or a third CTA, changed nothing. 32 rows at K = 3584, N =
+// 37888 take 50 us, 175 TFLOP/s: there the loads of the activations from
+// shared memory are the bound (64 % of its rate), the MMA is at 30 %.
 #include <algorithm>
 #include <type_traits>
 
@@ -44,17 +46,24 @@
 namespace starq {
 namespace {
 
-constexpr int WARPS = 8;
-constexpr int THREADS = WARPS * 32;
 constexpr int TILE = 16;               // output channels of a warp
-constexpr int CTA_N = WARPS * TILE;    // of a CTA
 constexpr int KB = 128;                // input channels of a block
 constexpr int STAGES = 4;              // blocks of a warp on their way
 constexpr int MAX_SLICES = 8;          // CTAs of a cluster
 constexpr int X_ROW = KB * 2;          // bytes of an activation row in a block
 constexpr int CODES = TILE * KB / 2;   // bytes of a stage's codes
 template <int GROUP> constexpr int STAGE = CODES + TILE * (KB / GROUP) * 4;       // and of its scales behind them
-template <int GROUP> constexpr int RING = WARPS * STAGES * STAGE<GROUP>;
+
+// A CTA of W warps: 16 instead of 8 where several tiles of activations make
+// their conversion, which the warps share, a large part of the work.
+template <int W> struct Cta {
+    static constexpr int THREADS = W * 32;
+    static constexpr int N = W * TILE;               // output channels
+    static constexpr int PER_SM = 16 / W;
+    static constexpr int SMEM = 220 * 1024 / PER_SM;
+    static constexpr int PART_ROW = N + 4;           // floats of a row of partial sums
+};
+template <int GROUP, int W> constexpr int RING = W * STAGES * STAGE<GROUP>;
 
 template <typename T> constexpr bool IS_HALF = std::is_same<T, __half>::value;
 
@@ -107,25 +116,29 @@ template <int GROUP> __device__ __forceinline__ int w_offset(int r, int c) {
 
 // 16-byte chunk c (of 16) of activation row i of a block; the four threads
 // and the two rows that are read together fall into different chunks of 128
-// bytes.
+// bytes. A reader's row is one of 8 next to each other: its parity is the
+// thread's, and with it the chunks' order.
 template <int GROUP> __device__ __forceinline__ uint32_t x_offset(int i, int c) {
     const int odd = i & 1;
     const int key = GROUP == 128 ? 2 * odd ^ ((c >> 3) & 1) : GROUP == 64 ? odd : 4 * odd;
     return i * X_ROW + ((c ^ key) << 4);
 }
+// Activation rows that a block has room for: with one tile the rows there
+// are, or else whole tiles (rows past L are read and not stored).
+template <int NT> __host__ __device__ __forceinline__ int x_rows(int L) { return NT == 1 ? L : 8 * NT; }
 
-template <int GROUP, int NT> constexpr int SUM_ROW = KB / GROUP * 8 * NT * 4;      // groups' sums of a block, bytes
+template <int GROUP, int NT> constexpr int SUM_ROW = KB / GROUP * 16 * NT * 4;     // groups' sums of a block (in pairs, twice), bytes
 template <int NT> constexpr int POW_ROW = 8 * NT * 4;                              // powers of two of a block, bytes
-constexpr int PART_ROW = CTA_N + 4;                                                // floats of a row of partial sums
 
-// NT tiles of 8 activation rows. A cluster of `slices` CTAs takes CTA_N output
+// NT tiles of 8 activation rows. A cluster of `slices` CTAs takes Cta::N output
 // channels, each CTA `per` blocks of K; the activations of `chunk` of them are
 // in shared memory at a time.
-template <typename T, int GROUP, int NT>
-__global__ void __launch_bounds__(THREADS, 2) w4g_linear_kernel(const W4gArgs a, int slices, int per, int chunk) {
+template <typename T, int GROUP, int NT, int W>
+__global__ void __launch_bounds__(Cta<W>::THREADS, Cta<W>::PER_SM) w4g_linear_kernel(const W4gArgs a, int slices, int per, int chunk) {
     constexpr int GB = KB / GROUP;                   // groups of a block
     constexpr int GW = GROUP / 32;                   // words of a thread in a group
-    constexpr int COLS = 8 * NT;
+    constexpr int COLS = 8 * NT, THREADS = Cta<W>::THREADS, CTA_N = Cta<W>::N;
+    constexpr int PART_ROW = Cta<W>::PART_ROW;
     extern __shared__ __align__(128) uint8_t smem[];
     grid_dependency_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -133,8 +146,10 @@ __global__ void __launch_bounds__(THREADS, 2) w4g_linear_kernel(const W4gArgs a,
     const int rank = blockIdx.x % slices, n0 = blockIdx.x / slices * CTA_N, nw = n0 + warp * TILE;
     const int k0 = min(rank * per, blocks), k1 = min(k0 + per, blocks);
     uint8_t* const ring = smem + warp * STAGES * STAGE<GROUP>;
-    uint8_t* const xs = smem + RING<GROUP>;
-    float* const sums = reinterpret_cast<float*>(xs + chunk * a.L * X_ROW);        // [chunk][GB][COLS]: -8 2^-24 sum x
+    const int xblock = x_rows<NT>(a.L) * X_ROW;      // bytes of a block's activations
+    uint8_t* const xs = smem + RING<GROUP, W>;
+    // [chunk][GB][COLS / 2][4]: a pair's -8 2^-24 sum x, twice
+    float* const sums = reinterpret_cast<float*>(xs + chunk * xblock);
     float* const pows = sums + chunk * (SUM_ROW<GROUP, NT> / 4);                   // [chunk][COLS]
 
     // --- a warp's weights: 16 rows of 64 bytes and their scales a block ---------
@@ -168,14 +183,19 @@ __global__ void __launch_bounds__(THREADS, 2) w4g_linear_kernel(const W4gArgs a,
     auto bring = [&](int c0) {
         constexpr int BATCH = 4;                     // loads of a thread on their way together
         const int pieces = min(chunk, k1 - c0) * a.L * 16;
+        const int hop = THREADS / 16 / a.L, skip = THREADS / 16 - hop * a.L;       // blocks and rows of a step
+        int b0 = (int)threadIdx.x / 16 / a.L, i0 = (int)threadIdx.x / 16 - b0 * a.L;
         for (int e0 = threadIdx.x; e0 < pieces; e0 += BATCH * THREADS) {
             uint4 raw[BATCH];
             int blk[BATCH], tok[BATCH];
             #pragma unroll
             for (int u = 0; u < BATCH; ++u) {
                 const int e = e0 + u * THREADS, c = e & 15;
-                blk[u] = (int)((unsigned)(e >> 4) / (unsigned)a.L);
-                tok[u] = (e >> 4) - blk[u] * a.L;
+                blk[u] = b0;
+                tok[u] = i0;
+                b0 += hop;
+                i0 += skip;
+                if (i0 >= a.L) { i0 -= a.L; ++b0; }
                 const int k = (c0 + blk[u]) * KB + 8 * c;
                 raw[u] = make_uint4(0, 0, 0, 0);
                 if (e < pieces && k < a.K) raw[u] = ld_global_nc_v4(static_cast<const T*>(a.X) + (size_t)tok[u] * a.ldx + k);
@@ -204,9 +224,11 @@ __global__ void __launch_bounds__(THREADS, 2) w4g_linear_kernel(const W4gArgs a,
                 float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
                 #pragma unroll
                 for (int d = 1; d < GROUP / 8; d <<= 1) sum += __shfl_xor_sync(half, sum, d);
-                *reinterpret_cast<uint4*>(xs + b * a.L * X_ROW + x_offset<GROUP>(i, c)) = paired(f);
-                if (c % (GROUP / 8) == 0)
-                    sums[(b * GB + c / (GROUP / 8)) * COLS + i] = sum * -4.76837158203125e-07f;         // -8 2^-24
+                *reinterpret_cast<uint4*>(xs + b * xblock + x_offset<GROUP>(i, c)) = paired(f);
+                if (c % (GROUP / 8) == 0) {
+                    float* p = sums + (b * GB + c / (GROUP / 8)) * (2 * COLS) + (i >> 1) * 4 + (i & 1);
+                    p[0] = p[2] = sum * -4.76837158203125e-07f;                                         // -8 2^-24
+                }
                 if (!IS_HALF<T> && c == 0) pows[b * COLS + i] = down;
             }
         }
@@ -220,6 +242,13 @@ __global__ void __launch_bounds__(THREADS, 2) w4g_linear_kernel(const W4gArgs a,
     for (int i = 0; i < NT; ++i)
         #pragma unroll
         for (int c = 0; c < 4; ++c) acc[i][c] = 0.f;
+    // this thread's activations: row g of a tile; chunks of the first group,
+    // word by word (of the first two groups, where a group is one word)
+    const int xrow = NT == 1 ? min(g, a.L - 1) : g;
+    constexpr int XO = GW == 1 ? 2 : GW;
+    uint32_t xo[XO];
+    #pragma unroll
+    for (int e = 0; e < XO; ++e) xo[e] = x_offset<GROUP>(xrow, GW == 1 ? t + 4 * e : GW * t + e);
     int st = 0, to = STAGES - 1;
     for (int c0 = k0; c0 < k1; c0 += chunk) {
         if (c0 != k0) __syncthreads();               // the last chunk is done with
@@ -233,7 +262,8 @@ __global__ void __launch_bounds__(THREADS, 2) w4g_linear_kernel(const W4gArgs a,
             if (++to == STAGES) to = 0;
             const uint8_t* const ws = ring + st * STAGE<GROUP>;
             if (++st == STAGES) st = 0;
-            const uint8_t* const xb = xs + (kb - c0) * a.L * X_ROW;
+            const uint8_t* const xb = xs + (kb - c0) * xblock;
+            const float* const sb = sums + (kb - c0) * (SUM_ROW<GROUP, NT> / 4) + 4 * t;
             float sc[2][GB];
             #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -242,17 +272,13 @@ __global__ void __launch_bounds__(THREADS, 2) w4g_linear_kernel(const W4gArgs a,
                 else if (GB == 2) *reinterpret_cast<float2*>(sc[h]) = *reinterpret_cast<const float2*>(p);
                 else sc[h][0] = *p;
             }
-            float2 pw[NT];
-            if (!IS_HALF<T>)
-                #pragma unroll
-                for (int i = 0; i < NT; ++i)
-                    pw[i] = *reinterpret_cast<const float2*>(pows + (kb - c0) * COLS + 8 * i + 2 * t);
+            float sum[NT][4];                        // of the block, before the powers of two
             #pragma unroll
             for (int j = 0; j < GB; ++j) {
-                float2 m8[NT];
+                float4 m8[NT];
                 #pragma unroll
                 for (int i = 0; i < NT; ++i)
-                    m8[i] = *reinterpret_cast<const float2*>(sums + ((kb - c0) * GB + j) * COLS + 8 * i + 2 * t);
+                    m8[i] = *reinterpret_cast<const float4*>(sb + j * (2 * COLS) + 16 * i);
                 uint32_t w[2][4];
                 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -271,12 +297,11 @@ __global__ void __launch_bounds__(THREADS, 2) w4g_linear_kernel(const W4gArgs a,
                     const uint32_t od[4] = {field(w0, m1, f1), field(w1, m1, f1), field(v0, m1, f1), field(v1, m1, f1)};
                     #pragma unroll
                     for (int i = 0; i < NT; ++i) {
-                        // columns past L repeat the last row (not stored)
                         const uint4 x = *reinterpret_cast<const uint4*>(
-                            xb + x_offset<GROUP>(min(8 * i + g, a.L - 1), GROUP / 8 * j + GW * t + e));
+                            xb + 8 * i * X_ROW + (GW == 1 ? xo[j & 1] + 128 * (j >> 1) : xo[e] + GROUP * 2 * j));
                         float(&l)[4] = lo[i], (&h)[4] = hi[i];
                         if (e == 0) {
-                            mma_16816(l, ev, x.x, x.y, m8[i].x, m8[i].y, m8[i].x, m8[i].y);
+                            mma_16816(l, ev, x.x, x.y, m8[i].x, m8[i].y, m8[i].z, m8[i].w);
                             mma_16816(h, od, x.z, x.w, 0.f, 0.f, 0.f, 0.f);
                         } else {
                             mma_16816(l, ev, x.x, x.y, l[0], l[1], l[2], l[3]);
@@ -288,11 +313,18 @@ __global__ void __launch_bounds__(THREADS, 2) w4g_linear_kernel(const W4gArgs a,
                 for (int i = 0; i < NT; ++i)
                     #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        float s = sc[k >> 1][j];
-                        if (!IS_HALF<T>) s *= k & 1 ? pw[i].y : pw[i].x;
-                        acc[i][k] = fmaf(fmaf(hi[i][k], 0.0625f, lo[i][k]), s, acc[i][k]);
+                        const float v = fmaf(hi[i][k], 0.0625f, lo[i][k]), s = sc[k >> 1][j];
+                        if (IS_HALF<T>) acc[i][k] = fmaf(v, s, acc[i][k]);
+                        else sum[i][k] = j == 0 ? v * s : fmaf(v, s, sum[i][k]);
                     }
             }
+            if (!IS_HALF<T>)
+                #pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    const float2 pw = *reinterpret_cast<const float2*>(pows + (kb - c0) * COLS + 8 * i + 2 * t);
+                    #pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[i][k] = fmaf(sum[i][k], k & 1 ? pw.y : pw.x, acc[i][k]);
+                }
         }
     }
 
@@ -332,32 +364,33 @@ __global__ void __launch_bounds__(THREADS, 2) w4g_linear_kernel(const W4gArgs a,
     if (slices > 1) cluster_sync();                  // the sums stay until every CTA has read them
 }
 
-template <typename T, int GROUP, int NT>
-cudaError_t launch_tiles(const W4gArgs& a, cudaStream_t s) {
-    const int blocks = (a.K + KB - 1) / KB, tiles = (a.N + CTA_N - 1) / CTA_N;
-    // Slices of K: as few as fill the SMs' 2 CTAs each, counted in blocks of
+template <typename T, int GROUP, int NT, int W>
+cudaError_t launch_ctas(const W4gArgs& a, cudaStream_t s) {
+    using C = Cta<W>;
+    const int blocks = (a.K + KB - 1) / KB, tiles = (a.N + C::N - 1) / C::N, slots = C::PER_SM * num_sms();
+    // Slices of K: as few as fill the SMs, counted in blocks of
     // the busiest SM slot, a CTA's start and end counting as 4.
     int slices = 1, best = 0;
     for (int q = 1; q <= MAX_SLICES && q <= blocks; q *= 2) {
-        const long long waves = ((long long)tiles * q + 2 * num_sms() - 1) / (2 * num_sms());
+        const long long waves = ((long long)tiles * q + slots - 1) / slots;
         const long long cost = waves * ((blocks + q - 1) / q + 4);
         if (q == 1 || cost < best) { best = (int)std::min(cost, 0x7fffffffLL); slices = q; }
     }
     const int per = (blocks + slices - 1) / slices;
-    const int xb = a.L * X_ROW + SUM_ROW<GROUP, NT> + POW_ROW<NT>;       // bytes of a block's activations
-    const int chunk = std::min(per, (110 * 1024 - RING<GROUP>) / xb);
-    const int smem = RING<GROUP> + chunk * xb;
+    const int xb = x_rows<NT>(a.L) * X_ROW + SUM_ROW<GROUP, NT> + POW_ROW<NT>;       // bytes of a block's activations
+    const int chunk = std::min(per, (C::SMEM - RING<GROUP, W>) / xb);
+    const int smem = RING<GROUP, W> + chunk * xb;
     static DeviceCache<int> ready;
     int dummy = 0;
     cudaError_t e = ready.get(&dummy, [](int, int* v) {
         *v = 1;
-        return cudaFuncSetAttribute(w4g_linear_kernel<T, GROUP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    110 * 1024);
+        return cudaFuncSetAttribute(w4g_linear_kernel<T, GROUP, NT, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    C::SMEM);
     });
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(tiles * slices));
-    cfg.blockDim = dim3(THREADS);
+    cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -367,7 +400,18 @@ cudaError_t launch_tiles(const W4gArgs& a, cudaStream_t s) {
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = slices > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, w4g_linear_kernel<T, GROUP, NT>, a, slices, per, chunk);
+    return cudaLaunchKernelEx(&cfg, w4g_linear_kernel<T, GROUP, NT, W>, a, slices, per, chunk);
+}
+
+// Several tiles of activations and channels that fill the SMs without
+// slices: 16 warps (measured at 32 rows, K = 3584, N = 37888: 50 us against
+// 59). With fewer channels the slices keep 8 (clusters of whole SMs do not
+// pack: 12 rows, K = 12288, N = 4096: 16 us against 30).
+template <typename T, int GROUP, int NT>
+cudaError_t launch_tiles(const W4gArgs& a, cudaStream_t s) {
+    if constexpr (NT > 1)
+        if (a.N >= num_sms() * Cta<16>::N * 3 / 4) return launch_ctas<T, GROUP, NT, 16>(a, s);
+    return launch_ctas<T, GROUP, NT, 8>(a, s);
 }
 
 template <typename T, int GROUP>
