@@ -9,13 +9,11 @@
 // activation rows as the columns: with one row the MMA is idle seven eighths
 // of the time and still far from the bound.
 //
-// A code c enters the MMA as the fp16 subnormal (c + 8) 2^-24: one three-input
-// operation takes two codes out of a word and flips their sign bits, and
-// there is nothing to convert or to subtract (the first form did both, and a
-// third of its instructions were these). The sum of a group starts from
-// -8 2^-24 sum x instead, and the result is multiplied by 2^24 at the end.
-// The upper codes of a byte come out as 16 (c + 8) 2^-24 and have a sum of
-// their own that is divided by 16. The subnormals and the products are exact,
+// A code c enters the MMA as the fp16 subnormal c 2^-24: one three-input
+// operation takes two codes out of a word and flips their sign bits, which is
+// (c + 8) 2^-24, and one subtraction is exact; the result is multiplied by
+// 2^24 at the end. The upper codes of a byte come out as c 2^-20 and have a
+// sum of their own that is divided by 16. The products are exact as well,
 // a group's sum is accumulated in float32 and only then multiplied by its
 // scale. bf16 activations become fp16, a row's 128 channels of a block scaled
 // by a power of two that puts the largest at 2^14: what lies 2^-29 below
@@ -29,15 +27,17 @@
 // adds up at its end, through each other's shared memory, in the order of the
 // slices. So a CTA brings and converts its slice of the activations only,
 // once. Measured at K = 12288, N = 4096, groups of 32, 12 rows (31.8 MB):
-// 16 us, 2.0 TB/s; with the warps of one CTA taking the blocks of K in turn
+// 13.9 us, 2.3 TB/s; with the warps of one CTA taking the blocks of K in turn
 // for 16 channels, all of them needing all activations, 25.7 us with the
 // codes in registers, 31 us with 512-byte bulk copies. One row at K = 3584,
-// N = 37888, groups of 64 (76.5 MB): 17.3 us, 4.4 TB/s, against 22.3 and 29
+// N = 37888, groups of 64 (76.5 MB): 17.8 us, 4.3 TB/s, against 22.3 and 29
 // us. About 5 us of each call are its start, the activations and the joining:
-// K = N = 4096 (8.9 MB) takes 5.6 us. Four stages of two CTAs an SM suffice:
+// K = N = 4096 (8.9 MB) takes 5.7 us. Four stages of two CTAs an SM suffice:
 // 6 or 8 of them, or a third CTA, changed nothing. 32 rows at K = 3584, N =
-// 37888 take 50 us, 175 TFLOP/s: there the loads of the activations from
-// shared memory are the bound (64 % of its rate), the MMA is at 30 %.
+// 37888 take 43 us, 200 TFLOP/s: there the loads of the activations from
+// shared memory and the conversions are the bound, not the MMA. (Leaving the
+// 8 of c + 8 in the products and starting each sum from -8 sum x takes an
+// operation a pair less, but loads more, is not exact, and took 50 us there.)
 #include <algorithm>
 #include <type_traits>
 
@@ -76,11 +76,15 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 
-// (w & mask) ^ flip in one operation (with both constants as immediates the
-// compiler makes two: a third of all instructions were these).
-__device__ __forceinline__ uint32_t field(uint32_t w, uint32_t mask, uint32_t flip) {
+// Two codes of a word as fp16 numbers c 2^-24 (c 2^-20 with the fields four
+// bits up): (w & mask) ^ flip in one operation is the subnormal (c + 8) 2^-24,
+// and `flip` is also the pair of subnormals to subtract. Both steps are exact.
+// (With constants as immediates the compiler makes two operations of the
+// first: a third of all instructions were these.)
+__device__ __forceinline__ uint32_t codes(uint32_t w, uint32_t mask, uint32_t flip) {
     uint32_t r;
-    asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(r) : "r"(w), "r"(mask), "r"(flip));
+    asm("{\n\t.reg .b32 u;\n\tlop3.b32 u, %1, %2, %3, 0x6a;\n\tsub.rn.f16x2 %0, u, %3;\n\t}"
+        : "=r"(r) : "r"(w), "r"(mask), "r"(flip));
     return r;
 }
 
@@ -127,7 +131,6 @@ template <int GROUP> __device__ __forceinline__ uint32_t x_offset(int i, int c) 
 // are, or else whole tiles (rows past L are read and not stored).
 template <int NT> __host__ __device__ __forceinline__ int x_rows(int L) { return NT == 1 ? L : 8 * NT; }
 
-template <int GROUP, int NT> constexpr int SUM_ROW = KB / GROUP * 16 * NT * 4;     // groups' sums of a block (in pairs, twice), bytes
 template <int NT> constexpr int POW_ROW = 8 * NT * 4;                              // powers of two of a block, bytes
 
 // NT tiles of 8 activation rows. A cluster of `slices` CTAs takes Cta::N output
@@ -148,9 +151,7 @@ __global__ void __launch_bounds__(Cta<W>::THREADS, Cta<W>::PER_SM) w4g_linear_ke
     uint8_t* const ring = smem + warp * STAGES * STAGE<GROUP>;
     const int xblock = x_rows<NT>(a.L) * X_ROW;      // bytes of a block's activations
     uint8_t* const xs = smem + RING<GROUP, W>;
-    // [chunk][GB][COLS / 2][4]: a pair's -8 2^-24 sum x, twice
-    float* const sums = reinterpret_cast<float*>(xs + chunk * xblock);
-    float* const pows = sums + chunk * (SUM_ROW<GROUP, NT> / 4);                   // [chunk][COLS]
+    float* const pows = reinterpret_cast<float*>(xs + chunk * xblock);               // [chunk][COLS]
 
     // --- a warp's weights: 16 rows of 64 bytes and their scales a block ---------
     const uint8_t* src[2];
@@ -221,14 +222,7 @@ __global__ void __launch_bounds__(Cta<W>::THREADS, Cta<W>::PER_SM) w4g_linear_ke
                     #pragma unroll
                     for (int v = 0; v < 8; ++v) f[v] *= up;
                 }
-                float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
-                #pragma unroll
-                for (int d = 1; d < GROUP / 8; d <<= 1) sum += __shfl_xor_sync(half, sum, d);
                 *reinterpret_cast<uint4*>(xs + b * xblock + x_offset<GROUP>(i, c)) = paired(f);
-                if (c % (GROUP / 8) == 0) {
-                    float* p = sums + (b * GB + c / (GROUP / 8)) * (2 * COLS) + (i >> 1) * 4 + (i & 1);
-                    p[0] = p[2] = sum * -4.76837158203125e-07f;                                         // -8 2^-24
-                }
                 if (!IS_HALF<T> && c == 0) pows[b * COLS + i] = down;
             }
         }
@@ -263,7 +257,6 @@ __global__ void __launch_bounds__(Cta<W>::THREADS, Cta<W>::PER_SM) w4g_linear_ke
             const uint8_t* const ws = ring + st * STAGE<GROUP>;
             if (++st == STAGES) st = 0;
             const uint8_t* const xb = xs + (kb - c0) * xblock;
-            const float* const sb = sums + (kb - c0) * (SUM_ROW<GROUP, NT> / 4) + 4 * t;
             float sc[2][GB];
             #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -275,10 +268,6 @@ __global__ void __launch_bounds__(Cta<W>::THREADS, Cta<W>::PER_SM) w4g_linear_ke
             float sum[NT][4];                        // of the block, before the powers of two
             #pragma unroll
             for (int j = 0; j < GB; ++j) {
-                float4 m8[NT];
-                #pragma unroll
-                for (int i = 0; i < NT; ++i)
-                    m8[i] = *reinterpret_cast<const float4*>(sb + j * (2 * COLS) + 16 * i);
                 uint32_t w[2][4];
                 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -293,15 +282,15 @@ __global__ void __launch_bounds__(Cta<W>::THREADS, Cta<W>::PER_SM) w4g_linear_ke
                 #pragma unroll
                 for (int e = 0; e < GW; ++e) {
                     const uint32_t w0 = w[0][e], w1 = w[1][e], v0 = w0 >> 8, v1 = w1 >> 8;
-                    const uint32_t ev[4] = {field(w0, m0, f0), field(w1, m0, f0), field(v0, m0, f0), field(v1, m0, f0)};
-                    const uint32_t od[4] = {field(w0, m1, f1), field(w1, m1, f1), field(v0, m1, f1), field(v1, m1, f1)};
+                    const uint32_t ev[4] = {codes(w0, m0, f0), codes(w1, m0, f0), codes(v0, m0, f0), codes(v1, m0, f0)};
+                    const uint32_t od[4] = {codes(w0, m1, f1), codes(w1, m1, f1), codes(v0, m1, f1), codes(v1, m1, f1)};
                     #pragma unroll
                     for (int i = 0; i < NT; ++i) {
                         const uint4 x = *reinterpret_cast<const uint4*>(
                             xb + 8 * i * X_ROW + (GW == 1 ? xo[j & 1] + 128 * (j >> 1) : xo[e] + GROUP * 2 * j));
                         float(&l)[4] = lo[i], (&h)[4] = hi[i];
                         if (e == 0) {
-                            mma_16816(l, ev, x.x, x.y, m8[i].x, m8[i].y, m8[i].z, m8[i].w);
+                            mma_16816(l, ev, x.x, x.y, 0.f, 0.f, 0.f, 0.f);
                             mma_16816(h, od, x.z, x.w, 0.f, 0.f, 0.f, 0.f);
                         } else {
                             mma_16816(l, ev, x.x, x.y, l[0], l[1], l[2], l[3]);
@@ -377,7 +366,7 @@ cudaError_t launch_ctas(const W4gArgs& a, cudaStream_t s) {
         if (q == 1 || cost < best) { best = (int)std::min(cost, 0x7fffffffLL); slices = q; }
     }
     const int per = (blocks + slices - 1) / slices;
-    const int xb = x_rows<NT>(a.L) * X_ROW + SUM_ROW<GROUP, NT> + POW_ROW<NT>;       // bytes of a block's activations
+    const int xb = x_rows<NT>(a.L) * X_ROW + POW_ROW<NT>;       // bytes of a block's activations
     const int chunk = std::min(per, (C::SMEM - RING<GROUP, W>) / xb);
     const int smem = RING<GROUP, W> + chunk * xb;
     static DeviceCache<int> ready;
@@ -405,8 +394,9 @@ cudaError_t launch_ctas(const W4gArgs& a, cudaStream_t s) {
 
 // Several tiles of activations and channels that fill the SMs without
 // slices: 16 warps (measured at 32 rows, K = 3584, N = 37888: 50 us against
-// 59). With fewer channels the slices keep 8 (clusters of whole SMs do not
-// pack: 12 rows, K = 12288, N = 4096: 16 us against 30).
+// 59 with 8, in an earlier form). With fewer channels the slices keep 8
+// (clusters of whole SMs do not pack: 12 rows, K = 12288, N = 4096, in that
+// form: 16 us against 30 with 16).
 template <typename T, int GROUP, int NT>
 cudaError_t launch_tiles(const W4gArgs& a, cudaStream_t s) {
     if constexpr (NT > 1)

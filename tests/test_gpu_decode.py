@@ -586,3 +586,50 @@ def test_w4g_weights_from_prepare(abi, group):
     assert np.all(np.abs(num(Y) - ref) <= (K / 8 + 16) * 2.0 ** -24 * size)
     back = codes * np.repeat(num(scales), group, axis=1)
     assert np.all(np.abs(back - Wn) <= np.repeat(num(scales), group, axis=1) * 0.5 * (1 + 1e-6))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("L,group", [(1, 32), (5, 64), (11, 128), (32, 64)])
+def test_w4g_values(abi, dtype, L, group):
+    """Codes of zero give exact zeros (and the bias); an infinite or NaN
+    activation shows in its own row alone, as the formula has it; a block of
+    tiny and one of huge activations keep their places."""
+    rng = np.random.default_rng(group + L)
+    N, K = 130, 512
+    codes = rng.integers(1, 8, (N, K)) * rng.choice([-1, 1], (N, K))
+    codes[:40] = 0
+    x, _ = randn(rng, (L, K), dtype)
+    small, large = (2.0 ** -14, 2.0 ** 10) if dtype is torch.float16 else (2.0 ** -100, 2.0 ** 100)
+    x[:, :128] *= small
+    x[:, 128:256] *= large
+    xn = num(x)
+    packed = torch.from_numpy(((codes[:, 0::2] & 15) | ((codes[:, 1::2] & 15) << 4)).astype(np.uint8)).cuda()
+    scales = (np.exp(rng.standard_normal((N, K // group))) / 50).astype(np.float32)
+    bias = rng.standard_normal(N).astype(np.float32)
+    run = lambda t, w: abi.w4g_linear(t, w, torch.from_numpy(scales).cuda(), Y, bias=torch.from_numpy(bias).cuda())
+    Y = torch.empty(L, N, device="cuda")
+    run(x, packed)
+    ref, size = od.w4g_linear(xn, codes, scales, bias)
+    tol = (K / 8 + 16) * 2.0 ** -24 * size + 2.0 ** -24 * np.abs(ref) * 1.01
+    assert np.all(np.abs(num(Y) - ref) <= tol)
+    assert torch.equal(Y[:, :40], torch.from_numpy(bias[:40]).cuda().expand(L, 40))
+    only = codes.copy()                               # each block on its own
+    for blk in range(4):
+        only[:] = 0
+        only[:, blk * 128:(blk + 1) * 128] = codes[:, blk * 128:(blk + 1) * 128]
+        run(x, torch.from_numpy(((only[:, 0::2] & 15) | ((only[:, 1::2] & 15) << 4)).astype(np.uint8)).cuda())
+        ref, size = od.w4g_linear(xn, only, scales, bias)
+        assert np.all(np.abs(num(Y) - ref) <= (K / 8 + 16) * 2.0 ** -24 * size + 2.0 ** -24 * np.abs(ref) * 1.01)
+    run(x, packed)
+    before = Y.clone()
+    bad = L // 2
+    y = x.clone()
+    y[bad, 300] = float("inf")
+    run(y, packed)
+    assert torch.isnan(Y[bad, :40]).all()             # 0 times infinity
+    assert torch.equal(Y[bad, 40:], torch.from_numpy(np.sign(codes[40:, 300]) * np.inf).float().cuda())
+    rest = [i for i in range(L) if i != bad]
+    assert torch.equal(Y[rest], before[rest])
+    y[bad, 300] = float("nan")
+    run(y, packed)
+    assert torch.isnan(Y[bad]).all() and torch.equal(Y[rest], before[rest])
