@@ -23,9 +23,10 @@ constexpr float LAZY = 8.f;            // m moves when x > m + LAZY
 constexpr float NEG_INF = -__builtin_huge_valf();
 
 // Workspace: prefix [B + 1] (tiles before each sequence), then the slots:
-// [rows][D] accumulators, then (m, l) for each row.
+// [rows][D] accumulators, then (m, l) for each row; an odd number of rows
+// takes the room of one more, so that every slot begins on 16 bytes.
 constexpr size_t prefix_bytes(int B) { return ((size_t)(B + 1) * 8 + 255) / 256 * 256; }
-constexpr size_t slot_floats(int rows, int D) { return (size_t)rows * (D + 2); }
+constexpr size_t slot_floats(int rows, int D) { return (size_t)(rows + (rows & 1)) * (D + 2); }
 
 __device__ __forceinline__ float ex2(float x) {
     float y;

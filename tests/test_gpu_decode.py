@@ -407,6 +407,18 @@ def test_attention_long(abi, new, H, Hkv, D):
         assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new,H,Hkv", [(7, 7, 1), (19, 2, 2), (3, 14, 2), (61, 1, 1), (37, 7, 1)])
+def test_attention_odd_rows(abi, new, H, Hkv, D):
+    """An odd number of rows of a key/value head: partial runs of theirs lie
+    side by side in the workspace."""
+    rng = np.random.default_rng(new + D)
+    pg = Paged(abi, rng, 3, 2300, Hkv, 32, D)
+    lens = [2300, 700, 1999]
+    fill(pg, rng, lens)
+    attend(abi, rng, pg, [new, new - 1, new], lens, H, torch.bfloat16, causal=new == 61)
+
+
 @pytest.mark.parametrize("new", [1, 20])
 def test_attention_many_sequences(abi, new):
     """More sequences than threads of a CTA."""
