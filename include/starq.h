@@ -835,6 +835,10 @@ int glue_rope_apply(const void* X, int ldx, int dtype, int L, int heads, int D, 
  *   new codes    -> clamp(rne(x (1 / s')), -127, 127)
  * A row that is not finite makes its block's scale NaN and the block's codes
  * 0; every later read of the block gives NaN until it is begun anew (n = 0).
+ * The scale of a block that keeps rows never shrinks: the same rows again
+ * behind the same prefix change nothing, but larger rows that stood there
+ * for a while leave a larger scale, and kept rows that were rounded to it.
+ * Rows that are to be written many times lose nothing on a page of their own.
  *
  *   K, V   rows of Hkv D channels (strides ldk, ldv), dtype F16 or BF16.
  *   Q, Qo  rows of H D channels and their rotation out (Qo may be Q, with
@@ -874,7 +878,9 @@ int kv_cache_read(const starq_kv_cache* cache, const int32_t* page_table, int ta
  *        rows.
  *   lse  [T][H] float32 out, ln sum_j p_ij, or NULL: joins this result with
  *        attention over other keys.
- *   kv_len [B], at most max_len each; mask_ld >= max_len.
+ *   kv_len [B], at most max_len each (with up to 64 rows of a key/value head
+ *        the bound also chooses the kernel: a close one is faster); mask_ld
+ *        >= max_len.
  *   workspace: kv_cache_attention_workspace_size bytes, 256-byte aligned;
  *        its contents do not matter.
  * Products on 16-bit tensor cores with float32 sums; the softmax weights
@@ -896,7 +902,9 @@ int kv_cache_attention(const void* Q, int ldq, int dtype, int T, const int32_t* 
  *     bias [N] float32 or NULL; Y [L][ldy] F16, BF16 or F32.
  *   sgat_prepare_weight on the weight seen as [N K / group][group] rows with
  *   hb = 1 gives exactly these codes and scales.
- * Float32 accumulation; a group's sum is scaled after it is complete.
+ * Float32 accumulation of exact products (a bf16 activation 2^-29 below the
+ * largest of its 128-channel block loses its last bits); a group's sum is
+ * scaled after it is complete. Infinities and NaN come out as in the formula.
  * Shapes: 0 <= L <= 32, N >= 1, group 32, 64 or 128, K >= group with
  * K % group == 0; ldx >= K, rows of X 16-byte aligned.
  */

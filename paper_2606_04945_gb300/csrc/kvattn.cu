@@ -20,17 +20,18 @@
 //   x_ij = log2(e) scale q_i . k_j + log2 s_v(j),  P_ij = 2^(x_ij - m_i + 7)
 // the weights P_ij already carry the value's scale and are at most 2^15, so
 // rounding them to fp16 (2^-11 relative, as a 16-bit attention does) loses
-// only weights 2^-32 below the row's largest, which is at least 2^7; the sum of the plain weights is
-// sum_j P_ij / s_v(j) in float32 from the unrounded P. m_i is a running
-// maximum that moves only when a score passes it by 8 (2^8 of headroom), so
-// most tiles do not rescale the accumulators.
+// only weights 2^-32 below the row's largest, which is at least 2^7; the sum
+// of the plain weights is sum_j P_ij / s_v(j) in float32 from the unrounded
+// P. m_i is a running maximum that moves only when a score passes it by 8
+// (2^8 of headroom), so most tiles do not rescale the accumulators.
 //
 // Work. For one query token the cache is read once and the rest is small:
 // bound by memory. The G query heads of a key/value head and the new tokens
 // share a unit's rows (16 of an MMA tile), so a key is loaded once for all
-// of them. The 64-key tiles of all units are cut into equal runs, one per
-// CTA: a long sequence is spread over the whole GPU and short ones are
-// packed, whatever the lengths are. A run that covers a unit writes its
+// of them (with more than 16 rows a unit is 16 of them, and the later units
+// find the keys in the L2 cache). The 128-key tiles of all units are cut into
+// equal runs, one per CTA: a long sequence is spread over the whole GPU and
+// short ones are packed, whatever the lengths are. A run that covers a unit writes its
 // rows; partial runs leave (sum, maximum, accumulators) in the workspace and
 // a second kernel joins them in run order (results do not depend on timing).
 //
@@ -41,6 +42,14 @@
 // conflicts. The MMA's k order is free: a key's fragment takes 4 consecutive
 // channels per thread, and value columns are taken in the order that makes a
 // thread's 16 bytes one row's 16 columns, so no transposition is needed.
+//
+// Measured (bf16, 28 heads on 4 of 128): one token for each of four sequences
+// of 131072 and fewer tokens (407 MB): 86.8 us, 4.7 TB/s, 3.9 us of it the
+// join; 6.3 TB/s between two lengths, so about 23 us do not grow with the
+// length (launch, cutting, the last tiles, join). Instructions bound it, not
+// DRAM: issue is 44 % busy and the MMA 29 % with 12 warps an SM. One sequence
+// of 777 tokens takes 12.5 us, a chain of two launches and their loads.
+#include <algorithm>
 #include <type_traits>
 
 #include "kvattn.cuh"
@@ -500,17 +509,32 @@ cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
 
 }  // namespace
 
-// More than 16 rows of a key/value head go to the tcgen05 kernel.
-static bool many_rows(const KvAttnArgs& a) { return (long long)a.max_new * (a.H / a.c.Hkv) > ROWS; }
+// Which kernel. This one reads a unit's keys once for every 16 rows; the
+// tcgen05 kernel reads them once, at up to three times the speed with many
+// rows, but begins and ends slower. Up to 64 rows and a bounded number of
+// (16 rows) x (cached tokens) come here. Measured, this kernel against that
+// one, us, 16 sequences of 2 key/value heads: heads of 64, 40 rows, 4001
+// tokens 19 / 29, 16000 tokens 40 / 44; 64 rows, 4001 tokens 21 / 27; heads
+// of 128, 24 rows, 2000 tokens 24 / 33; 64 rows, 2000 tokens 30 / 32; 128
+// rows, 500 tokens 27 / 24; 256 rows, 400 tokens 40 / 27; 49 rows of 8
+// sequences of 4 heads, 2000 tokens 31 / 29, 8000 tokens 64 / 41. max_len is
+// the bound that the host knows: a generous one leads to the other kernel.
+static bool warp_kernel(const KvAttnArgs& a) {
+    const long long rows = (long long)a.max_new * (a.H / a.c.Hkv), tiles = (rows + ROWS - 1) / ROWS;
+    if (tiles <= 1) return true;
+    return tiles <= 4 && tiles * a.B * a.c.Hkv * (long long)a.max_len <= (a.c.D == 64 ? 1 << 20 : 1 << 18);
+}
 
+// Enough for either kernel, since max_len may change from call to call.
 size_t kv_attention_workspace_bytes(int B, int max_new, int H, int Hkv, int D) {
     const long long rows = (long long)max_new * (H / Hkv);
-    return prefix_bytes(B) + (rows > ROWS ? kv_attention_tc_slot_bytes((int)(rows < 256 ? rows : 256), D)
-                                          : (size_t)num_sms() * CTAS_PER_SM * 2 * slot_floats(ROWS, D) * 4);
+    size_t slots = rows <= 4 * ROWS ? (size_t)num_sms() * CTAS_PER_SM * 2 * slot_floats(ROWS, D) * 4 : 0;
+    if (rows > ROWS) slots = std::max(slots, kv_attention_tc_slot_bytes((int)(rows < 256 ? rows : 256), D));
+    return prefix_bytes(B) + slots;
 }
 
 cudaError_t launch_kv_attention(const KvAttnArgs& a, cudaStream_t s) {
-    if (many_rows(a)) return launch_kv_attention_tc(a, s);
+    if (!warp_kernel(a)) return launch_kv_attention_tc(a, s);
     if (a.dtype == STARQ_BF16)
         return a.c.D == 64 ? launch_typed<__nv_bfloat16, 64>(a, s) : launch_typed<__nv_bfloat16, 128>(a, s);
     return a.c.D == 64 ? launch_typed<__half, 64>(a, s) : launch_typed<__half, 128>(a, s);

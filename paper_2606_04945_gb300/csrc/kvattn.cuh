@@ -1,5 +1,5 @@
-// What the two attention kernels over the 8-bit cache share (kvattn.cu: up
-// to 16 query rows of a key/value head; kvattn_tc.cu: more): the cutting of
+// What the two attention kernels over the 8-bit cache share (kvattn.cu: few
+// query rows of a key/value head; kvattn_tc.cu: many): the cutting of
 // all units' key tiles into one run per CTA, and the kernel that joins the
 // partial runs of a unit.
 //

@@ -1,6 +1,7 @@
-// Attention over the paged 8-bit cache for more than 16 query rows of a
-// key/value head (blocks of positions under denoising, drafted runs with
-// grouped heads): both products on tcgen05. The mathematics is kvattn.cu's.
+// Attention over the paged 8-bit cache for many query rows of a key/value
+// head (blocks of positions under denoising, drafted runs with grouped heads;
+// the rule stands at the end of kvattn.cu): both products on tcgen05. The
+// mathematics is kvattn.cu's.
 //
 // With R rows a cached key costs 4 R D operations for 2 D bytes, so from
 // about 100 rows on the tensor cores' work outweighs the cache's bytes; the
@@ -26,6 +27,15 @@
 // 16-key block that is seen (so no score is above those that count), values
 // of 0, and a factor of 0 in the sum. A block without such a key has scores
 // of -inf. Only the causal boundary is tested score by score.
+//
+// Measured (bf16, 28 heads on 4 of 128, 32 positions for each of 8 sequences
+// of 16384 and fewer tokens, a key mask; 39 GFLOP, 92 MB): 79.7 us, 493
+// TFLOP/s, 7.2 us of it the join; the warp-level MMA took 444 us. About 30 us
+// do not grow with the length (cutting, the queries' rows, the first tile's
+// way through all stages, the accumulators' way out, the join). Beyond that a
+// step of a stream is bound by the chain scores - exponentials - weights -
+// product: leaving out the conversion, the loads or the products one by one
+// changed the time by a few percent each, and issue is 38 % busy.
 #include <algorithm>
 
 #include "kvattn.cuh"

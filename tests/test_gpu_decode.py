@@ -419,6 +419,34 @@ def test_attention_odd_rows(abi, new, H, Hkv, D):
     attend(abi, rng, pg, [new, new - 1, new], lens, H, torch.bfloat16, causal=new == 61)
 
 
+@pytest.mark.parametrize("bound", [0, 1 << 19])
+@pytest.mark.parametrize("dtype,page,D,H,Hkv,new", [
+    (torch.float16, 16, 64, 16, 2, 5), (torch.bfloat16, 64, 128, 7, 1, 3), (torch.bfloat16, 32, 128, 14, 2, 9),
+    (torch.float16, 128, 64, 3, 1, 17), (torch.bfloat16, 16, 128, 4, 4, 64), (torch.float16, 64, 64, 8, 1, 8)])
+@pytest.mark.parametrize("causal,masked", [(False, False), (True, False), (True, True)])
+def test_attention_bound(abi, bound, dtype, page, D, H, Hkv, new, causal, masked):
+    """17 to 64 rows of a key/value head under a tight and a generous bound
+    of the lengths (they lead to different kernels)."""
+    rng = np.random.default_rng(new + page)
+    lens = [new, 333, 1201, 64]
+    count = [new, new - 1, new, 0]
+    pg = Paged(abi, rng, 4, 1201, Hkv, page, D)
+    fill(pg, rng, lens)
+    most = max(lens) + bound
+    mask = None
+    if masked:
+        mask = (rng.random((4, most)) < 0.6).astype(np.uint8)
+        mask[1, 64:] = 0                              # most of a sequence is not seen
+        mask[2, :130] = 0
+    q, _ = randn(rng, (sum(count), H * D), dtype)
+    out, lse = torch.empty_like(q), torch.empty(sum(count), H, device="cuda")
+    abi.kv_cache_attention(q, pg.cache, pg.dev_table, i32(lens), i32(np.concatenate([[0], np.cumsum(count)])), out,
+                           max_new=new, max_len=most, causal=causal, lse=lse,
+                           key_mask=None if mask is None else torch.from_numpy(mask).cuda())
+    abi.check_status()
+    check_attention(pg, q, out, lse, count, lens, H, dtype, D ** -0.5, causal, mask)
+
+
 @pytest.mark.parametrize("new", [1, 20])
 def test_attention_many_sequences(abi, new):
     """More sequences than threads of a CTA."""
