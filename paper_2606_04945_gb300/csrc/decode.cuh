@@ -59,6 +59,7 @@ struct KvAttnArgs {
     void* Out; int ldo; float* lse;
     void* workspace;
     unsigned* status;
+    int whole;                       // units are not cut (set by the launcher)
 };
 size_t kv_attention_workspace_bytes(int B, int max_new, int H, int Hkv, int D);
 cudaError_t launch_kv_attention(const KvAttnArgs& a, cudaStream_t s);

@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
     Cursor<ROWS, TILE> cur;
     cur.start(a, G, run);
     Cursor<ROWS, TILE> pre = cur;
-    int left = (int)(run.tau1 - run.tau0);   // tiles of the run
+    int left = cur.tiles(a, G, run);         // tiles of the run
     int pre_left = left;                     // tiles still to be fetched
 
     const uint32_t ring = smem_addr(smem) + warp * (STAGES * SM::STAGE);
@@ -502,7 +502,7 @@ cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
     long long* prefix = static_cast<long long*>(a.workspace);
     float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + prefix_bytes(a.B));
     if ((e = launch_overlapped(kv_attention_kernel<T, D>, dim3(ctas), THREADS, AttnSmem<T, D>::BYTES, s, a, G, prefix,
-                               slots)) != cudaSuccess)
+                               slots)) != cudaSuccess || a.whole)
         return e;
     return launch_join<T, D, ROWS, TILE>(a, G, ctas, ROWS, prefix, slots, s);
 }
@@ -533,8 +533,10 @@ size_t kv_attention_workspace_bytes(int B, int max_new, int H, int Hkv, int D) {
     return prefix_bytes(B) + slots;
 }
 
-cudaError_t launch_kv_attention(const KvAttnArgs& a, cudaStream_t s) {
+cudaError_t launch_kv_attention(const KvAttnArgs& args, cudaStream_t s) {
+    KvAttnArgs a = args;
     if (!warp_kernel(a)) return launch_kv_attention_tc(a, s);
+    a.whole = whole_units(a, ROWS, TILE, num_sms() * CTAS_PER_SM);
     if (a.dtype == STARQ_BF16)
         return a.c.D == 64 ? launch_typed<__nv_bfloat16, 64>(a, s) : launch_typed<__nv_bfloat16, 128>(a, s);
     return a.c.D == 64 ? launch_typed<__half, 64>(a, s) : launch_typed<__half, 128>(a, s);

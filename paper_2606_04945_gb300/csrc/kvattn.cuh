@@ -9,8 +9,11 @@
 // of equal length. A unit inside one run is written at once; otherwise each
 // of its runs leaves, in slot 2 c (the run of CTA c begins with or inside the
 // unit) or 2 c + 1 (it ends in it), the rows' accumulators, maxima and sums.
+// Where the sequences are short by their bound, the units themselves are
+// dealt out instead (`whole`), and there is nothing to join.
 #pragma once
 
+#include <algorithm>
 #include <type_traits>
 
 #include "decode.cuh"
@@ -65,13 +68,15 @@ __device__ __forceinline__ SeqShape seq_shape(const KvAttnArgs& a, int G, int b,
         if (report) atomicOr(a.status, STATUS_RANGE);
         s.n = 0; s.len = 0; s.row0 = 0;
     }
-    s.nt = s.n > 0 ? (s.len + TILE - 1) / TILE : 0;
+    // (a whole unit without keys has a tile all the same: its CTA writes its rows)
+    s.nt = s.n > 0 ? max((s.len + TILE - 1) / TILE, a.whole) : 0;
     s.rt = (s.n * G + ROWS - 1) / ROWS;
     return s;
 }
 
-// This CTA's run [tau0, tau1) of the flat list of tiles, the sequence that
-// tau0 falls into and the tiles before that sequence. CTA 0 writes `prefix`.
+// This CTA's run [tau0, tau1) of the flat list of tiles (whole: of units), the
+// sequence that tau0 falls into and the tiles (units) before that sequence.
+// CTA 0 writes `prefix`.
 struct Run { long long tau0, tau1, before; int b; };
 template <int ROWS, int TILE, int THREADS>
 __device__ __forceinline__ Run find_run(const KvAttnArgs& a, int G, long long* prefix) {
@@ -82,7 +87,7 @@ __device__ __forceinline__ Run find_run(const KvAttnArgs& a, int G, long long* p
     auto tiles_of = [&](int b, bool report) {
         if (b >= a.B) return 0ll;
         const SeqShape s = seq_shape<ROWS, TILE>(a, G, b, report);
-        return (long long)s.nt * s.rt * a.c.Hkv;
+        return (long long)(a.whole ? s.nt > 0 : s.nt) * s.rt * a.c.Hkv;
     };
     // inclusive sums over the CTA's threads; part sums of the warps in s_part
     auto scan = [&](long long v) {
@@ -145,8 +150,8 @@ struct Cursor {
     __device__ __forceinline__ void start(const KvAttnArgs& a, int G, const Run& r) {
         b = r.b;
         s = seq_shape<ROWS, TILE>(a, G, b, false);
-        const long long off = r.tau0 - r.before, unit = off / s.nt;
-        kt = (int)(off - unit * s.nt);
+        const long long off = r.tau0 - r.before, unit = a.whole ? off : off / s.nt;
+        kt = a.whole ? 0 : (int)(off - unit * s.nt);
         h = (int)(unit / s.rt);
         rt = (int)(unit - (long long)h * s.rt);
     }
@@ -161,7 +166,32 @@ struct Cursor {
             s = seq_shape<ROWS, TILE>(a, G, b, false);
         } while (s.nt == 0);
     }
+    // Tiles of the run that begins here.
+    __device__ __forceinline__ int tiles(const KvAttnArgs& a, int G, const Run& r) const {
+        if (!a.whole) return (int)(r.tau1 - r.tau0);
+        Cursor q = *this;
+        int n = q.s.nt;
+        for (long long u = r.tau0 + 1; u < r.tau1; ++u) {
+            q.next_unit(a, G);
+            n += q.s.nt;
+        }
+        return n;
+    }
 };
+
+// Whether units are dealt out whole, from the bounds that the host knows.
+// Counted in key tiles of the busiest CTA, cutting and joining cost 2 and, as
+// the joins are many, 4 for each unit a CTA; beyond 8 tiles the spread of the
+// lengths under their bound would weigh more. Measured, cut / whole, us: one
+// row of 28 heads on 4, 100 tokens 11.8 / 10.1, 256 tokens 12.0 / 11.3, 500
+// tokens 12.5 / 14.5 (cut); 64 such sequences, up to 300 tokens 24.5 / 17.7,
+// 1000 tokens 35.1 / 28.1; 32 rows of them, 8 sequences, 250 tokens 20.9 /
+// 18.6, 500 tokens 21.9 / 23.4 (cut); 32 sequences, 500 tokens 48 / 24.8.
+inline bool whole_units(const KvAttnArgs& a, int rows, int tile, int ctas) {
+    const long long t = std::max(1, (a.max_len + tile - 1) / tile);
+    const long long n = ((long long)a.max_new * (a.H / a.c.Hkv) + rows - 1) / rows * a.B * a.c.Hkv;      // units
+    return t <= 8 && t * ((n + ctas - 1) / ctas) * ctas <= std::max<long long>(ctas, n * t) + 2 * ctas + 4 * n;
+}
 
 // Joins the partial runs of a row's unit, and writes the rows that no key
 // reaches. SHARE warps take a row: one where there are many rows (their units

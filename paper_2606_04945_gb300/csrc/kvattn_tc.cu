@@ -218,8 +218,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
     const uint32_t tmem = sh->tmem_base;
     grid_dependency_wait();
     const Run run = find_run<ROWS, TILE, THREADS>(a, G, prefix);
-    const int count = (int)(run.tau1 - run.tau0);
-    bool ok = count > 0;
 
     // Every role walks the run segment by segment (a segment is the run's
     // part of one unit). In a segment of n key tiles the streams' steps are
@@ -227,7 +225,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
     // stream u & 1; shared = 0: key tile u for stream u & 1. Either way it is
     // the stream's step u / 2 of the segment.
     Cur cur;
-    if (count > 0) cur.start(a, G, run);
+    int count = 0;
+    if (run.tau0 < run.tau1) {
+        cur.start(a, G, run);
+        count = cur.tiles(a, G, run);
+    }
+    bool ok = count > 0;
     auto unit_rows = [&](const Cur& c) { return min(ROWS, c.s.n * G - c.rt * ROWS); };
     auto segment = [&](const Cur& c, int left) { return min(left, c.s.nt - c.kt); };
 
@@ -797,7 +800,7 @@ cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
     long long* prefix = static_cast<long long*>(a.workspace);
     float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + prefix_bytes(a.B));
     if ((e = launch_overlapped(kv_attention_tc_kernel<T, D>, dim3(ctas), THREADS, Layout<D>::SMEM, s, a, G, slot_rows,
-                               prefix, slots)) != cudaSuccess)
+                               prefix, slots)) != cudaSuccess || a.whole)
         return e;
     return launch_join<T, D, ROWS, TILE>(a, G, ctas, slot_rows, prefix, slots, s);
 }
@@ -808,7 +811,9 @@ size_t kv_attention_tc_slot_bytes(int max_rows, int D) {
     return (size_t)num_sms() * 2 * slot_floats(max_rows, D) * 4;
 }
 
-cudaError_t launch_kv_attention_tc(const KvAttnArgs& a, cudaStream_t s) {
+cudaError_t launch_kv_attention_tc(const KvAttnArgs& args, cudaStream_t s) {
+    KvAttnArgs a = args;
+    a.whole = whole_units(a, ROWS, TILE, num_sms());
     if (a.dtype == STARQ_BF16)
         return a.c.D == 64 ? launch_typed<__nv_bfloat16, 64>(a, s) : launch_typed<__nv_bfloat16, 128>(a, s);
     return a.c.D == 64 ? launch_typed<__half, 64>(a, s) : launch_typed<__half, 128>(a, s);

@@ -673,3 +673,36 @@ def test_w4g_values(abi, dtype, L, group):
     y[bad, 300] = float("nan")
     run(y, packed)
     assert torch.isnan(Y[bad]).all() and torch.equal(Y[rest], before[rest])
+
+
+@pytest.mark.parametrize("dtype,page,D,H,Hkv,B,new", [
+    (torch.bfloat16, 16, 128, 7, 1, 40, 1), (torch.float16, 64, 64, 8, 4, 200, 2), (torch.bfloat16, 32, 128, 28, 4, 9, 32),
+    (torch.float16, 128, 64, 6, 2, 90, 100), (torch.bfloat16, 64, 64, 2, 2, 1, 300)])
+@pytest.mark.parametrize("most", [1, 100, 256, 1000])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_short(abi, dtype, page, D, H, Hkv, B, new, most, causal):
+    """Many short sequences, some without tokens in the cache, some without
+    rows: units that are not cut have nothing to join, and rows without keys
+    are written by their unit."""
+    rng = np.random.default_rng(B + most)
+    lens = [int(v) for v in rng.integers(0, most + 1, B)]
+    lens[0] = most
+    count = [int(v) for v in rng.integers(0, new + 1, B)]
+    count[0] = new
+    pg = Paged(abi, rng, B, most, Hkv, page, D)
+    fill(pg, rng, lens)
+    q, _ = randn(rng, (sum(count), H * D), dtype)
+    out, lse = torch.full_like(q, 7.0), torch.full((sum(count), H), 7.0, device="cuda")
+    start = np.concatenate([[0], np.cumsum(count)])
+    abi.kv_cache_attention(q, pg.cache, pg.dev_table, i32(lens), i32(start), out, max_new=new, max_len=most,
+                           causal=causal, lse=lse)
+    abi.check_status()
+    for b in [0] + [int(v) for v in rng.choice(B, min(B, 12), replace=False)]:
+        r = slice(start[b], start[b + 1])
+        one = Paged.__new__(Paged)
+        one.__dict__.update(pg.__dict__)
+        one.table = pg.table[b:b + 1]
+        check_attention(one, q[r], out[r], lse[r], [count[b]], [lens[b]], H, dtype, D ** -0.5, causal, None)
+    empty = np.repeat(np.asarray(lens) == 0, count)
+    assert torch.isfinite(out).all() and not (out == 7.0).all(dim=1).any()
+    assert torch.isneginf(lse[torch.from_numpy(empty).cuda()]).all()
