@@ -53,6 +53,12 @@ __device__ __forceinline__ void row_power(float top, float& up, float& down) {
     down = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
 }
 
+// a / b, a >= 0 (64-bit divisions take a hundred instructions each; few lists
+// of tiles need them).
+__device__ __forceinline__ long long quotient(long long a, int b) {
+    return a < (1ll << 31) ? (long long)((unsigned)a / (unsigned)b) : a / b;
+}
+
 struct SeqShape { int len, n, row0, nt, rt; };       // cached tokens, new tokens, first row, key tiles, row tiles
 
 // The lengths of sequence b; a sequence whose numbers do not fit their
@@ -113,7 +119,7 @@ __device__ __forceinline__ Run find_run(const KvAttnArgs& a, int G, long long* p
         scan(rest);
         for (int w = 0; w < WARPS; ++w) total += s_part[w];
     }
-    const long long share = (total + gridDim.x - 1) / gridDim.x;
+    const long long share = quotient(total + gridDim.x - 1, (int)gridDim.x);
     Run r;
     r.tau0 = share * blockIdx.x;
     r.tau1 = min(total, r.tau0 + share);
@@ -150,9 +156,9 @@ struct Cursor {
     __device__ __forceinline__ void start(const KvAttnArgs& a, int G, const Run& r) {
         b = r.b;
         s = seq_shape<ROWS, TILE>(a, G, b, false);
-        const long long off = r.tau0 - r.before, unit = a.whole ? off : off / s.nt;
+        const long long off = r.tau0 - r.before, unit = a.whole ? off : quotient(off, s.nt);
         kt = a.whole ? 0 : (int)(off - unit * s.nt);
-        h = (int)(unit / s.rt);
+        h = (int)quotient(unit, s.rt);
         rt = (int)(unit - (long long)h * s.rt);
     }
     __device__ __forceinline__ void next_unit(const KvAttnArgs& a, int G) {

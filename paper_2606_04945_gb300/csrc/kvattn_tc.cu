@@ -164,6 +164,10 @@ __device__ __forceinline__ void store_codes(uint32_t tile, int r, int c, const u
     }
 }
 
+__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAttnArgs a, int G, int slot_rows,
                                                                     long long* prefix, float* slots) {
@@ -507,43 +511,54 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
             const bool valid = (shared ? s * TILE : 0) + row < rows;
             const bool active = __any_sync(0xffffffffu, valid);
             const int lim = !valid ? 0 : a.causal ? max(0, cur.s.len - cur.s.n + i + 1) : cur.s.len;
-            // the unit's query rows, as the A operand (with few rows both streams use the first tile)
+            // The unit's query rows, as the A operand (with few rows both streams use the first tile): asynchronous
+            // copies along the rows, and bf16 rows become fp16 in place, a thread a row. In rolled loops: the same
+            // work unrolled ran from cold instruction lines (7 us of a call, now 2).
             float down = 1.f;
-            const T* src = static_cast<const T*>(a.Q) + (size_t)(cur.s.row0 + (valid ? i : 0)) * a.ldq +
-                           (size_t)(valid ? head : 0) * D;
-            float up = 1.f;
-            if (shared || s == 0 || std::is_same<T, __nv_bfloat16>::value) {
-                uint4 q[D / 8];                                                 // the whole row on its way at once
-                #pragma unroll
-                for (int k = 0; k < D / 8; ++k) q[k] = ld_global_nc_v4(src + 8 * k);
-                if (std::is_same<T, __nv_bfloat16>::value) {
+            constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
+            if (shared || s == 0 || BF16) {
+                constexpr int CH = D / 8, RPC = 32 / CH;                        // 16-byte chunks of a row, rows a copy
+                const uint32_t tile = base + L::Q + s * L::TILE_BYTES;
+                const long long from = valid ? (long long)(cur.s.row0 + i) * a.ldq + (long long)head * D : 0;
+                #pragma unroll 4
+                for (int r0 = 0; r0 < 32; r0 += RPC) {
+                    const int rr = r0 + lane / CH, k = lane % CH;
+                    const long long off = __shfl_sync(0xffffffffu, from, rr);
+                    const bool real = __shfl_sync(0xffffffffu, (int)valid, rr) != 0;
+                    cp_async16_or_zero(tile + (k >> 3) * L::HALF + sw128_offset((warp & 3) * 32 + rr, k & 7),
+                                       static_cast<const T*>(a.Q) + off + 8 * k, real);
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                __syncwarp();
+                if (BF16) {
                     // the largest magnitude: bf16 numbers without their sign are ordered as integers
+                    auto chunk = [&](int k) {
+                        return reinterpret_cast<uint4*>(smem + L::Q + s * L::TILE_BYTES + (k >> 3) * L::HALF +
+                                                        sw128_offset(row, k & 7));
+                    };
                     uint32_t top = 0;
-                    #pragma unroll
-                    for (int k = 0; k < D / 8; ++k) {
-                        const uint32_t w[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+                    #pragma unroll 4
+                    for (int k = 0; k < CH; ++k) {
+                        const uint4 v = *chunk(k);
+                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
                         #pragma unroll
                         for (int e = 0; e < 4; ++e) top = max(top, max(w[e] << 16 & 0x7fff0000u, w[e] & 0x7fff0000u));
                     }
+                    float up;
                     row_power(__uint_as_float(top), up, down);
-                }
-                if (shared || s == 0) {
-                    #pragma unroll
-                    for (int k = 0; k < D / 8; ++k) {
-                        uint4 v = valid ? q[k] : make_uint4(0, 0, 0, 0);
-                        if (std::is_same<T, __nv_bfloat16>::value) {
-                            const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
-                            uint32_t o[4];
+                    if (shared || s == 0) {
+                        #pragma unroll 2
+                        for (int k = 0; k < CH; ++k) {
+                            uint4 v = *chunk(k);
+                            uint32_t w[4] = {v.x, v.y, v.z, v.w};
                             #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const float2 f = __bfloat1622float2(h[e]);
-                                const __half2 p = __floats2half2_rn(f.x * up, f.y * up);
-                                o[e] = *reinterpret_cast<const uint32_t*>(&p);
+                                const __half2 p = __floats2half2_rn(__uint_as_float(w[e] << 16) * up,
+                                                                    __uint_as_float(w[e] & 0xffff0000u) * up);
+                                w[e] = *reinterpret_cast<const uint32_t*>(&p);
                             }
-                            v = make_uint4(o[0], o[1], o[2], o[3]);
+                            *chunk(k) = make_uint4(w[0], w[1], w[2], w[3]);
                         }
-                        st_shared_v4(base + L::Q + s * L::TILE_BYTES + (k >> 3) * L::HALF + sw128_offset(row, k & 7), v.x,
-                                     v.y, v.z, v.w);
                     }
                 }
             }
