@@ -29,13 +29,14 @@
 // of -inf. Only the causal boundary is tested score by score.
 //
 // Measured (bf16, 28 heads on 4 of 128, 32 positions for each of 8 sequences
-// of 16384 and fewer tokens, a key mask; 39 GFLOP, 92 MB): 79.7 us, 493
-// TFLOP/s, 7.2 us of it the join; the warp-level MMA took 444 us. About 30 us
-// do not grow with the length (cutting, the queries' rows, the first tile's
-// way through all stages, the accumulators' way out, the join). Beyond that a
-// step of a stream is bound by the chain scores - exponentials - weights -
-// product: leaving out the conversion, the loads or the products one by one
-// changed the time by a few percent each, and issue is 38 % busy.
+// of 16384 and fewer tokens, a key mask; 39 GFLOP, 92 MB): 68.9 us, 570
+// TFLOP/s, 7 us of it the join; the warp-level MMA took 444 us. In clocks of a
+// CTA: cutting 4.5 thousand, the queries' rows 10 (beside the first codes), a
+// tile's step 4.5 (a stream waits 1.8 for weights - values - next scores,
+// takes the maximum in 0.7 and the weights in 1.9; the products need 2.0 of
+// the tensor cores), the rows' way out 7.5. Loads from TMEM one at a time made
+// the step 5.3 (75.5 us); leaving out the conversion or the codes' copies
+// changes it by a few percent.
 #include <algorithm>
 
 #include "kvattn.cuh"
@@ -162,6 +163,16 @@ __device__ __forceinline__ void store_codes(uint32_t tile, int r, int c, const u
         st_shared_v4(lo, h[0], h[1], h[2], h[3]);
         st_shared_v4(hi, h[4], h[5], h[6], h[7]);
     }
+}
+
+// Waits for the loads from TMEM; x comes from one of them.
+__device__ __forceinline__ void tmem_arrived(uint32_t (&x)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]), "+r"(x[4]), "+r"(x[5]), "+r"(x[6]), "+r"(x[7]),
+                   "+r"(x[8]), "+r"(x[9]), "+r"(x[10]), "+r"(x[11]), "+r"(x[12]), "+r"(x[13]), "+r"(x[14]), "+r"(x[15]),
+                   "+r"(x[16]), "+r"(x[17]), "+r"(x[18]), "+r"(x[19]), "+r"(x[20]), "+r"(x[21]), "+r"(x[22]), "+r"(x[23]),
+                   "+r"(x[24]), "+r"(x[25]), "+r"(x[26]), "+r"(x[27]), "+r"(x[28]), "+r"(x[29]), "+r"(x[30]), "+r"(x[31])
+                 :: "memory");
 }
 
 __device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool real) {
@@ -578,12 +589,39 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                     const bool edge = ti.edge != 0;  // the causal boundary is in the tile
                     float top = NEG_INF;
                     unsigned met = edge ? 0u : ti.met;                          // blocks of which the row sees a key
-                    #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t x[32];
-                        tmem_ld_32x32b_x32(t_s + 32 * c, x);
-                        tmem_ld_wait();
-                        if (edge) {
+                    // Two chunks of 32 keys at a time, the second on its way from TMEM while the first is worked on.
+                    auto chunks = [&](auto&& work) {
+                        #pragma unroll 1
+                        for (int c = 0; c < 4; c += 2) {
+                            uint32_t x[32], y[32];
+                            tmem_ld_32x32b_x32(t_s + 32 * c, x);
+                            tmem_arrived(x);
+                            tmem_ld_32x32b_x32(t_s + 32 * c + 32, y);
+                            work(c, x);
+                            tmem_arrived(y);
+                            work(c + 1, y);
+                        }
+                    };
+                    auto largest = [&](const uint32_t* y) {
+                        float t = __uint_as_float(y[0]);
+                        #pragma unroll
+                        for (int k = 1; k < 15; k += 2) t = max3(t, __uint_as_float(y[k]), __uint_as_float(y[k + 1]));
+                        return fmaxf(t, __uint_as_float(y[15]));
+                    };
+                    if (!edge) {
+                        chunks([&](int c, const uint32_t (&x)[32]) {
+                            #pragma unroll
+                            for (int q = 0; q < 2; ++q) {
+                                const float4 b = ti.blk[2 * c + q];
+                                top = fmaxf(top, fmaf(largest(&x[16 * q]), b.x * down, b.y));
+                            }
+                        });
+                    } else {
+                        #pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t x[32];
+                            tmem_ld_32x32b_x32(t_s + 32 * c, x);
+                            tmem_arrived(x);
                             const int see = lim - ti.key0 - 32 * c;
                             #pragma unroll
                             for (int k = 0; k < 32; ++k)
@@ -594,23 +632,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                                 #pragma unroll
                                 for (int k = 0; k < 16; ++k) y[k] = x[16 * q + k];
                                 tmem_st_32x32b_x16(t_s + 32 * c + 16 * q, y);
-                            }
-                        }
-                        #pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            const uint32_t* y = &x[16 * q];
-                            float t = __uint_as_float(y[0]);
-                            #pragma unroll
-                            for (int k = 1; k < 15; k += 2) t = max3(t, __uint_as_float(y[k]), __uint_as_float(y[k + 1]));
-                            t = fmaxf(t, __uint_as_float(y[15]));
-                            const float4 b = ti.blk[2 * c + q];
-                            if (edge) {
+                                const float t = largest(y);
+                                const float4 b = ti.blk[2 * c + q];
                                 if (b.y != NEG_INF && t != NEG_INF) {
                                     met |= 1u << (2 * c + q);
                                     top = fmaxf(top, fmaf(t, b.x * down, b.y));
                                 }
-                            } else {
-                                top = fmaxf(top, fmaf(t, b.x * down, b.y));
                             }
                         }
                     }
@@ -640,11 +667,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                     // `all`: every row sees a key of every block. Else a block without one weighs nothing,
                     // whatever its scales are.
                     auto weights = [&](auto all) {
-                        #pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            uint32_t x[32], p[16];
-                            tmem_ld_32x32b_x32(t_s + 32 * c, x);
-                            tmem_ld_wait();
+                        chunks([&](int c, const uint32_t (&x)[32]) {
+                            uint32_t p[16];
                             #pragma unroll
                             for (int q = 0; q < 2; ++q) {
                                 const float4 b = ti.blk[2 * c + q];
@@ -671,7 +695,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                                 }
                             }
                             tmem_st_32x32b_x16(t_s + 16 * c, p);                // over scores of chunks up to c / 2
-                        }
+                        });
                     };
                     if (__all_sync(0xffffffffu, met == 0xffu)) weights(std::true_type{});
                     else weights(std::false_type{});
