@@ -95,6 +95,27 @@ __device__ __forceinline__ Run find_run(const KvAttnArgs& a, int G, long long* p
         const SeqShape s = seq_shape<ROWS, TILE>(a, G, b, report);
         return (long long)(a.whole ? s.nt > 0 : s.nt) * s.rt * a.c.Hkv;
     };
+    if (a.B <= 32) {                                          // every warp by itself, without barriers
+        const long long cnt = tiles_of(lane, blockIdx.x == 0 && warp == 0);
+        long long sum = cnt;
+        #pragma unroll
+        for (int m = 1; m < 32; m <<= 1) {
+            const long long u = __shfl_up_sync(0xffffffffu, sum, m);
+            if (lane >= m) sum += u;
+        }
+        const long long total = __shfl_sync(0xffffffffu, sum, 31);
+        const long long share = quotient(total + gridDim.x - 1, (int)gridDim.x);
+        Run r;
+        r.tau0 = share * blockIdx.x;
+        r.tau1 = min(total, r.tau0 + share);
+        r.b = __ffs(__ballot_sync(0xffffffffu, r.tau0 >= sum - cnt && r.tau0 < sum)) - 1;
+        r.before = __shfl_sync(0xffffffffu, sum - cnt, max(r.b, 0));
+        if (blockIdx.x == 0 && warp == 0) {
+            if (lane < a.B) prefix[lane] = sum - cnt;
+            if (lane == 0) prefix[a.B] = total;
+        }
+        return r;
+    }
     // inclusive sums over the CTA's threads; part sums of the warps in s_part
     auto scan = [&](long long v) {
         #pragma unroll
