@@ -82,6 +82,13 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// Transposes an 8 x 8 matrix of 16-bit numbers (a row in four threads).
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
 // Bytes 0 and 1 (2 and 3) of a word as the halves of a register.
 __device__ __forceinline__ uint32_t widen_lo(uint32_t w) { return prmt(w, 0u, 0x4140u); }
 __device__ __forceinline__ uint32_t widen_hi(uint32_t w) { return prmt(w, 0u, 0x4342u); }
@@ -142,12 +149,17 @@ struct AttnSmem {
     static constexpr int BYTES = RING + MERGE;
 };
 
-template <typename T, int D>
+// NARROW: at most 8 rows. Then the keys are the MMA's 16-row operand and the
+// query rows its 8 columns (scores^T = K Q^T, out^T = V^T P^T): half the MMAs
+// and half the exponentials, none of them for rows that do not exist. A
+// thread has the columns (rows of the unit) 2t and 2t + 1.
+template <typename T, int D, bool NARROW>
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(const KvAttnArgs a, int G, long long* prefix_out,
                                                                  float* slots) {
     using SM = AttnSmem<T, D>;
     constexpr int KH = D / 64;               // 64-channel halves of a key
     constexpr int DN = D / 8;                // value columns per thread, and column tiles
+    constexpr int HELD = NARROW ? 8 : ROWS;  // rows that can be there
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
 
@@ -209,7 +221,9 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
     for (int i = 0; i < STAGES - 1; ++i) fetch(i);
 
     uint4* const query = reinterpret_cast<uint4*>(smem + SM::QUERY) + lane;      // this lane's fragment of k step 0
-    float o[DN][4], m[2], l[2], rs[2], qs[2];
+    constexpr int OT = NARROW ? DN / 2 : DN; // tiles of the accumulators
+    uint32_t qb[NARROW ? KH : 1][4][2];      // NARROW: the query fragments
+    float o[OT][4], m[2], l[2], rs[2], qs[2];
     int lim[2];                              // keys [0, lim) are visible to the rows (causal limit and length)
     const float unit_scale = a.scale * 1.4426950408889634f;
     bool fresh = true;
@@ -223,7 +237,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
             if (fresh) {                     // a new unit: its query rows
                 uint32_t q2[2][KH][4][2];
                 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
+                for (int k = 0; k < (NARROW ? 1 : 2); ++k) {
                     const int r = cur.rt * ROWS + g + 8 * k, i = r / G, j = r - i * G;
                     const T* row = nullptr;
                     lim[k] = 0;
@@ -233,8 +247,23 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                         lim[k] = a.causal ? max(0, cur.s.len - cur.s.n + i + 1) : cur.s.len;
                     }
                     rs[k] = load_row<T, D>(row, t, q2[k], qs[k]);
-                    m[k] = NEG_INF; l[k] = 0.f;
                 }
+                m[0] = m[1] = NEG_INF;
+                l[0] = l[1] = 0.f;
+                if constexpr (NARROW) {
+                    #pragma unroll
+                    for (int h = 0; h < KH; ++h)
+                        #pragma unroll
+                        for (int s = 0; s < 4; ++s) { qb[h][s][0] = q2[0][h][s][0]; qb[h][s][1] = q2[0][h][s][1]; }
+                    const float r = rs[0], q = qs[0];
+                    const int v = lim[0];
+                    #pragma unroll
+                    for (int k = 0; k < 2; ++k) {           // from the threads of row g = 2t + k
+                        rs[k] = __shfl_sync(0xffffffffu, r, 4 * (2 * t + k));
+                        qs[k] = __shfl_sync(0xffffffffu, q, 4 * (2 * t + k));
+                        lim[k] = __shfl_sync(0xffffffffu, v, 4 * (2 * t + k));
+                    }
+                } else {
                 // every warp has the fragments; each stores its part of them for all
                 #pragma unroll
                 for (int h = 0; h < KH; ++h)
@@ -244,8 +273,9 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                             query[(4 * h + s) * 32] = make_uint4(q2[0][h][s][0], q2[1][h][s][0], q2[0][h][s][1],
                                                                  q2[1][h][s][1]);
                 __syncthreads();             // (the unit before ended with a barrier: its fragments are done with)
+                }
                 #pragma unroll
-                for (int j = 0; j < DN; ++j)
+                for (int j = 0; j < OT; ++j)
                     #pragma unroll
                     for (int k = 0; k < 4; ++k) o[j][k] = 0.f;
                 fresh = false;
@@ -258,9 +288,10 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
             if (key0 < cur.s.len) {
                 const uint8_t* stage = smem + warp * (STAGES * SM::STAGE) + st * SM::STAGE;
                 // --- scores of 32 keys: four column tiles, a k step for all of them ---
-                float x[4][4];
+                constexpr int XT = NARROW ? 2 : 4;           // tiles: NARROW 16 keys x 8 rows, else 16 rows x 8 keys
+                float x[XT][4];
                 #pragma unroll
-                for (int nt = 0; nt < 4; ++nt)
+                for (int nt = 0; nt < XT; ++nt)
                     #pragma unroll
                     for (int k = 0; k < 4; ++k) x[nt][k] = 0.f;
                 #pragma unroll
@@ -271,15 +302,28 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                         w[nt] = *reinterpret_cast<const uint4*>(stage + stage_offset<D>(nt * 8 + g, 4 * h + t));
                     #pragma unroll
                     for (int s = 0; s < 4; ++s) {
-                        const uint4 q = query[(4 * h + s) * 32];
-                        const uint32_t qa[4] = {q.x, q.y, q.z, q.w};
-                        #pragma unroll
-                        for (int nt = 0; nt < 4; ++nt) {
-                            const uint32_t ws = s == 0 ? w[nt].x : s == 1 ? w[nt].y : s == 2 ? w[nt].z : w[nt].w;
-                            mma_16816(x[nt], qa, widen_lo(ws), widen_hi(ws));
+                        auto word = [&](int nt) { return s == 0 ? w[nt].x : s == 1 ? w[nt].y : s == 2 ? w[nt].z : w[nt].w; };
+                        if constexpr (NARROW) {
+                            #pragma unroll
+                            for (int b = 0; b < 2; ++b) {
+                                const uint32_t u = word(2 * b), v = word(2 * b + 1);
+                                const uint32_t ka[4] = {widen_lo(u), widen_lo(v), widen_hi(u), widen_hi(v)};
+                                mma_16816(x[b], ka, qb[h][s][0], qb[h][s][1]);
+                            }
+                        } else {
+                            const uint4 q = query[(4 * h + s) * 32];
+                            const uint32_t qa[4] = {q.x, q.y, q.z, q.w};
+                            #pragma unroll
+                            for (int nt = 0; nt < 4; ++nt) mma_16816(x[nt], qa, widen_lo(word(nt)), widen_hi(word(nt)));
                         }
                     }
                 }
+                // element k of a tile: which of the thread's two rows, and which key of the warp's 32
+                auto row_of = [](int k) { return NARROW ? k & 1 : k >> 1; };
+                auto key_of = [&](int nt, int k) {
+                    return NARROW ? 16 * nt + g + 8 * (k >> 1) : 8 * nt + 2 * t + (k & 1);
+                };
+                auto block_of = [](int nt) { return NARROW ? nt : nt >> 1; };
                 const float4 scales = *reinterpret_cast<const float4*>(stage + 2 * WKEYS * D);
                 float iv[2];
                 #pragma unroll
@@ -294,12 +338,9 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                     const float b0 = fmaf(-128.f * k0, qs[0], lv), b1 = fmaf(-128.f * k1, qs[1], lv);
                     const float a0 = k0 * 16777216.f, a1 = k1 * 16777216.f;
                     #pragma unroll
-                    for (int nt = 2 * b; nt < 2 * b + 2; ++nt) {
-                        x[nt][0] = fmaf(x[nt][0], a0, b0);
-                        x[nt][1] = fmaf(x[nt][1], a0, b0);
-                        x[nt][2] = fmaf(x[nt][2], a1, b1);
-                        x[nt][3] = fmaf(x[nt][3], a1, b1);
-                    }
+                    for (int nt = b * (XT / 2); nt < (b + 1) * (XT / 2); ++nt)
+                        #pragma unroll
+                        for (int k = 0; k < 4; ++k) x[nt][k] = row_of(k) ? fmaf(x[nt][k], a1, b1) : fmaf(x[nt][k], a0, b0);
                 }
                 const bool edge = key0 + WKEYS > cur.s.len || a.key_mask != nullptr ||
                                   (a.causal && key0 + WKEYS > cur.s.len - cur.s.n + 1);
@@ -307,11 +348,11 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                 if (edge) {
                     seen = 0;
                     #pragma unroll
-                    for (int nt = 0; nt < 4; ++nt)
+                    for (int nt = 0; nt < XT; ++nt)
                         #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const int key = key0 + nt * 8 + 2 * t + (k & 1);
-                            bool ok = key < lim[k >> 1];
+                            const int key = key0 + key_of(nt, k);
+                            bool ok = key < lim[row_of(k)];
                             if (ok && a.key_mask != nullptr)
                                 ok = __ldg(a.key_mask + (size_t)cur.b * a.mask_ld + key) != 0;
                             if (ok) seen |= 1u << (4 * nt + k);
@@ -319,13 +360,15 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                         }
                 }
                 // --- running maximum, moved only when it is passed by LAZY ---
-                float top0 = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1])),
-                                   fmaxf(fmaxf(x[2][0], x[2][1]), fmaxf(x[3][0], x[3][1])));
-                float top1 = fmaxf(fmaxf(fmaxf(x[0][2], x[0][3]), fmaxf(x[1][2], x[1][3])),
-                                   fmaxf(fmaxf(x[2][2], x[2][3]), fmaxf(x[3][2], x[3][3])));
+                float top0 = NEG_INF, top1 = NEG_INF;
+                #pragma unroll
+                for (int nt = 0; nt < XT; ++nt) {
+                    top0 = fmaxf(top0, fmaxf(x[nt][0], x[nt][NARROW ? 2 : 1]));
+                    top1 = fmaxf(top1, fmaxf(x[nt][NARROW ? 1 : 2], x[nt][3]));
+                }
                 if (__any_sync(0xffffffffu, top0 > m[0] + LAZY || top1 > m[1] + LAZY)) {
                     #pragma unroll
-                    for (int d = 1; d < 4; d <<= 1) {
+                    for (int d = NARROW ? 4 : 1; d < (NARROW ? 32 : 4); d <<= 1) {
                         top0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, d));
                         top1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, d));
                     }
@@ -334,35 +377,42 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                     m[0] = n0; m[1] = n1;
                     l[0] *= f0; l[1] *= f1;
                     #pragma unroll
-                    for (int j = 0; j < DN; ++j) { o[j][0] *= f0; o[j][1] *= f0; o[j][2] *= f1; o[j][3] *= f1; }
+                    for (int j = 0; j < OT; ++j)
+                        #pragma unroll
+                        for (int k = 0; k < 4; ++k) o[j][k] *= row_of(k) ? f1 : f0;
                 }
                 const float s0 = m[0] == NEG_INF ? 0.f : m[0] - HEAD, s1 = m[1] == NEG_INF ? 0.f : m[1] - HEAD;
                 #pragma unroll
-                for (int nt = 0; nt < 4; ++nt)
+                for (int nt = 0; nt < XT; ++nt)
                     #pragma unroll
-                    for (int k = 0; k < 4; ++k) x[nt][k] = ex2(x[nt][k] - (k < 2 ? s0 : s1));
+                    for (int k = 0; k < 4; ++k) x[nt][k] = ex2(x[nt][k] - (row_of(k) ? s1 : s0));
                 if (!edge) {
                     #pragma unroll
-                    for (int nt = 0; nt < 4; ++nt)
+                    for (int nt = 0; nt < XT; ++nt)
                         #pragma unroll
-                        for (int k = 0; k < 4; ++k) l[k >> 1] = fmaf(x[nt][k], iv[nt >> 1], l[k >> 1]);
+                        for (int k = 0; k < 4; ++k) l[row_of(k)] = fmaf(x[nt][k], iv[block_of(nt)], l[row_of(k)]);
                 } else {
                     // a masked weight is 0 whatever its block's scale is
                     #pragma unroll
-                    for (int nt = 0; nt < 4; ++nt)
+                    for (int nt = 0; nt < XT; ++nt)
                         #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            if (seen >> (4 * nt + k) & 1) l[k >> 1] = fmaf(x[nt][k], iv[nt >> 1], l[k >> 1]);
+                            if (seen >> (4 * nt + k) & 1) l[row_of(k)] = fmaf(x[nt][k], iv[block_of(nt)], l[row_of(k)]);
                 }
                 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    uint32_t p[4];
+                    uint32_t p[4];                           // NARROW: two registers, keys along a thread
                     #pragma unroll
-                    for (int nt = 0; nt < 2; ++nt) {
-                        const __half2 pa = __floats2half2_rn(x[2 * b + nt][0], x[2 * b + nt][1]);
-                        const __half2 pb = __floats2half2_rn(x[2 * b + nt][2], x[2 * b + nt][3]);
+                    for (int nt = 0; nt < XT / 2; ++nt) {
+                        const int xt = b * (XT / 2) + nt;
+                        const __half2 pa = __floats2half2_rn(x[xt][0], x[xt][1]);
+                        const __half2 pb = __floats2half2_rn(x[xt][2], x[xt][3]);
                         p[2 * nt] = *reinterpret_cast<const uint32_t*>(&pa);
                         p[2 * nt + 1] = *reinterpret_cast<const uint32_t*>(&pb);
+                    }
+                    if constexpr (NARROW) {
+                        p[0] = transposed(p[0]);
+                        p[1] = transposed(p[1]);
                     }
                     // --- values: keys 2t, 2t+1, 2t+8, 2t+9 of the block, columns DN g .. ---
                     const uint8_t* vst = stage + (WKEYS + 16 * b) * D;
@@ -383,15 +433,25 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                             const uint32_t k8w = w ? r[2].y : r[2].x, k9w = w ? r[3].y : r[3].x;
                             const uint32_t lo01 = prmt(k0w, k1w, 0x5140u), hi01 = prmt(k0w, k1w, 0x7362u);
                             const uint32_t lo89 = prmt(k8w, k9w, 0x5140u), hi89 = prmt(k8w, k9w, 0x7362u);
-                            const int j = 8 * c + 4 * w;
-                            mma_16816(o[j], p, codes_half2(prmt(lo01, 0x64646464u, 0x4140u)),
-                                      codes_half2(prmt(lo89, 0x64646464u, 0x4140u)));
-                            mma_16816(o[j + 1], p, codes_half2(prmt(lo01, 0x64646464u, 0x4342u)),
-                                      codes_half2(prmt(lo89, 0x64646464u, 0x4342u)));
-                            mma_16816(o[j + 2], p, codes_half2(prmt(hi01, 0x64646464u, 0x4140u)),
-                                      codes_half2(prmt(hi89, 0x64646464u, 0x4140u)));
-                            mma_16816(o[j + 3], p, codes_half2(prmt(hi01, 0x64646464u, 0x4342u)),
-                                      codes_half2(prmt(hi89, 0x64646464u, 0x4342u)));
+                            // two keys' codes of channels 4w .. 4w + 3 of the eight
+                            const uint32_t e[4] = {codes_half2(prmt(lo01, 0x64646464u, 0x4140u)),
+                                                   codes_half2(prmt(lo01, 0x64646464u, 0x4342u)),
+                                                   codes_half2(prmt(hi01, 0x64646464u, 0x4140u)),
+                                                   codes_half2(prmt(hi01, 0x64646464u, 0x4342u))};
+                            const uint32_t f[4] = {codes_half2(prmt(lo89, 0x64646464u, 0x4140u)),
+                                                   codes_half2(prmt(lo89, 0x64646464u, 0x4342u)),
+                                                   codes_half2(prmt(hi89, 0x64646464u, 0x4140u)),
+                                                   codes_half2(prmt(hi89, 0x64646464u, 0x4342u))};
+                            if constexpr (NARROW) {
+                                #pragma unroll
+                                for (int k = 0; k < 2; ++k) {
+                                    const uint32_t va[4] = {e[2 * k], e[2 * k + 1], f[2 * k], f[2 * k + 1]};
+                                    mma_16816(o[4 * c + 2 * w + k], va, p[0], p[1]);
+                                }
+                            } else {
+                                #pragma unroll
+                                for (int k = 0; k < 4; ++k) mma_16816(o[8 * c + 4 * w + k], p, e[k], f[k]);
+                            }
                         }
                     }
                 }
@@ -407,10 +467,12 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                 #pragma unroll
                 for (int k = 0; k < 2; ++k)
                     #pragma unroll
-                    for (int d = 1; d < 4; d <<= 1) l[k] += __shfl_xor_sync(0xffffffffu, l[k], d);
-                if (t == 0) {
-                    ml[warp * ROWS + g] = make_float2(m[0], l[0]);
-                    ml[warp * ROWS + g + 8] = make_float2(m[1], l[1]);
+                    for (int d = NARROW ? 4 : 1; d < (NARROW ? 32 : 4); d <<= 1) l[k] += __shfl_xor_sync(0xffffffffu, l[k], d);
+                const int own[2] = {NARROW ? 2 * t : g, NARROW ? 2 * t + 1 : g + 8};       // this thread's rows
+                const bool first_of_row = (NARROW ? g : t) == 0;
+                if (first_of_row) {
+                    ml[warp * ROWS + own[0]] = make_float2(m[0], l[0]);
+                    ml[warp * ROWS + own[1]] = make_float2(m[1], l[1]);
                 }
                 __syncthreads();
                 float mm[2], ll[2];
@@ -418,26 +480,33 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                 for (int k = 0; k < 2; ++k) {
                     float top = NEG_INF;
                     #pragma unroll
-                    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, ml[w * ROWS + g + 8 * k].x);
+                    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, ml[w * ROWS + own[k]].x);
                     float sum = 0.f;
                     #pragma unroll
                     for (int w = 0; w < WARPS; ++w) {
-                        const float2 v = ml[w * ROWS + g + 8 * k];
+                        const float2 v = ml[w * ROWS + own[k]];
                         if (v.x != NEG_INF || v.y != 0.f) sum += v.y * (v.x == top ? 1.f : ex2(v.x - top));
                     }
                     mm[k] = top; ll[k] = sum;
                     const float f = m[k] == top ? 1.f : ex2(m[k] - top);           // 0 for a warp that saw nothing
                     #pragma unroll
-                    for (int j = 0; j < DN; ++j) { o[j][2 * k] *= f; o[j][2 * k + 1] *= f; }
+                    for (int j = 0; j < OT; ++j) {
+                        o[j][NARROW ? k : 2 * k] *= f;
+                        o[j][NARROW ? 2 + k : 2 * k + 1] *= f;
+                    }
                 }
                 for (int w = 0; w < WARPS; ++w) {
                     if (warp == w) {
                         #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            float4* dst = reinterpret_cast<float4*>(buf + (g + 8 * (k >> 1)) * D + DN * (2 * t + (k & 1)));
+                        for (int k = 0; k < (NARROW ? 2 : 4); ++k) {
+                            float4* dst = reinterpret_cast<float4*>(
+                                buf + (NARROW ? own[k & 1] * D + DN * g : own[k >> 1] * D + DN * (2 * t + (k & 1))));
                             #pragma unroll
                             for (int j = 0; j < DN; j += 4) {
-                                float4 v = make_float4(o[j][k], o[j + 1][k], o[j + 2][k], o[j + 3][k]);
+                                float4 v;
+                                if constexpr (NARROW)
+                                    v = make_float4(o[j / 2][k], o[j / 2][2 + k], o[j / 2 + 1][k], o[j / 2 + 1][2 + k]);
+                                else v = make_float4(o[j][k], o[j + 1][k], o[j + 2][k], o[j + 3][k]);
                                 if (w > 0) {
                                     const float4 u = dst[j / 4];
                                     v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
@@ -448,14 +517,14 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                     }
                     __syncthreads();
                 }
-                if (warp == 0 && t == 0) {
-                    ml[g] = make_float2(mm[0], ll[0]);
-                    ml[g + 8] = make_float2(mm[1], ll[1]);
+                if (warp == 0 && first_of_row) {
+                    ml[own[0]] = make_float2(mm[0], ll[0]);
+                    ml[own[1]] = make_float2(mm[1], ll[1]);
                 }
                 __syncthreads();
                 const bool whole = seg_kt0 == 0 && cur.kt == cur.s.nt;
                 if (whole) {
-                    for (int e = tid; e < ROWS * (D / 8); e += THREADS) {
+                    for (int e = tid; e < HELD * (D / 8); e += THREADS) {
                         const int r = e / (D / 8), c = e % (D / 8);
                         const int rr = cur.rt * ROWS + r, i = rr / G, j = rr - i * G;
                         if (i >= cur.s.n) continue;
@@ -474,9 +543,9 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                     // slot 0: the run begins with (or inside) this unit; slot 1: it ends in it
                     const bool first = tau == cur.kt - seg_kt0;
                     float* dst = slots + ((size_t)blockIdx.x * 2 + (first ? 0 : 1)) * slot_floats(ROWS, D);
-                    for (int e = tid; e < ROWS * D / 4; e += THREADS)
+                    for (int e = tid; e < HELD * D / 4; e += THREADS)
                         reinterpret_cast<float4*>(dst)[e] = reinterpret_cast<const float4*>(buf)[e];
-                    if (tid < ROWS) reinterpret_cast<float2*>(dst + ROWS * D)[tid] = ml[tid];
+                    if (tid < HELD) reinterpret_cast<float2*>(dst + ROWS * D)[tid] = ml[tid];
                 }
                 __syncthreads();
                 if (left > 0) cur.next_unit(a, G);
@@ -487,24 +556,29 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
     cp_async_wait<0>();
 }
 
-template <typename T, int D>
-cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
+template <typename T, int D, bool NARROW>
+cudaError_t launch_rows(const KvAttnArgs& a, cudaStream_t s) {
     const int G = a.H / a.c.Hkv;
     static DeviceCache<int> ready;
     int dummy = 0;
     cudaError_t e = ready.get(&dummy, [](int, int* v) {
         *v = 1;
-        return cudaFuncSetAttribute(kv_attention_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        return cudaFuncSetAttribute(kv_attention_kernel<T, D, NARROW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                     AttnSmem<T, D>::BYTES);
     });
     if (e != cudaSuccess) return e;
     const int ctas = num_sms() * CTAS_PER_SM;
     long long* prefix = static_cast<long long*>(a.workspace);
     float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + prefix_bytes(a.B));
-    if ((e = launch_overlapped(kv_attention_kernel<T, D>, dim3(ctas), THREADS, AttnSmem<T, D>::BYTES, s, a, G, prefix,
+    if ((e = launch_overlapped(kv_attention_kernel<T, D, NARROW>, dim3(ctas), THREADS, AttnSmem<T, D>::BYTES, s, a, G, prefix,
                                slots)) != cudaSuccess || a.whole)
         return e;
     return launch_join<T, D, ROWS, TILE>(a, G, ctas, ROWS, prefix, slots, s);
+}
+
+template <typename T, int D>
+cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
+    return a.max_new * (a.H / a.c.Hkv) <= 8 ? launch_rows<T, D, true>(a, s) : launch_rows<T, D, false>(a, s);
 }
 
 }  // namespace
