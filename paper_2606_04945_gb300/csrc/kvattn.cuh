@@ -210,10 +210,10 @@ struct Cursor {
 // Counted in key tiles of the busiest CTA, cutting and joining cost 2 and, as
 // the joins are many, 4 for each unit a CTA; beyond 8 tiles the spread of the
 // lengths under their bound would weigh more. Measured, cut / whole, us: one
-// row of 28 heads on 4, 100 tokens 11.8 / 10.1, 256 tokens 12.0 / 11.3, 500
-// tokens 12.5 / 14.5 (cut); 64 such sequences, up to 300 tokens 24.5 / 17.7,
-// 1000 tokens 35.1 / 28.1; 32 rows of them, 8 sequences, 250 tokens 20.9 /
-// 18.6, 500 tokens 21.9 / 23.4 (cut); 32 sequences, 500 tokens 48 / 24.8.
+// row of 28 heads on 4, 100 tokens 7.8 / 6.2, 256 tokens 8.2 / 7.4, 500 tokens
+// 8.5 / 9.9 (cut); 64 such sequences, up to 300 tokens 14.8 / 11.1, 1000
+// tokens 21.5 / 19.7; 32 rows of them, 8 sequences, 250 tokens 20.9 / 18.6,
+// 500 tokens 21.9 / 23.4 (cut); 32 sequences, 500 tokens 48 / 24.8.
 inline bool whole_units(const KvAttnArgs& a, int rows, int tile, int ctas) {
     const long long t = std::max(1, (a.max_len + tile - 1) / tile);
     const long long n = ((long long)a.max_new * (a.H / a.c.Hkv) + rows - 1) / rows * a.B * a.c.Hkv;      // units
