@@ -44,7 +44,7 @@
 // thread's 16 bytes one row's 16 columns, so no transposition is needed.
 //
 // Measured (bf16, 28 heads on 4 of 128): one token for each of four sequences
-// of 131072 and fewer tokens (407 MB): 77.7 us, 5.2 TB/s, 3.9 us of it the
+// of 131072 and fewer tokens (407 MB): 74.2 us, 5.5 TB/s, 3.9 us of it the
 // join. Most instructions turn bytes into fragments. One sequence of 777
 // tokens takes 8.5 us, a chain of two launches and their loads.
 #include <algorithm>
@@ -60,8 +60,13 @@ constexpr int THREADS = WARPS * 32;
 constexpr int ROWS = 16;               // query rows of a unit
 constexpr int WKEYS = 32;              // keys of a warp in a tile: two 16-key blocks
 constexpr int TILE = WARPS * WKEYS;    // 128 keys
-constexpr int STAGES = 2;
-constexpr int CTAS_PER_SM = 3;
+// Tiles of a warp that are there or on their way, and CTAs an SM. Up to 8 rows
+// need fewer instructions a tile and wait for memory sooner: 74.3 us with 3
+// tiles and 2 CTAs for 77.3 with 2 and 3 (four sequences of 131072 tokens);
+// 40 rows over 4001 tokens the other way round, 19.2 for 20.3.
+constexpr int MOST_CTAS = 3;
+template <bool NARROW> constexpr int STAGES = NARROW ? 3 : 2;
+template <bool NARROW> constexpr int CTAS_PER_SM = NARROW ? 2 : MOST_CTAS;
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
 }
@@ -138,10 +143,10 @@ __device__ __forceinline__ float load_row(const T* row, int t, uint32_t (&q)[D /
     return down;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool NARROW>
 struct AttnSmem {
     static constexpr int STAGE = 2 * WKEYS * D + 16;            // bytes of a warp's stage: keys, values, the blocks' scales
-    static constexpr int RING = WARPS * STAGES * STAGE;
+    static constexpr int RING = WARPS * STAGES<NARROW> * STAGE;
     static constexpr int MERGE = ROWS * D * 4 + WARPS * ROWS * 8;
     static constexpr int QUERY = RING;                          // fragments [D / 16][32 lanes][4], until the merge
     static constexpr int BYTES = RING + MERGE;
@@ -154,9 +159,9 @@ struct AttnSmem {
 // above, against the 16-row form): four long sequences 77.7 us for 86.0, one
 // of 777 tokens 8.5 for 12.2, 64 of up to 1000 tokens 19.7 for 28.
 template <typename T, int D, bool NARROW>
-__global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(const KvAttnArgs a, int G, long long* prefix_out,
+__global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_kernel(const KvAttnArgs a, int G, long long* prefix_out,
                                                                  float* slots) {
-    using SM = AttnSmem<T, D>;
+    using SM = AttnSmem<T, D, NARROW>;
     constexpr int KH = D / 64;               // 64-channel halves of a key
     constexpr int DN = D / 8;                // value columns per thread, and column tiles
     constexpr int HELD = NARROW ? 8 : ROWS;  // rows that can be there
@@ -172,7 +177,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
     int left = cur.tiles(a, G, run);         // tiles of the run
     int pre_left = left;                     // tiles still to be fetched
 
-    const uint32_t ring = smem_addr(smem) + warp * (STAGES * SM::STAGE);
+    const uint32_t ring = smem_addr(smem) + warp * (STAGES<NARROW> * SM::STAGE);
     const int shift = __ffs(a.c.page) - 1;
     const size_t block_bytes = (size_t)a.c.page * D;
     // where this lane's 16-byte chunks of a 16-key block go
@@ -218,7 +223,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
         cp_async_commit();
     };
     #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) fetch(i);
+    for (int i = 0; i < STAGES<NARROW> - 1; ++i) fetch(i);
 
     uint4* const query = reinterpret_cast<uint4*>(smem + SM::QUERY) + lane;      // this lane's fragment of k step 0
     constexpr int OT = NARROW ? DN / 2 : DN; // tiles of the accumulators
@@ -281,12 +286,12 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                 fresh = false;
                 seg_kt0 = cur.kt;
             }
-            fetch((st + STAGES - 1) % STAGES);
-            cp_async_wait<STAGES - 1>();
+            fetch((st + STAGES<NARROW> - 1) % STAGES<NARROW>);
+            cp_async_wait<STAGES<NARROW> - 1>();
             __syncwarp();
             const int key0 = cur.kt * TILE + warp * WKEYS;
             if (key0 < cur.s.len) {
-                const uint8_t* stage = smem + warp * (STAGES * SM::STAGE) + st * SM::STAGE;
+                const uint8_t* stage = smem + warp * (STAGES<NARROW> * SM::STAGE) + st * SM::STAGE;
                 // --- scores of 32 keys: four column tiles, a k step for all of them ---
                 constexpr int XT = NARROW ? 2 : 4;           // tiles: NARROW 16 keys x 8 rows, else 16 rows x 8 keys
                 float x[XT][4];
@@ -457,7 +462,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
                 }
             }
             __syncwarp();
-            st = (st + 1) % STAGES;
+            st = (st + 1) % STAGES<NARROW>;
             --left;
             ++tau;
             if (++cur.kt == cur.s.nt || left == 0) {
@@ -557,21 +562,23 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) kv_attention_kernel(cons
 }
 
 template <typename T, int D, bool NARROW>
-cudaError_t launch_rows(const KvAttnArgs& a, cudaStream_t s) {
+cudaError_t launch_rows(const KvAttnArgs& args, cudaStream_t s) {
+    const int ctas = num_sms() * CTAS_PER_SM<NARROW>;
+    KvAttnArgs a = args;
+    a.whole = whole_units(a, ROWS, TILE, ctas);
     const int G = a.H / a.c.Hkv;
     static DeviceCache<int> ready;
     int dummy = 0;
     cudaError_t e = ready.get(&dummy, [](int, int* v) {
         *v = 1;
         return cudaFuncSetAttribute(kv_attention_kernel<T, D, NARROW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    AttnSmem<T, D>::BYTES);
+                                    AttnSmem<T, D, NARROW>::BYTES);
     });
     if (e != cudaSuccess) return e;
-    const int ctas = num_sms() * CTAS_PER_SM;
     long long* prefix = static_cast<long long*>(a.workspace);
     float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + prefix_bytes(a.B));
-    if ((e = launch_overlapped(kv_attention_kernel<T, D, NARROW>, dim3(ctas), THREADS, AttnSmem<T, D>::BYTES, s, a, G, prefix,
-                               slots)) != cudaSuccess || a.whole)
+    if ((e = launch_overlapped(kv_attention_kernel<T, D, NARROW>, dim3(ctas), THREADS, AttnSmem<T, D, NARROW>::BYTES, s,
+                               a, G, prefix, slots)) != cudaSuccess || a.whole)
         return e;
     return launch_join<T, D, ROWS, TILE>(a, G, ctas, ROWS, prefix, slots, s);
 }
@@ -602,15 +609,13 @@ static bool warp_kernel(const KvAttnArgs& a) {
 // Enough for either kernel, since max_len may change from call to call.
 size_t kv_attention_workspace_bytes(int B, int max_new, int H, int Hkv, int D) {
     const long long rows = (long long)max_new * (H / Hkv);
-    size_t slots = rows <= 4 * ROWS ? (size_t)num_sms() * CTAS_PER_SM * 2 * slot_floats(ROWS, D) * 4 : 0;
+    size_t slots = rows <= 4 * ROWS ? (size_t)num_sms() * MOST_CTAS * 2 * slot_floats(ROWS, D) * 4 : 0;
     if (rows > ROWS) slots = std::max(slots, kv_attention_tc_slot_bytes((int)(rows < 256 ? rows : 256), D));
     return prefix_bytes(B) + slots;
 }
 
-cudaError_t launch_kv_attention(const KvAttnArgs& args, cudaStream_t s) {
-    KvAttnArgs a = args;
+cudaError_t launch_kv_attention(const KvAttnArgs& a, cudaStream_t s) {
     if (!warp_kernel(a)) return launch_kv_attention_tc(a, s);
-    a.whole = whole_units(a, ROWS, TILE, num_sms() * CTAS_PER_SM);
     if (a.dtype == STARQ_BF16)
         return a.c.D == 64 ? launch_typed<__nv_bfloat16, 64>(a, s) : launch_typed<__nv_bfloat16, 128>(a, s);
     return a.c.D == 64 ? launch_typed<__half, 64>(a, s) : launch_typed<__half, 128>(a, s);
