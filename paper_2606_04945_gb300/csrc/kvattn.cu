@@ -291,6 +291,11 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
             __syncwarp();
             const int key0 = cur.kt * TILE + warp * WKEYS;
             if (key0 < cur.s.len) {
+                // one byte a lane, on its way beside the scores (a byte for each score took 59 us for 42 where 55
+                // sequences of 8 heads and up to 575 tokens have 64 rows)
+                uint8_t mask_byte = 1;
+                if (a.key_mask != nullptr && key0 + lane < cur.s.len)
+                    mask_byte = __ldg(a.key_mask + (size_t)cur.b * a.mask_ld + key0 + lane);
                 const uint8_t* stage = smem + warp * (STAGES<NARROW> * SM::STAGE) + st * SM::STAGE;
                 // --- scores of 32 keys: four column tiles, a k step for all of them ---
                 constexpr int XT = NARROW ? 2 : 4;           // tiles: NARROW 16 keys x 8 rows, else 16 rows x 8 keys
@@ -351,15 +356,14 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
                                   (a.causal && key0 + WKEYS > cur.s.len - cur.s.n + 1);
                 unsigned seen = 0xffff;      // bit 4 nt + k: x[nt][k] counts
                 if (edge) {
+                    const unsigned live = __ballot_sync(0xffffffffu, mask_byte != 0);       // bit i: key key0 + i
                     seen = 0;
                     #pragma unroll
                     for (int nt = 0; nt < XT; ++nt)
                         #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const int key = key0 + key_of(nt, k);
-                            bool ok = key < lim[row_of(k)];
-                            if (ok && a.key_mask != nullptr)
-                                ok = __ldg(a.key_mask + (size_t)cur.b * a.mask_ld + key) != 0;
+                            const bool ok = key < lim[row_of(k)] && (live >> key_of(nt, k) & 1);
                             if (ok) seen |= 1u << (4 * nt + k);
                             else x[nt][k] = NEG_INF;
                         }
@@ -595,7 +599,8 @@ cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
 // rows, but begins and ends slower. Up to 64 rows and a bounded number of
 // (16 rows) x (cached tokens) come here. Measured, this kernel against that
 // one, us, 16 sequences of 2 key/value heads: heads of 64, 40 rows, 4001
-// tokens 19 / 29, 16000 tokens 40 / 44; 64 rows, 4001 tokens 21 / 27; heads
+// tokens 19 / 29, 16000 tokens 40 / 44; 64 rows, 4001 tokens 21 / 27 (55
+// sequences of 8 heads, 575 tokens, a mask 42 / 35); heads
 // of 128, 24 rows, 2000 tokens 24 / 33; 64 rows, 2000 tokens 30 / 32; 128
 // rows, 500 tokens 27 / 24; 256 rows, 400 tokens 40 / 27; 49 rows of 8
 // sequences of 4 heads, 2000 tokens 31 / 29, 8000 tokens 64 / 41. max_len is
@@ -603,7 +608,7 @@ cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
 static bool warp_kernel(const KvAttnArgs& a) {
     const long long rows = (long long)a.max_new * (a.H / a.c.Hkv), tiles = (rows + ROWS - 1) / ROWS;
     if (tiles <= 1) return true;
-    return tiles <= 4 && tiles * a.B * a.c.Hkv * (long long)a.max_len <= (a.c.D == 64 ? 1 << 20 : 1 << 18);
+    return tiles <= 4 && tiles * a.B * a.c.Hkv * (long long)a.max_len <= (a.c.D == 64 ? 1 << 20 : 1 << 18) >> (tiles == 4);
 }
 
 // Enough for either kernel, since max_len may change from call to call.
