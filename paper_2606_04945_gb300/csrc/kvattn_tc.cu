@@ -57,6 +57,7 @@ constexpr int K_STAGES = 1, V_STAGES = 1, CK_STAGES = 3, CV_STAGES = 2;
 constexpr int INFOS = 4;                           // descriptions of tiles
 constexpr uint32_t TM_S = 0, TM_O = 256;           // TMEM columns: two score tiles, two accumulators
 constexpr int BLOCKS = TILE / 16;                  // 16-key blocks of a tile (each inside one page)
+constexpr float SMALLEST = 1.17549435e-38f;        // 2^-126
 
 struct TileInfo {                                  // what the other warps need of a key tile
     float4 blk[BLOCKS];                            // log2(e) scale s_k, log2 s_v, 1 / s_v
@@ -310,8 +311,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
             float4 d = make_float4(0.f, NEG_INF, 0.f, 0.f);
             if (any && page >= 0) {
                 const float vs = raw.sv < KV_SCALE_FLOOR ? KV_SCALE_FLOOR : raw.sv;
-                d = make_float4(fmaxf_nan(raw.sk, 1e-37f) * (a.scale * 1.4426950408889634f), __log2f(vs),
-                                __fdividef(1.f, vs), 0.f);
+                d = make_float4(raw.sk * (a.scale * 1.4426950408889634f), __log2f(vs), __fdividef(1.f, vs), 0.f);
             } else if (any) {
                 if (lane < BLOCKS) atomicOr(a.status, STATUS_RANGE);
                 d = make_float4(__uint_as_float(0x7fffffffu), 0.f, 1.f, 0.f);      // the rows that see it become NaN
@@ -672,7 +672,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                             #pragma unroll
                             for (int q = 0; q < 2; ++q) {
                                 const float4 b = ti.blk[2 * c + q];
-                                const float ax = b.x * down, cx = b.y - sub;
+                                // a factor that underflows (a zero row, a zero block, a tiny scale) times
+                                // the -inf of an unseen key would be NaN; at this floor no score counts
+                                const float ax = fmaxf_nan(b.x * down, SMALLEST), cx = b.y - sub;
                                 const bool any = decltype(all)::value || (met >> (2 * c + q) & 1);
                                 #pragma unroll
                                 for (int k = 0; k < 16; k += 4) {
