@@ -292,8 +292,14 @@ def sgat_linear_asym(X, mask, a_m, a_u, hb, d_sh, d_m, d_u, We, s_w, Y, workspac
                                 workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
-def _ws(n, device):
-    return torch.empty(int(n), dtype=torch.uint8, device=device)
+def _ws(n, device, stream=None):
+    """A workspace of n bytes out of the pool of the stream that uses it: when
+    the call returns it goes back there, where only later work of that stream
+    can take it."""
+    if stream is None:
+        return torch.empty(int(n), dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(int(n), dtype=torch.uint8, device=device)
 
 
 def sgat_quantize_act_dense(X, mask, a_m, a_u, Pt, d_sh, d_m, d_u, Xq, s_a, Xe=None, workspace=None, stream=None):
@@ -709,7 +715,8 @@ def kv_cache_attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, ma
     """Attention of the rows of Q [T][H D] (sequence b: rows seq_start[b] ..,
     at most max_new) over the kv_len[b] (at most max_len) cached tokens into
     Out [T][H D]; lse [T][H] receives the log-sum-exp. key_mask uint8
-    [B][>= max_len]: 0 = not seen. scale: default 1 / sqrt(D)."""
+    [B][>= max_len]: 0 = not seen. scale: default 1 / sqrt(D). workspace:
+    default of this call's own, on its stream."""
     shape, B, D, dtype = Q.shape, kv_len.shape[0], cache.D, Q.dtype
     T = shape[0]
     H = shape[1] // D
@@ -727,7 +734,7 @@ def kv_cache_attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, ma
             raise ValueError(f"starq expects key_mask rows of at least max_len = {max_len} bytes")
     if workspace is None:
         size = lib.kv_cache_attention_workspace_size(B, max_new, H, cache.Hkv, D)
-        workspace = torch.empty(size, dtype=_U8, device=Q.device)
+        workspace = _ws(size, Q.device, stream)
     else:
         size = workspace.numel() * workspace.element_size()
     _check(lib.kv_cache_attention(q, ldq, _CODES[dtype], T, _ints("seq_start", seq_start, B + 1), B, max_new, H,

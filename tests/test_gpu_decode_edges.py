@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from oracle import decode as od
-from tests.test_gpu_decode import Paged, attend, fill, randn
+from tests.test_gpu_decode import Paged, attend, check_attention, fill, i32, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -42,3 +42,40 @@ def test_causal_zero_rows(abi, dtype, page, D, H, Hkv, new, scale, masked):
     q[2::5, :D] = 0                                   # one head of a row
     mask = (rng.random((len(lens), max(lens))) < 0.6).astype(np.uint8) if masked else None
     attend(abi, rng, pg, count, lens, H, dtype, causal=True, mask=mask, scale=scale, q=q)
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_attention_on_another_stream(abi, monkeypatch, new):
+    """Without a workspace of the caller's: it comes from the pool of the
+    call's stream, and tensors that the current stream makes and fills right
+    behind the call do not touch it."""
+    rng = np.random.default_rng(new)
+    lens, H = [4000, 2001], 2
+    pg = Paged(abi, rng, 2, 4000, 1, 32, 64)
+    fill(pg, rng, lens)
+    q, _ = randn(rng, (2 * new, H * 64), torch.float16)
+    out, lse = torch.empty_like(q), torch.empty(2 * new, H, device="cuda")
+    lens32, start = i32(lens), i32([0, new, 2 * new])
+    where, real = [], abi.lib
+
+    class Library:
+        def __getattr__(self, name):
+            if name == "kv_cache_attention":
+                return lambda *args: where.append(args[-3]) or real.kv_cache_attention(*args)
+            return getattr(real, name)
+
+    monkeypatch.setattr(abi, "lib", Library())
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    size = abi.kv_cache_attention_workspace_size(2, new, H, 1, 64)
+    for _ in range(20):
+        abi.kv_cache_attention(q, pg.cache, pg.dev_table, lens32, start, out, max_new=new, max_len=4000, lse=lse,
+                               stream=side)
+        torch.empty(size, dtype=torch.uint8, device="cuda").fill_(255)
+    side.synchronize()
+    abi.check_status()
+    check_attention(pg, q, out, lse, [new, new], lens, H, torch.float16, 0.125, False, None)
+    pools = [(s["address"], s["address"] + s["total_size"], s["stream"]) for s in torch.cuda.memory_snapshot()]
+    assert len(where) == 20
+    for p in where:
+        assert [s for a, b, s in pools if a <= p < b] == [side.cuda_stream]
