@@ -307,7 +307,7 @@ def sgat_quantize_act_dense(X, mask, a_m, a_u, Pt, d_sh, d_m, d_u, Xq, s_a, Xe=N
     workspace (optional) holds the scaled rows and V = X^s P (float16)."""
     L, K = X.shape
     if workspace is None:
-        workspace = _ws(lib.sgat_dense_workspace_size(L, K), X.device)
+        workspace = _ws(lib.sgat_dense_workspace_size(L, K), X.device, stream)
     _contig(X, mask, a_m, a_u, Pt, Xq, s_a, Xe, workspace)
     _check(lib.sgat_quantize_act_dense(_p(X), dtype_code(X), L, K, _p(mask), _p(a_m), _p(a_u), _p(Pt), d_sh, d_m,
                                        d_u, _p(Xq), _p(s_a), _p(Xe), _p(workspace),
@@ -318,7 +318,7 @@ def sgat_quantize_act_dense(X, mask, a_m, a_u, Pt, d_sh, d_m, d_u, Xq, s_a, Xe=N
 def sgat_prepare_weight_dense(W, inv_a_w, Pt, Wq, s_w, workspace=None, stream=None):
     N, K = W.shape
     if workspace is None:
-        workspace = _ws(lib.sgat_dense_workspace_size(N, K), W.device)
+        workspace = _ws(lib.sgat_dense_workspace_size(N, K), W.device, stream)
     _contig(W, inv_a_w, Pt, Wq, s_w, workspace)
     _check(lib.sgat_prepare_weight_dense(_p(W), dtype_code(W), N, K, _p(inv_a_w), _p(Pt), _p(Wq), _p(s_w),
                                          _p(workspace), workspace.numel() * workspace.element_size(),
@@ -457,7 +457,7 @@ def tac_calibrate(Z_fp, Z_q, g, M, d, workspace=None, rho=3e-4, eps=1e-8, eta=0.
     N, C = Z_fp.shape
     assert Z_q.shape == Z_fp.shape and Z_q.dtype == Z_fp.dtype
     if workspace is None:
-        workspace = torch.empty(tac_calibrate_workspace_size(C, g), dtype=torch.uint8, device=Z_fp.device)
+        workspace = _ws(tac_calibrate_workspace_size(C, g), Z_fp.device, stream)
     _check(lib.tac_calibrate(_p(Z_fp), _p(Z_q), dtype_code(Z_fp), N, C, g, rho, eps, eta, alpha, _p(M), _p(d),
                              _p(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
 
@@ -479,7 +479,7 @@ def attention_pv_tac(Q, K, V, H, Mp, d, Z, workspace=None, dbg_codes=None, dbg_l
     Hkv = H if Hkv is None else Hkv
     _contig(Mp, d, Z, workspace, dbg_codes, dbg_l, dbg_acc)
     if workspace is None:
-        workspace = torch.empty(attention_pv_tac_workspace_size(L, Hkv), dtype=torch.uint8, device=Q.device)
+        workspace = _ws(attention_pv_tac_workspace_size(L, Hkv), Q.device, stream)
     _check(lib.attention_pv_tac_gqa(_p(Q), _p(K), _p(V), ld, L, H, Hkv, dtype_code(Q), _p(Mp), _p(d), _p(Z),
                                     _p(dbg_codes), _p(dbg_l), _p(dbg_acc), _p(workspace),
                                     workspace.numel() * workspace.element_size(), _stream(stream)))

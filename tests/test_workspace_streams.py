@@ -57,3 +57,17 @@ def test_cache_attention(taken, stream):
     abi.kv_cache_attention(half(3, 64), cache, i(0, 1)[None], i(3), i(0, 3), half(3, 64), max_new=3, max_len=3,
                            stream=stream)
     assert streams == [stream]
+
+
+@pytest.mark.parametrize("stream", [None, Side()])
+@pytest.mark.parametrize("call", ["sgat_quantize_act_dense", "sgat_prepare_weight_dense", "tac_calibrate",
+                                  "attention_pv_tac"])
+def test_quantised_calls(taken, call, stream):
+    abi, streams = taken
+    x, byte, f = half(4, 128), torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(4)
+    args = dict(sgat_quantize_act_dense=(x, None, f, f, x, 128, 0, 0, byte, f),
+                sgat_prepare_weight_dense=(x, f, x, byte, f),
+                tac_calibrate=(x, x, 64, torch.zeros(2, 64, 64), torch.zeros(2, 64)),
+                attention_pv_tac=(x, x, x, 1, byte, f, half(4, 128)))[call]
+    getattr(abi, call)(*args, stream=stream)
+    assert streams == [stream]
