@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from oracle import decode as od
-from tests.test_gpu_decode import Paged, attend, check_attention, fill, i32, randn
+from tests.test_gpu_decode import TINY, U, Paged, attend, check_attention, fill, i32, num, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -79,3 +79,33 @@ def test_attention_on_another_stream(abi, monkeypatch, new):
     assert len(where) == 20
     for p in where:
         assert [s for a, b, s in pools if a <= p < b] == [side.cuda_stream]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("L,N,K,group,bias", [
+    (12, 29201, 256, 32, True),          # CTAs of 16 warps (more than 8 rows, channels that fill the SMs)
+    (17, 29187, 1408, 128, False),
+    (32, 29230, 2560, 64, True),         # and more blocks than their shared memory has room for
+    (24, 37888, 3584, 64, False),
+    (32, 48, 18944, 64, False),          # CTAs of 8 warps, a slice in several chunks
+    (27, 130, 12288, 32, True)])
+def test_w4g_wide_and_deep(abi, dtype, L, N, K, group, bias):
+    """The forms of the linear that many channels or a long K lead to."""
+    rng = np.random.default_rng(L + N + K)
+    x, xn = randn(rng, (L, K + 8), dtype)
+    x, xn = x[:, :K], xn[:, :K]
+    codes = rng.integers(-8, 8, (N, K), dtype=np.int8)
+    packed = torch.from_numpy(((codes[:, 0::2] & 15) | ((codes[:, 1::2] & 15) << 4)).astype(np.uint8)).cuda()
+    scales = (np.exp(rng.standard_normal((N, K // group))) / 50).astype(np.float32)
+    b = rng.standard_normal(N).astype(np.float32) if bias else None
+    parts = [od.w4g_linear(xn, codes[n:n + 2048], scales[n:n + 2048], None if b is None else b[n:n + 2048])
+             for n in range(0, N, 2048)]
+    ref, size = (np.concatenate(p, axis=1) for p in zip(*parts))
+    for ydt in (dtype, torch.float32):
+        Y = torch.full((L, N + 3), 7.0, dtype=ydt, device="cuda")
+        abi.w4g_linear(x, packed, torch.from_numpy(scales).cuda(), Y[:, :N],
+                       bias=None if b is None else torch.from_numpy(b).cuda())
+        abi.check_status()
+        tol = (K / 8 + 16) * 2.0 ** -24 * size + U[ydt] * np.abs(ref) * 1.01 + TINY[ydt]
+        assert np.all(np.abs(num(Y)[:, :N] - ref) <= tol)
+        assert torch.all(Y[:, N:] == 7.0)
