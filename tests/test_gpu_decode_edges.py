@@ -109,3 +109,113 @@ def test_w4g_wide_and_deep(abi, dtype, L, N, K, group, bias):
         tol = (K / 8 + 16) * 2.0 ** -24 * size + U[ydt] * np.abs(ref) * 1.01 + TINY[ydt]
         assert np.all(np.abs(num(Y)[:, :N] - ref) <= tol)
         assert torch.all(Y[:, N:] == 7.0)
+
+
+# --------------------------------------------------------------------------
+# More than 64 rows of a key/value head: the tcgen05 kernel, whatever the
+# lengths are
+# --------------------------------------------------------------------------
+@pytest.mark.parametrize("which", ["k_scale", "v_scale"])
+@pytest.mark.parametrize("new", [40, 70])
+def test_tcgen05_not_finite(abi, which, new):
+    """A poisoned block makes the rows that see it NaN, and no others; a NaN
+    query its own row alone."""
+    rng = np.random.default_rng(new)
+    L, H = 96, 2
+    pg = Paged(abi, rng, 1, L, 1, 32, 64)
+    fill(pg, rng, [L])
+    q, _ = randn(rng, (new, H * 64), torch.float16)
+    out, lse = torch.empty_like(q), torch.empty(new, H, device="cuda")
+
+    def go(causal=False, mask=None):
+        abi.kv_cache_attention(q, pg.cache, pg.dev_table, i32([L]), i32([0, new]), out, max_new=new, max_len=L,
+                               causal=causal, key_mask=mask, lse=lse)
+        abi.check_status()
+
+    scale = getattr(pg.cache, which)
+    keep = scale.clone()
+    scale[pg.table[0, 1]] = float("nan")
+    go()
+    assert torch.isnan(out).all()
+    mask = np.ones((1, L), np.uint8)
+    mask[0, 32:64] = 0
+    for causal in (False, True):
+        go(causal, torch.from_numpy(mask).cuda())
+        check_attention(pg, q, out, lse, [new], [L], H, torch.float16, 0.125, causal, mask)
+    scale.copy_(keep)
+    scale[pg.table[0, 2]] = float("nan")              # slots 64 .. 95, which row i sees from 64 <= L - new + i on
+    go(True)
+    few = 64 - (L - new)
+    assert torch.isnan(out[few:]).all()
+    check_attention(pg, q[:few], out[:few], lse[:few], [few], [64], H, torch.float16, 0.125, True, None)
+    scale.copy_(keep)
+    q[0, 3] = float("nan")
+    go()
+    assert torch.isnan(out[0, :64]).all() and torch.isfinite(out[0, 64:]).all() and torch.isfinite(out[1:]).all()
+
+
+def test_tcgen05_outside_its_bounds(abi):
+    rng = np.random.default_rng(4)
+    new = 70
+    pg = Paged(abi, rng, 2, 64, 1, 16, 64)
+    fill(pg, rng, [64, 64])
+    q, _ = randn(rng, (2 * new, 64), torch.float16)
+    out, lse = torch.empty_like(q), torch.empty(2 * new, 1, device="cuda")
+    wrong = pg.dev_table.clone()
+    wrong[0, 2] = pg.pages
+    none = pg.dev_table.clone()
+    none[1, 0] = -1
+    fits = [0, new, 2 * new]
+    for table, lens, start, most in ((wrong, [64, 64], fits, 64), (none, [64, 64], fits, 64),
+                                     (pg.dev_table, [65, 64], fits, 64), (pg.dev_table, [64, -1], fits, 64),
+                                     (pg.dev_table, [64, 64], [0, new, 2 * new + 1], 64),
+                                     (pg.dev_table, [64, 64], [0, new, new - 1], 64),
+                                     (pg.dev_table, [80, 64], fits, 80), (pg.dev_table, [80, 64], fits, 1 << 19)):
+        abi.kv_cache_attention(q, pg.cache, table, i32(lens), i32(start), out, max_new=new, max_len=most)
+        with pytest.raises(abi.StarqError) as e:
+            abi.check_status()
+        assert e.value.code == abi.ERR_RANGE
+    abi.kv_cache_attention(q, pg.cache, pg.dev_table, i32([64, 64]), i32(fits), out, max_new=new, max_len=64, lse=lse)
+    abi.check_status()
+    check_attention(pg, q, out, lse, [new, new], [64, 64], 1, torch.float16, 0.125, False, None)
+
+
+def test_tcgen05_far_pages(abi):
+    """Pages whose byte offsets pass 32 bits."""
+    page, D, Hkv, L, new = 128, 128, 2, 300, 80
+    pages = (1 << 32) // (page * D * Hkv) + 9
+    K, V = (torch.empty(pages, Hkv, page, D, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.full((pages, Hkv), float("nan"), device="cuda") for _ in range(2))
+    cache = abi.KVCache(K, V, ks, vs)
+    rng = np.random.default_rng(8)
+    near = Paged(abi, rng, 1, L, Hkv, page, D)        # the same rows in a small cache, for the oracle
+    fill(near, rng, [L])
+    far = [pages - 1, 3, pages - 5]
+    for big, small in ((K, near.cache.K), (V, near.cache.V), (ks, near.cache.k_scale), (vs, near.cache.v_scale)):
+        big[far] = small[near.table[0].tolist()]
+    q, _ = randn(rng, (new, Hkv * D), torch.float16)
+    out, lse = torch.empty_like(q), torch.empty(new, Hkv, device="cuda")
+    for causal in (False, True):
+        abi.kv_cache_attention(q, cache, i32(far)[None], i32([L]), i32([0, new]), out, max_new=new, max_len=L,
+                               causal=causal, lse=lse)
+        abi.check_status()
+        check_attention(near, q, out, lse, [new], [L], Hkv, torch.float16, D ** -0.5, causal, None)
+
+
+@pytest.mark.parametrize("bound", [0, 1 << 19])
+@pytest.mark.parametrize("causal", [False, True])
+def test_tcgen05_many_sequences(abi, bound, causal):
+    """More sequences than threads of a CTA, dealt out whole and cut."""
+    B, new = 1100, 70
+    rng = np.random.default_rng(B)
+    lens = [int(v) for v in rng.integers(0, 70, B)]
+    count = [0 if b % 7 == 3 else new if b % 5 == 0 else int(rng.integers(0, 9)) for b in range(B)]
+    count[-1] = new
+    pg = Paged(abi, rng, B, 70, 1, 16, 64)
+    fill(pg, rng, lens)
+    q, _ = randn(rng, (sum(count), 64), torch.float16)
+    out, lse = torch.full_like(q, 7.0), torch.full((sum(count), 1), 7.0, device="cuda")
+    abi.kv_cache_attention(q, pg.cache, pg.dev_table, i32(lens), i32(np.concatenate([[0], np.cumsum(count)])), out,
+                           max_new=new, max_len=70 + bound, causal=causal, lse=lse)
+    abi.check_status()
+    check_attention(pg, q, out, lse, count, lens, 1, torch.float16, 0.125, causal, None)
