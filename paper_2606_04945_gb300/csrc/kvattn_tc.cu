@@ -623,9 +623,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                             tmem_ld_32x32b_x32(t_s + 32 * c, x);
                             tmem_arrived(x);
                             const int see = lim - ti.key0 - 32 * c;
+                            uint32_t live[4];                                   // bit k / 4 of word k % 4: key 32 c + k
+                            #pragma unroll
+                            for (int j = 0; j < 4; ++j) live[j] = ti.seen[j] >> (8 * c);
                             #pragma unroll
                             for (int k = 0; k < 32; ++k)
-                                if (k >= see || ti.inv[32 * c + k] == 0.f) x[k] = 0xff800000u;
+                                if (k >= see || !(live[k & 3] >> (k >> 2) & 1)) x[k] = 0xff800000u;
                             #pragma unroll
                             for (int q = 0; q < 2; ++q) {                       // for the second pass
                                 uint32_t y[16];

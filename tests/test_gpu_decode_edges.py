@@ -219,3 +219,24 @@ def test_tcgen05_many_sequences(abi, bound, causal):
                            max_new=new, max_len=70 + bound, causal=causal, lse=lse)
     abi.check_status()
     check_attention(pg, q, out, lse, count, lens, 1, torch.float16, 0.125, causal, None)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("new", [2, 70])
+def test_infinite_value_scale(abi, causal, new):
+    """A block whose value scale is infinite shows in every row that sees it,
+    and in no other."""
+    rng = np.random.default_rng(new)
+    L = 96
+    pg = Paged(abi, rng, 1, L, 1, 32, 64)
+    fill(pg, rng, [L])
+    pg.cache.v_scale[pg.table[0, 2]] = float("inf")   # slots 64 .. 95
+    q, _ = randn(rng, (new, 64), torch.float16)
+    out, lse = torch.empty_like(q), torch.empty(new, 1, device="cuda")
+    abi.kv_cache_attention(q, pg.cache, pg.dev_table, i32([L]), i32([0, new]), out, max_new=new, max_len=L,
+                           causal=causal, lse=lse)
+    abi.check_status()
+    few = max(0, 64 - (L - new)) if causal else 0     # rows before slot 64
+    assert not torch.isfinite(out[few:]).any()
+    if few:
+        check_attention(pg, q[:few], out[:few], lse[:few], [few], [64], 1, torch.float16, 0.125, True, None)
