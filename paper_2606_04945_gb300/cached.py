@@ -126,6 +126,8 @@ class CachedStack:
         sees what each operator read and wrote (for tests)."""
         c = self.cfg
         n = tok.shape[1]
+        if self.held + n > c.capacity:
+            raise ValueError(f"{self.held} cached and {n} new positions are more than the cache's {c.capacity} tokens")
         b = self._buffers(n)
         hk = hook or (lambda layer, name, values: None)
         kq, kv = c.heads * c.dim, c.kv_heads * c.dim
@@ -175,7 +177,8 @@ class CachedStack:
     def capture(self):
         """Records a pass over a block in a CUDA graph; returns (graph, token
         buffer [batch][block], logits). It reads `past` where it is, so one
-        graph serves every block."""
+        graph serves every block. (The recording itself is a pass over masked
+        positions behind the prefix, which has to leave them room.)"""
         c = self.cfg
         tok = torch.full((c.batch, c.block), self.mask_id, dtype=torch.long, device=self.device)
         side = torch.cuda.Stream()
