@@ -6,13 +6,13 @@
 // log-sum-exp of -inf.
 //
 // Arithmetic. The codes c, e are integers of magnitude <= 127, exact in
-// fp16, so both products run on the 16-bit MMA with float32 accumulators. The
-// keys enter as their bytes u = c + 128: widened to 16 bits a byte reads, as
-// an fp16 subnormal, u 2^-24, and the offset leaves through linearity,
-// sum q c = sum q u - 128 sum q (once a row; it is a few times the codes' size
-// and costs two of float32's 24 bits of the score). The values' codes are
-// made exactly: a channel of which the heavy keys' codes are 0 would show
-// the offset's rounding.
+// fp16, so both products run on the 16-bit MMA with float32 accumulators.
+// (Keys as their bytes c + 128, with the offset taken off the score by
+// linearity, save a subtraction for every two codes: 75.0 us for 75.6 over
+// four sequences of 131072 tokens, 56.5 for 58.2 with heads of 64. But where
+// a few loud channels set a block's scale the other codes are a few units,
+// and the offset's rounding is up to 2^-14 of the score. Of the values, a
+// channel in which the heavy keys' codes are 0 would show it.)
 // A bf16 query row is scaled by a power of two into fp16's range: its eight
 // significand bits fit, so only values below 2^-28 of the row's largest
 // lose bits. s_k and the softmax scale multiply the float32 score. s_v
@@ -92,9 +92,9 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     return y;
 }
 
-// Bytes 0 and 1 (2 and 3) of a word as the halves of a register.
-__device__ __forceinline__ uint32_t widen_lo(uint32_t w) { return prmt(w, 0u, 0x4140u); }
-__device__ __forceinline__ uint32_t widen_hi(uint32_t w) { return prmt(w, 0u, 0x4342u); }
+// The codes of bytes 0 and 1 (2 and 3) of a word.
+__device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return codes_half2(prmt(w, 0x64646464u, 0x4140u)); }
+__device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return codes_half2(prmt(w, 0x64646464u, 0x4342u)); }
 
 // Byte offset of 16-byte chunk c of row r (of 16) in a warp's stage.
 template <int D> __device__ __forceinline__ uint32_t stage_offset(int r, int c) {
@@ -103,10 +103,10 @@ template <int D> __device__ __forceinline__ uint32_t stage_offset(int r, int c) 
 }
 
 // Fragments of one query row (half of the A operand's registers): channels
-// 64 h + 16 t + 4 s + {0, 1} in q[h][s][0], {2, 3} in q[h][s][1], the row's
-// sum, and the power of two that undoes the row's scaling.
+// 64 h + 16 t + 4 s + {0, 1} in q[h][s][0], {2, 3} in q[h][s][1]; returns the
+// power of two that undoes the row's scaling.
 template <typename T, int D>
-__device__ __forceinline__ float load_row(const T* row, int t, uint32_t (&q)[D / 64][4][2], float& sum) {
+__device__ __forceinline__ float load_row(const T* row, int t, uint32_t (&q)[D / 64][4][2]) {
     float v[D / 64][16], top = 0.f;
     #pragma unroll
     for (int h = 0; h < D / 64; ++h) {
@@ -121,7 +121,6 @@ __device__ __forceinline__ float load_row(const T* row, int t, uint32_t (&q)[D /
         }
     }
     float up = 1.f, down = 1.f;
-    sum = 0.f;
     if (std::is_same<T, __nv_bfloat16>::value) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
@@ -135,11 +134,7 @@ __device__ __forceinline__ float load_row(const T* row, int t, uint32_t (&q)[D /
             for (int k = 0; k < 2; ++k) {
                 const __half2 p = __floats2half2_rn(v[h][4 * s + 2 * k] * up, v[h][4 * s + 2 * k + 1] * up);
                 q[h][s][k] = *reinterpret_cast<const uint32_t*>(&p);
-                const float2 back = __half22float2(p);
-                sum += back.x + back.y;
             }
-    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
     return down;
 }
 
@@ -228,7 +223,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
     uint4* const query = reinterpret_cast<uint4*>(smem + SM::QUERY) + lane;      // this lane's fragment of k step 0
     constexpr int OT = NARROW ? DN / 2 : DN; // tiles of the accumulators
     uint32_t qb[NARROW ? KH : 1][4][2];      // NARROW: the query fragments
-    float o[OT][4], m[2], l[2], rs[2], qs[2];
+    float o[OT][4], m[2], l[2], rs[2];
     int lim[2];                              // keys [0, lim) are visible to the rows (causal limit and length)
     const float unit_scale = a.scale * 1.4426950408889634f;
     bool fresh = true;
@@ -251,7 +246,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
                               (size_t)(cur.h * G + j) * D;
                         lim[k] = a.causal ? max(0, cur.s.len - cur.s.n + i + 1) : cur.s.len;
                     }
-                    rs[k] = load_row<T, D>(row, t, q2[k], qs[k]);
+                    rs[k] = load_row<T, D>(row, t, q2[k]);
                 }
                 m[0] = m[1] = NEG_INF;
                 l[0] = l[1] = 0.f;
@@ -260,12 +255,11 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
                     for (int h = 0; h < KH; ++h)
                         #pragma unroll
                         for (int s = 0; s < 4; ++s) { qb[h][s][0] = q2[0][h][s][0]; qb[h][s][1] = q2[0][h][s][1]; }
-                    const float r = rs[0], q = qs[0];
+                    const float r = rs[0];
                     const int v = lim[0];
                     #pragma unroll
                     for (int k = 0; k < 2; ++k) {           // from the threads of row g = 2t + k
                         rs[k] = __shfl_sync(0xffffffffu, r, 4 * (2 * t + k));
-                        qs[k] = __shfl_sync(0xffffffffu, q, 4 * (2 * t + k));
                         lim[k] = __shfl_sync(0xffffffffu, v, 4 * (2 * t + k));
                     }
                 } else {
@@ -317,14 +311,14 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
                             #pragma unroll
                             for (int b = 0; b < 2; ++b) {
                                 const uint32_t u = word(2 * b), v = word(2 * b + 1);
-                                const uint32_t ka[4] = {widen_lo(u), widen_lo(v), widen_hi(u), widen_hi(v)};
+                                const uint32_t ka[4] = {codes_lo(u), codes_lo(v), codes_hi(u), codes_hi(v)};
                                 mma_16816(x[b], ka, qb[h][s][0], qb[h][s][1]);
                             }
                         } else {
                             const uint4 q = query[(4 * h + s) * 32];
                             const uint32_t qa[4] = {q.x, q.y, q.z, q.w};
                             #pragma unroll
-                            for (int nt = 0; nt < 4; ++nt) mma_16816(x[nt], qa, widen_lo(word(nt)), widen_hi(word(nt)));
+                            for (int nt = 0; nt < 4; ++nt) mma_16816(x[nt], qa, codes_lo(word(nt)), codes_hi(word(nt)));
                         }
                     }
                 }
@@ -343,14 +337,11 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
                     const float vs = sv < KV_SCALE_FLOOR ? KV_SCALE_FLOOR : sv;
                     const float lv = __log2f(vs);
                     iv[b] = __fdividef(1.f, vs);
-                    // x = log2(e) scale s_k (2^24 sum q u 2^-24 - 128 sum q) + log2 s_v
                     const float k0 = ks * rs[0], k1 = ks * rs[1];
-                    const float b0 = fmaf(-128.f * k0, qs[0], lv), b1 = fmaf(-128.f * k1, qs[1], lv);
-                    const float a0 = k0 * 16777216.f, a1 = k1 * 16777216.f;
                     #pragma unroll
                     for (int nt = b * (XT / 2); nt < (b + 1) * (XT / 2); ++nt)
                         #pragma unroll
-                        for (int k = 0; k < 4; ++k) x[nt][k] = row_of(k) ? fmaf(x[nt][k], a1, b1) : fmaf(x[nt][k], a0, b0);
+                        for (int k = 0; k < 4; ++k) x[nt][k] = fmaf(x[nt][k], row_of(k) ? k1 : k0, lv);
                 }
                 const bool edge = key0 + WKEYS > cur.s.len || a.key_mask != nullptr ||
                                   (a.causal && key0 + WKEYS > cur.s.len - cur.s.n + 1);

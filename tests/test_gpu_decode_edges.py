@@ -240,3 +240,27 @@ def test_infinite_value_scale(abi, causal, new):
     assert not torch.isfinite(out[few:]).any()
     if few:
         check_attention(pg, q[:few], out[:few], lse[:few], [few], [64], 1, torch.float16, 0.125, True, None)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("D,H,Hkv,new", [(128, 7, 1, 1), (64, 8, 4, 2), (128, 4, 2, 7), (64, 6, 2, 5), (128, 2, 1, 19),
+                                         (64, 8, 1, 9)])
+@pytest.mark.parametrize("loud", [1, 4])
+def test_attention_loud_channels(abi, dtype, D, H, Hkv, new, loud):
+    """A few channels set the scale of a block of keys and the others have
+    codes of a few units, and the queries have a mean: the bits of a score are
+    those of sum q c, not of the largest codes."""
+    rng = np.random.default_rng(new + D + loud)
+    lens = [300, 77]
+    pg = Paged(abi, rng, 2, 300, Hkv, 32, D)
+    fill(pg, rng, lens)
+    pg.k[:] = np.clip(np.rint(rng.standard_normal(pg.k.shape) * 2), -127, 127)
+    at = rng.permutation(D)[:loud]
+    pg.k[..., at] = rng.choice([-127, 127], pg.k[..., at].shape)
+    pg.ks[:] = 0.5
+    pg.cache.K.copy_(torch.from_numpy((pg.k + 128).astype(np.uint8)))
+    pg.cache.k_scale.copy_(torch.from_numpy(pg.ks))
+    x = rng.standard_normal((2 * new, H, D)) + 2
+    x[..., at] = rng.standard_normal(x[..., at].shape) / 32
+    q = torch.from_numpy(x.reshape(2 * new, H * D)).to(dtype).cuda()
+    attend(abi, rng, pg, [new, new], lens, H, dtype, q=q, causal=new > 5)
