@@ -219,7 +219,7 @@ class CachedStack:
                 graph.replay()
             self.keep(c.block)
             out.append(tok.clone())
-        return torch.cat(out, 1)
+        return torch.cat(out, 1) if out else tok[:, :0].clone()
 
 
 def main():
