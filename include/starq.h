@@ -884,7 +884,9 @@ int kv_cache_read(const starq_kv_cache* cache, const int32_t* page_table, int ta
  *   workspace: kv_cache_attention_workspace_size bytes, 256-byte aligned;
  *        its contents do not matter.
  * Products on 16-bit tensor cores with float32 sums; the softmax weights
- * are rounded to fp16 once before they meet the values.
+ * are rounded to fp16 once before they meet the values. A key whose weight
+ * times value scale lies 2^-125 below the row's largest counts as 0, in the
+ * sums as well: of scales 2^125 apart in one sequence only the large count.
  */
 size_t kv_cache_attention_workspace_size(int B, int max_new, int H, int Hkv, int D);
 int kv_cache_attention(const void* Q, int ldq, int dtype, int T, const int32_t* seq_start, int B, int max_new, int H,
@@ -904,7 +906,8 @@ int kv_cache_attention(const void* Q, int ldq, int dtype, int T, const int32_t* 
  *   hb = 1 gives exactly these codes and scales.
  * Float32 accumulation of exact products (a bf16 activation 2^-29 below the
  * largest of its 128-channel block loses its last bits); a group's sum is
- * scaled after it is complete. Infinities and NaN come out as in the formula.
+ * scaled after it is complete. Infinities and NaN come out as in the formula;
+ * results below 2^-102 lose bits.
  * Shapes: 0 <= L <= 32, N >= 1, group 32, 64 or 128, K >= group with
  * K % group == 0; ldx >= K, rows of X 16-byte aligned.
  */

@@ -181,7 +181,8 @@ def _contig(*ts):
 
 
 def check_status(stream=None):
-    """Synchronise and raise if a kernel gave up a bounded wait."""
+    """Synchronise and raise if a kernel gave up a bounded wait or met an
+    index outside its array."""
     _check(lib.starq_check_status(_stream(stream)))
 
 

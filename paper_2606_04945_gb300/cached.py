@@ -25,7 +25,10 @@ torch holds the buffers, multiplies silu(g) u and picks the tokens.
 
 `python -m paper_2606_04945_gb300.cached` generates and prints the time of a
 step. A linear takes at most 32 rows a call: a prompt goes through it in
-slices, so a long prompt is not this module's strength.
+slices, so a long prompt is not this module's strength. Attention is given
+the capacity as the bound of the lengths, since one recorded pass serves every
+block: with up to 64 rows of a key/value head a short prefix in a large cache
+takes the kernel for long ones.
 """
 
 from dataclasses import dataclass

@@ -23,7 +23,11 @@
 // only weights 2^-32 below the row's largest, which is at least 2^7; the sum
 // of the plain weights is sum_j P_ij / s_v(j) in float32 from the unrounded
 // P. m_i is a running maximum that moves only when a score passes it by 8
-// (2^8 of headroom), so most tiles do not rescale the accumulators.
+// (2^8 of headroom), so most tiles do not rescale the accumulators. Below
+// 2^-126 of that scale, i.e. p_ij s_v(j) some 2^-125 below the row's largest,
+// a key drops out of the sum too: in blocks of values that are all 0 (s_v at
+// its floor) weights of 2^-24 of the largest still count beside blocks of
+// values up to 6 10^4, fp16's range.
 //
 // Work. For one query token the cache is read once and the rest is small:
 // bound by memory. The G query heads of a key/value head and the new tokens
@@ -36,15 +40,16 @@
 // a second kernel joins them in run order (results do not depend on timing).
 //
 // In a CTA each of four warps owns 32 keys of a tile (two blocks) and a
-// private pair of cp.async stages, so warps meet only at the ends of a unit;
-// the query fragments, alike for all, are in shared memory. 16-byte chunks
+// private ring of cp.async stages (three with up to 8 rows, else two), so
+// warps meet only at the ends of a unit; the query fragments, alike for all,
+// are in shared memory (with up to 8 rows in registers). 16-byte chunks
 // are XOR-swizzled by row so that both fragments read without bank
 // conflicts. The MMA's k order is free: a key's fragment takes 4 consecutive
 // channels per thread, and value columns are taken in the order that makes a
 // thread's 16 bytes one row's 16 columns, so no transposition is needed.
 //
 // Measured (bf16, 28 heads on 4 of 128): one token for each of four sequences
-// of 131072 and fewer tokens (407 MB): 74.2 us, 5.5 TB/s, 3.9 us of it the
+// of 131072 and fewer tokens (407 MB): 76.2 us, 5.3 TB/s, 3.6 us of it the
 // join. Most instructions turn bytes into fragments. One sequence of 777
 // tokens takes 8.5 us, a chain of two launches and their loads.
 #include <algorithm>
@@ -63,7 +68,8 @@ constexpr int TILE = WARPS * WKEYS;    // 128 keys
 // Tiles of a warp that are there or on their way, and CTAs an SM. Up to 8 rows
 // need fewer instructions a tile and wait for memory sooner: 74.3 us with 3
 // tiles and 2 CTAs for 77.3 with 2 and 3 (four sequences of 131072 tokens);
-// 40 rows over 4001 tokens the other way round, 19.2 for 20.3.
+// 40 rows over 4001 tokens the other way round, 19.2 for 20.3. (Both with
+// the keys' offset taken off the scores.)
 constexpr int MOST_CTAS = 3;
 template <bool NARROW> constexpr int STAGES = NARROW ? 3 : 2;
 template <bool NARROW> constexpr int CTAS_PER_SM = NARROW ? 2 : MOST_CTAS;
@@ -151,8 +157,9 @@ struct AttnSmem {
 // query rows its 8 columns (scores^T = K Q^T, out^T = V^T P^T): half the MMAs
 // and half the exponentials, none of them for rows that do not exist. A
 // thread has the columns (rows of the unit) 2t and 2t + 1. Measured (7 rows, as
-// above, against the 16-row form): four long sequences 77.7 us for 86.0, one
-// of 777 tokens 8.5 for 12.2, 64 of up to 1000 tokens 19.7 for 28.
+// above, both forms with the keys' offset and two stages): four long sequences
+// 77.7 us for 86.0, one of 777 tokens 8.5 for 12.2, 64 of up to 1000 tokens
+// 19.7 for 28.
 template <typename T, int D, bool NARROW>
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_kernel(const KvAttnArgs a, int G, long long* prefix_out,
                                                                  float* slots) {
@@ -588,14 +595,21 @@ cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
 // Which kernel. This one reads a unit's keys once for every 16 rows; the
 // tcgen05 kernel reads them once, at up to three times the speed with many
 // rows, but begins and ends slower. Up to 64 rows and a bounded number of
-// (16 rows) x (cached tokens) come here. Measured, this kernel against that
-// one, us, 16 sequences of 2 key/value heads: heads of 64, 40 rows, 4001
-// tokens 19 / 29, 16000 tokens 40 / 44; 64 rows, 4001 tokens 21 / 27 (55
-// sequences of 8 heads, 575 tokens, a mask 42 / 35); heads
-// of 128, 24 rows, 2000 tokens 24 / 33; 64 rows, 2000 tokens 30 / 32; 128
-// rows, 500 tokens 27 / 24; 256 rows, 400 tokens 40 / 27; 49 rows of 8
-// sequences of 4 heads, 2000 tokens 31 / 29, 8000 tokens 64 / 41. max_len is
-// the bound that the host knows: a generous one leads to the other kernel.
+// (16 rows) x (cached tokens) come here, half as many with four times 16 rows,
+// whose keys are converted most often. max_len is the bound that the host
+// knows: a generous one leads to the other kernel. Measured, this kernel / that
+// one, us (bf16, 8 query heads on a key/value head, causal; units = sequences x
+// key/value heads; a key mask changes either by less than a tenth):
+//   heads of 64, 24 rows: 64 units of 4000 tokens 20 / 27, 16000 tokens 50 / 58;
+//     40 rows: 32 units of 8000 tokens 25 / 27, 64 of 16000 66 / 59; 64 rows:
+//     32 units of 4000 tokens 21 / 23, 8000 tokens 30 / 27, 440 of 300 32 / 31
+//   heads of 128, 24 rows: 32 units of 4000 tokens 28 / 31, 64 of 16000 79 / 77;
+//     40 rows: 32 units of 2000 tokens 26 / 28, 4000 tokens 32 / 31, 64 of 2000
+//     35 / 32; 64 rows: 32 units of 1000 tokens 24 / 27, 2000 tokens 29 / 28,
+//     64 of 600 22 / 20, 2 of 8000 (this one) 21 / 17
+// Where it errs: up to 32 rows of hundreds of units (440 of 2000 tokens, 24
+// rows: 53 / 84 with heads of 64, 92 / 119 with heads of 128) go to the slower
+// kernel, and 64 rows of 64 units of 1000 tokens with heads of 128 (27 / 29).
 static bool warp_kernel(const KvAttnArgs& a) {
     const long long rows = (long long)a.max_new * (a.H / a.c.Hkv), tiles = (rows + ROWS - 1) / ROWS;
     if (tiles <= 1) return true;

@@ -29,8 +29,8 @@
 // of -inf. Only the causal boundary is tested score by score.
 //
 // Measured (bf16, 28 heads on 4 of 128, 32 positions for each of 8 sequences
-// of 16384 and fewer tokens, a key mask; 39 GFLOP, 92 MB): 68.9 us, 570
-// TFLOP/s, 7 us of it the join; the warp-level MMA took 444 us. In clocks of a
+// of 16384 and fewer tokens, a key mask; 39 GFLOP, 92 MB): 68.1 us, 577
+// TFLOP/s, 7.6 us of it the join; the warp-level MMA took 444 us. In clocks of a
 // CTA: cutting 4.5 thousand, the queries' rows 10 (beside the first codes), a
 // tile's step 4.5 (a stream waits 1.8 for weights - values - next scores,
 // takes the maximum in 0.7 and the weights in 1.9; the products need 2.0 of
