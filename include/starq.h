@@ -914,6 +914,68 @@ int kv_cache_attention(const void* Q, int ldq, int dtype, int T, const int32_t* 
 int w4g_linear(const void* X, int ldx, int dtype, int L, int K, const uint8_t* Wq, const float* scales, int group,
                int N, const float* bias, void* Y, int ldy, int y_dtype, void* stream);
 
+/*
+ * Rules on the logits of new tokens. Rows of logits are packed like the rows
+ * of cached decoding: sequence b owns rows seq_start[b] .. seq_start[b + 1]
+ * - 1 of T, at most max_new; rows that no sequence owns are not touched. A
+ * row has V tokens. All rules are optional (NULL):
+ *   params         [B][4] float32: temperature t, repetition factor r,
+ *                  presence p and frequency f penalty; NULL = 1, 1, 0, 0.
+ *                  t and r within 1e-30 .. 1e30; one outside is reported as
+ *                  STARQ_ERR_RANGE and counts as 1.
+ *   history        [B][history_ld] int32, the first history_len[b] tokens of
+ *                  a row were written before: c is how often v is one of them
+ *   bias_ids, bias_values  [B][bias_ld] int32 and float32, bias_len[b]
+ *                  entries; of several entries of a token the last counts
+ *   allowed        [B][allowed_ld] 32-bit words, or [T][allowed_ld] with
+ *                  allowed_by_row != 0: bit v % 32 of word v / 32 is 1 where
+ *                  token v may be taken; allowed_ld >= ceil(V / 32)
+ * A token outside 0 .. V - 1 in a history or a list is skipped and reported
+ * as STARQ_ERR_RANGE, and so is a length outside 0 .. ld (taken as 0). With
+ * x the logit as float32 and every step rounded to float32:
+ *   z = c == 0 ? x : (x > 0 ? x / r : x r) - (f c + p);  z += bias of v
+ *   y = z (1 / t), -inf for tokens that are not allowed
+ * (presence, frequency and biases follow the formula if they are not finite).
+ */
+typedef struct {
+    const float* params;
+    const int32_t* history;
+    int history_ld;
+    const int32_t* history_len;
+    const int32_t* bias_ids;
+    const float* bias_values;
+    int bias_ld;
+    const int32_t* bias_len;
+    const uint32_t* allowed;
+    int allowed_ld;
+    int allowed_by_row;
+} starq_logits_rules;
+
+/*
+ * logits_apply_rules -- Y = y, rounded once to dtype. X [T][ldx], Y [T][ldy]
+ * of dtype F16, BF16 or F32, aligned to their elements; Y may be X (with ldy
+ * = ldx), otherwise they must not overlap. rules NULL = none.
+ *
+ * logits_pick -- of every row, without writing its logits:
+ *   token      [T] int32 out: the allowed token with the largest z, the lowest
+ *              of equal ones; -1 where every allowed z is -inf or none is
+ *              allowed. A NaN counts as the largest.
+ *   confidence [T] float32 out or NULL: with P = softmax(y),
+ *     STARQ_CONFIDENCE_PROBABILITY  P of the token
+ *     STARQ_CONFIDENCE_MARGIN       less P of the second best (0 if none)
+ *     STARQ_CONFIDENCE_ENTROPY      sum P ln P, the negative entropy
+ *     0 with token -1; NaN in a row with NaN or +inf.
+ *   lse        [T] float32 out or NULL: ln sum e^y, -inf with token -1.
+ * Sums in float32, in an order that the sizes alone determine.
+ *
+ * Shapes: 1 <= V <= 2^28, 0 <= T, max_new <= 2^28, 0 <= B <= 65535.
+ */
+enum starq_confidence { STARQ_CONFIDENCE_PROBABILITY = 0, STARQ_CONFIDENCE_MARGIN = 1, STARQ_CONFIDENCE_ENTROPY = 2 };
+int logits_apply_rules(const void* X, int ldx, int dtype, int T, int V, const int32_t* seq_start, int B, int max_new,
+                       const starq_logits_rules* rules, void* Y, int ldy, void* stream);
+int logits_pick(const void* X, int ldx, int dtype, int T, int V, const int32_t* seq_start, int B, int max_new,
+                const starq_logits_rules* rules, int kind, int32_t* token, float* confidence, float* lse, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -30,6 +30,7 @@ EXPORTED = (
     "w4a4_gemm_mma_sync", "starq_set_gemm_pair_limit", "w4a4_gemm_grouped", "sgat_quantize_act_grouped",
     "glue_rope_table", "glue_rope_apply", "kv_cache_append", "kv_cache_read",
     "kv_cache_attention_workspace_size", "kv_cache_attention", "w4g_linear",
+    "logits_apply_rules", "logits_pick",
 )
 
 
@@ -53,6 +54,14 @@ class StarqKvCache(ctypes.Structure):
     _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
                 ("v_scale", ctypes.c_void_p), ("pages", ctypes.c_int), ("page", ctypes.c_int),
                 ("Hkv", ctypes.c_int), ("D", ctypes.c_int)]
+
+
+class StarqLogitsRules(ctypes.Structure):
+    """starq_logits_rules: what tokens are held against, or given."""
+    _fields_ = [("params", ctypes.c_void_p), ("history", ctypes.c_void_p), ("history_ld", ctypes.c_int),
+                ("history_len", ctypes.c_void_p), ("bias_ids", ctypes.c_void_p), ("bias_values", ctypes.c_void_p),
+                ("bias_ld", ctypes.c_int), ("bias_len", ctypes.c_void_p), ("allowed", ctypes.c_void_p),
+                ("allowed_ld", ctypes.c_int), ("allowed_by_row", ctypes.c_int)]
 
 
 def _tac_struct(M, d, g, Mp, scratch):
@@ -145,6 +154,8 @@ def _load():
     lib.kv_cache_attention.argtypes = [vp, i, i, i, vp, i, i, i, vp, vp, i, vp, i, i, vp, i, ctypes.c_float, vp, i, f_p,
                                        vp, ctypes.c_size_t, vp]
     lib.w4g_linear.argtypes = [vp, i, i, i, i, u8p, f_p, i, i, f_p, vp, i, i, vp]
+    lib.logits_apply_rules.argtypes = [vp, i, i, i, i, vp, i, i, vp, vp, i, vp]
+    lib.logits_pick.argtypes = [vp, i, i, i, i, vp, i, i, vp, i, vp, f_p, f_p, vp]
     return lib
 
 
@@ -759,3 +770,112 @@ def w4g_linear(X, Wq, scales, Y, bias=None, stream=None):
     _check(lib.w4g_linear(x, ldx, _CODES[X.dtype], L, K, Wq.data_ptr(), _f32("scales", scales, sc), K // groups, N,
                           None if bias is None else _f32("bias", bias, (N,)), y, ldy, _CODES[Y.dtype],
                           _stream(stream)))
+
+
+CONFIDENCE = {"probability": 0, "margin": 1, "entropy": 2}
+
+
+class LogitsRules:
+    """Rules on the logits of B sequences over `vocab` tokens (see
+    include/starq.h); each may be None. params float32 [B][4]: temperature,
+    repetition factor, presence and frequency penalty. history int32
+    [B][tokens], of which a sequence has history_len[b]. bias_ids int32 and
+    bias_values float32 [B][entries], bias_len[b] of them. allowed int32
+    [B][words] (allowed_by_row: [T][words]): bit v % 32 of word v / 32. Holds
+    the tensors; what they hold may change from call to call."""
+    __slots__ = ("vocab", "B", "rows", "tensors", "c", "ref")
+
+    def __init__(self, vocab, params=None, history=None, history_len=None, bias_ids=None, bias_values=None,
+                 bias_len=None, allowed=None, allowed_by_row=False):
+        self.vocab, self.B, self.rows = vocab, None, None
+        self.tensors = (params, history, history_len, bias_ids, bias_values, bias_len, allowed)
+
+        def rows(name, t, dtype, width=None):
+            """[B][width], contiguous: (pointer, width)"""
+            if t.dtype is not dtype or t.dim() != 2 or not t.is_contiguous() or (width is not None and t.shape[1] != width):
+                raise ValueError(f"starq expects {name} as contiguous {dtype} [sequences][{width or 'n'}]")
+            self._sequences(name, t.shape[0])
+            return t.data_ptr(), t.shape[1]
+
+        def lengths(name, t):
+            if t is None:
+                raise ValueError(f"starq expects {name} with what it counts")
+            if t.dim() == 1:
+                self._sequences(name, t.shape[0])
+            return _ints(name, t, self.B)
+
+        p = h = hl = bi = bv = bl = al = None
+        hld = bld = ald = 0
+        if params is not None:
+            p, _ = rows("params", params, _FP32, 4)
+        if history is not None:
+            h, hld = rows("history", history, _I32)
+            hl = lengths("history_len", history_len)
+        if (bias_ids is None) != (bias_values is None):
+            raise ValueError("starq expects bias_ids and bias_values together")
+        if bias_ids is not None:
+            bi, bld = rows("bias_ids", bias_ids, _I32)
+            bv, _ = rows("bias_values", bias_values, _FP32, bld)
+            bl = lengths("bias_len", bias_len)
+        if allowed is not None:
+            words = (vocab + 31) // 32
+            if allowed.dtype is not _I32 or allowed.dim() != 2 or allowed.shape[1] < words:
+                raise ValueError(f"starq expects allowed as int32 rows of at least {words} words")
+            al, ald = _logits_rows(allowed, "allowed")
+            if allowed_by_row:
+                self.rows = allowed.shape[0]
+            else:
+                self._sequences("allowed", allowed.shape[0])
+        self.c = StarqLogitsRules(p, h, hld, hl, bi, bv, bld, bl, al, ald, int(allowed_by_row))
+        self.ref = ctypes.byref(self.c)
+
+    def _sequences(self, name, n):
+        if self.B is None:
+            self.B = n
+        if n != self.B:
+            raise ValueError(f"starq expects {name} for {self.B} sequences, not {n}")
+
+
+def _logits_rows(t, name):
+    """A matrix with unit column stride, of which a single row may have any
+    stride: (pointer, row stride)."""
+    p, ld = _rows(t, name)
+    return p, ld if t.shape[0] > 1 else max(ld, t.shape[1])
+
+
+def _logits(X, seq_start, rules):
+    """(pointer, row stride, type, rows, tokens, sequences, seq_start, rules)"""
+    T, V = X.shape
+    x, ldx = _logits_rows(X, "X")
+    B = seq_start.shape[0] - 1
+    if B < 0:
+        raise ValueError("starq expects seq_start with an entry more than sequences")
+    ref = None
+    if rules is not None:
+        if rules.vocab != V or (rules.B is not None and rules.B != B) or (rules.rows is not None and rules.rows != T):
+            raise ValueError(f"starq expects rules for {B} sequences, {T} rows and {V} tokens")
+        ref = rules.ref
+    return x, ldx, _CODES[X.dtype], T, V, _ints("seq_start", seq_start, B + 1), B, ref
+
+
+def logits_apply_rules(X, seq_start, rules, max_new, Y=None, stream=None):
+    """Writes the logits X [T][V] (sequence b: rows seq_start[b] .., at most
+    max_new) under the rules (a LogitsRules, or None) into Y (default: in
+    place)."""
+    if Y is None:
+        Y = X
+    if Y.shape != X.shape or Y.dtype is not X.dtype:
+        raise ValueError("starq expects X and Y as logits of one shape and type")
+    x, ldx, dtype, T, V, start, B, ref = _logits(X, seq_start, rules)
+    y, ldy = _logits_rows(Y, "Y")
+    _check(lib.logits_apply_rules(x, ldx, dtype, T, V, start, B, max_new, ref, y, ldy, _stream(stream)))
+
+
+def logits_pick(X, seq_start, rules, token, confidence=None, *, max_new, kind="probability", lse=None, stream=None):
+    """The most likely token of every row of the logits X [T][V] under the
+    rules into token [T] int32 (-1: none is allowed), its confidence
+    ("probability", "margin" to the second best or "entropy", negative) and
+    the log-sum-exp into float32 [T]."""
+    x, ldx, dtype, T, V, start, B, ref = _logits(X, seq_start, rules)
+    _check(lib.logits_pick(x, ldx, dtype, T, V, start, B, max_new, ref, CONFIDENCE[kind], _ints("token", token, T),
+                           _f32("confidence", confidence, (T,)), _f32("lse", lse, (T,)), _stream(stream)))

@@ -5,6 +5,7 @@
 #include <cstdio>
 
 #include "decode.cuh"
+#include "logits.cuh"
 
 namespace starq {
 namespace {
@@ -58,6 +59,42 @@ int check_rows(const char* who, const char* name, const void* p, int ld, int wid
     if (!aligned(p, 16) || ((size_t)ld * elem) % 16 != 0)
         return fail(STARQ_ERR_ALIGN, "%s: %s and its rows must be 16-byte aligned", who, name);
     return STARQ_OK;
+}
+
+// What logits_apply_rules and logits_pick have in common, and their rules.
+int check_logits(const char* who, const void* X, int ldx, int dtype, int T, int V, const int32_t* seq_start, int B,
+                 int max_new, const starq_logits_rules* rules, LogitsArgs* a) {
+    if (!any_type(dtype)) return fail(STARQ_ERR_ARG, "%s: unknown dtype %d", who, dtype);
+    int rc = check_sequences(who, T, B, max_new, 0);
+    if (rc) return rc;
+    if (V < 1 || V > MAX_ROWS) return fail(STARQ_ERR_SHAPE, "%s: V=%d: need 1 <= V <= 2^28", who, V);
+    if (ldx < V) return fail(STARQ_ERR_SHAPE, "%s: ldx=%d is less than V=%d", who, ldx, V);
+    starq_logits_rules r = {};
+    if (rules) r = *rules;
+    if (r.history_ld < 0 || r.bias_ld < 0)
+        return fail(STARQ_ERR_SHAPE, "%s: history_ld=%d, bias_ld=%d: need >= 0", who, r.history_ld, r.bias_ld);
+    if (r.allowed && r.allowed_ld < (V + 31) / 32)
+        return fail(STARQ_ERR_SHAPE, "%s: allowed_ld=%d: %d tokens need %d words", who, r.allowed_ld, V, (V + 31) / 32);
+    if (r.history && !r.history_len) return fail(STARQ_ERR_ARG, "%s: a history without history_len", who);
+    if ((r.bias_ids != nullptr) != (r.bias_values != nullptr) || (r.bias_ids && !r.bias_len))
+        return fail(STARQ_ERR_ARG, "%s: bias_ids, bias_values and bias_len go together", who);
+    if (!aligned(r.params, 4) || !aligned(r.history, 4) || !aligned(r.history_len, 4) || !aligned(r.bias_ids, 4) ||
+        !aligned(r.bias_values, 4) || !aligned(r.bias_len, 4) || !aligned(r.allowed, 4))
+        return fail(STARQ_ERR_ALIGN, "%s: the rules' arrays must be 4-byte aligned", who);
+    *a = LogitsArgs{X, ldx, dtype, T, V, seq_start, B, max_new, r, nullptr, 0, 0, nullptr, nullptr, nullptr, nullptr};
+    return STARQ_OK;
+}
+
+int run_logits(const char* who, LogitsArgs& a, void* stream) {
+    if (!aligned(a.X, a.dtype == STARQ_F32 ? 4 : 2) || !aligned(a.seq_start, 4))
+        return fail(STARQ_ERR_ALIGN, "%s: X and seq_start must be aligned to their elements", who);
+    int rc = STARQ_OK;
+    a.status = device_status(&rc);
+    if (!a.status) return rc;
+    const cudaError_t e = launch_logits(a, static_cast<cudaStream_t>(stream));
+    if (e == cudaErrorInvalidValue)
+        return fail(STARQ_ERR_SHAPE, "%s: B=%d sequences of up to %d rows need more than 2^31 CTAs", who, a.B, a.max_new);
+    return launched(e, who);
 }
 
 }  // namespace
@@ -234,6 +271,42 @@ int w4g_linear(const void* X, int ldx, int dtype, int L, int K, const uint8_t* W
         return fail(STARQ_ERR_ALIGN, "%s: X, its rows and Wq must be 16-byte aligned, the others to their elements", who);
     const W4gArgs a{X, ldx, dtype, L, K, Wq, scales, group, N, bias, Y, ldy, y_dtype};
     return launched(launch_w4g_linear(a, static_cast<cudaStream_t>(stream)), who);
+}
+
+int logits_apply_rules(const void* X, int ldx, int dtype, int T, int V, const int32_t* seq_start, int B, int max_new,
+                       const starq_logits_rules* rules, void* Y, int ldy, void* stream) {
+    const char* who = "logits_apply_rules";
+    LogitsArgs a;
+    const int rc = check_logits(who, X, ldx, dtype, T, V, seq_start, B, max_new, rules, &a);
+    if (rc) return rc;
+    if (ldy < V) return fail(STARQ_ERR_SHAPE, "%s: ldy=%d is less than V=%d", who, ldy, V);
+    if (X && X == Y && ldx != ldy) return fail(STARQ_ERR_ARG, "%s: in place needs ldy = ldx", who);
+    if (T == 0 || B == 0 || max_new == 0) return STARQ_OK;
+    if (!X || !Y || !seq_start) return fail(STARQ_ERR_ARG, "%s: NULL X, Y or seq_start", who);
+    if (!aligned(Y, dtype == STARQ_F32 ? 4 : 2)) return fail(STARQ_ERR_ALIGN, "%s: Y must be aligned to its elements", who);
+    a.Y = Y;
+    a.ldy = ldy;
+    a.kind = -1;
+    return run_logits(who, a, stream);
+}
+
+int logits_pick(const void* X, int ldx, int dtype, int T, int V, const int32_t* seq_start, int B, int max_new,
+                const starq_logits_rules* rules, int kind, int32_t* token, float* confidence, float* lse, void* stream) {
+    const char* who = "logits_pick";
+    LogitsArgs a;
+    const int rc = check_logits(who, X, ldx, dtype, T, V, seq_start, B, max_new, rules, &a);
+    if (rc) return rc;
+    if (kind < STARQ_CONFIDENCE_PROBABILITY || kind > STARQ_CONFIDENCE_ENTROPY)
+        return fail(STARQ_ERR_ARG, "%s: unknown confidence %d", who, kind);
+    if (T == 0 || B == 0 || max_new == 0) return STARQ_OK;
+    if (!X || !token || !seq_start) return fail(STARQ_ERR_ARG, "%s: NULL X, token or seq_start", who);
+    if (!aligned(token, 4) || !aligned(confidence, 4) || !aligned(lse, 4))
+        return fail(STARQ_ERR_ALIGN, "%s: token, confidence and lse must be 4-byte aligned", who);
+    a.kind = kind;
+    a.token = token;
+    a.confidence = confidence;
+    a.lse = lse;
+    return run_logits(who, a, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,329 @@
+"""Rules on logits and the choice of a token against oracle/logits.py.
+
+Tolerances. The definition fixes every float32 step of z and y, so the
+logits under the rules are bit-exact (one more rounding for the 16-bit types)
+and so is the token. A row's sum l of V exponentials is added up by at least
+32 threads, so the longest chain of additions is V / 32 + 64 (the joins
+included), each step of which rounds once (2^-24) and may move the maximum (a
+product by an exponential, 2^-22): R = (V / 32 + 64) 2^-22 of l. A term's
+exponent d = (z - m) log2(e) / t has four roundings, 2^-22 |d|, the weight's
+logarithm; D is the largest |d| that weighs anything. So with E = R + 2^-21 (D
++ 1): a probability is off by E of itself, a margin by E plus 2^-22 / l, a
+log-sum-exp by E + 2^-22 (|m / t| + |lse|), and the entropy's mean of d, whose
+terms carry E too, by E (2 D + 2) and 2^-22 |ln l|.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import logits as ol
+
+pytestmark = pytest.mark.gpu
+
+KINDS = ("probability", "margin", "entropy")
+i32 = lambda v: torch.tensor(np.asarray(v, dtype=np.int32), device="cuda")
+starts = lambda n: i32(np.concatenate([[0], np.cumsum(n)]))
+num = lambda t: t.detach().float().cpu().numpy()
+
+
+def pack(bits):
+    """[R][V] booleans to int32 words, [R][ceil(V / 32)]."""
+    R, V = bits.shape
+    words = (V + 31) // 32
+    padded = np.zeros((R, words * 32), np.uint64)
+    padded[:, :V] = bits
+    w = (padded.reshape(R, words, 32) << np.arange(32, dtype=np.uint64)).sum(-1).astype(np.uint32)
+    return torch.from_numpy(w.view(np.int32)).cuda()
+
+
+class Case:
+    """Random logits of ragged sequences with all rules, and what the oracle
+    says of every row."""
+
+    def __init__(self, seed, dtype, V, rows, history=0, biases=0, masked=False, by_row=False, params=True, pad=0, lead=0,
+                 behind=0, logits=None):
+        rng = np.random.default_rng(seed)
+        B, T = len(rows), int(sum(rows))
+        self.V, self.T, self.B, self.rows, self.dtype = V, T, B, rows, dtype
+        self.first = np.concatenate([[0], np.cumsum(rows)])
+        x = rng.standard_normal((T + behind, V + pad)).astype(np.float32) * 3 if logits is None else logits
+        store = torch.zeros(lead + x.size, dtype=dtype, device="cuda")
+        self.X = store[lead:].view(x.shape)
+        self.X.copy_(torch.from_numpy(x))
+        self.X = self.X[:, :V]
+        self.start = starts(rows)
+        self.kw = {}
+        self.params = np.tile(np.float32([1, 1, 0, 0]), (B, 1))
+        if params:
+            self.params = np.stack([rng.uniform(0.3, 2, B), rng.uniform(0.8, 1.6, B), rng.uniform(-0.5, 1, B),
+                                    rng.uniform(-0.2, 0.5, B)], 1).astype(np.float32)
+            self.kw["params"] = torch.from_numpy(self.params).cuda()
+        self.history = [np.zeros(0, np.int32)] * B
+        if history:
+            table = (rng.random((B, history)) ** 3 * V).astype(np.int32)
+            lengths = [history if b == 0 else int(rng.integers(0, history + 1)) for b in range(B)]
+            self.kw.update(history=i32(table), history_len=i32(lengths))
+            self.history = [table[b, :lengths[b]] for b in range(B)]
+        self.biases = [[]] * B
+        if biases:
+            ids = rng.integers(0, V, (B, biases)).astype(np.int32)
+            ids[:, -1] = ids[:, 0]                                # one is given twice
+            values = (rng.standard_normal((B, biases)) * 4).astype(np.float32)
+            lengths = [biases if b == 0 else int(rng.integers(0, biases + 1)) for b in range(B)]
+            self.kw.update(bias_ids=i32(ids), bias_values=torch.from_numpy(values).cuda(), bias_len=i32(lengths))
+            self.biases = [list(zip(ids[b, :lengths[b]], values[b, :lengths[b]])) for b in range(B)]
+        self.allowed = None
+        if masked:
+            R = T + behind if by_row else B
+            self.allowed = rng.random((R, V)) < rng.choice([0.02, 0.5, 0.98], R)[:, None]
+            self.allowed[R // 2] = False
+            self.kw.update(allowed=pack(self.allowed), allowed_by_row=by_row)
+        self.by_row = by_row
+
+    def rules(self, abi):
+        return abi.LogitsRules(self.V, **self.kw)
+
+    def reference(self):
+        """z and y [T][V] float32."""
+        x = num(self.X)
+        z, y = np.zeros((self.T, self.V), np.float32), np.zeros((self.T, self.V), np.float32)
+        for b in range(self.B):
+            for r in range(self.first[b], self.first[b + 1]):
+                ok = None if self.allowed is None else self.allowed[r if self.by_row else b]
+                z[r], y[r] = ol.rules(x[r], self.params[b], self.history[b], self.biases[b], ok)
+        return z, y
+
+    def check_pick(self, abi, kind, z=None, **kw):
+        n = self.X.shape[0]
+        token = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+        conf, lse = torch.full((n,), 7.0, device="cuda"), torch.full((n,), 7.0, device="cuda")
+        abi.logits_pick(self.X, self.start, self.rules(abi) if self.kw else None, token, conf,
+                        max_new=kw.pop("max_new", max(self.rows, default=0)), kind=kind, lse=lse, **kw)
+        abi.check_status()
+        z = self.reference()[0] if z is None else z
+        token, conf, lse = token.cpu().numpy(), num(conf).astype(np.float64), num(lse).astype(np.float64)
+        for b in range(self.B):
+            t = self.params[b, 0]
+            for r in range(self.first[b], self.first[b + 1]):
+                want, c, s, D = ol.pick(z[r], t, kind)
+                assert token[r] == want, (r, token[r], want)
+                if not np.isfinite(c) or not np.isfinite(s):
+                    assert np.array_equal(np.isnan(conf[r]), np.isnan(c)) and (lse[r] == s or np.isnan(s) == np.isnan(lse[r]))
+                    assert want >= 0 or (conf[r] == 0 and lse[r] == -np.inf)
+                    continue
+                m = abs(float(z[r][want]) / t)
+                E = (self.V / 32 + 64) * 2.0 ** -22 + 2.0 ** -21 * (1.4427 * D + 1)
+                top = np.exp(min(0.0, float(z[r][want]) / t - s))     # 1 / l
+                tol = {"probability": E * c, "margin": E * c + 2.0 ** -22 * top,
+                       "entropy": E * (2.9 * D + 2) + 2.0 ** -22 * abs(np.log(top))}[kind]
+                assert abs(conf[r] - c) <= tol, (kind, r, conf[r], c, tol)
+                assert abs(lse[r] - s) <= E + 2.0 ** -22 * (m + abs(s)), (r, lse[r], s)
+        end = self.first[-1]
+        assert np.all(token[end:] == -7) and np.all(conf[end:] == 7) and np.all(lse[end:] == 7)
+
+
+SHAPES = [  # V, rows of the sequences, padding of a row, elements before the first
+    (1, (1,), 0, 0), (2, (1, 3), 0, 0), (7, (2, 0, 1), 1, 0), (33, (1,), 0, 1), (1000, (5, 0, 9), 0, 0),
+    (1003, (3, 1), 0, 3), (4096, (1,) * 5, 8, 0), (8193, (17,), 0, 0), (20011, (1, 2), 5, 7), (50257, (2,), 0, 0),
+    (70000, (3, 30, 8), 0, 0)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("V,rows,pad,lead", SHAPES)
+@pytest.mark.parametrize("kw", [dict(params=False), dict(history=9, biases=3), dict(masked=True, by_row=True),
+                                dict(history=700, biases=40, masked=True)])
+def test_rules(abi, dtype, V, rows, pad, lead, kw):
+    c = Case(V + len(rows), dtype, V, rows, pad=pad, lead=lead, behind=2, **kw)
+    y = torch.full((c.T + 2, V + pad), 5.0, dtype=dtype, device="cuda")[:, :V]
+    abi.logits_apply_rules(c.X, c.start, c.rules(abi) if c.kw else None, max_new=max(rows), Y=y)
+    abi.check_status()
+    want = torch.from_numpy(c.reference()[1]).to(dtype)
+    assert torch.equal(y[:c.T].cpu(), want)
+    assert torch.all(y[c.T:] == 5.0)                              # rows of no sequence
+    tail = c.X[c.T:].clone()
+    abi.logits_apply_rules(c.X, c.start, c.rules(abi) if c.kw else None, max_new=max(rows) + 3)      # in place
+    abi.check_status()
+    assert torch.equal(c.X[:c.T].cpu(), want) and torch.equal(c.X[c.T:], tail)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("V,rows,pad,lead", SHAPES)
+@pytest.mark.parametrize("kw", [dict(params=False), dict(history=9, biases=3), dict(masked=True, by_row=True),
+                                dict(history=700, biases=40, masked=True)])
+def test_pick(abi, dtype, V, rows, pad, lead, kw):
+    c = Case(V + len(rows), dtype, V, rows, pad=pad, lead=lead, behind=2, **kw)
+    z = c.reference()[0]
+    for kind in KINDS:
+        c.check_pick(abi, kind, z)
+
+
+def test_padding_of_a_row_is_left(abi):
+    c = Case(5, torch.bfloat16, 101, (2, 1), history=5, pad=11)
+    store = torch.full((3, 128), 9.0, dtype=torch.bfloat16, device="cuda")
+    abi.logits_apply_rules(c.X, c.start, c.rules(abi), max_new=2, Y=store[:, 13:114])
+    assert torch.equal(store[:, 13:114].cpu(), torch.from_numpy(c.reference()[1]).bfloat16())
+    assert torch.all(store[:, :13] == 9) and torch.all(store[:, 114:] == 9)
+
+
+@pytest.mark.parametrize("V", [5, 3000, 40000])
+def test_values_that_are_not_finite(abi, V):
+    """NaN is above everything, +inf leaves no probabilities, -inf cannot be
+    taken; what the mask hides does not count whatever it is."""
+    rng = np.random.default_rng(V)
+    x = rng.standard_normal((9, V)).astype(np.float32)
+    x[0, V - 2] = np.nan
+    x[1, [1, V - 1]] = np.inf
+    x[2] = -np.inf
+    x[3, : V - 1] = -np.inf
+    x[4, [2, V - 3]] = np.nan
+    x[4, 0] = np.inf
+    x[5, 1:] = np.nan                                              # hidden below
+    x[6] = 0.25                                                    # all equal
+    x[7, 3] = -np.inf
+    x[8, 3] = 3e38
+    c = Case(1, torch.float32, V, (9,), logits=x, params=False)
+    c.allowed = np.ones((9, V), bool)
+    c.allowed[5, 1:] = False
+    c.by_row = True
+    c.kw = dict(allowed=pack(c.allowed), allowed_by_row=True)
+    for kind in KINDS:
+        c.check_pick(abi, kind)
+    y = torch.empty_like(c.X)
+    abi.logits_apply_rules(c.X, c.start, c.rules(abi), max_new=9, Y=y)
+    assert torch.equal(y.cpu().nan_to_num(nan=77.0), torch.from_numpy(c.reference()[1]).nan_to_num(nan=77.0))
+
+
+def test_ties_go_to_the_lowest_token(abi):
+    """Equal values in every thread, warp and CTA of a row; and a temperature
+    whose rounding would make two tokens equal."""
+    V = 40000
+    x = np.zeros((4, V), np.float32)
+    x[1, 17:] = 2
+    x[2, [39999, 30001, 8192]] = 5
+    x[3, 100], x[3, 20000] = np.float32(1) + 2.0 ** -23, np.float32(1) + 2.0 ** -22
+    x[3, 5] = 1
+    c = Case(1, torch.float32, V, (4,), logits=x, params=False)
+    c.params[:, 0] = 3.0
+    c.kw = dict(params=torch.from_numpy(c.params).cuda())
+    for kind in KINDS:
+        c.check_pick(abi, kind)
+
+
+@pytest.mark.parametrize("t", [1e-30, 1e-3, 1e30])
+def test_temperatures_at_the_ends(abi, t):
+    c = Case(2, torch.float32, 999, (3,), history=20)
+    c.params[:, 0] = t
+    c.kw["params"] = torch.from_numpy(c.params).cuda()
+    for kind in ("probability", "margin"):
+        c.check_pick(abi, kind)
+
+
+def test_empty_calls(abi):
+    x = torch.zeros(3, 8, device="cuda")
+    out = torch.full((3,), -7, dtype=torch.int32, device="cuda")
+    abi.logits_pick(x, i32([0, 0]), None, out, max_new=4)          # a sequence without rows
+    abi.logits_pick(x, i32([0, 2]), None, out, max_new=0)
+    abi.logits_pick(x[:0], i32([0]), None, out[:0], max_new=4)
+    abi.logits_apply_rules(x[:0], i32([0]), None, max_new=4)
+    abi.check_status()
+    assert torch.all(out == -7)
+    abi.logits_pick(x, i32([0, 3]), None, out, max_new=3)          # confidence and lse are optional
+    assert out.tolist() == [0, 0, 0]
+
+
+def test_indexes_out_of_range(abi):
+    """A token, a length, a temperature or a row outside its array is skipped
+    and reported; the other sequences are right."""
+    c = Case(3, torch.float32, 500, (2, 2), history=6, biases=4)
+    z = c.reference()[0]
+
+    def reported(**kw):
+        out = torch.full((4,), -7, dtype=torch.int32, device="cuda")
+        abi.logits_pick(c.X, kw.pop("start", c.start), abi.LogitsRules(500, **dict(c.kw, **kw)), out, max_new=2)
+        with pytest.raises(abi.StarqError) as e:
+            abi.check_status()
+        assert e.value.code == abi.ERR_RANGE
+        abi.check_status()
+        return out.tolist()
+
+    right = [ol.pick(z[r], 1.0, "probability")[0] for r in range(4)]
+    h = c.kw["history"].clone()
+    h[1, 0] = 500
+    assert reported(history=h, history_len=i32([6, 1]))[:2] == right[:2]
+    h[1, 0] = -1
+    assert reported(history=h, history_len=i32([6, 1]))[:2] == right[:2]
+    assert reported(history_len=i32([6, 7]))[:2] == right[:2]
+    assert reported(history_len=i32([6, -1]))[:2] == right[:2]
+    ids = c.kw["bias_ids"].clone()
+    ids[1, 0] = 1 << 30
+    assert reported(bias_ids=ids, bias_len=i32([4, 1]))[:2] == right[:2]
+    assert reported(bias_len=i32([4, 5]))[:2] == right[:2]
+    p = c.kw["params"].clone()
+    for at, bad in ((0, 0.0), (0, float("nan")), (0, float("inf")), (1, -1.0), (1, 0.0)):
+        q = p.clone()
+        q[1, at] = bad
+        assert reported(params=q)[:2] == right[:2]
+    assert reported(start=i32([0, 2, 5])) == right[:2] + [-7, -7]
+    assert reported(start=i32([0, 2, 1])) == right[:2] + [-7, -7]
+
+
+def test_rows_far_apart(abi):
+    """Row offsets beyond 2^32 bytes, with a history that names the far rows'
+    tokens."""
+    V, ld = 1000, (1 << 30) + 8
+    store = torch.zeros(2 * ld + V, dtype=torch.bfloat16, device="cuda")
+    X = store.as_strided((3, V), (ld, 1))
+    rng = np.random.default_rng(0)
+    X.copy_(torch.from_numpy(rng.standard_normal((3, V)).astype(np.float32)))
+    c = Case(1, torch.bfloat16, V, (1, 2), history=30)
+    c.X = X
+    c.check_pick(abi, "entropy")
+    want = c.reference()[1]
+    abi.logits_apply_rules(X, c.start, c.rules(abi), max_new=2)
+    assert torch.equal(X.cpu(), torch.from_numpy(want).bfloat16())
+
+
+def test_many_sequences(abi):
+    rows = [(i * 7) % 3 for i in range(1500)]
+    c = Case(8, torch.float32, 64, rows, history=4)
+    c.check_pick(abi, "margin")
+
+
+def test_a_long_history(abi):
+    c = Case(9, torch.float32, 300, (1,), history=40000)
+    c.check_pick(abi, "probability")
+    y = torch.empty_like(c.X)
+    abi.logits_apply_rules(c.X, c.start, c.rules(abi), max_new=1, Y=y)
+    assert torch.equal(y.cpu(), torch.from_numpy(c.reference()[1]))
+
+
+def test_graph_and_stream(abi):
+    """A captured call reads the rules where they are; a call on a stream of
+    the caller's; the same inputs give the same bits."""
+    c = Case(4, torch.float32, 30000, (3, 5), history=50, biases=6, masked=True)
+    rules, z = c.rules(abi), c.reference()[0]
+    out = [torch.zeros(8, dtype=torch.int32, device="cuda"), torch.zeros(8, device="cuda"), torch.zeros(8, device="cuda")]
+    call = lambda stream=None: abi.logits_pick(c.X, c.start, rules, out[0], out[1], max_new=5, kind="entropy", lse=out[2],
+                                               stream=stream)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    call(side)
+    side.synchronize()
+    first = [t.clone() for t in out]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for t in out:
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, out))
+    assert out[0].tolist() == [ol.pick(z[r], 1.0, "margin")[0] for r in range(8)]
+    c.kw["history_len"].zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    c.history = [np.zeros(0, np.int32)] * 2
+    z = c.reference()[0]
+    assert out[0].tolist() == [ol.pick(z[r], 1.0, "margin")[0] for r in range(8)]
+    abi.check_status()

@@ -1,0 +1,124 @@
+"""Rules on logits without a GPU: the oracle against closed forms, and the
+argument checks (nothing is launched by a refused call)."""
+
+import ctypes
+import types
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import logits as ol
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2606_04945_gb300 import build
+    build.build()
+    from paper_2606_04945_gb300 import abi
+    return abi
+
+
+def test_oracle_rules():
+    x = np.float32([2, -2, 0, 1])
+    z, y = ol.rules(x, (0.5, 2, 0.25, 0.125), history=[0, 1, 1], biases=[(3, 9), (3, -1)],
+                    allowed=np.array([1, 1, 0, 1], bool))
+    assert z.tolist() == [1 - 0.375, -4 - 0.5, -np.inf, 0] and y.tolist() == [1.25, -9, -np.inf, 0]
+
+
+def test_oracle_pick_against_softmax():
+    rng = np.random.default_rng(0)
+    z = rng.standard_normal(40).astype(np.float32)
+    z[7] = -np.inf
+    p = torch.softmax(torch.from_numpy(z).double() / 0.5, 0)
+    top = p.topk(2)
+    for kind, want in (("probability", top.values[0]), ("margin", top.values[0] - top.values[1]),
+                       ("entropy", torch.special.xlogy(p, p).sum())):
+        token, c, lse, _ = ol.pick(z, 0.5, kind)
+        assert token == top.indices[0] and np.isclose(c, want)
+        assert np.isclose(lse, torch.logsumexp(torch.from_numpy(z).double() / 0.5, 0))
+    assert ol.pick(np.full(3, -np.inf, np.float32), 1, "margin")[:3] == (-1, 0.0, -np.inf)
+    assert ol.pick(np.float32([4]), 1, "margin")[1] == 1 and ol.pick(np.float32([4]), 1, "entropy")[1] == 0
+
+
+P = ctypes.c_void_p(4096)          # a non-null, aligned stand-in; never dereferenced
+ODD = ctypes.c_void_p(4097)
+
+RULES = dict(params=4096, history=4096, history_ld=8, history_len=4096, bias_ids=4096, bias_values=4096, bias_ld=4,
+             bias_len=4096, allowed=4096, allowed_ld=4, allowed_by_row=0)
+
+
+def rules(lib, **kw):
+    f = dict(RULES)
+    f.update(kw)
+    return ctypes.byref(lib.StarqLogitsRules(*[f[n] for n, _ in lib.StarqLogitsRules._fields_]))
+
+
+BAD_RULES = [(dict(history_ld=-1), -2), (dict(bias_ld=-1), -2), (dict(allowed_ld=3), -2), (dict(history_len=None), -1),
+             (dict(bias_values=None), -1), (dict(bias_ids=None), -1), (dict(bias_len=None), -1), (dict(params=4098), -3),
+             (dict(allowed=4097), -3)]
+BAD = [(dict(rules=r), c) for r, c in BAD_RULES] + [
+    (dict(dtype=3), -1), (dict(dtype=-1), -1), (dict(T=-1), -2), (dict(V=0), -2), (dict(V=(1 << 28) + 1), -2),
+    (dict(ldx=99), -2), (dict(B=-1), -2), (dict(B=65536), -2), (dict(max_new=-1), -2), (dict(X=None), -1),
+    (dict(seq_start=None), -1), (dict(X=ODD), -3), (dict(seq_start=ctypes.c_void_p(4098)), -3)]
+APPLY = "X ldx dtype T V seq_start B max_new rules Y ldy stream".split()
+PICK = "X ldx dtype T V seq_start B max_new rules kind token confidence lse stream".split()
+
+
+def refuse(lib, fn, names, base, changes, code):
+    changes = dict(changes)
+    if "rules" in changes:
+        changes["rules"] = rules(lib, **changes["rules"])
+    args = dict(base, **changes)
+    assert getattr(lib.lib, fn)(*[args[n] for n in names]) == code, changes
+    assert lib.lib.starq_last_error()
+
+
+@pytest.mark.parametrize("changes,code", BAD + [(dict(ldy=99), -2), (dict(Y=None), -1), (dict(Y=ODD), -3),
+                                                (dict(X=P, Y=P, ldy=128), -1)])
+def test_apply_refusals(lib, changes, code):
+    base = dict(X=P, ldx=100, dtype=0, T=3, V=100, seq_start=P, B=1, max_new=3, rules=rules(lib),
+                Y=ctypes.c_void_p(1 << 20), ldy=100, stream=None)
+    refuse(lib, "logits_apply_rules", APPLY, base, changes, code)
+
+
+@pytest.mark.parametrize("changes,code", BAD + [(dict(kind=3), -1), (dict(kind=-1), -1), (dict(token=None), -1),
+                                                (dict(lse=ODD), -3), (dict(confidence=ODD), -3)])
+def test_pick_refusals(lib, changes, code):
+    base = dict(X=P, ldx=100, dtype=0, T=3, V=100, seq_start=P, B=1, max_new=3, rules=rules(lib), kind=0, token=P,
+                confidence=P, lse=P, stream=None)
+    refuse(lib, "logits_pick", PICK, base, changes, code)
+
+
+def test_nothing_to_do(lib):
+    for T, B, n in ((0, 1, 1), (1, 0, 1), (1, 1, 0)):
+        assert lib.lib.logits_apply_rules(None, 8, 0, T, 8, None, B, n, None, None, 8, None) == 0
+        assert lib.lib.logits_pick(None, 8, 0, T, 8, None, B, n, None, 0, None, None, None, None) == 0
+
+
+def test_binding_refusals(lib):
+    """The binding's own checks of shapes, types and strides (host tensors:
+    nothing reaches the library)."""
+    t, i = torch.zeros, lambda *v: torch.tensor(v, dtype=torch.int32)
+    grid = lambda n, m: t(n, m, dtype=torch.int32)
+    bad = [dict(params=t(2, 3)), dict(params=t(2, 4).double()), dict(history=grid(2, 5)),
+           dict(history=grid(2, 5), history_len=i(1)), dict(history=grid(2, 10)[:, ::2], history_len=i(1, 1)),
+           dict(history=t(2, 5, dtype=torch.long), history_len=i(1, 1)), dict(bias_ids=grid(2, 3)),
+           dict(bias_ids=grid(2, 3), bias_values=t(2, 4), bias_len=i(1, 1)), dict(bias_ids=grid(2, 3), bias_values=t(2, 3)),
+           dict(allowed=grid(2, 3)), dict(allowed=t(2, 4)), dict(params=t(2, 4), allowed=grid(3, 4))]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            lib.LogitsRules(100, **kw)
+    r = lib.LogitsRules(100, params=t(2, 4), allowed=grid(3, 4), allowed_by_row=True)
+    x, start, token = t(3, 100), i(0, 1, 3), i(0, 0, 0)
+    for X, s, out, kw in ((x[:, :99], start, token, {}), (x, i(0, 3), token, {}), (t(4, 100), start, i(0, 0, 0, 0), {}),
+                          (x, start, token[:2], {}), (x, start, token.long(), {}), (x, start, token, dict(lse=t(2))),
+                          (x, start, token, dict(lse=t(3).half())), (t(3, 200)[:, ::2], start, token, {}),
+                          (x, start.long(), token, {})):
+        with pytest.raises(ValueError):
+            lib.logits_pick(X, s, r, out, max_new=2, **kw)
+    with pytest.raises(ValueError):
+        lib.logits_apply_rules(x, start, r, max_new=2, Y=t(3, 100).half())
+    none = types.SimpleNamespace(cuda_stream=0)
+    with pytest.raises(lib.StarqError):                             # rows that overlap
+        lib.logits_apply_rules(t(1, 100).expand(3, 100), start, r, max_new=2, Y=t(3, 100), stream=none)
