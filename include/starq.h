@@ -895,6 +895,53 @@ int kv_cache_attention(const void* Q, int ldq, int dtype, int T, const int32_t* 
                        float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * kv_cache_attention_window -- kv_cache_attention with a sliding window and
+ * a few first slots that stay visible. Row i of a sequence with n new tokens
+ * stands at slot s = kv_len[b] - n + i, whatever `causal` is, and sees of the
+ * slots that it would see without a window those with
+ *   j > s - window  or  j < sinks
+ * (window 1: itself; slots behind s, which a row without `causal` sees too,
+ * are never outside). Only blocks with a slot that some row of a sequence's
+ * first tokens may see are read, so pages that the window has left for good
+ * may be given away: their entries of page_table are not looked up (16 slots
+ * at a time; a block of 16 slots that begins outside the first row's window
+ * and first slots and ends inside is read).
+ *   window >= 1, sinks >= 0; a window of kv_len or more is no window.
+ * Other arguments, workspace and result as kv_cache_attention.
+ *
+ * kv_cache_attention_shared -- kv_cache_attention for sequences that share a
+ * prefix (several answers to one prompt, requests behind one instruction):
+ * the same result, up to the order of float32 sums, with the prefix read once
+ * for all of them.
+ *   group_start [groups + 1] device int32, not decreasing: group g holds the
+ *          sequences group_start[g] .. group_start[g + 1] - 1; sequences
+ *          before the first or behind the last group share nothing.
+ *   shared_len [groups] device int32: the group's sequences have slots 0 ..
+ *          shared_len[g] - 1 in common: the same pages (those of its first
+ *          sequence are read), the same key mask there, all of them before
+ *          the new tokens (shared_len[g] <= kv_len[b] - n, else the sequence
+ *          is reported as STARQ_ERR_RANGE and has no rows). Any length, not
+ *          only whole pages.
+ *   max_rows, max_shared  bounds of a group's rows and of shared_len.
+ *   workspace: kv_cache_attention_shared_workspace_size bytes.
+ * Where the bounds say that there is little to share the call is
+ * kv_cache_attention's.
+ */
+int kv_cache_attention_window(const void* Q, int ldq, int dtype, int T, const int32_t* seq_start, int B, int max_new,
+                              int H, const starq_kv_cache* cache, const int32_t* page_table, int table_ld,
+                              const int32_t* kv_len, int max_len, int causal, int window, int sinks,
+                              const uint8_t* key_mask, int mask_ld, float scale, void* Out, int ldo, float* lse,
+                              void* workspace, size_t workspace_bytes, void* stream);
+size_t kv_cache_attention_shared_workspace_size(int T, int B, int max_new, int groups, int max_rows, int H, int Hkv,
+                                                int D);
+int kv_cache_attention_shared(const void* Q, int ldq, int dtype, int T, const int32_t* seq_start, int B, int max_new,
+                              int H, const starq_kv_cache* cache, const int32_t* page_table, int table_ld,
+                              const int32_t* kv_len, int max_len, int causal, const int32_t* group_start,
+                              const int32_t* shared_len, int groups, int max_rows, int max_shared,
+                              const uint8_t* key_mask, int mask_ld, float scale, void* Out, int ldo, float* lse,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * w4g_linear -- a linear layer of a few rows with 4-bit weights that carry
  * one scale per group of input channels (weight-only: activations stay
  * 16-bit):

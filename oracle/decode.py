@@ -133,3 +133,34 @@ def w4g_linear(x, codes, scales, bias=None):
     if bias is not None:
         y, size = y + bias.astype(np.float64), size + np.abs(bias.astype(np.float64))
     return y, size
+
+
+def window_sees(n, L, window, sinks, causal, key_mask=None):
+    """[n][L]: which slots the n new tokens (the last of L) see through a
+    window and the first `sinks` slots."""
+    see = np.zeros((n, L), bool)
+    for i in range(n):
+        own = L - n + i
+        for j in range(L):
+            see[i, j] = (j > own - window or j < sinks) and (j <= own or not causal) and (key_mask is None or key_mask[j] != 0)
+    return see
+
+
+def attention_of(q, k, v, scale, see):
+    """attention() for any see [n][L]; the same four results."""
+    n, H, D = q.shape
+    out, mag = np.zeros((n, H, D)), np.zeros((n, H, D))
+    lse, size = np.full((n, H), -np.inf), np.zeros((n, H))
+    G = H // k.shape[1]
+    for h in range(H):
+        kk, vv = k[:, h // G], v[:, h // G]
+        for i in range(n):
+            at = np.flatnonzero(see[i])
+            if len(at) == 0:
+                continue
+            s = kk[at] @ q[i, h] * scale
+            p = np.exp(s - s.max())
+            out[i, h], mag[i, h] = p @ vv[at] / p.sum(), p @ np.abs(vv[at]) / p.sum()
+            lse[i, h] = s.max() + np.log(p.sum())
+            size[i, h] = (np.abs(kk[at]) @ np.abs(q[i, h])).max() * scale
+    return out, lse, mag, size

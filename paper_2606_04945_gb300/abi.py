@@ -30,6 +30,7 @@ EXPORTED = (
     "w4a4_gemm_mma_sync", "starq_set_gemm_pair_limit", "w4a4_gemm_grouped", "sgat_quantize_act_grouped",
     "glue_rope_table", "glue_rope_apply", "kv_cache_append", "kv_cache_read",
     "kv_cache_attention_workspace_size", "kv_cache_attention", "w4g_linear",
+    "kv_cache_attention_window", "kv_cache_attention_shared_workspace_size", "kv_cache_attention_shared",
     "logits_apply_rules", "logits_pick",
 )
 
@@ -153,6 +154,12 @@ def _load():
     lib.kv_cache_attention_workspace_size.restype = ctypes.c_size_t
     lib.kv_cache_attention.argtypes = [vp, i, i, i, vp, i, i, i, vp, vp, i, vp, i, i, vp, i, ctypes.c_float, vp, i, f_p,
                                        vp, ctypes.c_size_t, vp]
+    lib.kv_cache_attention_window.argtypes = [vp, i, i, i, vp, i, i, i, vp, vp, i, vp, i, i, i, i, vp, i, ctypes.c_float,
+                                              vp, i, f_p, vp, ctypes.c_size_t, vp]
+    lib.kv_cache_attention_shared_workspace_size.argtypes = [i, i, i, i, i, i, i, i]
+    lib.kv_cache_attention_shared_workspace_size.restype = ctypes.c_size_t
+    lib.kv_cache_attention_shared.argtypes = [vp, i, i, i, vp, i, i, i, vp, vp, i, vp, i, i, vp, vp, i, i, i, vp, i,
+                                              ctypes.c_float, vp, i, f_p, vp, ctypes.c_size_t, vp]
     lib.w4g_linear.argtypes = [vp, i, i, i, i, u8p, f_p, i, i, f_p, vp, i, i, vp]
     lib.logits_apply_rules.argtypes = [vp, i, i, i, i, vp, i, i, vp, vp, i, vp]
     lib.logits_pick.argtypes = [vp, i, i, i, i, vp, i, i, vp, i, vp, f_p, f_p, vp]
@@ -722,13 +729,9 @@ def kv_cache_attention_workspace_size(B, max_new, H, Hkv, D):
     return int(lib.kv_cache_attention_workspace_size(B, max_new, H, Hkv, D))
 
 
-def kv_cache_attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, causal=False, key_mask=None,
-                       scale=None, lse=None, workspace=None, stream=None):
-    """Attention of the rows of Q [T][H D] (sequence b: rows seq_start[b] ..,
-    at most max_new) over the kv_len[b] (at most max_len) cached tokens into
-    Out [T][H D]; lse [T][H] receives the log-sum-exp. key_mask uint8
-    [B][>= max_len]: 0 = not seen. scale: default 1 / sqrt(D). workspace:
-    default of this call's own, on its stream."""
+def _attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, key_mask, lse):
+    """What the attention calls have in common: (arguments up to max_len,
+    those from key_mask to mask_ld, those from Out to lse, sequences, heads)."""
     shape, B, D, dtype = Q.shape, kv_len.shape[0], cache.D, Q.dtype
     T = shape[0]
     H = shape[1] // D
@@ -744,16 +747,66 @@ def kv_cache_attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, ma
         mk, mld = _rows(key_mask, "key_mask")
         if key_mask.shape[1] < max_len:
             raise ValueError(f"starq expects key_mask rows of at least max_len = {max_len} bytes")
+    return ((q, ldq, _CODES[dtype], T, _ints("seq_start", seq_start, B + 1), B, max_new, H, cache.ref, pt, pld,
+             _ints("kv_len", kv_len, B), max_len), (mk, mld),
+            (o, ldo, None if lse is None else _f32("lse", lse, (T, H))), B, H)
+
+
+def kv_cache_attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, causal=False, key_mask=None,
+                       scale=None, lse=None, workspace=None, stream=None):
+    """Attention of the rows of Q [T][H D] (sequence b: rows seq_start[b] ..,
+    at most max_new) over the kv_len[b] (at most max_len) cached tokens into
+    Out [T][H D]; lse [T][H] receives the log-sum-exp. key_mask uint8
+    [B][>= max_len]: 0 = not seen. scale: default 1 / sqrt(D). workspace:
+    default of this call's own, on its stream."""
+    first, mask, out, B, H = _attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, key_mask, lse)
     if workspace is None:
-        size = lib.kv_cache_attention_workspace_size(B, max_new, H, cache.Hkv, D)
+        size = lib.kv_cache_attention_workspace_size(B, max_new, H, cache.Hkv, cache.D)
         workspace = _ws(size, Q.device, stream)
     else:
         size = workspace.numel() * workspace.element_size()
-    _check(lib.kv_cache_attention(q, ldq, _CODES[dtype], T, _ints("seq_start", seq_start, B + 1), B, max_new, H,
-                                  cache.ref, pt, pld, _ints("kv_len", kv_len, B), max_len, causal, mk, mld,
-                                  D ** -0.5 if scale is None else scale, o, ldo,
-                                  None if lse is None else _f32("lse", lse, (T, H)), workspace.data_ptr(), size,
-                                  _stream(stream)))
+    _check(lib.kv_cache_attention(*first, causal, *mask, cache.D ** -0.5 if scale is None else scale, *out,
+                                  workspace.data_ptr(), size, _stream(stream)))
+
+
+def kv_cache_attention_window(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, window, sinks=0,
+                              causal=False, key_mask=None, scale=None, lse=None, workspace=None, stream=None):
+    """kv_cache_attention in which a row at slot s sees, of the slots up to
+    its own, the last `window` (itself among them) and the first `sinks`.
+    Entries of page_table outside may be anything."""
+    first, mask, out, B, H = _attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, key_mask, lse)
+    if workspace is None:
+        size = lib.kv_cache_attention_workspace_size(B, max_new, H, cache.Hkv, cache.D)
+        workspace = _ws(size, Q.device, stream)
+    else:
+        size = workspace.numel() * workspace.element_size()
+    _check(lib.kv_cache_attention_window(*first, causal, window, sinks, *mask,
+                                         cache.D ** -0.5 if scale is None else scale, *out, workspace.data_ptr(), size,
+                                         _stream(stream)))
+
+
+def kv_cache_attention_shared_workspace_size(T, B, max_new, groups, max_rows, H, Hkv, D):
+    return int(lib.kv_cache_attention_shared_workspace_size(T, B, max_new, groups, max_rows, H, Hkv, D))
+
+
+def kv_cache_attention_shared(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, group_start, shared_len,
+                              max_rows, max_shared, causal=False, key_mask=None, scale=None, lse=None, workspace=None,
+                              stream=None):
+    """kv_cache_attention for groups of sequences with a common prefix, which
+    is read once: group g holds the sequences group_start[g] ..
+    group_start[g + 1] - 1, whose first shared_len[g] (at most max_shared)
+    tokens are in the same pages; at most max_rows rows of Q are a group's."""
+    first, mask, out, B, H = _attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, key_mask, lse)
+    groups = shared_len.shape[0]
+    if workspace is None:
+        size = lib.kv_cache_attention_shared_workspace_size(Q.shape[0], B, max_new, groups, max_rows, H, cache.Hkv, cache.D)
+        workspace = _ws(size, Q.device, stream)
+    else:
+        size = workspace.numel() * workspace.element_size()
+    _check(lib.kv_cache_attention_shared(*first, causal, _ints("group_start", group_start, groups + 1),
+                                         _ints("shared_len", shared_len, groups), groups, max_rows, max_shared, *mask,
+                                         cache.D ** -0.5 if scale is None else scale, *out, workspace.data_ptr(), size,
+                                         _stream(stream)))
 
 
 def w4g_linear(X, Wq, scales, Y, bias=None, stream=None):

@@ -61,6 +61,51 @@ int check_rows(const char* who, const char* name, const void* p, int ld, int wid
     return STARQ_OK;
 }
 
+// What the attention calls have in common. Fills *a unless there is nothing to do.
+int check_attention(const char* who, const void* Q, int ldq, int dtype, int T, const int32_t* seq_start, int B,
+                    int max_new, int H, const starq_kv_cache* cache, const int32_t* page_table, int table_ld,
+                    const int32_t* kv_len, int max_len, int causal, const uint8_t* key_mask, int mask_ld, float scale,
+                    void* Out, int ldo, float* lse, void* workspace, KvAttnArgs* a) {
+    int rc = check_cache(who, cache);
+    if (rc) return rc;
+    if (!half_type(dtype)) return fail(STARQ_ERR_ARG, "%s: dtype must be F16 or BF16", who);
+    if ((rc = check_sequences(who, T, B, max_new, table_ld))) return rc;
+    if (H < 1 || H > 65535 || H % cache->Hkv != 0)
+        return fail(STARQ_ERR_SHAPE, "%s: H=%d: need a multiple of Hkv=%d, at most 65535", who, H, cache->Hkv);
+    if ((long long)max_new * H > MAX_ROWS)
+        return fail(STARQ_ERR_SHAPE, "%s: max_new * H = %lld: at most 2^28", who, (long long)max_new * H);
+    if (max_len < 0 || max_len > MAX_ROWS) return fail(STARQ_ERR_SHAPE, "%s: max_len=%d: need 0 .. 2^28", who, max_len);
+    if (key_mask && mask_ld < max_len)
+        return fail(STARQ_ERR_SHAPE, "%s: mask_ld=%d is less than max_len=%d", who, mask_ld, max_len);
+    if (!(scale > 0.f) || !(scale < 1e30f)) return fail(STARQ_ERR_ARG, "%s: scale must be positive and finite", who);
+    if (T == 0 || B == 0 || max_new == 0) return STARQ_OK;
+    if ((rc = check_cache_pointers(who, cache))) return rc;
+    const int w = H * cache->D;
+    if ((rc = check_rows(who, "Q", Q, ldq, w, 2)) || (rc = check_rows(who, "Out", Out, ldo, w, 2))) return rc;
+    if (!seq_start || !kv_len || (!page_table && table_ld > 0) || !workspace)
+        return fail(STARQ_ERR_ARG, "%s: NULL seq_start, kv_len, page_table or workspace", who);
+    if (!aligned(seq_start, 4) || !aligned(kv_len, 4) || !aligned(page_table, 4) || !aligned(lse, 4) ||
+        !aligned(workspace, 256))
+        return fail(STARQ_ERR_ALIGN, "%s: index arrays and lse must be 4-byte aligned, workspace 256", who);
+    a->c = *cache;
+    a->Q = Q; a->ldq = ldq; a->dtype = dtype; a->T = T;
+    a->seq_start = seq_start; a->B = B; a->max_new = max_new; a->H = H;
+    a->page_table = page_table; a->table_ld = table_ld; a->kv_len = kv_len; a->max_len = max_len;
+    a->causal = causal != 0; a->key_mask = key_mask; a->mask_ld = mask_ld; a->scale = scale;
+    a->Out = Out; a->ldo = ldo; a->lse = lse; a->workspace = workspace;
+    return STARQ_OK;
+}
+
+template <typename F>
+int run_attention(const char* who, KvAttnArgs& a, size_t need, size_t workspace_bytes, F&& launch) {
+    if (workspace_bytes < need)
+        return fail(STARQ_ERR_ARG, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
+    int rc = STARQ_OK;
+    a.status = device_status(&rc);
+    if (!a.status) return rc;
+    return launched(launch(), who);
+}
+
 // What logits_apply_rules and logits_pick have in common, and their rules.
 int check_logits(const char* who, const void* X, int ldx, int dtype, int T, int V, const int32_t* seq_start, int B,
                  int max_new, const starq_logits_rules* rules, LogitsArgs* a) {
@@ -222,34 +267,69 @@ int kv_cache_attention(const void* Q, int ldq, int dtype, int T, const int32_t* 
                        int max_len, int causal, const uint8_t* key_mask, int mask_ld, float scale, void* Out, int ldo,
                        float* lse, void* workspace, size_t workspace_bytes, void* stream) {
     const char* who = "kv_cache_attention";
-    int rc = check_cache(who, cache);
+    KvAttnArgs a = {};
+    const int rc = check_attention(who, Q, ldq, dtype, T, seq_start, B, max_new, H, cache, page_table, table_ld, kv_len,
+                                   max_len, causal, key_mask, mask_ld, scale, Out, ldo, lse, workspace, &a);
+    if (rc || T == 0 || B == 0 || max_new == 0) return rc;
+    return run_attention(who, a, kv_attention_workspace_bytes(B, max_new, H, cache->Hkv, cache->D), workspace_bytes,
+                         [&] { return launch_kv_attention(a, static_cast<cudaStream_t>(stream)); });
+}
+
+int kv_cache_attention_window(const void* Q, int ldq, int dtype, int T, const int32_t* seq_start, int B, int max_new,
+                              int H, const starq_kv_cache* cache, const int32_t* page_table, int table_ld,
+                              const int32_t* kv_len, int max_len, int causal, int window, int sinks,
+                              const uint8_t* key_mask, int mask_ld, float scale, void* Out, int ldo, float* lse,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+    const char* who = "kv_cache_attention_window";
+    KvAttnArgs a = {};
+    if (window < 1 || window > MAX_ROWS || sinks < 0 || sinks > MAX_ROWS)
+        return fail(STARQ_ERR_SHAPE, "%s: window=%d, sinks=%d: need 1 <= window <= 2^28, 0 <= sinks <= 2^28", who, window,
+                    sinks);
+    const int rc = check_attention(who, Q, ldq, dtype, T, seq_start, B, max_new, H, cache, page_table, table_ld, kv_len,
+                                   max_len, causal, key_mask, mask_ld, scale, Out, ldo, lse, workspace, &a);
+    if (rc || T == 0 || B == 0 || max_new == 0) return rc;
+    a.window = window;
+    a.sinks = sinks;
+    return run_attention(who, a, kv_attention_workspace_bytes(B, max_new, H, cache->Hkv, cache->D), workspace_bytes,
+                         [&] { return launch_kv_attention_window(a, static_cast<cudaStream_t>(stream)); });
+}
+
+size_t kv_cache_attention_shared_workspace_size(int T, int B, int max_new, int groups, int max_rows, int H, int Hkv,
+                                                int D) {
+    if (T < 0 || T > MAX_ROWS || groups < 0 || groups > 65535 || max_rows < 0 || max_rows > MAX_ROWS ||
+        kv_cache_attention_workspace_size(B, max_new, H, Hkv, D) == 0)
+        return 0;
+    return kv_attention_shared_workspace_bytes(T, B, max_new, groups, max_rows, H, Hkv, D);
+}
+
+int kv_cache_attention_shared(const void* Q, int ldq, int dtype, int T, const int32_t* seq_start, int B, int max_new,
+                              int H, const starq_kv_cache* cache, const int32_t* page_table, int table_ld,
+                              const int32_t* kv_len, int max_len, int causal, const int32_t* group_start,
+                              const int32_t* shared_len, int groups, int max_rows, int max_shared,
+                              const uint8_t* key_mask, int mask_ld, float scale, void* Out, int ldo, float* lse,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+    const char* who = "kv_cache_attention_shared";
+    KvAttnArgs a = {};
+    if (groups < 0 || groups > 65535 || max_rows < 0 || max_rows > MAX_ROWS || max_shared < 0 || max_shared > MAX_ROWS)
+        return fail(STARQ_ERR_SHAPE, "%s: groups=%d, max_rows=%d, max_shared=%d: need 0 <= groups <= 65535, "
+                    "0 <= max_rows, max_shared <= 2^28", who, groups, max_rows, max_shared);
+    const int rc = check_attention(who, Q, ldq, dtype, T, seq_start, B, max_new, H, cache, page_table, table_ld, kv_len,
+                                   max_len, causal, key_mask, mask_ld, scale, Out, ldo, lse, workspace, &a);
     if (rc) return rc;
-    if (!half_type(dtype)) return fail(STARQ_ERR_ARG, "%s: dtype must be F16 or BF16", who);
-    if ((rc = check_sequences(who, T, B, max_new, table_ld))) return rc;
-    if (H < 1 || H > 65535 || H % cache->Hkv != 0)
-        return fail(STARQ_ERR_SHAPE, "%s: H=%d: need a multiple of Hkv=%d, at most 65535", who, H, cache->Hkv);
-    if ((long long)max_new * H > MAX_ROWS)
-        return fail(STARQ_ERR_SHAPE, "%s: max_new * H = %lld: at most 2^28", who, (long long)max_new * H);
-    if (max_len < 0 || max_len > MAX_ROWS) return fail(STARQ_ERR_SHAPE, "%s: max_len=%d: need 0 .. 2^28", who, max_len);
-    if (key_mask && mask_ld < max_len)
-        return fail(STARQ_ERR_SHAPE, "%s: mask_ld=%d is less than max_len=%d", who, mask_ld, max_len);
-    if (!(scale > 0.f) || !(scale < 1e30f)) return fail(STARQ_ERR_ARG, "%s: scale must be positive and finite", who);
+    if ((long long)max_rows * H > MAX_ROWS)
+        return fail(STARQ_ERR_SHAPE, "%s: max_rows * H = %lld: at most 2^28", who, (long long)max_rows * H);
+    if (key_mask && mask_ld < max_shared)
+        return fail(STARQ_ERR_SHAPE, "%s: mask_ld=%d is less than max_shared=%d", who, mask_ld, max_shared);
     if (T == 0 || B == 0 || max_new == 0) return STARQ_OK;
-    if ((rc = check_cache_pointers(who, cache))) return rc;
-    const int w = H * cache->D;
-    if ((rc = check_rows(who, "Q", Q, ldq, w, 2)) || (rc = check_rows(who, "Out", Out, ldo, w, 2))) return rc;
-    if (!seq_start || !kv_len || (!page_table && table_ld > 0) || !workspace)
-        return fail(STARQ_ERR_ARG, "%s: NULL seq_start, kv_len, page_table or workspace", who);
-    if (!aligned(seq_start, 4) || !aligned(kv_len, 4) || !aligned(page_table, 4) || !aligned(lse, 4) ||
-        !aligned(workspace, 256))
-        return fail(STARQ_ERR_ALIGN, "%s: index arrays and lse must be 4-byte aligned, workspace 256", who);
-    const size_t need = kv_attention_workspace_bytes(B, max_new, H, cache->Hkv, cache->D);
-    if (workspace_bytes < need)
-        return fail(STARQ_ERR_ARG, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
-    KvAttnArgs a{*cache, Q, ldq, dtype, T, seq_start, B, max_new, H, page_table, table_ld, kv_len, max_len,
-                 causal != 0, key_mask, mask_ld, scale, Out, ldo, lse, workspace, device_status(&rc)};
-    if (!a.status) return rc;
-    return launched(launch_kv_attention(a, static_cast<cudaStream_t>(stream)), who);
+    if (groups > 0 && (!group_start || !shared_len)) return fail(STARQ_ERR_ARG, "%s: NULL group_start or shared_len", who);
+    if (!aligned(group_start, 4) || !aligned(shared_len, 4))
+        return fail(STARQ_ERR_ALIGN, "%s: index arrays must be 4-byte aligned", who);
+    a.groups = groups;
+    a.group_start = group_start;
+    a.shared_len = shared_len;
+    return run_attention(who, a, kv_attention_shared_workspace_bytes(T, B, max_new, groups, max_rows, H, cache->Hkv, cache->D),
+                         workspace_bytes,
+                         [&] { return launch_kv_attention_shared(a, max_rows, max_shared, static_cast<cudaStream_t>(stream)); });
 }
 
 int w4g_linear(const void* X, int ldx, int dtype, int L, int K, const uint8_t* Wq, const float* scales, int group,

@@ -60,9 +60,19 @@ struct KvAttnArgs {
     void* workspace;
     unsigned* status;
     int whole;                       // units are not cut (set by the launcher)
+    int likely_len;                  // keys of a sequence that are looked at, as the host expects (chooses kernels)
+    // KV_WINDOW: row i sees the slots below `sinks` and the last `window` up to its own
+    int window; int sinks;
+    // KV_SPLIT: rows of a group over the slots that its sequences share (prefix; B counts the groups), or of a sequence
+    // over its other slots. Nothing is written but sums: of whole units to `sums`, [T][H][D], then the (m, l) of each.
+    int prefix; int sequences; int groups; const int32_t* group_start; const int32_t* shared_len;
+    float* sums;
 };
 size_t kv_attention_workspace_bytes(int B, int max_new, int H, int Hkv, int D);
 cudaError_t launch_kv_attention(const KvAttnArgs& a, cudaStream_t s);
+cudaError_t launch_kv_attention_window(const KvAttnArgs& a, cudaStream_t s);
+size_t kv_attention_shared_workspace_bytes(int T, int B, int max_new, int groups, int max_rows, int H, int Hkv, int D);
+cudaError_t launch_kv_attention_shared(const KvAttnArgs& a, int max_rows, int max_shared, cudaStream_t s);
 
 struct W4gArgs {
     const void* X; int ldx; int dtype; int L; int K;

@@ -160,7 +160,7 @@ struct AttnSmem {
 // above, both forms with the keys' offset and two stages): four long sequences
 // 77.7 us for 86.0, one of 777 tokens 8.5 for 12.2, 64 of up to 1000 tokens
 // 19.7 for 28.
-template <typename T, int D, bool NARROW>
+template <typename T, int D, bool NARROW, int FORM>
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_kernel(const KvAttnArgs a, int G, long long* prefix_out,
                                                                  float* slots) {
     using SM = AttnSmem<T, D, NARROW>;
@@ -171,11 +171,11 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
 
     grid_dependency_wait();
-    const Run run = find_run<ROWS, TILE, THREADS>(a, G, prefix_out);
+    const Run run = find_run<ROWS, TILE, THREADS, FORM>(a, G, prefix_out);
     if (run.tau0 >= run.tau1) return;
-    Cursor<ROWS, TILE> cur;
+    Cursor<ROWS, TILE, FORM> cur;
     cur.start(a, G, run);
-    Cursor<ROWS, TILE> pre = cur;
+    Cursor<ROWS, TILE, FORM> pre = cur;
     int left = cur.tiles(a, G, run);         // tiles of the run
     int pre_left = left;                     // tiles still to be fetched
 
@@ -192,11 +192,13 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
         if (pre_left > 0) {
             #pragma unroll
             for (int blk16 = 0; blk16 < WKEYS / 16; ++blk16) {
-                const int key0 = pre.kt * TILE + warp * WKEYS + 16 * blk16;
-                if (key0 < pre.s.len) {
+                const int key0 = pre.slot0() + warp * WKEYS + 16 * blk16;
+                // (blocks before the window of every row are not looked at: they may have no page any more)
+                const bool met = FORM == KV_PLAIN || key0 + 16 > pre.low || (FORM == KV_WINDOW && key0 < a.sinks);
+                if (key0 < pre.s.len && met) {
                     const int page_i = key0 >> shift;
                     int page = -1;
-                    if (page_i < a.table_ld) page = __ldg(a.page_table + (size_t)pre.b * a.table_ld + page_i);
+                    if (page_i < a.table_ld) page = __ldg(a.page_table + (size_t)pre.s.at * a.table_ld + page_i);
                     const uint32_t dst = ring + slot * SM::STAGE, dst_s = dst + 2 * WKEYS * D + 8 * blk16;
                     if (page < 0 || page >= a.c.pages) {
                         if (lane == 0) {
@@ -231,7 +233,9 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
     constexpr int OT = NARROW ? DN / 2 : DN; // tiles of the accumulators
     uint32_t qb[NARROW ? KH : 1][4][2];      // NARROW: the query fragments
     float o[OT][4], m[2], l[2], rs[2];
-    int lim[2];                              // keys [0, lim) are visible to the rows (causal limit and length)
+    int lim[2];                              // keys [0, lim) are visible to the rows (causal limit and length),
+    int low[2];                              // those below low only if they are first slots
+    int low_most = 0;                        // low of the unit's last row
     const float unit_scale = a.scale * 1.4426950408889634f;
     bool fresh = true;
     int seg_kt0 = cur.kt;
@@ -247,11 +251,12 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
                 for (int k = 0; k < (NARROW ? 1 : 2); ++k) {
                     const int r = cur.rt * ROWS + g + 8 * k, i = r / G, j = r - i * G;
                     const T* row = nullptr;
-                    lim[k] = 0;
+                    lim[k] = low[k] = 0;
                     if (i < cur.s.n) {
                         row = static_cast<const T*>(a.Q) + (size_t)(cur.s.row0 + i) * a.ldq +
                               (size_t)(cur.h * G + j) * D;
                         lim[k] = a.causal ? max(0, cur.s.len - cur.s.n + i + 1) : cur.s.len;
+                        low[k] = low_of<FORM>(a, cur.s, i);
                     }
                     rs[k] = load_row<T, D>(row, t, q2[k]);
                 }
@@ -263,11 +268,12 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
                         #pragma unroll
                         for (int s = 0; s < 4; ++s) { qb[h][s][0] = q2[0][h][s][0]; qb[h][s][1] = q2[0][h][s][1]; }
                     const float r = rs[0];
-                    const int v = lim[0];
+                    const int v = lim[0], w = low[0];
                     #pragma unroll
                     for (int k = 0; k < 2; ++k) {           // from the threads of row g = 2t + k
                         rs[k] = __shfl_sync(0xffffffffu, r, 4 * (2 * t + k));
                         lim[k] = __shfl_sync(0xffffffffu, v, 4 * (2 * t + k));
+                        if (FORM != KV_PLAIN) low[k] = __shfl_sync(0xffffffffu, w, 4 * (2 * t + k));
                     }
                 } else {
                 // every warp has the fragments; each stores its part of them for all
@@ -284,19 +290,20 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
                 for (int j = 0; j < OT; ++j)
                     #pragma unroll
                     for (int k = 0; k < 4; ++k) o[j][k] = 0.f;
+                if (FORM != KV_PLAIN) low_most = low_of<FORM>(a, cur.s, min(cur.s.n - 1, (cur.rt * ROWS + ROWS - 1) / G));
                 fresh = false;
                 seg_kt0 = cur.kt;
             }
             fetch((st + STAGES<NARROW> - 1) % STAGES<NARROW>);
             cp_async_wait<STAGES<NARROW> - 1>();
             __syncwarp();
-            const int key0 = cur.kt * TILE + warp * WKEYS;
-            if (key0 < cur.s.len) {
+            const int key0 = cur.slot0() + warp * WKEYS;
+            if (key0 < cur.s.len && (FORM == KV_PLAIN || key0 + WKEYS > cur.low || (FORM == KV_WINDOW && key0 < a.sinks))) {
                 // one byte a lane, on its way beside the scores (a byte for each score took 59 us for 42 where 55
                 // sequences of 8 heads and up to 575 tokens have 64 rows)
                 uint8_t mask_byte = 1;
                 if (a.key_mask != nullptr && key0 + lane < cur.s.len)
-                    mask_byte = __ldg(a.key_mask + (size_t)cur.b * a.mask_ld + key0 + lane);
+                    mask_byte = __ldg(a.key_mask + (size_t)cur.s.at * a.mask_ld + key0 + lane);
                 const uint8_t* stage = smem + warp * (STAGES<NARROW> * SM::STAGE) + st * SM::STAGE;
                 // --- scores of 32 keys: four column tiles, a k step for all of them ---
                 constexpr int XT = NARROW ? 2 : 4;           // tiles: NARROW 16 keys x 8 rows, else 16 rows x 8 keys
@@ -351,7 +358,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
                         for (int k = 0; k < 4; ++k) x[nt][k] = fmaf(x[nt][k], row_of(k) ? k1 : k0, lv);
                 }
                 const bool edge = key0 + WKEYS > cur.s.len || a.key_mask != nullptr ||
-                                  (a.causal && key0 + WKEYS > cur.s.len - cur.s.n + 1);
+                                  (a.causal && key0 + WKEYS > causal_edge<ROWS, FORM>(cur.s, G, cur.rt)) ||
+                                  (FORM != KV_PLAIN && key0 < low_most && (FORM != KV_WINDOW || key0 + WKEYS > a.sinks));
                 unsigned seen = 0xffff;      // bit 4 nt + k: x[nt][k] counts
                 if (edge) {
                     const unsigned live = __ballot_sync(0xffffffffu, mask_byte != 0);       // bit i: key key0 + i
@@ -361,7 +369,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
                         #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const int key = key0 + key_of(nt, k);
-                            const bool ok = key < lim[row_of(k)] && (live >> key_of(nt, k) & 1);
+                            bool ok = key < lim[row_of(k)] && (live >> key_of(nt, k) & 1);
+                            if (FORM != KV_PLAIN) ok &= key >= low[row_of(k)] || (FORM == KV_WINDOW && key < a.sinks);
                             if (ok) seen |= 1u << (4 * nt + k);
                             else x[nt][k] = NEG_INF;
                         }
@@ -530,7 +539,16 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
                 }
                 __syncthreads();
                 const bool whole = seg_kt0 == 0 && cur.kt == cur.s.nt;
-                if (whole) {
+                if (whole && FORM == KV_SPLIT) {
+                    for (int e = tid; e < HELD * (D / 4); e += THREADS) {
+                        const int r = e / (D / 4), c = e % (D / 4);
+                        const int rr = cur.rt * ROWS + r, i = rr / G, j = rr - i * G;
+                        if (i >= cur.s.n) continue;
+                        const size_t to = (size_t)(cur.s.row0 + i) * a.H + cur.h * G + j;
+                        reinterpret_cast<float4*>(a.sums + to * D)[c] = reinterpret_cast<const float4*>(buf + r * D)[c];
+                        if (c == 0) reinterpret_cast<float2*>(a.sums + (size_t)a.T * a.H * D)[to] = ml[r];
+                    }
+                } else if (whole) {
                     for (int e = tid; e < HELD * (D / 8); e += THREADS) {
                         const int r = e / (D / 8), c = e % (D / 8);
                         const int rr = cur.rt * ROWS + r, i = rr / G, j = rr - i * G;
@@ -563,8 +581,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
     cp_async_wait<0>();
 }
 
-template <typename T, int D, bool NARROW>
-cudaError_t launch_rows(const KvAttnArgs& args, cudaStream_t s) {
+template <typename T, int D, bool NARROW, int FORM>
+cudaError_t launch_rows(const KvAttnArgs& args, KvCut* cut, cudaStream_t s) {
     const int ctas = num_sms() * CTAS_PER_SM<NARROW>;
     KvAttnArgs a = args;
     a.whole = whole_units(a, ROWS, TILE, ctas);
@@ -573,21 +591,24 @@ cudaError_t launch_rows(const KvAttnArgs& args, cudaStream_t s) {
     int dummy = 0;
     cudaError_t e = ready.get(&dummy, [](int, int* v) {
         *v = 1;
-        return cudaFuncSetAttribute(kv_attention_kernel<T, D, NARROW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        return cudaFuncSetAttribute(kv_attention_kernel<T, D, NARROW, FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                     AttnSmem<T, D, NARROW>::BYTES);
     });
     if (e != cudaSuccess) return e;
     long long* prefix = static_cast<long long*>(a.workspace);
     float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + prefix_bytes(a.B));
-    if ((e = launch_overlapped(kv_attention_kernel<T, D, NARROW>, dim3(ctas), THREADS, AttnSmem<T, D, NARROW>::BYTES, s,
-                               a, G, prefix, slots)) != cudaSuccess || a.whole)
+    if (cut) *cut = KvCut{ctas, ROWS, ROWS, a.whole, prefix, slots};
+    if ((e = launch_overlapped(kv_attention_kernel<T, D, NARROW, FORM>, dim3(ctas), THREADS,
+                               AttnSmem<T, D, NARROW>::BYTES, s, a, G, prefix, slots)) != cudaSuccess || a.whole ||
+        FORM == KV_SPLIT)
         return e;
-    return launch_join<T, D, ROWS, TILE>(a, G, ctas, ROWS, prefix, slots, s);
+    return launch_join<T, D, ROWS, TILE, FORM>(a, G, ctas, ROWS, prefix, slots, s);
 }
 
-template <typename T, int D>
-cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
-    return a.max_new * (a.H / a.c.Hkv) <= 8 ? launch_rows<T, D, true>(a, s) : launch_rows<T, D, false>(a, s);
+template <typename T, int D, int FORM>
+cudaError_t launch_typed(const KvAttnArgs& a, KvCut* cut, cudaStream_t s) {
+    return (long long)a.max_new * (a.H / a.c.Hkv) <= 8 ? launch_rows<T, D, true, FORM>(a, cut, s)
+                                                       : launch_rows<T, D, false, FORM>(a, cut, s);
 }
 
 }  // namespace
@@ -610,10 +631,10 @@ cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
 // Where it errs: up to 32 rows of hundreds of units (440 of 2000 tokens, 24
 // rows: 53 / 84 with heads of 64, 92 / 119 with heads of 128) go to the slower
 // kernel, and 64 rows of 64 units of 1000 tokens with heads of 128 (27 / 29).
-static bool warp_kernel(const KvAttnArgs& a) {
+bool kv_attention_by_warps(const KvAttnArgs& a) {
     const long long rows = (long long)a.max_new * (a.H / a.c.Hkv), tiles = (rows + ROWS - 1) / ROWS;
     if (tiles <= 1) return true;
-    return tiles <= 4 && tiles * a.B * a.c.Hkv * (long long)a.max_len <= (a.c.D == 64 ? 1 << 20 : 1 << 18) >> (tiles == 4);
+    return tiles <= 4 && tiles * a.B * a.c.Hkv * (long long)a.likely_len <= (a.c.D == 64 ? 1 << 20 : 1 << 18) >> (tiles == 4);
 }
 
 // Enough for either kernel, since max_len may change from call to call.
@@ -624,11 +645,30 @@ size_t kv_attention_workspace_bytes(int B, int max_new, int H, int Hkv, int D) {
     return prefix_bytes(B) + slots;
 }
 
-cudaError_t launch_kv_attention(const KvAttnArgs& a, cudaStream_t s) {
-    if (!warp_kernel(a)) return launch_kv_attention_tc(a, s);
+template <int FORM>
+cudaError_t launch_kv_attention_warp(const KvAttnArgs& a, KvCut* cut, cudaStream_t s) {
     if (a.dtype == STARQ_BF16)
-        return a.c.D == 64 ? launch_typed<__nv_bfloat16, 64>(a, s) : launch_typed<__nv_bfloat16, 128>(a, s);
-    return a.c.D == 64 ? launch_typed<__half, 64>(a, s) : launch_typed<__half, 128>(a, s);
+        return a.c.D == 64 ? launch_typed<__nv_bfloat16, 64, FORM>(a, cut, s)
+                           : launch_typed<__nv_bfloat16, 128, FORM>(a, cut, s);
+    return a.c.D == 64 ? launch_typed<__half, 64, FORM>(a, cut, s) : launch_typed<__half, 128, FORM>(a, cut, s);
+}
+template cudaError_t launch_kv_attention_warp<KV_SPLIT>(const KvAttnArgs&, KvCut*, cudaStream_t);
+
+cudaError_t launch_kv_attention(const KvAttnArgs& args, cudaStream_t s) {
+    KvAttnArgs a = args;
+    a.likely_len = a.max_len;
+    return kv_attention_by_warps(a) ? launch_kv_attention_warp<KV_PLAIN>(a, nullptr, s)
+                                    : launch_kv_attention_tc<KV_PLAIN>(a, nullptr, s);
+}
+
+// Attention with a window: no more slots are looked at than the first ones and
+// those that the windows of the new tokens reach.
+cudaError_t launch_kv_attention_window(const KvAttnArgs& args, cudaStream_t s) {
+    KvAttnArgs a = args;
+    const long long reach = (long long)a.sinks + a.window + (a.causal ? std::min(a.max_new, 256) : a.max_new);
+    a.likely_len = (int)std::min<long long>(a.max_len, reach);
+    return kv_attention_by_warps(a) ? launch_kv_attention_warp<KV_WINDOW>(a, nullptr, s)
+                                    : launch_kv_attention_tc<KV_WINDOW>(a, nullptr, s);
 }
 
 }  // namespace starq

@@ -11,6 +11,11 @@
 // unit) or 2 c + 1 (it ends in it), the rows' accumulators, maxima and sums.
 // Where the sequences are short by their bound, the units themselves are
 // dealt out instead (`whole`), and there is nothing to join.
+//
+// Forms. KV_WINDOW: the tiles that no row of a unit sees, between the first
+// slots and its window, are not in its list. KV_SPLIT: the lists of a group's
+// prefix, whose rows are those of all its sequences, or of what a sequence
+// has behind it; the rows' sums of both go to a join of their own.
 #pragma once
 
 #include <algorithm>
@@ -59,32 +64,92 @@ __device__ __forceinline__ long long quotient(long long a, int b) {
     return a < (1ll << 31) ? (long long)((unsigned)a / (unsigned)b) : a / b;
 }
 
-struct SeqShape { int len, n, row0, nt, rt; };       // cached tokens, new tokens, first row, key tiles, row tiles
+enum KvForm { KV_PLAIN, KV_WINDOW, KV_SPLIT };
 
-// The lengths of sequence b; a sequence whose numbers do not fit their
-// bounds counts as having no rows.
-template <int ROWS, int TILE>
+struct SeqShape {
+    int len, n, row0, nt, rt;          // cached tokens, new tokens, first row, key tiles, row tiles
+    int at;                            // the sequence whose pages and key mask are read
+    int low;                           // KV_SPLIT: the first slot that is seen
+    int sink_tiles;                    // KV_WINDOW: tiles with first slots, before those of a window
+};
+
+// The group of sequence b: the last one that begins with or before it; -1 if
+// b stands outside all groups.
+__device__ __forceinline__ int group_of(const KvAttnArgs& a, int b) {
+    int lo = 0, hi = a.groups;                                // group_start[lo - 1] <= b < group_start[hi + 1]
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (__ldg(a.group_start + mid) <= b) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo == a.groups || __ldg(a.group_start + lo) > b ? -1 : lo;
+}
+
+// The lengths of sequence b (KV_SPLIT with prefix: of group b); a sequence
+// whose numbers do not fit their bounds counts as having no rows.
+template <int ROWS, int TILE, int FORM>
 __device__ __forceinline__ SeqShape seq_shape(const KvAttnArgs& a, int G, int b, bool report) {
     SeqShape s;
-    s.row0 = __ldg(a.seq_start + b);
-    s.n = __ldg(a.seq_start + b + 1) - s.row0;
-    s.len = __ldg(a.kv_len + b);
-    const bool bad = s.n < 0 || s.n > a.max_new || s.row0 < 0 || s.row0 > a.T - s.n || s.len < 0 || s.len > a.max_len;
+    s.at = b;
+    s.low = s.sink_tiles = 0;
+    bool bad;
+    if (FORM == KV_SPLIT && a.prefix) {
+        const int s0 = __ldg(a.group_start + b), s1 = __ldg(a.group_start + b + 1);
+        bad = s0 < 0 || s1 < s0 || s1 > a.sequences;
+        s.at = bad ? 0 : s0;
+        s.row0 = bad ? 0 : __ldg(a.seq_start + s0);
+        s.n = bad ? 0 : __ldg(a.seq_start + s1) - s.row0;
+        s.len = __ldg(a.shared_len + b);
+    } else {
+        s.row0 = __ldg(a.seq_start + b);
+        s.n = __ldg(a.seq_start + b + 1) - s.row0;
+        s.len = __ldg(a.kv_len + b);
+        bad = false;
+    }
+    bad |= s.n < 0 || s.n > a.max_new || s.row0 < 0 || s.row0 > a.T - s.n || s.len < 0 || s.len > a.max_len;
+    if (FORM == KV_SPLIT && !a.prefix) {
+        const int g = group_of(a, b);
+        if (g >= 0) s.low = __ldg(a.shared_len + g);
+        bad |= s.low < 0 || (s.low > 0 && s.low > s.len - s.n);      // the new tokens are not shared
+    }
     if (bad) {
         if (report) atomicOr(a.status, STATUS_RANGE);
-        s.n = 0; s.len = 0; s.row0 = 0;
+        s.n = 0; s.len = 0; s.row0 = 0; s.low = 0;
+    }
+    int nt = (s.len + TILE - 1) / TILE;
+    if (FORM == KV_SPLIT) nt -= s.low / TILE;
+    if (FORM == KV_WINDOW) {
+        s.sink_tiles = min((min(a.sinks, s.len) + TILE - 1) / TILE, nt);
+        nt -= max(0, max(0, s.len - s.n - a.window + 1) / TILE - s.sink_tiles);
+        // A row tile holds the rows of up to `tokens` tokens, whose windows together are window + tokens - 1 slots.
+        const int tokens = (ROWS + G - 1) / G + 1;
+        if (a.causal) nt = min(nt, s.sink_tiles + (a.window + tokens + 2 * TILE - 3) / TILE);
     }
     // (a whole unit without keys has a tile all the same: its CTA writes its rows)
-    s.nt = s.n > 0 ? max((s.len + TILE - 1) / TILE, a.whole) : 0;
+    s.nt = s.n > 0 ? max(nt, a.whole) : 0;
     s.rt = (s.n * G + ROWS - 1) / ROWS;
     return s;
+}
+
+// Slots from this one on are hidden from some row of a row tile by the causal
+// limit (the first token's; with KV_PLAIN the sequence's).
+template <int ROWS, int FORM>
+__device__ __forceinline__ int causal_edge(const SeqShape& s, int G, int rt) {
+    return s.len - s.n + (FORM == KV_WINDOW ? rt * ROWS / G : 0) + 1;
+}
+
+// Lowest slot of row i's window (and of KV_SPLIT's part).
+template <int FORM>
+__device__ __forceinline__ int low_of(const KvAttnArgs& a, const SeqShape& s, int i) {
+    if (FORM == KV_WINDOW) return max(0, s.len - s.n + i - a.window + 1);
+    return FORM == KV_SPLIT ? s.low : 0;
 }
 
 // This CTA's run [tau0, tau1) of the flat list of tiles (whole: of units), the
 // sequence that tau0 falls into and the tiles (units) before that sequence.
 // CTA 0 writes `prefix`.
 struct Run { long long tau0, tau1, before; int b; };
-template <int ROWS, int TILE, int THREADS>
+template <int ROWS, int TILE, int THREADS, int FORM>
 __device__ __forceinline__ Run find_run(const KvAttnArgs& a, int G, long long* prefix) {
     constexpr int WARPS = THREADS / 32;
     __shared__ long long s_part[WARPS], s_before;
@@ -92,7 +157,7 @@ __device__ __forceinline__ Run find_run(const KvAttnArgs& a, int G, long long* p
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     auto tiles_of = [&](int b, bool report) {
         if (b >= a.B) return 0ll;
-        const SeqShape s = seq_shape<ROWS, TILE>(a, G, b, report);
+        const SeqShape s = seq_shape<ROWS, TILE, FORM>(a, G, b, report);
         return (long long)(a.whole ? s.nt > 0 : s.nt) * s.rt * a.c.Hkv;
     };
     if (a.B <= 32) {                                          // every warp by itself, without barriers
@@ -170,28 +235,40 @@ __device__ __forceinline__ Run find_run(const KvAttnArgs& a, int G, long long* p
 }
 
 // Position in the flat list of tiles: sequence, head, row tile, key tile.
-template <int ROWS, int TILE>
+template <int ROWS, int TILE, int FORM>
 struct Cursor {
     int b, h, rt, kt;
+    int low, gap;                                             // first slot of the row tile's windows, tiles left out
     SeqShape s;
+    __device__ __forceinline__ void look(const KvAttnArgs& a, int G) {
+        if (FORM == KV_PLAIN) return;
+        low = low_of<FORM>(a, s, rt * ROWS / G);
+        gap = max(0, low / TILE - s.sink_tiles);
+    }
+    // First slot of the current key tile.
+    __device__ __forceinline__ int slot0() const {
+        return (FORM == KV_PLAIN || kt < s.sink_tiles ? kt : kt + gap) * TILE;
+    }
     __device__ __forceinline__ void start(const KvAttnArgs& a, int G, const Run& r) {
         b = r.b;
-        s = seq_shape<ROWS, TILE>(a, G, b, false);
+        s = seq_shape<ROWS, TILE, FORM>(a, G, b, false);
         const long long off = r.tau0 - r.before, unit = a.whole ? off : quotient(off, s.nt);
         kt = a.whole ? 0 : (int)(off - unit * s.nt);
         h = (int)quotient(unit, s.rt);
         rt = (int)(unit - (long long)h * s.rt);
+        look(a, G);
     }
     __device__ __forceinline__ void next_unit(const KvAttnArgs& a, int G) {
         kt = 0;
-        if (++rt < s.rt) return;
+        if (++rt < s.rt) { look(a, G); return; }
         rt = 0;
-        if (++h < a.c.Hkv) return;
+        if (++h < a.c.Hkv) { look(a, G); return; }
         h = 0;
         do {
             if (++b >= a.B) return;
-            s = seq_shape<ROWS, TILE>(a, G, b, false);
+            s = seq_shape<ROWS, TILE, FORM>(a, G, b, false);
         } while (s.nt == 0);
+        look(a, G);
     }
     // Tiles of the run that begins here.
     __device__ __forceinline__ int tiles(const KvAttnArgs& a, int G, const Run& r) const {
@@ -215,7 +292,7 @@ struct Cursor {
 // tokens 21.5 / 19.7; 32 rows of them, 8 sequences, 250 tokens 20.9 / 18.6,
 // 500 tokens 21.9 / 23.4 (cut); 32 sequences, 500 tokens 48 / 24.8.
 inline bool whole_units(const KvAttnArgs& a, int rows, int tile, int ctas) {
-    const long long t = std::max(1, (a.max_len + tile - 1) / tile);
+    const long long t = std::max(1, (a.likely_len + tile - 1) / tile);
     const long long n = ((long long)a.max_new * (a.H / a.c.Hkv) + rows - 1) / rows * a.B * a.c.Hkv;      // units
     return t <= 8 && t * ((n + ctas - 1) / ctas) * ctas <= std::max<long long>(ctas, n * t) + 2 * ctas + 4 * n;
 }
@@ -227,7 +304,7 @@ inline bool whole_units(const KvAttnArgs& a, int rows, int tile, int ctas) {
 // order, AT_ONCE of them on their way together, and the warps' sums are added
 // in warp order.
 constexpr int JOIN_WARPS = 8;
-template <typename T, int D, int ROWS, int TILE, int SHARE>
+template <typename T, int D, int ROWS, int TILE, int FORM, int SHARE>
 __global__ void __launch_bounds__(JOIN_WARPS * 32)
 kv_attention_join_kernel(const KvAttnArgs a, int G, int ctas, int slot_rows, const long long* prefix,
                          const float* slots) {
@@ -237,7 +314,7 @@ kv_attention_join_kernel(const KvAttnArgs a, int G, int ctas, int slot_rows, con
     grid_dependency_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % SHARE;
     const int b = blockIdx.y;
-    const SeqShape s = seq_shape<ROWS, TILE>(a, G, b, false);
+    const SeqShape s = seq_shape<ROWS, TILE, FORM>(a, G, b, false);
     const long long total = prefix[a.B], before = prefix[b];
     const int idx = blockIdx.x * (JOIN_WARPS / SHARE) + warp / SHARE;      // token * H + head
     const int i = idx / a.H, head = idx - i * a.H;
@@ -332,23 +409,33 @@ kv_attention_join_kernel(const KvAttnArgs a, int G, int ctas, int slot_rows, con
         a.lse[row * a.H + head] = l == 0.f ? NEG_INF : (log2f(l) + (top - HEAD)) * 0.6931471805599453f;
 }
 
-template <typename T, int D, int ROWS, int TILE>
+template <typename T, int D, int ROWS, int TILE, int FORM>
 cudaError_t launch_join(const KvAttnArgs& a, int G, int ctas, int slot_rows, const long long* prefix,
                         const float* slots, cudaStream_t s) {
     const size_t rows = (size_t)a.max_new * a.H;
     if (rows * a.B <= 4 * (size_t)num_sms())              // up to four CTAs an SM
-        return launch_overlapped(kv_attention_join_kernel<T, D, ROWS, TILE, JOIN_WARPS>,
+        return launch_overlapped(kv_attention_join_kernel<T, D, ROWS, TILE, FORM, JOIN_WARPS>,
                                  dim3((unsigned)rows, (unsigned)a.B), JOIN_WARPS * 32, 0, s, a, G, ctas, slot_rows,
                                  prefix, slots);
-    return launch_overlapped(kv_attention_join_kernel<T, D, ROWS, TILE, 1>,
+    return launch_overlapped(kv_attention_join_kernel<T, D, ROWS, TILE, FORM, 1>,
                              dim3((unsigned)((rows + JOIN_WARPS - 1) / JOIN_WARPS), (unsigned)a.B), JOIN_WARPS * 32, 0,
                              s, a, G, ctas, slot_rows, prefix, slots);
 }
 
 }  // namespace
 
+// How a pass of KV_SPLIT was cut, for the join of the two.
+struct KvCut {
+    int ctas, rows, slot_rows, whole;
+    const long long* prefix;
+    const float* slots;
+};
+
 // kvattn_tc.cu
 size_t kv_attention_tc_slot_bytes(int max_rows, int D);
-cudaError_t launch_kv_attention_tc(const KvAttnArgs& a, cudaStream_t s);
+template <int FORM> cudaError_t launch_kv_attention_tc(const KvAttnArgs& a, KvCut* cut, cudaStream_t s);
+// kvattn.cu
+template <int FORM> cudaError_t launch_kv_attention_warp(const KvAttnArgs& a, KvCut* cut, cudaStream_t s);
+bool kv_attention_by_warps(const KvAttnArgs& a);
 
 }  // namespace starq

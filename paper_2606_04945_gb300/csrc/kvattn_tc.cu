@@ -64,7 +64,7 @@ struct TileInfo {                                  // what the other warps need 
     float inv[TILE];                               // 1 / s_v for each key, 0 for one that is not seen
     uint32_t seen[4];                              // bit b of word j: key 4 b + j is seen
     uint32_t met;                                  // bit b: some key of block b is seen
-    int key0, edge;                                // first key; whether the causal boundary is inside
+    int key0, edge;                                // first key; whether a row's boundary is inside
 };
 
 struct Shared {
@@ -180,11 +180,11 @@ __device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
 
-template <typename T, int D>
+template <typename T, int D, int FORM>
 __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAttnArgs a, int G, int slot_rows,
                                                                     long long* prefix, float* slots) {
     using L = Layout<D>;
-    using Cur = Cursor<ROWS, TILE>;
+    using Cur = Cursor<ROWS, TILE, FORM>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t* smem = smem_raw + (base - raw);
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
     tc_fence_after();
     const uint32_t tmem = sh->tmem_base;
     grid_dependency_wait();
-    const Run run = find_run<ROWS, TILE, THREADS>(a, G, prefix);
+    const Run run = find_run<ROWS, TILE, THREADS, FORM>(a, G, prefix);
 
     // Every role walks the run segment by segment (a segment is the run's
     // part of one unit). In a segment of n key tiles the streams' steps are
@@ -261,9 +261,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
             if (--left > 0 && ++q.kt == q.s.nt) q.next_unit(a, G);
         };
         auto page_of = [&](const Cur& q) {
-            const int key = q.kt * TILE + 16 * b, i = key >> shift;
+            const int key = q.slot0() + 16 * b, i = key >> shift;
             int p = -1;
-            if (key < q.s.len && i < a.table_ld) p = __ldg(a.page_table + (size_t)q.b * a.table_ld + i);
+            if (key < q.s.len && i < a.table_ld) p = __ldg(a.page_table + (size_t)q.s.at * a.table_ld + i);
             return p;
         };
         struct Raw { int page; float sk, sv; uint8_t mask[4]; };
@@ -278,9 +278,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
             }
             #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int key = q.kt * TILE + 4 * lane + j;
+                const int key = q.slot0() + 4 * lane + j;
                 r.mask[j] = key < q.s.len;
-                if (r.mask[j] && a.key_mask != nullptr) r.mask[j] = __ldg(a.key_mask + (size_t)q.b * a.mask_ld + key);
+                // (keys before the window of every row are not looked at: they may have no page any more)
+                if (FORM != KV_PLAIN) r.mask[j] &= key >= q.low || (FORM == KV_WINDOW && key < a.sinks);
+                if (r.mask[j] && a.key_mask != nullptr) r.mask[j] = __ldg(a.key_mask + (size_t)q.s.at * a.mask_ld + key);
             }
             return r;
         };
@@ -292,7 +294,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
         int next_page = left_ahead > 0 ? page_of(nxt) : -1;
         int k_sent = 0, v_sent = 0;                          // tiles whose codes were asked for
         for (int it = 0; it < count; ++it) {
-            const int key0 = cur.kt * TILE, slot = it % INFOS;
+            const int key0 = cur.slot0(), slot = it % INFOS;
             Raw raw_next = raw;
             if (left_ahead > 0) raw_next = raw_of(nxt, next_page);
             advance(ahead, left_ahead);
@@ -316,7 +318,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                 if (lane < BLOCKS) atomicOr(a.status, STATUS_RANGE);
                 d = make_float4(__uint_as_float(0x7fffffffu), 0.f, 1.f, 0.f);      // the rows that see it become NaN
             }
-            const int edge = a.causal && key0 + TILE > cur.s.len - cur.s.n + 1;
+            int edge = a.causal && key0 + TILE > causal_edge<ROWS, FORM>(cur.s, G, cur.rt);
+            if (FORM == KV_WINDOW)
+                edge |= key0 < low_of<FORM>(a, cur.s, min(cur.s.n - 1, (cur.rt * ROWS + ROWS - 1) / G)) &&
+                        key0 + TILE > a.sinks;
             cur = nxt;
             nxt = ahead;
             raw = raw_next;
@@ -522,6 +527,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
             const bool valid = (shared ? s * TILE : 0) + row < rows;
             const bool active = __any_sync(0xffffffffu, valid);
             const int lim = !valid ? 0 : a.causal ? max(0, cur.s.len - cur.s.n + i + 1) : cur.s.len;
+            const int low = FORM == KV_WINDOW ? low_of<FORM>(a, cur.s, i) : 0;
             // The unit's query rows, as the A operand (with few rows both streams use the first tile): asynchronous
             // copies along the rows, and bf16 rows become fp16 in place, a thread a row. In rolled loops: the same
             // work unrolled ran from cold instruction lines (7 us of a call, now 2).
@@ -629,6 +635,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                             #pragma unroll
                             for (int k = 0; k < 32; ++k)
                                 if (k >= see || !(live[k & 3] >> (k >> 2) & 1)) x[k] = 0xff800000u;
+                            if (FORM == KV_WINDOW) {
+                                const int from = low - ti.key0 - 32 * c, sink = a.sinks - ti.key0 - 32 * c;
+                                #pragma unroll
+                                for (int k = 0; k < 32; ++k)
+                                    if (k < from && k >= sink) x[k] = 0xff800000u;
+                            }
                             #pragma unroll
                             for (int q = 0; q < 2; ++q) {                       // for the second pass
                                 uint32_t y[16];
@@ -756,10 +768,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                 // area, or its quarter of the stream's Q tile), so that the stores run along the rows.
                 constexpr int C4 = D / 8, RPW = 32 / C4;                        // float4s of half a row, rows a warp store
                 const float inv = whole ? (l == 0.f ? 0.f : __fdiv_rn(1.f, l)) : 1.f;
-                float* slot = slots + ((size_t)blockIdx.x * 2 + (tile0 == 0 ? 0 : 1)) * slot_floats(slot_rows, D);
+                const bool to_sums = FORM == KV_SPLIT && whole;
+                float* slot = to_sums ? a.sums : slots + ((size_t)blockIdx.x * 2 + (tile0 == 0 ? 0 : 1)) * slot_floats(slot_rows, D);
                 const int srow = (shared ? s * TILE : 0) + row;
-                const long long at = whole ? (long long)(cur.s.row0 + i) * a.ldo + (long long)head * D
-                                           : (long long)srow * D;
+                const long long at = to_sums ? ((long long)(cur.s.row0 + i) * a.H + head) * D
+                                     : whole ? (long long)(cur.s.row0 + i) * a.ldo + (long long)head * D
+                                             : (long long)srow * D;
                 float* stage = reinterpret_cast<float*>(smem + L::Q + s * L::TILE_BYTES + (warp & 3) * (64 * D));
                 auto stage_at = [&](int r, int c) { return stage + r * (D / 2) + ((c ^ (r & (C4 - 1))) << 2); };
                 #pragma unroll 1
@@ -793,7 +807,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                         const int jr = row - lane + r;                          // the row in the join area
                         const float4 v = *reinterpret_cast<const float4*>(
                             shared ? stage_at(r, c) : join + jr * D + ((c4 ^ (jr & (D / 4 - 1))) << 2));
-                        if (put && whole) {
+                        if (put && whole && !to_sums) {
                             // (no key seen: accumulators and scale are 0)
                             const T e[4] = {(T)(v.x * scale), (T)(v.y * scale), (T)(v.z * scale), (T)(v.w * scale)};
                             *reinterpret_cast<uint2*>(static_cast<T*>(a.Out) + to + 4 * c4) =
@@ -805,7 +819,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                     __syncwarp();
                 }
                 if (valid) {
-                    if (!whole)
+                    if (to_sums)
+                        reinterpret_cast<float2*>(a.sums + (size_t)a.T * a.H * D)[(size_t)(cur.s.row0 + i) * a.H + head] =
+                            make_float2(m, l);
+                    else if (!whole)
                         reinterpret_cast<float2*>(slot + (size_t)slot_rows * D)[srow] = make_float2(m, l);
                     else if (a.lse != nullptr)
                         a.lse[(size_t)(cur.s.row0 + i) * a.H + head] =
@@ -827,14 +844,14 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
     if (warp == MMA_WARP) tmem_dealloc(tmem, 512);
 }
 
-template <typename T, int D>
-cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
+template <typename T, int D, int FORM>
+cudaError_t launch_typed(const KvAttnArgs& a, KvCut* cut, cudaStream_t s) {
     const int G = a.H / a.c.Hkv;
     static DeviceCache<int> ready;
     int dummy = 0;
     cudaError_t e = ready.get(&dummy, [](int, int* v) {
         *v = 1;
-        return cudaFuncSetAttribute(kv_attention_tc_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        return cudaFuncSetAttribute(kv_attention_tc_kernel<T, D, FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                     Layout<D>::SMEM);
     });
     if (e != cudaSuccess) return e;
@@ -843,10 +860,11 @@ cudaError_t launch_typed(const KvAttnArgs& a, cudaStream_t s) {
     const int slot_rows = (int)std::min<long long>(ROWS, most);
     long long* prefix = static_cast<long long*>(a.workspace);
     float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + prefix_bytes(a.B));
-    if ((e = launch_overlapped(kv_attention_tc_kernel<T, D>, dim3(ctas), THREADS, Layout<D>::SMEM, s, a, G, slot_rows,
-                               prefix, slots)) != cudaSuccess || a.whole)
+    if (cut) *cut = KvCut{ctas, ROWS, slot_rows, a.whole, prefix, slots};
+    if ((e = launch_overlapped(kv_attention_tc_kernel<T, D, FORM>, dim3(ctas), THREADS, Layout<D>::SMEM, s, a, G,
+                               slot_rows, prefix, slots)) != cudaSuccess || a.whole || FORM == KV_SPLIT)
         return e;
-    return launch_join<T, D, ROWS, TILE>(a, G, ctas, slot_rows, prefix, slots, s);
+    return launch_join<T, D, ROWS, TILE, FORM>(a, G, ctas, slot_rows, prefix, slots, s);
 }
 
 }  // namespace
@@ -855,12 +873,17 @@ size_t kv_attention_tc_slot_bytes(int max_rows, int D) {
     return (size_t)num_sms() * 2 * slot_floats(max_rows, D) * 4;
 }
 
-cudaError_t launch_kv_attention_tc(const KvAttnArgs& args, cudaStream_t s) {
+template <int FORM>
+cudaError_t launch_kv_attention_tc(const KvAttnArgs& args, KvCut* cut, cudaStream_t s) {
     KvAttnArgs a = args;
     a.whole = whole_units(a, ROWS, TILE, num_sms());
     if (a.dtype == STARQ_BF16)
-        return a.c.D == 64 ? launch_typed<__nv_bfloat16, 64>(a, s) : launch_typed<__nv_bfloat16, 128>(a, s);
-    return a.c.D == 64 ? launch_typed<__half, 64>(a, s) : launch_typed<__half, 128>(a, s);
+        return a.c.D == 64 ? launch_typed<__nv_bfloat16, 64, FORM>(a, cut, s)
+                           : launch_typed<__nv_bfloat16, 128, FORM>(a, cut, s);
+    return a.c.D == 64 ? launch_typed<__half, 64, FORM>(a, cut, s) : launch_typed<__half, 128, FORM>(a, cut, s);
 }
+template cudaError_t launch_kv_attention_tc<KV_PLAIN>(const KvAttnArgs&, KvCut*, cudaStream_t);
+template cudaError_t launch_kv_attention_tc<KV_WINDOW>(const KvAttnArgs&, KvCut*, cudaStream_t);
+template cudaError_t launch_kv_attention_tc<KV_SPLIT>(const KvAttnArgs&, KvCut*, cudaStream_t);
 
 }  // namespace starq

@@ -1,0 +1,97 @@
+"""Attention with a window and over shared prefixes without a GPU: the oracle
+against closed forms, and the argument checks (nothing is launched by a
+refused call)."""
+
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode as od
+from tests.test_decode_host import ATTEND, BAD_CACHE, ODD, P, cache, lib, refuse  # noqa: F401  (lib: a fixture)
+
+
+def test_window_oracle():
+    rng = np.random.default_rng(2)
+    q, k, v = rng.standard_normal((3, 4, 8)), rng.standard_normal((7, 2, 8)), rng.standard_normal((7, 2, 8))
+    for causal in (False, True):
+        a, b = od.attention(q, k, v, 0.3, causal), od.attention_of(q, k, v, 0.3, od.window_sees(3, 7, 99, 0, causal))
+        assert all(np.allclose(x, y) for x, y in zip(a, b))
+    see = od.window_sees(3, 7, 2, 1, True)              # own slots 4, 5, 6
+    assert [list(np.flatnonzero(r)) for r in see] == [[0, 3, 4], [0, 4, 5], [0, 5, 6]]
+    assert [list(np.flatnonzero(r)) for r in od.window_sees(2, 4, 1, 0, False)] == [[2, 3], [3]]
+
+
+WINDOW = [n for n in ATTEND if n != "stream"]
+WINDOW[WINDOW.index("causal") + 1:WINDOW.index("causal") + 1] = ["window", "sinks"]
+SHARED = [n for n in ATTEND if n != "stream"]
+SHARED[SHARED.index("causal") + 1:SHARED.index("causal") + 1] = "group_start shared_len groups max_rows max_shared".split()
+WINDOW.append("stream")
+SHARED.append("stream")
+COMMON = [(dict(cache=c), r) for c, r in BAD_CACHE] + [
+    (dict(dtype=2), -1), (dict(T=-1), -2), (dict(H=3), -2), (dict(H=0), -2), (dict(max_new=1 << 27), -2),
+    (dict(max_len=-1), -2), (dict(key_mask=P, mask_ld=63), -2), (dict(scale=0.0), -1), (dict(scale=float("nan")), -1),
+    (dict(Q=None), -1), (dict(ldq=255), -2), (dict(ldo=260), -3), (dict(Out=ODD), -3), (dict(kv_len=None), -1),
+    (dict(workspace=None), -1), (dict(workspace=ctypes.c_void_p(4096 + 128)), -3), (dict(workspace_bytes=64), -1)]
+
+
+def base(lib, **kw):
+    return dict(Q=P, ldq=256, dtype=0, T=3, seq_start=P, B=1, max_new=3, H=4, cache=cache(lib), page_table=P, table_ld=4,
+                kv_len=P, max_len=64, causal=0, key_mask=None, mask_ld=0, scale=0.125, Out=P, ldo=256, lse=None,
+                workspace=P, workspace_bytes=1 << 40, stream=None, **kw)
+
+
+def changed(lib, changes):
+    return dict(cache=cache(lib, **changes["cache"])) if "cache" in changes else changes
+
+
+@pytest.mark.parametrize("changes,code", COMMON + [(dict(window=0), -2), (dict(window=-3), -2), (dict(sinks=-1), -2),
+                                                   (dict(window=(1 << 28) + 1), -2), (dict(sinks=1 << 29), -2)])
+def test_window_refusals(lib, changes, code):  # noqa: F811
+    refuse(lib, "kv_cache_attention_window", WINDOW, base(lib, window=8, sinks=0), changed(lib, changes), code)
+
+
+@pytest.mark.parametrize("changes,code", COMMON + [
+    (dict(groups=-1), -2), (dict(groups=65536), -2), (dict(max_rows=-1), -2), (dict(max_rows=1 << 27), -2),
+    (dict(max_shared=-1), -2), (dict(key_mask=P, mask_ld=64, max_shared=65), -2), (dict(group_start=None), -1),
+    (dict(shared_len=None), -1), (dict(group_start=ctypes.c_void_p(4098)), -3)])
+def test_shared_refusals(lib, changes, code):  # noqa: F811
+    refuse(lib, "kv_cache_attention_shared", SHARED,
+           base(lib, group_start=P, shared_len=P, groups=1, max_rows=3, max_shared=32), changed(lib, changes), code)
+
+
+def test_shared_workspace(lib):  # noqa: F811
+    size = lib.lib.kv_cache_attention_shared_workspace_size
+    assert size(8, 4, 2, 1, 8, 28, 4, 128) > lib.lib.kv_cache_attention_workspace_size(4, 2, 28, 4, 128)
+    assert size(-1, 4, 2, 1, 8, 28, 4, 128) == 0 and size(8, 4, 2, -1, 8, 28, 4, 128) == 0
+    assert size(8, 4, 2, 1, 8, 27, 4, 128) == 0 and size(8, 4, 2, 1, -8, 28, 4, 128) == 0
+    need = size(3, 1, 3, 1, 3, 4, 2, 64)
+    refuse(lib, "kv_cache_attention_shared", SHARED,
+           base(lib, group_start=P, shared_len=P, groups=1, max_rows=3, max_shared=32), dict(workspace_bytes=need - 1), -1)
+
+
+def test_nothing_to_do(lib):  # noqa: F811
+    c = cache(lib)
+    none = dict(base(lib), T=0, Q=None, Out=None, seq_start=None, kv_len=None, workspace=None, cache=c)
+    w = dict(none, window=1, sinks=0)
+    assert lib.lib.kv_cache_attention_window(*[w[n] for n in WINDOW]) == 0
+    s = dict(none, group_start=None, shared_len=None, groups=2, max_rows=0, max_shared=0)
+    assert lib.lib.kv_cache_attention_shared(*[s[n] for n in SHARED]) == 0
+
+
+def test_binding_refusals(lib):  # noqa: F811
+    t, i = torch.zeros, lambda *v: torch.tensor(v, dtype=torch.int32)
+    c = lib.KVCache(t(2, 1, 16, 64, dtype=torch.uint8), t(2, 1, 16, 64, dtype=torch.uint8), t(2, 1), t(2, 1))
+    x = t(3, 64, dtype=torch.float16)
+    with pytest.raises(ValueError):
+        lib.kv_cache_attention_window(x, c, i(0, 1)[None], i(3), i(0, 3), t(3, 64), max_new=3, max_len=3, window=4)
+    with pytest.raises(ValueError):
+        lib.kv_cache_attention_window(x, c, i(0, 1)[None], i(3), i(0, 3), x, max_new=3, max_len=3, window=4,
+                                      key_mask=t(1, 2, dtype=torch.uint8))
+    kw = dict(max_new=3, max_len=3, max_rows=3, max_shared=3)
+    ws = t(1, dtype=torch.uint8)
+    for start, shared in ((i(0), i(1)), (torch.tensor([0, 1]), i(1)), (i(0, 1), torch.tensor([1]))):
+        with pytest.raises(ValueError):
+            lib.kv_cache_attention_shared(x, c, i(0, 1)[None], i(3), i(0, 3), x, group_start=start, shared_len=shared,
+                                          workspace=ws, **kw)

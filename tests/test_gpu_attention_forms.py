@@ -1,0 +1,367 @@
+"""Attention over the cache with a sliding window, and for sequences that
+share a prefix, against oracle/decode.py. The tolerances are those of
+test_gpu_decode.py: the sums are the same ones over fewer keys, or in one more
+part (a product by a power of two's rounding, within the 2^-20 there)."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode as od
+from tests.test_gpu_decode import TINY, U, Paged, fill, i32, num, randn
+
+pytestmark = pytest.mark.gpu
+
+starts = lambda n: i32(np.concatenate([[0], np.cumsum(n)]))
+
+
+def check(pg, q, out, lse, new, lens, H, dtype, sees, scale=None):
+    """sees(b): [n][L]."""
+    start, D = np.concatenate([[0], np.cumsum(new)]), pg.D
+    scale = D ** -0.5 if scale is None else scale
+    q, out, lse = num(q).reshape(-1, H, D), num(out).reshape(-1, H, D), num(lse)
+    for b, L in enumerate(lens):
+        r = slice(start[b], start[b + 1])
+        # (slots that nobody may see can be in no page)
+        k, v = (od.read(c, s, np.maximum(pg.table[b], 0), 0, L, pg.page) for c, s in ((pg.k, pg.ks), (pg.v, pg.vs)))
+        ref, rl, mag, size = od.attention_of(q[r], k, v, scale, sees(b))
+        d = ((D + 4) * 2.0 ** -24 * size)[..., None]
+        rel = 2 * (2 * d + 2.0 ** -20) + 2.0 ** -11 + L * 2.0 ** -24 + 2.0 ** -20
+        err = np.abs(out[r] - ref)
+        assert np.all(err <= mag * rel + U[dtype] * np.abs(ref) * (1 + rel) + TINY[dtype]), (b, L, np.nanmax(err))
+        empty = np.isneginf(rl)
+        assert np.array_equal(empty, np.isneginf(lse[r])) and np.all(out[r][empty] == 0), b
+        tol = 2 * d[..., 0] + L * 2.0 ** -24 + 2.0 ** -19 * (1 + np.abs(np.where(empty, 0, rl)))
+        assert np.all(np.abs(np.where(empty, 0, lse[r]) - np.where(empty, 0, rl)) <= tol), (b, L)
+
+
+# --------------------------------------------------------------------------
+# A window
+# --------------------------------------------------------------------------
+def windowed(abi, rng, pg, new, lens, H, dtype, window, sinks, causal, mask=None, most=None, table=None, pad=0, q=None):
+    T, D = sum(new), pg.D
+    if q is None:
+        q, _ = randn(rng, (T, H * D + pad), dtype)
+        q = q[:, : H * D]
+    out = torch.full((T + 1, H * D + pad), 7.0, dtype=dtype, device="cuda")
+    lse = torch.full((T, H), 7.0, device="cuda")
+    abi.kv_cache_attention_window(q, pg.cache, pg.dev_table if table is None else table, i32(lens), starts(new),
+                                  out[:T, : H * D], max_new=max(new), max_len=max(lens) if most is None else most,
+                                  window=window, sinks=sinks, causal=causal, lse=lse,
+                                  key_mask=None if mask is None else torch.from_numpy(mask).cuda())
+    abi.check_status()
+    assert torch.all(out[:, H * D:] == 7.0) and torch.all(out[T:] == 7.0)
+    check(pg, q, out[:T, : H * D], lse, new, lens, H, dtype, lambda b: od.window_sees(
+        new[b], lens[b], window, sinks, causal, None if mask is None else mask[b]))
+    return out[:T, : H * D], lse
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("page,D,H,Hkv", [(16, 64, 2, 1), (32, 128, 7, 1), (64, 128, 4, 4), (128, 64, 6, 2), (16, 128, 16, 1)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (5, 1), (16, 4), (33, 0), (100, 130), (129, 20), (1 << 28, 0)])
+@pytest.mark.parametrize("causal,masked", [(False, False), (True, True), (True, False)])
+def test_window(abi, dtype, page, D, H, Hkv, window, sinks, causal, masked):
+    """Lengths from none to several tiles, new tokens from none to more than
+    the sequence holds, masks that leave rows empty."""
+    rng = np.random.default_rng(page * 7 + D + H + window % 1000)
+    lens = [0, 1, 15, 16, 17, 63, 129, 300, 390]
+    new = [2, 1, 3, 16, 0, 5, 33, 9, 1]
+    pg = Paged(abi, rng, len(lens), max(lens), Hkv, page, D)
+    fill(pg, rng, lens)
+    mask = None
+    if masked:
+        mask = (rng.random((len(lens), max(lens) + 5)) < 0.6).astype(np.uint8) * 3
+        mask[5] = 0
+        mask[6, :128] = 0
+        mask[7, 200:] = 0
+    windowed(abi, rng, pg, new, lens, H, dtype, window, sinks, causal, mask, pad=8)
+
+
+@pytest.mark.parametrize("new,H,Hkv,D", [(1, 28, 4, 128), (5, 8, 1, 64), (32, 7, 1, 128), (64, 2, 2, 128)])
+@pytest.mark.parametrize("window,sinks,most", [(700, 0, None), (128, 300, 1 << 20), (1025, 4, None)])
+def test_window_long(abi, new, H, Hkv, D, window, sinks, most):
+    """Windows of several tiles, runs joined over CTAs; the same bits again."""
+    rng = np.random.default_rng(new + H)
+    lens = [3000, 130, 2049]
+    pg = Paged(abi, rng, 3, 3000, Hkv, 64, D)
+    fill(pg, rng, lens)
+    q, _ = randn(rng, (2 * new + 1, H * D), torch.bfloat16)
+    for causal in (False, True):
+        one = windowed(abi, rng, pg, [new, 1, new], lens, H, torch.bfloat16, window, sinks, causal, most=most, q=q)
+        two = windowed(abi, rng, pg, [new, 1, new], lens, H, torch.bfloat16, window, sinks, causal, most=most, q=q)
+        assert torch.equal(one[0], two[0]) and torch.equal(one[1], two[1])
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (40, 3), (200, 0), (333, 140)])
+@pytest.mark.parametrize("H,Hkv,D", [(7, 1, 128), (3, 3, 64), (40, 1, 64)])
+def test_window_prompt(abi, window, sinks, H, Hkv, D):
+    """Many row tiles, each with a window of its own, causal and not."""
+    rng = np.random.default_rng(window + H)
+    lens, new = [700, 301], [500, 301]
+    pg = Paged(abi, rng, 2, 700, Hkv, 32, D)
+    fill(pg, rng, lens)
+    for causal in (True, False):
+        windowed(abi, rng, pg, new, lens, H, torch.float16, window, sinks, causal)
+
+
+@pytest.mark.parametrize("new,most", [(1, 900), (6, 900), (6, 1 << 20), (30, 900)])
+@pytest.mark.parametrize("sinks", [0, 5, 64])
+def test_window_pages_given_away(abi, new, most, sinks):
+    """Pages that every row's window has left: their entries name no page, or
+    another's with scales NaN and infinite, and nothing is reported."""
+    rng = np.random.default_rng(new)
+    lens, window = [900, 555], 100
+    for causal in (False, True):
+        for gone in (-1, 1 << 30, None):
+            pg = Paged(abi, rng, 2, 900, 1, 16, 128)
+            fill(pg, rng, lens)
+            spare = next(p for p in range(pg.pages) if p not in pg.table)       # stale, never filled
+            for b, L in enumerate(lens):
+                for blk in range(pg.table.shape[1]):
+                    if blk * 16 >= sinks and blk * 16 + 16 <= L - new - window + 1:
+                        pg.table[b, blk] = spare if gone is None else gone
+            table = torch.tensor(pg.table, dtype=torch.int32, device="cuda")
+            pg.table[(pg.table < 0) | (pg.table >= pg.pages)] = spare
+            pg.ks[spare], pg.vs[spare] = 0, 0                       # (for the oracle: 0 times what is not seen)
+            windowed(abi, rng, pg, [new, new], lens, 7, torch.bfloat16, window, sinks, causal, most=most, table=table)
+
+
+def test_window_reports_a_missing_page(abi):
+    rng = np.random.default_rng(1)
+    for new in (1, 40):
+        pg = Paged(abi, rng, 1, 600, 1, 16, 64)
+        fill(pg, rng, [600])
+        table = pg.dev_table.clone()
+        table[0, 36] = -1                                           # slots 576 .. 591
+        q, _ = randn(rng, (new, 128), torch.float16)
+        out = torch.empty_like(q)
+        abi.kv_cache_attention_window(q, pg.cache, table, i32([600]), i32([0, new]), out, max_new=new, max_len=600, window=60)
+        with pytest.raises(abi.StarqError) as e:
+            abi.check_status()
+        assert e.value.code == abi.ERR_RANGE
+        assert torch.isnan(out[-1]).all()
+
+
+def test_window_graph_and_stream(abi):
+    """A captured call follows lengths that grow; a call on a stream of the
+    caller's."""
+    rng = np.random.default_rng(6)
+    pg = Paged(abi, rng, 2, 800, 2, 32, 64)
+    fill(pg, rng, [800, 800])
+    q, _ = randn(rng, (4, 4 * 64), torch.float16)
+    out, lse, lens = torch.empty_like(q), torch.empty(4, 4, device="cuda"), i32([300, 20])
+    start = i32([0, 2, 4])
+    ws = torch.empty(abi.kv_cache_attention_workspace_size(2, 2, 4, 2, 64), dtype=torch.uint8, device="cuda")
+    call = lambda **kw: abi.kv_cache_attention_window(q, pg.cache, pg.dev_table, lens, start, out, max_new=2, max_len=800,
+                                                      window=150, sinks=3, causal=True, lse=lse, **kw)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    call(stream=side)                                               # (a workspace of the call's own)
+    side.synchronize()
+    see = lambda b: od.window_sees(2, int(lens[b]), 150, 3, True)
+    check(pg, q, out, lse, [2, 2], [300, 20], 4, torch.float16, see)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(workspace=ws)
+    for now in ([300, 20], [777, 2], [800, 513]):
+        lens.copy_(i32(now))
+        out.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        check(pg, q, out, lse, [2, 2], now, 4, torch.float16, see)
+    abi.check_status()
+
+
+# --------------------------------------------------------------------------
+# A prefix that sequences share
+# --------------------------------------------------------------------------
+class Shared(Paged):
+    """first: sequences before each group and the end (groups may be empty,
+    sequences outside of them); lens are the whole lengths."""
+
+    def __init__(self, abi, rng, first, shared, lens, Hkv, page, D):
+        super().__init__(abi, rng, len(lens), max(lens), Hkv, page, D)
+        self.first, self.shared = first, shared
+        for g, s in enumerate(shared):
+            for b in range(first[g], first[g + 1]):
+                self.table[b, : (s + page - 1) // page] = self.table[first[g], : (s + page - 1) // page]
+        self.dev_table = torch.tensor(self.table, dtype=torch.int32, device="cuda")
+        fill(self, rng, lens)
+
+
+def share(abi, rng, pg, new, lens, H, dtype, causal=False, mask=None, q=None, pad=0, max_new=None, max_rows=None, most=None,
+          max_shared=None, verify=True, **kw):
+    T, D = sum(new), pg.D
+    if q is None:
+        q, _ = randn(rng, (T, H * D + pad), dtype)
+        q = q[:, : H * D]
+    out = torch.full((T + 1, H * D + pad), 7.0, dtype=dtype, device="cuda")
+    lse = torch.full((T, H), 7.0, device="cuda")
+    rows = [sum(new[a:b]) for a, b in zip(pg.first, pg.first[1:])]
+    abi.kv_cache_attention_shared(
+        q, pg.cache, pg.dev_table, i32(lens), starts(new), out[:T, : H * D], max_new=max_new or max(new),
+        max_len=most or max(lens), group_start=i32(pg.first), shared_len=i32(pg.shared),
+        max_rows=max_rows or max(rows, default=0), max_shared=max_shared or max(pg.shared, default=0), causal=causal, lse=lse,
+        key_mask=None if mask is None else torch.from_numpy(mask).cuda(), **kw)
+    if verify:
+        abi.check_status()
+        assert torch.all(out[:, H * D:] == 7.0) and torch.all(out[T:] == 7.0)
+        check(pg, q, out[:T, : H * D], lse, new, lens, H, dtype, lambda b: od.window_sees(
+            new[b], lens[b], 1 << 28, 0, causal, None if mask is None else mask[b]))
+    return out[:T, : H * D], lse
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("page,D,H,Hkv", [(16, 64, 2, 1), (32, 128, 7, 1), (64, 128, 4, 4), (128, 64, 12, 2)])
+@pytest.mark.parametrize("first,shared", [
+    ([0, 9], [17]), ([0, 4, 9], [128, 300]), ([1, 3, 3, 8], [130, 44, 1]), ([2, 4], [0]), ([0, 1, 9], [16, 15])])
+@pytest.mark.parametrize("causal,masked", [(False, False), (True, False), (False, True), (True, True)])
+def test_shared(abi, dtype, page, D, H, Hkv, first, shared, causal, masked):
+    """Groups of none to nine sequences, shared lengths of none to several
+    tiles that end inside a page, sequences outside of all groups, new tokens
+    from none on, own lengths from the new tokens alone on, masks that leave the
+    prefix, what follows or both empty."""
+    rng = np.random.default_rng(page * 7 + D + H + shared[0])
+    new = [2, 1, 3, 1, 0, 5, 1, 33, 9]
+    own = [2, 1, 40, 130, 17, 5, 300, 40, 9]
+    base = [0] * 9
+    for g, s in enumerate(shared):
+        base[first[g]:first[g + 1]] = [s] * (first[g + 1] - first[g])
+    lens = [s + o for s, o in zip(base, own)]
+    pg = Shared(abi, rng, first, shared, lens, Hkv, page, D)
+    mask = None
+    if masked:
+        mask = (rng.random((9, max(lens) + 5)) < 0.6).astype(np.uint8) * 3
+        for g, s in enumerate(shared):
+            if first[g] < 9:
+                mask[first[g]:first[g + 1], :s] = mask[first[g], :s]
+                if g == 1:
+                    mask[first[g]:first[g + 1], :s] = 0
+        for b in (2, 7):
+            mask[b, base[b]:] = 0
+    share(abi, rng, pg, new, lens, H, dtype, causal, mask, pad=8)
+
+
+@pytest.mark.parametrize("new,H,Hkv,D", [(1, 28, 4, 128), (1, 4, 4, 64), (32, 7, 1, 128), (61, 2, 2, 64), (3, 16, 1, 128)])
+@pytest.mark.parametrize("bound", [0, 1 << 20])
+def test_shared_long(abi, new, H, Hkv, D, bound):
+    """Prefixes and own parts of many tiles, cut into runs, under tight and
+    generous bounds; the same bits again."""
+    rng = np.random.default_rng(new + H)
+    first, shared, own = [0, 5, 7], [2500, 1111], [900, 61, 200, 61, 333, 1500, 64]
+    lens = [shared[b >= 5] + o for b, o in enumerate(own)]
+    pg = Shared(abi, rng, first, shared, lens, Hkv, 64, D)
+    q, _ = randn(rng, (7 * new, H * D), torch.bfloat16)
+    go = lambda: share(abi, rng, pg, [new] * 7, lens, H, torch.bfloat16, q=q, most=max(lens) + bound,
+                       max_shared=2500 + bound, max_rows=7 * new + 1)
+    one, two = go(), go()
+    assert torch.equal(one[0], two[0]) and torch.equal(one[1], two[1])
+    share(abi, rng, pg, [new] * 7, lens, H, torch.bfloat16, causal=True, q=q)
+
+
+def test_shared_many_groups(abi):
+    """More sequences and groups than threads of a CTA."""
+    rng = np.random.default_rng(3)
+    size = [int(x) for x in rng.integers(0, 5, 400)]
+    first = [0] + [int(x) for x in np.cumsum(size)]
+    shared = [int(x) for x in rng.integers(0, 40, 400)]
+    B = first[-1]
+    base = np.repeat(shared, size)
+    new = [int(x) for x in rng.integers(0, 3, B)]
+    lens = [int(base[b]) + new[b] + int(rng.integers(0, 9)) for b in range(B)]
+    pg = Shared(abi, rng, first, shared, lens, 1, 16, 64)
+    share(abi, rng, pg, new, lens, 2, torch.float16)
+
+
+def test_shared_is_the_plain_call_without_sharing(abi):
+    rng = np.random.default_rng(5)
+    lens, new = [200, 90], [3, 3]
+    pg = Shared(abi, rng, [0, 1, 2], [64, 64], lens, 2, 32, 64)
+    q, _ = randn(rng, (6, 4 * 64), torch.float16)
+    out, lse = torch.empty_like(q), torch.empty(6, 4, device="cuda")
+    abi.kv_cache_attention(q, pg.cache, pg.dev_table, i32(lens), starts(new), out, max_new=3, max_len=200, lse=lse)
+    got = share(abi, rng, pg, new, lens, 4, torch.float16, q=q)
+    assert torch.equal(got[0], out) and torch.equal(got[1], lse)
+    pg.first, pg.shared = [0], []                                   # no groups
+    got = share(abi, rng, pg, new, lens, 4, torch.float16, q=q)
+    assert torch.equal(got[0], out) and torch.equal(got[1], lse)
+
+
+def test_shared_outside_its_bounds(abi):
+    """What does not fit is reported, and the group of it alone is wrong."""
+    rng = np.random.default_rng(4)
+    lens, new = [150, 150, 150, 150], [2, 2, 2, 2]
+    pg = Shared(abi, rng, [0, 2, 4], [96, 128], lens, 1, 32, 64)
+    q, _ = randn(rng, (8, 7 * 64), torch.float16)
+    right = share(abi, rng, pg, new, lens, 7, torch.float16, q=q)[0]
+    for first, shared, kw in (([0, 2, 4], [96, 149], {}), ([0, 2, 4], [96, -1], {}), ([0, 2, 5], [96, 128], {}),
+                              ([0, 2, 1], [96, 128], {}), ([0, 2, 4], [96, 128], dict(max_shared=100)),
+                              ([0, 2, 4], [96, 140], dict(max_shared=128))):
+        pg.first, pg.shared = first, shared
+        out = share(abi, rng, pg, new, lens, 7, torch.float16, q=q, verify=False, max_rows=4, **kw)[0]
+        with pytest.raises(abi.StarqError) as e:
+            abi.check_status()
+        assert e.value.code == abi.ERR_RANGE, (first, shared, kw)
+        assert torch.equal(out[:4], right[:4])
+    pg.first, pg.shared = [0, 2, 4], [96, 128]
+    share(abi, rng, pg, new, lens, 7, torch.float16, q=q, verify=False, max_rows=3)
+    with pytest.raises(abi.StarqError):
+        abi.check_status()
+    share(abi, rng, pg, new, lens, 7, torch.float16, q=q)
+
+
+@pytest.mark.parametrize("new", [1, 20])
+def test_shared_not_finite(abi, new):
+    """A poisoned block of the prefix shows in its group's rows, one of a
+    sequence's own in its rows; the others are finite."""
+    rng = np.random.default_rng(9)
+    lens = [300, 290, 310, 300]
+    pg = Shared(abi, rng, [0, 2, 4], [256, 130], lens, 1, 16, 64)
+    q, _ = randn(rng, (4 * new, 7 * 64), torch.bfloat16)
+    row = lambda b: slice(b * new, (b + 1) * new)
+    for page, bad in ((pg.table[0, 3], [0, 1]), (pg.table[2, 2], [2, 3]), (pg.table[1, 17], [1])):
+        for scale in (pg.cache.k_scale, pg.cache.v_scale):
+            keep = scale[page].clone()
+            scale[page] = float("nan")
+            out, lse = share(abi, rng, pg, [new] * 4, lens, 7, torch.bfloat16, q=q, verify=False)
+            scale[page] = keep
+            for b in range(4):
+                assert torch.isnan(out[row(b)]).all() if b in bad else torch.isfinite(out[row(b)]).all(), (b, bad)
+    abi.check_status()
+
+
+def test_shared_graph_and_stream(abi):
+    """A captured call follows lengths that change; two graphs with
+    workspaces of their own; a call on a stream of the caller's."""
+    rng = np.random.default_rng(6)
+    pg = Shared(abi, rng, [0, 3], [256], [700] * 3, 2, 32, 64)
+    q, _ = randn(rng, (6, 4 * 64), torch.float16)
+    lens, start, first, common = i32([300, 258, 400]), i32([0, 2, 4, 6]), i32([0, 3]), i32([256])
+    see = lambda b: od.window_sees(2, int(lens[b]), 1 << 28, 0, True)
+    size = abi.kv_cache_attention_shared_workspace_size(6, 3, 2, 1, 6, 4, 2, 64)
+    outs = [torch.empty_like(q) for _ in range(3)]
+    lses = [torch.empty(6, 4, device="cuda") for _ in range(3)]
+    call = lambda k, **kw: abi.kv_cache_attention_shared(
+        q, pg.cache, pg.dev_table, lens, start, outs[k], max_new=2, max_len=700, group_start=first, shared_len=common,
+        max_rows=6, max_shared=512, causal=True, lse=lses[k], **kw)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    call(0, stream=side)
+    side.synchronize()
+    check(pg, q, outs[0], lses[0], [2] * 3, [300, 258, 400], 4, torch.float16, see)
+    graphs = []
+    for k in (1, 2):
+        ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+        graphs.append((torch.cuda.CUDAGraph(), ws))
+        with torch.cuda.graph(graphs[-1][0]):
+            call(k, workspace=ws)
+    for now, s in (([300, 258, 400], 256), ([600, 602, 700], 512), ([600, 602, 700], 0)):
+        lens.copy_(i32(now))
+        common.fill_(min(s, 256))                       # (the pages beyond 256 are the sequences' own)
+        for g, _ in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for k in (1, 2):
+            check(pg, q, outs[k], lses[k], [2] * 3, now, 4, torch.float16, see)
+        assert torch.equal(outs[1], outs[2])
+    abi.check_status()
