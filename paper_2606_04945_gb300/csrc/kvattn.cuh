@@ -69,7 +69,7 @@ enum KvForm { KV_PLAIN, KV_WINDOW, KV_SPLIT };
 struct SeqShape {
     int len, n, row0, nt, rt;          // cached tokens, new tokens, first row, key tiles, row tiles
     int at;                            // the sequence whose pages and key mask are read
-    int low;                           // KV_SPLIT: the first slot that is seen
+    int group, low;                    // KV_SPLIT: the group (-1: none), the first slot that is seen
     int sink_tiles;                    // KV_WINDOW: tiles with first slots, before those of a window
 };
 
@@ -92,6 +92,7 @@ __device__ __forceinline__ SeqShape seq_shape(const KvAttnArgs& a, int G, int b,
     SeqShape s;
     s.at = b;
     s.low = s.sink_tiles = 0;
+    s.group = -1;
     bool bad;
     if (FORM == KV_SPLIT && a.prefix) {
         const int s0 = __ldg(a.group_start + b), s1 = __ldg(a.group_start + b + 1);
@@ -108,8 +109,8 @@ __device__ __forceinline__ SeqShape seq_shape(const KvAttnArgs& a, int G, int b,
     }
     bad |= s.n < 0 || s.n > a.max_new || s.row0 < 0 || s.row0 > a.T - s.n || s.len < 0 || s.len > a.max_len;
     if (FORM == KV_SPLIT && !a.prefix) {
-        const int g = group_of(a, b);
-        if (g >= 0) s.low = __ldg(a.shared_len + g);
+        s.group = group_of(a, b);
+        if (s.group >= 0) s.low = __ldg(a.shared_len + s.group);
         bad |= s.low < 0 || (s.low > 0 && s.low > s.len - s.n);      // the new tokens are not shared
     }
     if (bad) {
@@ -291,10 +292,11 @@ struct Cursor {
 // 8.5 / 9.9 (cut); 64 such sequences, up to 300 tokens 14.8 / 11.1, 1000
 // tokens 21.5 / 19.7; 32 rows of them, 8 sequences, 250 tokens 20.9 / 18.6,
 // 500 tokens 21.9 / 23.4 (cut); 32 sequences, 500 tokens 48 / 24.8.
+// (A window makes the units of longer sequences alike: up to 32 tiles.)
 inline bool whole_units(const KvAttnArgs& a, int rows, int tile, int ctas) {
     const long long t = std::max(1, (a.likely_len + tile - 1) / tile);
     const long long n = ((long long)a.max_new * (a.H / a.c.Hkv) + rows - 1) / rows * a.B * a.c.Hkv;      // units
-    return t <= 8 && t * ((n + ctas - 1) / ctas) * ctas <= std::max<long long>(ctas, n * t) + 2 * ctas + 4 * n;
+    return t <= (a.window > 0 ? 32 : 8) && t * ((n + ctas - 1) / ctas) * ctas <= std::max<long long>(ctas, n * t) + 2 * ctas + 4 * n;
 }
 
 // Joins the partial runs of a row's unit, and writes the rows that no key

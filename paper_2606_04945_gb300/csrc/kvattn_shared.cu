@@ -12,6 +12,7 @@
 // leave sums relative to a row's running maximum; the join adds a row's runs of
 // both, in their order.
 #include <algorithm>
+#include <cmath>
 
 #include "kvattn.cuh"
 
@@ -29,120 +30,131 @@ struct Runs {
     int count;
 };
 
-template <int D>
-__device__ __forceinline__ Runs runs_of(const KvAttnArgs& a, const KvCut& cut, int G, const SeqShape& s, int b, int i,
-                                        int head) {
-    Runs r = {nullptr, nullptr, 0, 0, 0};
-    if (s.n <= 0 || s.nt <= 0) return r;
-    const int h = head / G, row = i * G + (head - h * G);
-    const size_t at = (size_t)(s.row0 + i) * a.H + head;
-    r.acc = a.sums + at * D;
-    r.ml = a.sums + (size_t)a.T * a.H * D + 2 * at;
-    r.count = 1;
-    if (cut.whole) return r;
-    const int tile = row / cut.rows, rr = row - tile * cut.rows, tiles = (s.n * G + cut.rows - 1) / cut.rows;
-    const long long total = cut.prefix[a.B], share = quotient(total + cut.ctas - 1, cut.ctas);
-    const long long u0 = cut.prefix[b] + ((long long)h * tiles + tile) * s.nt;
-    int c0, c1;
-    if (total < (1ll << 31)) {
-        c0 = (int)((unsigned)u0 / (unsigned)share);
-        c1 = (int)((unsigned)(u0 + s.nt - 1) / (unsigned)share);
-    } else {
-        c0 = (int)(u0 / share);
-        c1 = (int)((u0 + s.nt - 1) / share);
-    }
-    if (c0 == c1) return r;                               // one run covered the unit
-    r.count = c1 - c0 + 1;
-    r.step = 2 * slot_floats(cut.slot_rows, D);
-    r.second = u0 > (long long)c0 * share ? slot_floats(cut.slot_rows, D) : 0;
-    r.acc = cut.slots + c0 * r.step + (size_t)rr * D;
-    r.ml = cut.slots + c0 * r.step + (size_t)cut.slot_rows * D + 2 * rr;
-    return r;
-}
+// Both passes: of a sequence's own slots, and of its group's.
+struct Passes {
+    KvAttnArgs a[2];
+    KvCut cut[2];
+};
 
 template <typename T, int D, int SHARE>
-__global__ void __launch_bounds__(JOIN_WARPS * 32)
-kv_attention_split_join_kernel(const KvAttnArgs pre, const KvCut pre_cut, const KvAttnArgs own, const KvCut own_cut, int G) {
+__global__ void __launch_bounds__(JOIN_WARPS * 32, 4)
+kv_attention_split_join_kernel(const __grid_constant__ Passes p, int G) {
     constexpr int PER = D / 32, AT_ONCE = 4;
-    __shared__ float s_acc[SHARE > 1 ? SHARE : 1][D];
-    __shared__ float2 s_ml[SHARE > 1 ? SHARE : 1];
+    __shared__ float s_acc[SHARE > 1 ? JOIN_WARPS : 1][D];
+    __shared__ float2 s_ml[SHARE > 1 ? JOIN_WARPS : 1];
     grid_dependency_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % SHARE;
-    const int b = blockIdx.y;
-    const SeqShape s = seq_shape<16, TILE, KV_SPLIT>(own, G, b, false);
+    const KvAttnArgs& own = p.a[0];
     const int idx = blockIdx.x * (JOIN_WARPS / SHARE) + warp / SHARE;      // token * H + head
-    const int i = idx / own.H, head = idx - i * own.H;
-    if (i >= s.n) return;
-    const size_t row = (size_t)(s.row0 + i);
-    Runs from[2] = {{nullptr, nullptr, 0, 0, 0}, runs_of<D>(own, own_cut, G, s, b, i, head)};
-    const int g = group_of(own, b);
-    if (g >= 0) {
-        const SeqShape p = seq_shape<16, TILE, KV_SPLIT>(pre, G, g, false);
-        const int at = s.row0 + i - p.row0;               // (outside only where the starts are not in order)
-        if (at >= 0 && at < p.n) from[0] = runs_of<D>(pre, pre_cut, G, p, g, at, head);
+    int i = idx / own.H, b = blockIdx.y;
+    const int head = idx - i * own.H, h = head / G;
+    size_t row = 0;
+    Runs mine = {nullptr, nullptr, 0, 0, 0}, ours = mine;
+    bool real = false;
+    // (a loop, not two copies: a launch's code runs once, from cold instruction lines)
+    #pragma unroll 1
+    for (int q = 0; q < 2; ++q) {
+        const KvAttnArgs& a = p.a[q];
+        const KvCut& cut = p.cut[q];
+        const SeqShape s = seq_shape<16, TILE, KV_SPLIT>(a, G, b, false);
+        if (q == 0) {
+            if (i >= s.n) break;                          // (no row; of a CTA's rows, others may be)
+            row = (size_t)(s.row0 + i);
+            real = true;
+        } else {
+            i = (int)row - s.row0;
+            if (i < 0 || i >= s.n) break;                 // (only where the starts are not in order)
+        }
+        Runs r = {nullptr, nullptr, 0, 0, 0};
+        if (s.nt > 0) {
+            const size_t at = row * a.H + head;
+            r.acc = a.sums + at * D;
+            r.ml = a.sums + (size_t)a.T * a.H * D + 2 * at;
+            r.count = 1;
+            if (!cut.whole) {
+                const int unit_row = i * G + (head - h * G), tile = unit_row / cut.rows, rr = unit_row - tile * cut.rows;
+                const int tiles = (s.n * G + cut.rows - 1) / cut.rows;
+                const long long total = cut.prefix[a.B], u0 = cut.prefix[b] + ((long long)h * tiles + tile) * s.nt;
+                const long long share = quotient(total + cut.ctas - 1, cut.ctas);
+                const int c0 = (int)(u0 / share), c1 = (int)((u0 + s.nt - 1) / share);
+                if (c0 < c1) {                            // (else one run covered the unit)
+                    r.count = c1 - c0 + 1;
+                    r.step = 2 * slot_floats(cut.slot_rows, D);
+                    r.second = u0 > (long long)c0 * share ? slot_floats(cut.slot_rows, D) : 0;
+                    r.acc = cut.slots + c0 * r.step + (size_t)rr * D;
+                    r.ml = cut.slots + c0 * r.step + (size_t)cut.slot_rows * D + 2 * rr;
+                }
+            }
+        }
+        if (q == 0) mine = r;
+        else ours = r;
+        b = s.group;
+        if (b < 0) break;
     }
+    if (SHARE == 1 && !real) return;
     float top = NEG_INF, l = 0.f, acc[PER];
     #pragma unroll
     for (int k = 0; k < PER; ++k) acc[k] = 0.f;
-    #pragma unroll 1
-    for (int q = 0; q < 2; ++q) {
-        const Runs& r = from[q];
-        for (int c = part; c < r.count; c += AT_ONCE * SHARE) {
-            float2 ml[AT_ONCE];
-            float v[AT_ONCE][PER];
+    // the group's runs, then the sequence's, in one list
+    const int runs = ours.count + mine.count;
+    for (int c = part; c < runs; c += AT_ONCE * SHARE) {
+        float2 ml[AT_ONCE];
+        float v[AT_ONCE][PER];
+        #pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int cu = c + u * SHARE;
+            ml[u] = make_float2(NEG_INF, 0.f);
             #pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) {
-                const int cu = c + u * SHARE;
-                ml[u] = make_float2(NEG_INF, 0.f);
+            for (int k = 0; k < PER; ++k) v[u][k] = 0.f;
+            if (cu < runs) {
+                const bool first = cu < ours.count;
+                const int q = first ? cu : cu - ours.count;
+                const size_t off = q * (first ? ours.step : mine.step) + (q > 0 ? 0 : first ? ours.second : mine.second);
+                ml[u] = *reinterpret_cast<const float2*>((first ? ours.ml : mine.ml) + off);
+                const float* acc_of = (first ? ours.acc : mine.acc) + off + lane * PER;
                 #pragma unroll
-                for (int k = 0; k < PER; ++k) v[u][k] = 0.f;
-                if (cu < r.count) {
-                    const size_t off = cu * r.step + (cu == 0 ? r.second : 0);
-                    ml[u] = *reinterpret_cast<const float2*>(r.ml + off);
-                    #pragma unroll
-                    for (int k = 0; k < PER; k += 2) {
-                        const float2 w = *reinterpret_cast<const float2*>(r.acc + off + lane * PER + k);
-                        v[u][k] = w.x; v[u][k + 1] = w.y;
-                    }
+                for (int k = 0; k < PER; k += 2) {
+                    const float2 w = *reinterpret_cast<const float2*>(acc_of + k);
+                    v[u][k] = w.x; v[u][k + 1] = w.y;
                 }
             }
-            float to = top;
+        }
+        float to = top;
+        #pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) to = fmaxf(to, ml[u].x);
+        const float f0 = top == to ? 1.f : ex2(top - to);
+        top = to;
+        l *= f0;
+        #pragma unroll
+        for (int k = 0; k < PER; ++k) acc[k] *= f0;
+        #pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const float f = ml[u].x == top ? 1.f : ex2(ml[u].x - top);
+            l = fmaf(ml[u].y, f, l);
             #pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) to = fmaxf(to, ml[u].x);
-            const float f0 = top == to ? 1.f : ex2(top - to);
-            top = to;
-            l *= f0;
-            #pragma unroll
-            for (int k = 0; k < PER; ++k) acc[k] *= f0;
-            #pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) {
-                const float f = ml[u].x == top ? 1.f : ex2(ml[u].x - top);
-                l = fmaf(ml[u].y, f, l);
-                #pragma unroll
-                for (int k = 0; k < PER; ++k) acc[k] = fmaf(v[u][k], f, acc[k]);
-            }
+            for (int k = 0; k < PER; ++k) acc[k] = fmaf(v[u][k], f, acc[k]);
         }
     }
-    if (SHARE > 1) {                                      // one row a CTA: the warps' results
+    if (SHARE > 1) {                                      // a row's warps' results
         #pragma unroll
-        for (int k = 0; k < PER; ++k) s_acc[part][lane * PER + k] = acc[k];
-        if (lane == 0) s_ml[part] = make_float2(top, l);
+        for (int k = 0; k < PER; ++k) s_acc[warp][lane * PER + k] = acc[k];
+        if (lane == 0) s_ml[warp] = make_float2(top, l);
         __syncthreads();
-        if (part != 0) return;
+        if (part != 0 || !real) return;
         float to = NEG_INF;
         #pragma unroll
-        for (int w = 0; w < SHARE; ++w) to = fmaxf(to, s_ml[w].x);
+        for (int w = 0; w < SHARE; ++w) to = fmaxf(to, s_ml[warp + w].x);
         top = to;
         l = 0.f;
         #pragma unroll
         for (int k = 0; k < PER; ++k) acc[k] = 0.f;
         #pragma unroll
         for (int w = 0; w < SHARE; ++w) {
-            const float2 ml = s_ml[w];
+            const float2 ml = s_ml[warp + w];
             const float f = ml.x == top ? 1.f : ex2(ml.x - top);
             l = fmaf(ml.y, f, l);
             #pragma unroll
-            for (int k = 0; k < PER; ++k) acc[k] = fmaf(s_acc[w][lane * PER + k], f, acc[k]);
+            for (int k = 0; k < PER; ++k) acc[k] = fmaf(s_acc[warp + w][lane * PER + k], f, acc[k]);
         }
     }
     const float inv = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
@@ -154,16 +166,41 @@ kv_attention_split_join_kernel(const KvAttnArgs pre, const KvCut pre_cut, const 
 }
 
 template <typename T, int D>
-cudaError_t launch_split_join(const KvAttnArgs& pre, const KvCut& pc, const KvAttnArgs& own, const KvCut& oc,
-                              cudaStream_t s) {
+cudaError_t launch_split_join(const Passes& p, cudaStream_t s) {
+    const KvAttnArgs& own = p.a[0];
     const int G = own.H / own.c.Hkv;
-    const size_t rows = (size_t)own.max_new * own.H;
-    if (rows * own.B <= 4 * (size_t)num_sms())            // up to four CTAs an SM
-        return launch_overlapped(kv_attention_split_join_kernel<T, D, JOIN_WARPS>, dim3((unsigned)rows, (unsigned)own.B),
-                                 JOIN_WARPS * 32, 0, s, pre, pc, own, oc, G);
-    return launch_overlapped(kv_attention_split_join_kernel<T, D, 1>,
-                             dim3((unsigned)((rows + JOIN_WARPS - 1) / JOIN_WARPS), (unsigned)own.B), JOIN_WARPS * 32, 0,
-                             s, pre, pc, own, oc, G);
+    const size_t rows = (size_t)own.max_new * own.H, all = rows * own.B;
+    auto go = [&](auto share) {
+        constexpr int SHARE = decltype(share)::value, PER_CTA = JOIN_WARPS / SHARE;
+        return launch_overlapped(kv_attention_split_join_kernel<T, D, SHARE>,
+                                 dim3((unsigned)((rows + PER_CTA - 1) / PER_CTA), (unsigned)own.B), JOIN_WARPS * 32, 0, s,
+                                 p, G);
+    };
+    // as many warps a row as are on the GPU at once, four CTAs an SM
+    if (all <= 4 * (size_t)num_sms()) return go(std::integral_constant<int, JOIN_WARPS>{});
+    if (all <= 16 * (size_t)num_sms()) return go(std::integral_constant<int, 2>{});
+    return go(std::integral_constant<int, 1>{});
+}
+
+// Whether the prefix is worth a pass of its own, from the bounds that the host
+// knows. A key tile (128 keys of a head) costs the GPU about 5 ns with up to 16
+// rows (4 with heads of 64), 11 (8) with up to 128 and 16 for every 256 rows;
+// what the shared tiles cost less once a group than once a sequence has to
+// make up for about 16 us of two more launches and the sums' way through
+// memory. Measured, plain / shared, us (bf16, 200 own tokens; 170 settings, on
+// average 0.6 % above the better of each): 28 heads on 4, one token of 8
+// sequences, 8192 shared 21 / 35, 32768 shared 52 / 42; of 32, 2048 shared
+// 23 / 28, 8192 shared 53 / 33, 32768 shared 168 / 51; 32 tokens of each of 8
+// (the tensor cores are full either way), 8192 shared 56 / 70; 32 heads with
+// keys of their own, 8 sequences, 2048 shared 34 / 22, 32768 shared 328 / 68.
+bool worth_sharing(const KvAttnArgs& a, int max_rows, int max_shared) {
+    if (a.groups == 0 || max_rows <= a.max_new || max_shared == 0) return false;
+    const int G = a.H / a.c.Hkv;
+    const double few = a.c.D == 64 ? 4 : 5, some = a.c.D == 64 ? 8 : 11;
+    auto tile_ns = [&](double rows) { return rows <= 16 ? few : rows <= 128 ? some : 16 * std::ceil(rows / 256); };
+    const double sequences = std::min<double>(a.B, (double)a.groups * max_rows / a.max_new);
+    const double each = tile_ns((double)a.max_new * G), once = tile_ns((double)max_rows * G);
+    return std::ceil(max_shared / (double)TILE) * a.c.Hkv * (sequences * each - a.groups * once) > 16e3;
 }
 
 constexpr size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -178,8 +215,7 @@ size_t kv_attention_shared_workspace_bytes(int T, int B, int max_new, int groups
 }
 
 cudaError_t launch_kv_attention_shared(const KvAttnArgs& a, int max_rows, int max_shared, cudaStream_t s) {
-    // nothing is shared, as far as the bounds tell
-    if (a.groups == 0 || max_rows <= a.max_new || max_shared == 0) return launch_kv_attention(a, s);
+    if (!worth_sharing(a, max_rows, max_shared)) return launch_kv_attention(a, s);
     const int H = a.H, Hkv = a.c.Hkv, D = a.c.D;
     uint8_t* w = static_cast<uint8_t*>(a.workspace);
     KvAttnArgs own = a, pre = a;
@@ -196,19 +232,19 @@ cudaError_t launch_kv_attention_shared(const KvAttnArgs& a, int max_rows, int ma
     pre.max_new = max_rows;
     pre.max_len = pre.likely_len = max_shared;
     pre.causal = 0;                                       // a shared slot lies before all new tokens
-    auto pass = [&](KvAttnArgs& p, KvCut* cut) {
-        const cudaError_t e = kv_attention_by_warps(p) ? launch_kv_attention_warp<KV_SPLIT>(p, cut, s)
-                                                       : launch_kv_attention_tc<KV_SPLIT>(p, cut, s);
-        p.whole = cut->whole;
-        return e;
-    };
-    KvCut pc, oc;
-    cudaError_t e = pass(pre, &pc);
-    if (e != cudaSuccess || (e = pass(own, &oc)) != cudaSuccess) return e;
+    Passes p;
+    p.a[0] = own;
+    p.a[1] = pre;
+    for (int q = 1; q >= 0; --q) {
+        KvAttnArgs& pass = p.a[q];
+        const cudaError_t e = kv_attention_by_warps(pass) ? launch_kv_attention_warp<KV_SPLIT>(pass, &p.cut[q], s)
+                                                          : launch_kv_attention_tc<KV_SPLIT>(pass, &p.cut[q], s);
+        if (e != cudaSuccess) return e;
+        pass.whole = p.cut[q].whole;
+    }
     if (a.dtype == STARQ_BF16)
-        return D == 64 ? launch_split_join<__nv_bfloat16, 64>(pre, pc, own, oc, s)
-                       : launch_split_join<__nv_bfloat16, 128>(pre, pc, own, oc, s);
-    return D == 64 ? launch_split_join<__half, 64>(pre, pc, own, oc, s) : launch_split_join<__half, 128>(pre, pc, own, oc, s);
+        return D == 64 ? launch_split_join<__nv_bfloat16, 64>(p, s) : launch_split_join<__nv_bfloat16, 128>(p, s);
+    return D == 64 ? launch_split_join<__half, 64>(p, s) : launch_split_join<__half, 128>(p, s);
 }
 
 }  // namespace starq

@@ -166,6 +166,13 @@ __device__ __forceinline__ void store_codes(uint32_t tile, int r, int c, const u
     }
 }
 
+// Bit i of a byte to bit 4 i.
+__device__ __forceinline__ uint32_t every_fourth(uint32_t x) {
+    x = (x | x << 12) & 0x000f000fu;
+    x = (x | x << 6) & 0x03030303u;
+    return (x | x << 3) & 0x11111111u;
+}
+
 // Waits for the loads from TMEM; x comes from one of them.
 __device__ __forceinline__ void tmem_arrived(uint32_t (&x)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -628,19 +635,17 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tc_kernel(const KvAtt
                             uint32_t x[32];
                             tmem_ld_32x32b_x32(t_s + 32 * c, x);
                             tmem_arrived(x);
-                            const int see = lim - ti.key0 - 32 * c;
-                            uint32_t live[4];                                   // bit k / 4 of word k % 4: key 32 c + k
+                            // bit k: the row sees key 32 c + k
+                            auto below = [](int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; };
+                            uint32_t live = 0;
                             #pragma unroll
-                            for (int j = 0; j < 4; ++j) live[j] = ti.seen[j] >> (8 * c);
+                            for (int j = 0; j < 4; ++j) live |= every_fourth(ti.seen[j] >> (8 * c) & 0xff) << j;
+                            live &= below(lim - ti.key0 - 32 * c);
+                            if (FORM == KV_WINDOW)
+                                live &= ~below(low - ti.key0 - 32 * c) | below(a.sinks - ti.key0 - 32 * c);
                             #pragma unroll
                             for (int k = 0; k < 32; ++k)
-                                if (k >= see || !(live[k & 3] >> (k >> 2) & 1)) x[k] = 0xff800000u;
-                            if (FORM == KV_WINDOW) {
-                                const int from = low - ti.key0 - 32 * c, sink = a.sinks - ti.key0 - 32 * c;
-                                #pragma unroll
-                                for (int k = 0; k < 32; ++k)
-                                    if (k < from && k >= sink) x[k] = 0xff800000u;
-                            }
+                                if (!(live >> k & 1)) x[k] = 0xff800000u;
                             #pragma unroll
                             for (int q = 0; q < 2; ++q) {                       // for the second pass
                                 uint32_t y[16];

@@ -56,8 +56,9 @@ def windowed(abi, rng, pg, new, lens, H, dtype, window, sinks, causal, mask=None
     return out[:T, : H * D], lse
 
 
-@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
-@pytest.mark.parametrize("page,D,H,Hkv", [(16, 64, 2, 1), (32, 128, 7, 1), (64, 128, 4, 4), (128, 64, 6, 2), (16, 128, 16, 1)])
+@pytest.mark.parametrize("dtype,page,D,H,Hkv", [
+    (torch.float16, 16, 64, 2, 1), (torch.bfloat16, 32, 128, 7, 1), (torch.float16, 64, 128, 4, 4),
+    (torch.bfloat16, 128, 64, 6, 2), (torch.bfloat16, 16, 128, 16, 1)])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (5, 1), (16, 4), (33, 0), (100, 130), (129, 20), (1 << 28, 0)])
 @pytest.mark.parametrize("causal,masked", [(False, False), (True, True), (True, False)])
 def test_window(abi, dtype, page, D, H, Hkv, window, sinks, causal, masked):
@@ -189,20 +190,27 @@ class Shared(Paged):
         fill(self, rng, lens)
 
 
-def share(abi, rng, pg, new, lens, H, dtype, causal=False, mask=None, q=None, pad=0, max_new=None, max_rows=None, most=None,
-          max_shared=None, verify=True, **kw):
+# A bound of the shared lengths under which the prefix gets a pass of its own
+# (with few sequences and short prefixes the call is kv_cache_attention's).
+APART = 1 << 20
+
+
+def share(abi, rng, pg, new, lens, H, dtype, causal=False, mask=None, q=None, pad=0, max_rows=None, most=None,
+          max_shared=APART, verify=True, **kw):
     T, D = sum(new), pg.D
     if q is None:
         q, _ = randn(rng, (T, H * D + pad), dtype)
         q = q[:, : H * D]
     out = torch.full((T + 1, H * D + pad), 7.0, dtype=dtype, device="cuda")
     lse = torch.full((T, H), 7.0, device="cuda")
-    rows = [sum(new[a:b]) for a, b in zip(pg.first, pg.first[1:])]
+    dm = None
+    if mask is not None:
+        dm = torch.zeros(len(lens), max(mask.shape[1], max_shared, most or 0), dtype=torch.uint8, device="cuda")
+        dm[:, : mask.shape[1]] = torch.from_numpy(mask).cuda()
     abi.kv_cache_attention_shared(
-        q, pg.cache, pg.dev_table, i32(lens), starts(new), out[:T, : H * D], max_new=max_new or max(new),
-        max_len=most or max(lens), group_start=i32(pg.first), shared_len=i32(pg.shared),
-        max_rows=max_rows or max(rows, default=0), max_shared=max_shared or max(pg.shared, default=0), causal=causal, lse=lse,
-        key_mask=None if mask is None else torch.from_numpy(mask).cuda(), **kw)
+        q, pg.cache, pg.dev_table, i32(lens), starts(new), out[:T, : H * D], max_new=max(new), max_len=most or max(lens),
+        group_start=i32(pg.first), shared_len=i32(pg.shared), max_rows=T + 1 if max_rows is None else max_rows,
+        max_shared=max_shared, causal=causal, lse=lse, key_mask=dm, **kw)
     if verify:
         abi.check_status()
         assert torch.all(out[:, H * D:] == 7.0) and torch.all(out[T:] == 7.0)
@@ -215,14 +223,17 @@ def share(abi, rng, pg, new, lens, H, dtype, causal=False, mask=None, q=None, pa
 @pytest.mark.parametrize("page,D,H,Hkv", [(16, 64, 2, 1), (32, 128, 7, 1), (64, 128, 4, 4), (128, 64, 12, 2)])
 @pytest.mark.parametrize("first,shared", [
     ([0, 9], [17]), ([0, 4, 9], [128, 300]), ([1, 3, 3, 8], [130, 44, 1]), ([2, 4], [0]), ([0, 1, 9], [16, 15])])
-@pytest.mark.parametrize("causal,masked", [(False, False), (True, False), (False, True), (True, True)])
-def test_shared(abi, dtype, page, D, H, Hkv, first, shared, causal, masked):
+@pytest.mark.parametrize("causal,masked,most", [(False, False, 1 << 21), (True, False, None), (False, True, None),
+                                                (True, True, 1 << 21)])
+def test_shared(abi, dtype, page, D, H, Hkv, first, shared, causal, masked, most):
     """Groups of none to nine sequences, shared lengths of none to several
     tiles that end inside a page, sequences outside of all groups, new tokens
     from none on, own lengths from the new tokens alone on, masks that leave the
-    prefix, what follows or both empty."""
+    prefix, what follows or both empty; a tight and a generous bound of the
+    lengths (they lead to different kernels), and the bounds under which nothing
+    is done apart."""
     rng = np.random.default_rng(page * 7 + D + H + shared[0])
-    new = [2, 1, 3, 1, 0, 5, 1, 33, 9]
+    new = [2, 1, 3, 1, 0, 5, 1, 4, 2]
     own = [2, 1, 40, 130, 17, 5, 300, 40, 9]
     base = [0] * 9
     for g, s in enumerate(shared):
@@ -239,24 +250,28 @@ def test_shared(abi, dtype, page, D, H, Hkv, first, shared, causal, masked):
                     mask[first[g]:first[g + 1], :s] = 0
         for b in (2, 7):
             mask[b, base[b]:] = 0
-    share(abi, rng, pg, new, lens, H, dtype, causal, mask, pad=8)
+    share(abi, rng, pg, new, lens, H, dtype, causal, mask, pad=8, most=most)
+    if dtype is torch.float16 and page == 32:
+        share(abi, rng, pg, new, lens, H, dtype, causal, mask, max_shared=max(shared))
 
 
-@pytest.mark.parametrize("new,H,Hkv,D", [(1, 28, 4, 128), (1, 4, 4, 64), (32, 7, 1, 128), (61, 2, 2, 64), (3, 16, 1, 128)])
-@pytest.mark.parametrize("bound", [0, 1 << 20])
-def test_shared_long(abi, new, H, Hkv, D, bound):
-    """Prefixes and own parts of many tiles, cut into runs, under tight and
-    generous bounds; the same bits again."""
+# rows of a key/value head of a sequence, of the first group: 7, 35 (28 heads on 4); 1, 5; 35, 175; 9, 45; 48, 240;
+# 48, 240
+@pytest.mark.parametrize("new,H,Hkv,D", [(1, 28, 4, 128), (1, 4, 4, 64), (5, 7, 1, 128), (9, 2, 2, 64), (3, 16, 1, 128),
+                                         (12, 4, 1, 64)])
+@pytest.mark.parametrize("most", [None, 1 << 21])
+def test_shared_long(abi, new, H, Hkv, D, most):
+    """Prefixes and own parts of many tiles, cut into runs; the same bits
+    again."""
     rng = np.random.default_rng(new + H)
     first, shared, own = [0, 5, 7], [2500, 1111], [900, 61, 200, 61, 333, 1500, 64]
     lens = [shared[b >= 5] + o for b, o in enumerate(own)]
     pg = Shared(abi, rng, first, shared, lens, Hkv, 64, D)
     q, _ = randn(rng, (7 * new, H * D), torch.bfloat16)
-    go = lambda: share(abi, rng, pg, [new] * 7, lens, H, torch.bfloat16, q=q, most=max(lens) + bound,
-                       max_shared=2500 + bound, max_rows=7 * new + 1)
+    go = lambda: share(abi, rng, pg, [new] * 7, lens, H, torch.bfloat16, q=q, most=most, max_rows=5 * new)
     one, two = go(), go()
     assert torch.equal(one[0], two[0]) and torch.equal(one[1], two[1])
-    share(abi, rng, pg, [new] * 7, lens, H, torch.bfloat16, causal=True, q=q)
+    share(abi, rng, pg, [new] * 7, lens, H, torch.bfloat16, causal=True, q=q, most=most, max_rows=5 * new)
 
 
 def test_shared_many_groups(abi):
@@ -270,7 +285,7 @@ def test_shared_many_groups(abi):
     new = [int(x) for x in rng.integers(0, 3, B)]
     lens = [int(base[b]) + new[b] + int(rng.integers(0, 9)) for b in range(B)]
     pg = Shared(abi, rng, first, shared, lens, 1, 16, 64)
-    share(abi, rng, pg, new, lens, 2, torch.float16)
+    share(abi, rng, pg, new, lens, 2, torch.float16, max_rows=8)
 
 
 def test_shared_is_the_plain_call_without_sharing(abi):
@@ -280,52 +295,51 @@ def test_shared_is_the_plain_call_without_sharing(abi):
     q, _ = randn(rng, (6, 4 * 64), torch.float16)
     out, lse = torch.empty_like(q), torch.empty(6, 4, device="cuda")
     abi.kv_cache_attention(q, pg.cache, pg.dev_table, i32(lens), starts(new), out, max_new=3, max_len=200, lse=lse)
-    got = share(abi, rng, pg, new, lens, 4, torch.float16, q=q)
+    got = share(abi, rng, pg, new, lens, 4, torch.float16, q=q, max_rows=3, max_shared=64)
     assert torch.equal(got[0], out) and torch.equal(got[1], lse)
     pg.first, pg.shared = [0], []                                   # no groups
-    got = share(abi, rng, pg, new, lens, 4, torch.float16, q=q)
+    got = share(abi, rng, pg, new, lens, 4, torch.float16, q=q, max_rows=0, max_shared=0)
     assert torch.equal(got[0], out) and torch.equal(got[1], lse)
 
 
 def test_shared_outside_its_bounds(abi):
     """What does not fit is reported, and the group of it alone is wrong."""
     rng = np.random.default_rng(4)
-    lens, new = [150, 150, 150, 150], [2, 2, 2, 2]
-    pg = Shared(abi, rng, [0, 2, 4], [96, 128], lens, 1, 32, 64)
-    q, _ = randn(rng, (8, 7 * 64), torch.float16)
-    right = share(abi, rng, pg, new, lens, 7, torch.float16, q=q)[0]
-    for first, shared, kw in (([0, 2, 4], [96, 149], {}), ([0, 2, 4], [96, -1], {}), ([0, 2, 5], [96, 128], {}),
-                              ([0, 2, 1], [96, 128], {}), ([0, 2, 4], [96, 128], dict(max_shared=100)),
-                              ([0, 2, 4], [96, 140], dict(max_shared=128))):
+    lens, new = [150] * 5, [2] * 5
+    pg = Shared(abi, rng, [0, 2, 5], [96, 128], lens, 1, 32, 64)
+    q, _ = randn(rng, (10, 7 * 64), torch.float16)
+    go = lambda **kw: share(abi, rng, pg, new, lens, 7, torch.float16, q=q, **kw)
+    go(max_rows=6)
+    for first, shared, kw in (([0, 2, 5], [96, 149], {}), ([0, 2, 5], [96, -1], {}), ([0, 2, 6], [96, 128], {}),
+                              ([0, 2, 1], [96, 128], {}), ([0, 2, 5], [96, APART + 1], {}),
+                              ([0, 2, 5], [96, 128], dict(max_rows=5))):
         pg.first, pg.shared = first, shared
-        out = share(abi, rng, pg, new, lens, 7, torch.float16, q=q, verify=False, max_rows=4, **kw)[0]
+        out, lse = go(verify=False, **dict(dict(max_rows=6), **kw))
         with pytest.raises(abi.StarqError) as e:
             abi.check_status()
         assert e.value.code == abi.ERR_RANGE, (first, shared, kw)
-        assert torch.equal(out[:4], right[:4])
-    pg.first, pg.shared = [0, 2, 4], [96, 128]
-    share(abi, rng, pg, new, lens, 7, torch.float16, q=q, verify=False, max_rows=3)
-    with pytest.raises(abi.StarqError):
-        abi.check_status()
-    share(abi, rng, pg, new, lens, 7, torch.float16, q=q)
+        check(pg, q[:4], out[:4], lse[:4], [2, 2], [150, 150], 7, torch.float16,
+              lambda b: od.window_sees(2, 150, 1 << 28, 0, False))
+    pg.first, pg.shared = [0, 2, 5], [96, 128]
+    go(max_rows=6)
 
 
-@pytest.mark.parametrize("new", [1, 20])
+@pytest.mark.parametrize("new", [1, 5])
 def test_shared_not_finite(abi, new):
     """A poisoned block of the prefix shows in its group's rows, one of a
     sequence's own in its rows; the others are finite."""
     rng = np.random.default_rng(9)
-    lens = [300, 290, 310, 300]
-    pg = Shared(abi, rng, [0, 2, 4], [256, 130], lens, 1, 16, 64)
-    q, _ = randn(rng, (4 * new, 7 * 64), torch.bfloat16)
+    lens = [300, 290, 310, 300, 301, 280]
+    pg = Shared(abi, rng, [0, 3, 6], [256, 130], lens, 1, 16, 64)
+    q, _ = randn(rng, (6 * new, 7 * 64), torch.bfloat16)
     row = lambda b: slice(b * new, (b + 1) * new)
-    for page, bad in ((pg.table[0, 3], [0, 1]), (pg.table[2, 2], [2, 3]), (pg.table[1, 17], [1])):
+    for page, bad in ((pg.table[0, 3], [0, 1, 2]), (pg.table[3, 2], [3, 4, 5]), (pg.table[1, 17], [1])):
         for scale in (pg.cache.k_scale, pg.cache.v_scale):
             keep = scale[page].clone()
             scale[page] = float("nan")
-            out, lse = share(abi, rng, pg, [new] * 4, lens, 7, torch.bfloat16, q=q, verify=False)
+            out, lse = share(abi, rng, pg, [new] * 6, lens, 7, torch.bfloat16, q=q, verify=False, max_rows=3 * new)
             scale[page] = keep
-            for b in range(4):
+            for b in range(6):
                 assert torch.isnan(out[row(b)]).all() if b in bad else torch.isfinite(out[row(b)]).all(), (b, bad)
     abi.check_status()
 
@@ -343,7 +357,7 @@ def test_shared_graph_and_stream(abi):
     lses = [torch.empty(6, 4, device="cuda") for _ in range(3)]
     call = lambda k, **kw: abi.kv_cache_attention_shared(
         q, pg.cache, pg.dev_table, lens, start, outs[k], max_new=2, max_len=700, group_start=first, shared_len=common,
-        max_rows=6, max_shared=512, causal=True, lse=lses[k], **kw)
+        max_rows=6, max_shared=APART, causal=True, lse=lses[k], **kw)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     call(0, stream=side)
