@@ -23,6 +23,16 @@ weights carry one scale per group of input channels, the cache 8-bit codes;
 activations stay 16-bit. The rotary table is filled once (glue_rope_table);
 torch holds the buffers, multiplies silu(g) u and picks the tokens.
 
+Three things may be asked for besides:
+- layers that see a sliding window and a few first tokens
+  (kv_cache_attention_window; every full_every-th layer still sees all);
+- several answers to one prompt: its pages are the sequences' common ones and
+  it is run once (prefill_shared), attention reads it once for all of them
+  (kv_cache_attention_shared);
+- rules on the answer's tokens, a sequence each: penalties for tokens of the
+  prompt and the answer so far, biases, masks, and the confidence by which
+  positions are chosen (logits_pick).
+
 `python -m paper_2606_04945_gb300.cached` generates and prints the time of a
 step. A linear takes at most 32 rows a call: a prompt goes through it in
 slices, so a long prompt is not this module's strength. Attention is given
@@ -60,6 +70,9 @@ class CachedConfig:
     scaling: str = "none"                   # of the rotary table
     factor: float = 1.0
     original: float = 0.0
+    window: int = 0                         # slots that a layer sees up to a position's own (0: all)
+    sinks: int = 0                          # first slots that a window leaves visible
+    full_every: int = 0                     # with a window: every full_every-th layer sees all slots (0: none)
     dtype: torch.dtype = torch.bfloat16
     seed: int = 0
 
@@ -105,48 +118,73 @@ class CachedStack:
         self.page_table = torch.arange(c.batch * pages, dtype=torch.int32, device=device).view(c.batch, pages)
         self.past = torch.zeros(c.batch, dtype=torch.int32, device=device)
         self.held = 0                       # past, on the host
+        # one group of all sequences, which have this many of their first tokens in common
+        self.own_pages = self.page_table.clone()
+        self.group = torch.tensor([0, c.batch], dtype=torch.int32, device=device)
+        self.shared_len = torch.zeros(1, dtype=torch.int32, device=device)
+        self.shared = 0                     # shared_len, on the host
         self.buffers = {}
 
-    def _buffers(self, n):
-        """Buffers and index vectors of a pass over n positions a sequence."""
-        if n not in self.buffers:
-            c, T, dev = self.cfg, self.cfg.batch * n, self.device
+    def _buffers(self, B, n):
+        """Buffers and index vectors of a pass over n positions of each of B
+        sequences."""
+        if (B, n) not in self.buffers:
+            c, T, dev = self.cfg, B * n, self.device
             t = lambda *s: torch.empty(*s, dtype=c.dtype, device=dev)
-            self.buffers[n] = dict(
+            size = max(abi.kv_cache_attention_workspace_size(B, n, c.heads, c.kv_heads, c.dim),
+                       abi.kv_cache_attention_shared_workspace_size(T, B, n, 1, T, c.heads, c.kv_heads, c.dim))
+            self.buffers[B, n] = dict(
                 x=t(T, c.hidden), h=t(T, c.hidden), qkv=t(T, self.width), q=t(T, c.heads * c.dim),
                 attn=t(T, c.heads * c.dim), o=t(T, c.hidden), gu=t(T, 2 * c.ffn), act=t(T, c.ffn), down=t(T, c.hidden),
                 logits=torch.empty(T, c.vocab, dtype=torch.float32, device=dev),
-                start=torch.arange(c.batch + 1, dtype=torch.int32, device=dev) * n,
+                start=torch.arange(B + 1, dtype=torch.int32, device=dev) * n,
                 step=torch.arange(n, dtype=torch.int32, device=dev),
-                workspace=torch.empty(abi.kv_cache_attention_workspace_size(c.batch, n, c.heads, c.kv_heads, c.dim),
-                                      dtype=torch.uint8, device=dev))
-        return self.buffers[n]
+                workspace=torch.empty(size, dtype=torch.uint8, device=dev))
+        return self.buffers[B, n]
+
+    def windowed(self, layer):
+        """Whether a layer sees a window."""
+        c = self.cfg
+        return c.window > 0 and not (c.full_every > 0 and layer % c.full_every == c.full_every - 1)
+
+    def _attention(self, layer, cache, q, held, b, n, out):
+        c, B = self.cfg, held.shape[0]
+        call = dict(max_new=n, max_len=c.capacity, workspace=b["workspace"])
+        at = (q, cache, self.page_table[:B], held, b["start"], out)
+        if self.windowed(layer):
+            abi.kv_cache_attention_window(*at, window=c.window, sinks=c.sinks, **call)
+        elif self.shared > 0 and B == c.batch:
+            abi.kv_cache_attention_shared(*at, group_start=self.group, shared_len=self.shared_len, max_rows=B * n,
+                                          max_shared=c.capacity, **call)
+        else:
+            abi.kv_cache_attention(*at, **call)
 
     def forward(self, tok, hook=None):
         """One pass over tok [batch][n], the n positions behind each
         sequence's past tokens: their keys and values go into the cache, and
-        the logits [batch n][vocab] are returned. hook(layer, name, values)
-        sees what each operator read and wrote (for tests)."""
+        the logits [batch n][vocab] are returned. (With fewer rows than
+        sequences: a pass of the first ones.) hook(layer, name, values) sees
+        what each operator read and wrote (for tests)."""
         c = self.cfg
-        n = tok.shape[1]
+        B, n = tok.shape
         if self.held + n > c.capacity:
             raise ValueError(f"{self.held} cached and {n} new positions are more than the cache's {c.capacity} tokens")
-        b = self._buffers(n)
+        b = self._buffers(B, n)
         hk = hook or (lambda layer, name, values: None)
         kq, kv = c.heads * c.dim, c.kv_heads * c.dim
-        pos = (self.past[:, None] + b["step"][None]).view(-1)
-        held = self.past + n
+        past, pages = self.past[:B], self.page_table[:B]
+        pos = (past[:, None] + b["step"][None]).view(-1)
+        held = past + n
         x, h, qkv = b["x"], b["h"], b["qkv"]
         x.copy_(self.embed[tok.reshape(-1)])
         abi.add_rmsnorm(x, self.gain, h, eps=EPS)
         for i, (m, cache) in enumerate(zip(self.layers, self.caches)):
             m["qkv"].run(h, qkv)
             hk(i, "qkv", (m["qkv"], h, qkv))
-            abi.kv_cache_append(cache, qkv[:, kq:kq + kv], qkv[:, kq + kv:], b["start"], self.past, self.page_table, pos,
+            abi.kv_cache_append(cache, qkv[:, kq:kq + kv], qkv[:, kq + kv:], b["start"], past, pages, pos,
                                 self.rope, max_new=n, Q=qkv[:, :kq], Q_out=b["q"])
             hk(i, "append", (cache, qkv, b["q"], pos))
-            abi.kv_cache_attention(b["q"], cache, self.page_table, held, b["start"], b["attn"], max_new=n,
-                                   max_len=c.capacity, workspace=b["workspace"])
+            self._attention(i, cache, b["q"], held, b, n, b["attn"])
             hk(i, "attention", (cache, b["q"], held, b["attn"]))
             m["o"].run(b["attn"], b["o"])
             hk(i, "o", (m["o"], b["attn"], b["o"]))
@@ -166,11 +204,36 @@ class CachedStack:
         another and stay in the cache."""
         if prompt.shape[1] > self.cfg.capacity:
             raise ValueError(f"the prompt is longer than the cache's {self.cfg.capacity} tokens")
-        self.past.zero_()
-        self.held = 0
+        self._begin()
         if prompt.shape[1] > 0:
             self.forward(prompt)
             self.keep(prompt.shape[1])
+
+    def _begin(self):
+        """No tokens, and every sequence on pages of its own."""
+        self.past.zero_()
+        self.held = self.shared = 0
+        self.shared_len.zero_()
+        self.page_table.copy_(self.own_pages)
+
+    def prefill_shared(self, prompt):
+        """One prompt [P] begins all sequences. Its whole pages are run once
+        and become common pages; the tokens behind them enter each sequence's
+        own pages."""
+        c, P = self.cfg, prompt.shape[0]
+        if P > c.capacity:
+            raise ValueError(f"the prompt is longer than the cache's {c.capacity} tokens")
+        self._begin()
+        common = P // c.page
+        if common > 0:
+            self.forward(prompt[None, : common * c.page])
+            self.page_table[:, :common] = self.own_pages[0, :common]
+            self.shared = common * c.page
+            self.shared_len.fill_(self.shared)
+            self.keep(self.shared)
+        if P > self.shared:
+            self.forward(prompt[None, self.shared:].expand(c.batch, -1))
+            self.keep(P - self.shared)
 
     def keep(self, n):
         """The last pass's n positions become part of the prefix."""
@@ -180,7 +243,9 @@ class CachedStack:
     def capture(self):
         """Records a pass over a block in a CUDA graph; returns (graph, token
         buffer [batch][block], logits). It reads `past` where it is, so one
-        graph serves every block. (The recording itself is a pass over masked
+        graph serves every block; recorded behind a shared prompt, it serves
+        prompts of the sequences' own too, and the other way round, but then
+        reads a shared prompt for each of them. (The recording itself is a pass over masked
         positions behind the prefix, which has to leave them room.)"""
         c = self.cfg
         tok = torch.full((c.batch, c.block), self.mask_id, dtype=torch.long, device=self.device)
@@ -194,13 +259,22 @@ class CachedStack:
             logits = self.forward(tok)
         return graph, tok, logits
 
-    def generate(self, prompt, blocks, captured=None):
-        """Prompt [batch][P], then `blocks` blocks of new tokens; returns
-        [batch][blocks x block]. captured: capture()'s result."""
+    def generate(self, prompt, blocks, captured=None, rules=None, confidence=None):
+        """Prompt [batch][P] ([P]: the same for all sequences), then `blocks`
+        blocks of new tokens; returns [batch][blocks x block]. captured:
+        capture()'s result. rules: arguments of abi.LogitsRules (params,
+        biases, allowed; the history is the prompt and the answer as fixed in
+        the steps before), confidence: "probability", "margin" or "entropy", by which a step
+        chooses its positions. With either a position for which nothing is allowed stays
+        masked."""
         c = self.cfg
-        if prompt.shape[1] + blocks * c.block > c.capacity:
+        if prompt.shape[-1] + blocks * c.block > c.capacity:
             raise ValueError(f"prompt and answer are longer than the cache's {c.capacity} tokens")
-        self.prefill(prompt)
+        if prompt.dim() == 1:
+            self.prefill_shared(prompt)
+        else:
+            self.prefill(prompt)
+        pick_tokens = self._picker(prompt, rules, confidence)
         graph, tok, logits = captured or (None, torch.empty(c.batch, c.block, dtype=torch.long, device=self.device), None)
         out = []
         for _ in range(blocks):
@@ -212,10 +286,12 @@ class CachedStack:
                 else:
                     graph.replay()
                 logits[:, self.mask_id] = float("-inf")                # a position never becomes masked again
-                best, new = torch.softmax(logits, -1).view(c.batch, c.block, -1).max(-1)
-                pick = best.masked_fill(~masked, -1.0).topk(min(c.unmask_per_step, left), dim=1).indices
-                tok.scatter_(1, pick, new.gather(1, pick))
+                best, new, history = pick_tokens(logits)
+                pick = best.masked_fill(~masked, float("-inf")).topk(min(c.unmask_per_step, left), dim=1).indices
+                fixed = new.gather(1, pick)
+                tok.scatter_(1, pick, fixed)
                 masked.scatter_(1, pick, False)
+                history(fixed)
             if graph is None:
                 self.forward(tok)
             else:
@@ -223,6 +299,52 @@ class CachedStack:
             self.keep(c.block)
             out.append(tok.clone())
         return torch.cat(out, 1) if out else tok[:, :0].clone()
+
+
+    def _picker(self, prompt, rules, confidence):
+        """logits -> (confidence and most likely token of every position,
+        what to call with the tokens that a step fixes)."""
+        c = self.cfg
+        if rules is None and confidence is None:
+            return lambda logits: (*torch.softmax(logits, -1).view(c.batch, c.block, -1).max(-1), lambda fixed: None)
+        # what was written: the prompt, then the answer in the order in which it is fixed
+        P, dev = prompt.shape[-1], self.device
+        written = torch.zeros(c.batch, c.capacity, dtype=torch.int32, device=dev)
+        written[:, :P] = prompt
+        count = torch.full((c.batch,), P, dtype=torch.int32, device=dev)
+        held = [P]
+        token = torch.empty(c.batch * c.block, dtype=torch.int32, device=dev)
+        best = torch.empty(c.batch * c.block, device=dev)
+        handle = abi.LogitsRules(c.vocab, history=written, history_len=count, **(rules or {}))
+        start = self._buffers(c.batch, c.block)["start"]
+
+        def history(fixed):
+            n = fixed.shape[1]
+            written[:, held[0]:held[0] + n] = fixed
+            held[0] += n
+            count.add_(n)
+
+        def pick(logits):
+            abi.logits_pick(logits, start, handle, token, best, max_new=c.block, kind=confidence or "probability")
+            # (token -1: nothing is allowed)
+            return best.view(c.batch, c.block), token.clamp(min=self.mask_id).long().view(c.batch, c.block), history
+
+        return pick
+
+
+def several_answers(answers=8, window=256):
+    """Answers to one prompt, each with penalties of its own, by layers that
+    see a window but for every other one."""
+    cfg = CachedConfig(batch=answers, unmask_per_step=8, window=window, sinks=4, full_every=2)
+    stack = CachedStack(cfg)
+    prompt = torch.randint(1, cfg.vocab, (520,), device="cuda")
+    stack.prefill_shared(prompt)
+    captured = stack.capture()
+    params = torch.tensor([[1.0, 1.0 + 0.1 * b, 0.2 * b, 0.05 * b] for b in range(answers)], device="cuda")
+    tokens = stack.generate(prompt, 2, captured, rules=dict(params=params), confidence="margin")
+    abi.check_status()
+    print(f"{answers} answers of {tokens.shape[1]} tokens to one prompt of {len(prompt)}, {stack.shared} of them shared, "
+          f"windows of {window}: {[len(set(t.tolist())) for t in tokens]} different tokens each")
 
 
 def main():
@@ -243,6 +365,7 @@ def main():
     abi.check_status()
     print(f"{tokens.shape[1]} tokens behind {prompt.shape[1]}: {tokens[0, :8].tolist()} ...; {cfg.layers} layers over "
           f"{cfg.block} positions and {stack.held} cached tokens: {start.elapsed_time(end) / passes:.3f} ms a step")
+    several_answers()
 
 
 if __name__ == "__main__":

@@ -1,0 +1,159 @@
+"""Block-wise denoising (cached.py) with windows, behind a shared prompt and
+under rules on tokens: the attention of every pass against oracle/decode.py on
+the GPU's own inputs (tolerances: test_gpu_decode.py), the tokens against the
+rules."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode as od
+from oracle import logits as ol
+from tests.test_gpu_cached import SHAPES, TINY, U, made, num
+
+pytestmark = pytest.mark.gpu
+
+
+class AttentionMirror:
+    """Checks each layer's attention against what its cache holds."""
+
+    def __init__(self, stack):
+        self.stack, self.seen = stack, 0
+
+    def __call__(self, layer, name, values):
+        if name != "attention":
+            return
+        stack, c = self.stack, self.stack.cfg
+        cache, q, held, out = values
+        q, out, held = num(q).reshape(-1, c.heads, c.dim), num(out).reshape(-1, c.heads, c.dim), held.cpu().numpy()
+        n = len(q) // len(held)
+        codes = [x.cpu().numpy().astype(np.int64) - 128 for x in (cache.K, cache.V)]
+        scales = [x.cpu().numpy() for x in (cache.k_scale, cache.v_scale)]
+        table = stack.page_table.cpu().numpy()
+        window = c.window if stack.windowed(layer) else 1 << 28
+        for b, L in enumerate(held):
+            r = slice(b * n, (b + 1) * n)
+            k, v = (od.read(x, s, table[b], 0, L, c.page) for x, s in zip(codes, scales))
+            ref, _, mag, size = od.attention_of(q[r], k, v, c.dim ** -0.5, od.window_sees(n, L, window, c.sinks, False))
+            d = ((c.dim + 4) * 2.0 ** -24 * size)[..., None]
+            rel = 2 * (2 * d + 2.0 ** -20) + 2.0 ** -11 + L * 2.0 ** -24 + 2.0 ** -20
+            assert np.all(np.abs(out[r] - ref) <= mag * rel + U[c.dtype] * np.abs(ref) * (1 + rel) + TINY[c.dtype]), layer
+        self.seen += 1
+
+
+def test_windows(abi):
+    """Two layers, the second of which sees everything; a replayed pass is
+    the eager one."""
+    stack, prompt, rng = made(dict(SHAPES[0], window=11, sinks=3, full_every=2))
+    c = stack.cfg
+    assert [stack.windowed(i) for i in range(4)] == [True, False, True, False]
+    mirror = AttentionMirror(stack)
+    stack.past.zero_()
+    stack.forward(prompt, mirror)
+    stack.keep(prompt.shape[1])
+    for last in (False, True, False):
+        tok = torch.from_numpy(rng.integers(0, c.vocab, (c.batch, c.block))).cuda()
+        stack.forward(tok, mirror)
+        if last:
+            stack.keep(c.block)
+    assert mirror.seen == 4 * c.layers
+    tokens = stack.generate(prompt, 2)
+    stack.prefill(prompt)
+    assert torch.equal(stack.generate(prompt, 2, stack.capture()), tokens)
+    abi.check_status()
+
+
+@pytest.mark.parametrize("P", [40, 48, 9])
+def test_shared_prompt(abi, P):
+    """The prompt's whole pages are common and run once; the answers' rows
+    go to pages of their own, so the common ones stay as they were."""
+    stack, _, rng = made(dict(SHAPES[0], batch=3))
+    c = stack.cfg
+    prompt = torch.from_numpy(rng.integers(1, c.vocab, P)).cuda()
+    stack.prefill_shared(prompt)
+    common = P // c.page
+    assert stack.shared == common * c.page == int(stack.shared_len) and stack.held == P == int(stack.past[2])
+    table = stack.page_table.cpu().numpy()
+    assert np.all(table[:, :common] == table[0, :common]) and len(np.unique(table[:, common:])) == table[:, common:].size
+    keep = [x.K[table[0, :common]].clone() for x in stack.caches]
+    mirror = AttentionMirror(stack)
+    for last in (False, True, False):
+        tok = torch.from_numpy(rng.integers(0, c.vocab, (c.batch, c.block))).cuda()
+        assert torch.isfinite(stack.forward(tok, mirror)).all()
+        if last:
+            stack.keep(c.block)
+    assert mirror.seen == 3 * c.layers
+    assert all(torch.equal(x.K[table[0, :common]], k) for x, k in zip(stack.caches, keep))
+    # replays of either recording, and prompts of the sequences' own afterwards
+    tokens = stack.generate(prompt, 2)
+    assert bool((tokens != stack.mask_id).all()) and torch.equal(tokens[0], tokens[1])
+    stack.prefill_shared(prompt)
+    captured = stack.capture()
+    assert torch.equal(stack.generate(prompt, 2, captured), tokens)
+    own = torch.from_numpy(rng.integers(1, c.vocab, (3, P))).cuda()
+    eager = stack.generate(own, 2)
+    assert stack.shared == 0 and torch.equal(stack.page_table, stack.own_pages)
+    assert torch.equal(stack.generate(own, 2, captured).ne(stack.mask_id), eager.ne(stack.mask_id))
+    abi.check_status()
+    with pytest.raises(ValueError):
+        stack.prefill_shared(torch.ones(97, dtype=torch.long, device="cuda"))
+
+
+@pytest.mark.parametrize("confidence", ["probability", "margin", "entropy"])
+def test_rules(abi, confidence):
+    """Masks, a penalty that nothing outweighs, and biases of a sequence."""
+    stack, prompt, rng = made(SHAPES[0])
+    c = stack.cfg
+    bits = rng.random((c.batch, c.vocab)) < 0.2
+    words = np.zeros((c.batch, 16 * 32), np.uint64)
+    words[:, : c.vocab] = bits
+    words = (words.reshape(c.batch, 16, 32) << np.arange(32, dtype=np.uint64)).sum(-1).astype(np.uint32).view(np.int32)
+    never = torch.tensor([[1.0, 1.0, 1e9, 0.0]] * c.batch, device="cuda")
+    once = stack.generate(prompt, 2, rules=dict(params=never, allowed=torch.from_numpy(words).cuda()), confidence=confidence)
+    for b, row in enumerate(once.tolist()):
+        assert bits[b][row].all() and not set(row) & set(prompt[b].tolist())
+        # a token can be chosen again in the step that fixes it alone, whose positions do not see each other's
+        assert max(row.count(t) for t in row) <= c.unmask_per_step
+    ids = torch.tensor([[7], [9]], dtype=torch.int32, device="cuda")
+    same = stack.generate(prompt, 1, rules=dict(bias_ids=ids, bias_values=torch.full((2, 1), 1e6, device="cuda"),
+                                                bias_len=torch.tensor([1, 1], dtype=torch.int32, device="cuda")))
+    assert same.tolist() == [[7] * c.block, [9] * c.block]
+    none = stack.generate(prompt, 1, rules=dict(allowed=torch.zeros(2, 16, dtype=torch.int32, device="cuda")),
+                          confidence=confidence)
+    assert bool((none == stack.mask_id).all())
+    abi.check_status()
+
+
+def test_a_run_together(abi):
+    """Windowed and full layers behind a shared prompt, tokens under rules:
+    every pass's attention and every choice of a token against the oracles."""
+    stack, _, rng = made(dict(SHAPES[1], batch=3, window=40, sinks=2, full_every=2))
+    c = stack.cfg
+    prompt = torch.from_numpy(rng.integers(1, c.vocab, 70)).cuda()
+    params = np.float32([[0.7, 1.3, 0.5, 0.1], [1.0, 1.0, 0.0, 0.0], [1.5, 0.9, -0.2, 0.3]])
+    stack.prefill_shared(prompt)
+    mirror = AttentionMirror(stack)
+    logits = stack.forward(torch.full((3, c.block), stack.mask_id, dtype=torch.long, device="cuda"), mirror)
+    assert mirror.seen == c.layers and stack.shared == 64
+    pick = stack._picker(prompt, dict(params=torch.from_numpy(params).cuda()), "margin")
+    written = [prompt.tolist()] * 3
+    for _ in range(2):
+        best, new, history = pick(logits)
+        x, best, new = logits.cpu().numpy(), best.cpu().numpy(), new.cpu().numpy()
+        for b in range(3):
+            for i in range(c.block):
+                z, _ = ol.rules(x[b * c.block + i], params[b], written[b])
+                token, conf, _, D = ol.pick(z, params[b][0], "margin")
+                E = (c.vocab / 32 + 64) * 2.0 ** -22 + 2.0 ** -21 * (1.4427 * D + 1)
+                assert new[b, i] == token and abs(best[b, i] - conf) <= E * conf + 2.0 ** -22
+        history(torch.from_numpy(new[:, :4]).cuda())
+        written = [w + new[b, :4].tolist() for b, w in enumerate(written)]
+    tokens = stack.generate(prompt, 1, rules=dict(params=torch.from_numpy(params).cuda()), confidence="margin")
+    assert tokens.shape == (3, c.block) and bool((tokens != stack.mask_id).all())
+    abi.check_status()
+
+
+def test_command(abi, capsys):
+    from paper_2606_04945_gb300 import cached
+    cached.several_answers(answers=3, window=100)
+    assert "3 answers of 64 tokens to one prompt of 520, 512 of them shared" in capsys.readouterr().out
