@@ -729,13 +729,80 @@ def kv_cache_attention_workspace_size(B, max_new, H, Hkv, D):
     return int(lib.kv_cache_attention_workspace_size(B, max_new, H, Hkv, D))
 
 
-def _attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, key_mask, lse):
-    """What the attention calls have in common: (arguments up to max_len,
-    those from key_mask to mask_ld, those from Out to lse, sequences, heads)."""
+def kv_cache_attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, causal=False, key_mask=None,
+                       scale=None, lse=None, workspace=None, stream=None):
+    """Attention of the rows of Q [T][H D] (sequence b: rows seq_start[b] ..,
+    at most max_new) over the kv_len[b] (at most max_len) cached tokens into
+    Out [T][H D]; lse [T][H] receives the log-sum-exp. key_mask uint8
+    [B][>= max_len]: 0 = not seen. scale: default 1 / sqrt(D). workspace:
+    default of this call's own, on its stream."""
     shape, B, D, dtype = Q.shape, kv_len.shape[0], cache.D, Q.dtype
     T = shape[0]
     H = shape[1] // D
     if shape != (T, H * D) or Out.shape != shape or Out.dtype is not dtype:
+        raise ValueError("starq expects Q and Out as T rows of H * D channels of one type")
+    q, ldq = _rows(Q, "Q")
+    o, ldo = _rows(Out, "Out")
+    pt, pld = _pages(page_table, B)
+    mk, mld = None, 0
+    if key_mask is not None:
+        if key_mask.dtype is not _U8 or key_mask.shape[0] != B:
+            raise ValueError(f"starq expects key_mask as uint8 [{B}][slots]")
+        mk, mld = _rows(key_mask, "key_mask")
+        if key_mask.shape[1] < max_len:
+            raise ValueError(f"starq expects key_mask rows of at least max_len = {max_len} bytes")
+    if workspace is None:
+        size = lib.kv_cache_attention_workspace_size(B, max_new, H, cache.Hkv, D)
+        workspace = _ws(size, Q.device, stream)
+    else:
+        size = workspace.numel() * workspace.element_size()
+    _check(lib.kv_cache_attention(q, ldq, _CODES[dtype], T, _ints("seq_start", seq_start, B + 1), B, max_new, H,
+                                  cache.ref, pt, pld, _ints("kv_len", kv_len, B), max_len, causal, mk, mld,
+                                  D ** -0.5 if scale is None else scale, o, ldo,
+                                  None if lse is None else _f32("lse", lse, (T, H)), workspace.data_ptr(), size,
+                                  _stream(stream)))
+
+
+# The calls below bring the host's part down to what a call of a few
+# microseconds bears: sizes are asked for once, a workspace of the call's own
+# is a block of torch's allocator without a tensor around it.
+_sizes = {}
+
+
+def _size(name, *args):
+    key = (torch._C._cuda_getDevice(), name, args)
+    n = _sizes.get(key)
+    if n is None:
+        n = _sizes[key] = int(getattr(lib, name)(*args))
+    return n
+
+
+def _with_workspace(fn, before, workspace, size, device, stream):
+    """fn(*before, workspace, its size, stream). A workspace of the call's
+    own (None) comes from the pool of the stream that uses it and goes back
+    there, where only later work of that stream can take it."""
+    if workspace is not None:
+        return _check(fn(*before, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
+    n = _size(*size)
+    if stream is not None or device.index != torch._C._cuda_getDevice():
+        workspace = _ws(n, device, stream)
+        return _check(fn(*before, workspace.data_ptr(), n, _stream(stream)))
+    stream = _stream(None)
+    ptr = torch._C._cuda_cudaCachingAllocator_raw_alloc(n, stream)
+    try:
+        rc = fn(*before, ptr, n, stream)
+    finally:
+        torch._C._cuda_cudaCachingAllocator_raw_delete(ptr)
+    _check(rc)
+
+
+def _attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, key_mask, lse):
+    """What the attention calls have in common: (arguments up to max_len,
+    those from key_mask to mask_ld, those from Out to lse, sequences, heads)."""
+    shape, D, dtype = Q.shape, cache.D, Q.dtype
+    B, (T, width) = kv_len.shape[0], shape
+    H = width // D
+    if width != H * D or Out.shape != shape or Out.dtype is not dtype:
         raise ValueError("starq expects Q and Out as T rows of H * D channels of one type")
     q, ldq = _rows(Q, "Q")
     o, ldo = _rows(Out, "Out")
@@ -752,37 +819,15 @@ def _attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, k
             (o, ldo, None if lse is None else _f32("lse", lse, (T, H))), B, H)
 
 
-def kv_cache_attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, causal=False, key_mask=None,
-                       scale=None, lse=None, workspace=None, stream=None):
-    """Attention of the rows of Q [T][H D] (sequence b: rows seq_start[b] ..,
-    at most max_new) over the kv_len[b] (at most max_len) cached tokens into
-    Out [T][H D]; lse [T][H] receives the log-sum-exp. key_mask uint8
-    [B][>= max_len]: 0 = not seen. scale: default 1 / sqrt(D). workspace:
-    default of this call's own, on its stream."""
-    first, mask, out, B, H = _attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, key_mask, lse)
-    if workspace is None:
-        size = lib.kv_cache_attention_workspace_size(B, max_new, H, cache.Hkv, cache.D)
-        workspace = _ws(size, Q.device, stream)
-    else:
-        size = workspace.numel() * workspace.element_size()
-    _check(lib.kv_cache_attention(*first, causal, *mask, cache.D ** -0.5 if scale is None else scale, *out,
-                                  workspace.data_ptr(), size, _stream(stream)))
-
-
 def kv_cache_attention_window(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, window, sinks=0,
                               causal=False, key_mask=None, scale=None, lse=None, workspace=None, stream=None):
     """kv_cache_attention in which a row at slot s sees, of the slots up to
     its own, the last `window` (itself among them) and the first `sinks`.
     Entries of page_table outside may be anything."""
     first, mask, out, B, H = _attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, key_mask, lse)
-    if workspace is None:
-        size = lib.kv_cache_attention_workspace_size(B, max_new, H, cache.Hkv, cache.D)
-        workspace = _ws(size, Q.device, stream)
-    else:
-        size = workspace.numel() * workspace.element_size()
-    _check(lib.kv_cache_attention_window(*first, causal, window, sinks, *mask,
-                                         cache.D ** -0.5 if scale is None else scale, *out, workspace.data_ptr(), size,
-                                         _stream(stream)))
+    _with_workspace(lib.kv_cache_attention_window,
+                    (*first, causal, window, sinks, *mask, cache.D ** -0.5 if scale is None else scale, *out), workspace,
+                    ("kv_cache_attention_workspace_size", B, max_new, H, cache.Hkv, cache.D), Q.device, stream)
 
 
 def kv_cache_attention_shared_workspace_size(T, B, max_new, groups, max_rows, H, Hkv, D):
@@ -798,15 +843,12 @@ def kv_cache_attention_shared(Q, cache, page_table, kv_len, seq_start, Out, max_
     tokens are in the same pages; at most max_rows rows of Q are a group's."""
     first, mask, out, B, H = _attention(Q, cache, page_table, kv_len, seq_start, Out, max_new, max_len, key_mask, lse)
     groups = shared_len.shape[0]
-    if workspace is None:
-        size = lib.kv_cache_attention_shared_workspace_size(Q.shape[0], B, max_new, groups, max_rows, H, cache.Hkv, cache.D)
-        workspace = _ws(size, Q.device, stream)
-    else:
-        size = workspace.numel() * workspace.element_size()
-    _check(lib.kv_cache_attention_shared(*first, causal, _ints("group_start", group_start, groups + 1),
-                                         _ints("shared_len", shared_len, groups), groups, max_rows, max_shared, *mask,
-                                         cache.D ** -0.5 if scale is None else scale, *out, workspace.data_ptr(), size,
-                                         _stream(stream)))
+    _with_workspace(lib.kv_cache_attention_shared,
+                    (*first, causal, _ints("group_start", group_start, groups + 1),
+                     _ints("shared_len", shared_len, groups), groups, max_rows, max_shared, *mask,
+                     cache.D ** -0.5 if scale is None else scale, *out), workspace,
+                    ("kv_cache_attention_shared_workspace_size", first[3], B, max_new, groups, max_rows, H, cache.Hkv,
+                     cache.D), Q.device, stream)
 
 
 def w4g_linear(X, Wq, scales, Y, bias=None, stream=None):
@@ -842,34 +884,19 @@ class LogitsRules:
                  bias_len=None, allowed=None, allowed_by_row=False):
         self.vocab, self.B, self.rows = vocab, None, None
         self.tensors = (params, history, history_len, bias_ids, bias_values, bias_len, allowed)
-
-        def rows(name, t, dtype, width=None):
-            """[B][width], contiguous: (pointer, width)"""
-            if t.dtype is not dtype or t.dim() != 2 or not t.is_contiguous() or (width is not None and t.shape[1] != width):
-                raise ValueError(f"starq expects {name} as contiguous {dtype} [sequences][{width or 'n'}]")
-            self._sequences(name, t.shape[0])
-            return t.data_ptr(), t.shape[1]
-
-        def lengths(name, t):
-            if t is None:
-                raise ValueError(f"starq expects {name} with what it counts")
-            if t.dim() == 1:
-                self._sequences(name, t.shape[0])
-            return _ints(name, t, self.B)
-
         p = h = hl = bi = bv = bl = al = None
         hld = bld = ald = 0
         if params is not None:
-            p, _ = rows("params", params, _FP32, 4)
+            p, _ = self._table("params", params, _FP32, 4)
         if history is not None:
-            h, hld = rows("history", history, _I32)
-            hl = lengths("history_len", history_len)
+            h, hld = self._table("history", history, _I32)
+            hl = self._lengths("history_len", history_len)
         if (bias_ids is None) != (bias_values is None):
             raise ValueError("starq expects bias_ids and bias_values together")
         if bias_ids is not None:
-            bi, bld = rows("bias_ids", bias_ids, _I32)
-            bv, _ = rows("bias_values", bias_values, _FP32, bld)
-            bl = lengths("bias_len", bias_len)
+            bi, bld = self._table("bias_ids", bias_ids, _I32)
+            bv, _ = self._table("bias_values", bias_values, _FP32, bld)
+            bl = self._lengths("bias_len", bias_len)
         if allowed is not None:
             words = (vocab + 31) // 32
             if allowed.dtype is not _I32 or allowed.dim() != 2 or allowed.shape[1] < words:
@@ -879,14 +906,28 @@ class LogitsRules:
                 self.rows = allowed.shape[0]
             else:
                 self._sequences("allowed", allowed.shape[0])
-        self.c = StarqLogitsRules(p, h, hld, hl, bi, bv, bld, bl, al, ald, int(allowed_by_row))
+        self.c = StarqLogitsRules(p, h, hld, hl, bi, bv, bld, bl, al, ald, allowed_by_row)
         self.ref = ctypes.byref(self.c)
 
     def _sequences(self, name, n):
         if self.B is None:
             self.B = n
-        if n != self.B:
+        elif n != self.B:
             raise ValueError(f"starq expects {name} for {self.B} sequences, not {n}")
+
+    def _table(self, name, t, dtype, width=None):
+        """[sequences][width], contiguous: (pointer, width)"""
+        shape = t.shape
+        if t.dtype is not dtype or len(shape) != 2 or not t.is_contiguous() or (width is not None and shape[1] != width):
+            raise ValueError(f"starq expects {name} as contiguous {dtype} [sequences][{width or 'n'}]")
+        if self.B != shape[0]:
+            self._sequences(name, shape[0])
+        return t.data_ptr(), shape[1]
+
+    def _lengths(self, name, t):
+        if t is None:
+            raise ValueError(f"starq expects {name} with what it counts")
+        return _ints(name, t, self.B)
 
 
 def _logits_rows(t, name):
