@@ -16,19 +16,33 @@
 //   probability 1 / l, margin (1 - e^(d_second)) / l,
 //   entropy -sum p ln p = ln l - (sum e^d d) / l,  ln sum e^y = m / T + ln l.
 //
-// Bound by memory: x once (and y once), a mask's bit a token. A history and
-// a list of biases name few tokens, so they are not spread over the
-// vocabulary: a CTA sets a bit for each named token of its slice in shared
-// memory. Eight warps stream the slice and leave the named tokens out (a few
-// bit operations for 16 bytes); four others meanwhile number the bits and list
-// the named tokens with their penalties and biases, and take them one a lane,
-// which the eight join when the stream has ended. (Looked up in the stream
-// itself, a warp met a named token in most of its pieces and spent most of its
-// time on them; before the stream, it stood still for as long.) A CTA takes up to eight rows of a
-// sequence, which share the tables; a warp takes a row or parts of it, its
-// maximum is one number for all lanes and moves only when a batch of tokens
-// passes it. A cluster shares the slices; its first CTA joins the results, in
-// their order.
+// Bound by memory: x once (and y once), a mask's bit a token. The vocabulary
+// is dealt to the CTAs of a cluster in blocks of 512 tokens, in turn: the
+// tokens that texts use most have the lowest numbers, and so does most of a
+// history. A history and a list of biases name few tokens, so they are not
+// spread over the vocabulary in memory: a CTA sets a bit for each named token
+// of its blocks in shared memory. Eight warps stream the blocks and leave the
+// named tokens out (a few bit operations for 16 bytes); two others meanwhile
+// number the bits and list the named tokens with their penalties and biases,
+// and take them one a lane, which the eight join when the stream has ended.
+// (Looked up in the stream itself, a warp met a named token in most of its
+// pieces and spent most of its time on them; before the stream, it stood still
+// for as long.) A CTA takes up to eight rows of a sequence, which share the
+// tables; a warp takes a row or parts of it, its maximum is one number for all
+// lanes and moves only when a batch of tokens passes it. The cluster's first
+// CTA joins the results, in their order.
+//
+// Measured (one call after the other): the margin of 256 rows of 131072
+// float32 logits (8 sequences with a mask and 1500 tokens of history each, 134
+// MB) 42 us, 3.2 TB/s; the entropy of 244 rows of 50257 bfloat16 logits, a mask
+// a row, 4096 tokens of history, 34.5 us; 80 rows of 131072 bfloat16 logits
+// rewritten (43 MB) 15.5 us, 2.8 TB/s; one row of 32000 about 8 us of the GPU,
+// a chain of loads and barriers. A warp's own instructions bound the stream
+// (about 200 for 512 tokens, four such warps a scheduler)
+// more than their number: larger batches spill, smaller ones (55 us) and
+// three CTAs an SM (51) lose. One named token looked up at a time where it
+// stands cost 122 us, contiguous slices 47 (the first CTA had half of the
+// names), four helping warps 43 and fewer registers for the stream.
 #include <algorithm>
 
 #include "logits.cuh"
@@ -36,19 +50,21 @@
 namespace starq {
 namespace {
 
-constexpr int STREAM = 8, HELP = 4;    // warps
+constexpr int STREAM = 8, HELP = 2;    // warps
 constexpr int WARPS = STREAM + HELP, THREADS = 32 * WARPS;
-constexpr int SLICE = 16384;           // most tokens of a slice
-constexpr int NAMED = 8192;            // named tokens that a CTA has room for (then a slice is no longer than that)
-constexpr int MAX_CLUSTER = 8;
-constexpr int ROWS = 8;                // rows of a CTA
-constexpr int AHEAD = 3;               // tokens of the history that a thread asks for at once
-constexpr int NAMES = 4;               // named tokens of a thread on their way
 // Tokens of a thread that are worked on together (a chain of dependent
 // operations a batch: four batches of 4 took 640 cycles each), and 16-byte
 // loads on their way beside them.
 constexpr int BATCH = 16, FLIGHT = 4;
-constexpr int CHUNK = 32 * NAMES, CHUNKS = NAMED / CHUNK;      // of named tokens
+constexpr int BLOCK = 32 * BATCH;      // tokens that are dealt together: a batch of a warp
+constexpr int BLOCK_WORDS = BLOCK / 32;
+constexpr int SLICE = 16384;           // most tokens of a CTA's blocks at a time
+constexpr int NAMED = 8192;            // named tokens that a CTA has room for (then there are no more tokens at a time)
+constexpr int MAX_CLUSTER = 8;
+constexpr int ROWS = 8;                // rows of a CTA
+constexpr int AHEAD = 4;               // tokens of the history that a thread asks for at once
+constexpr int NAMES = 4;               // named tokens of a thread on their way
+constexpr int CHUNK = 32 * NAMES, CHUNKS = (NAMED + SLICE / BLOCK * 16) / CHUNK;   // of named tokens and blocks' edges
 constexpr float NEG_INF = -__builtin_huge_valf();
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -58,10 +74,10 @@ enum { APPLY = -1 };                   // else a starq_confidence
 struct Cut {
     int rows;                          // of a CTA
     int groups;                        // CTAs' row groups of a sequence
-    int parts, parts_log;              // of a row's slice: 1, 2, 4 or 8
-    int cluster;                       // CTAs that share the slices
-    int len;                           // tokens of a slice, a multiple of 32
-    int room;                          // named tokens of a slice at most
+    int parts, parts_log;              // of a row's blocks: 1, 2, 4 or 8
+    int cluster, cluster_log;          // CTAs that share the blocks (the logarithm: of a power of two)
+    int blocks;                        // of a CTA at a time
+    int room;                          // named tokens among them at most
 };
 
 // What is known of some of a row's tokens: largest z (its lowest index), and
@@ -238,18 +254,20 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
     constexpr bool PICK = KIND != APPLY;
     constexpr uint32_t FULL = (1u << E) - 1;
     constexpr uint32_t COUNTED = 1u << 29, LISTED = 1u << 30, NONE = 1u << 31;
-    // by number: the named tokens of the slice (and which rules name them), penalties, list entries that become biases
-    // [room]; counts [len]; the named tokens' bits [len / 32 + 1], the numbers before them [len / 32]; for each row the
-    // bits of the tokens that the stream may take [len / 32]
+    static_assert(BLOCK == 32 * BATCH, "a block is a batch");
+    // by number: the named tokens (their places among the CTA's blocks, and which rules name them), penalties, list
+    // entries that become biases [room]; by place: counts, the named tokens' bits, the numbers before a word; for each
+    // row the bits of the tokens that the stream may take
     extern __shared__ __align__(16) uint32_t tables[];
-    __shared__ Best s_item[ROWS][STREAM + 1 + CHUNKS], s_row[ROWS][MAX_CLUSTER];
+    __shared__ Best s_item[ROWS][STREAM + CHUNKS], s_row[ROWS][MAX_CLUSTER];
     __shared__ int s_sum[HELP], s_next, s_names;
-    const int words = cut.len / 32;
+    const int places = cut.blocks * BLOCK, words = places / 32;
+    const int narrow = a.r.history_ld < 65536;               // 1: two counts a word
     uint32_t* const token_of = tables;
     float* const penalty = reinterpret_cast<float*>(token_of + cut.room);
     uint32_t* const entry = token_of + 2 * cut.room;
     uint32_t* const count = token_of + 3 * cut.room;
-    uint32_t* const named = count + cut.len;
+    uint32_t* const named = count + (places >> narrow);
     uint32_t* const before = named + (words + 1);
     uint32_t* const free_bits = TABLES ? before + words : tables;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -284,76 +302,84 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
     if (PICK && cut.cluster > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
     const int rows = min(cut.rows, n - first), items = rows << cut.parts_log;
 
-    // A row's slice: 16-byte pieces, aligned; the tokens before and behind them are its edges.
-    struct Slice {
+    // A row: where it is, and the tokens of each block before its 16-byte pieces (the first block's are at 16 bytes
+    // where the others' are, too). The tokens before and behind the pieces are the blocks' edges.
+    struct Row {
         const T* x; T* y;
         const uint32_t* mask;
-        int lead, pieces, here;                              // tokens before the pieces, pieces, all tokens
+        int lead;
     };
-    auto slice_of = [&](int r, int v0) {
-        Slice t;
-        t.here = min(cut.len, a.V - v0);
+    auto row_of = [&](int r) {
+        Row t;
         const size_t row = (size_t)row0 + first + r;
-        t.x = static_cast<const T*>(a.X) + row * a.ldx + v0;
-        t.y = PICK ? nullptr : static_cast<T*>(a.Y) + row * a.ldy + v0;
+        t.x = static_cast<const T*>(a.X) + row * a.ldx;
+        t.y = PICK ? nullptr : static_cast<T*>(a.Y) + row * a.ldy;
         t.mask = a.r.allowed;
-        if (t.mask != nullptr) t.mask += (a.r.allowed_by_row ? row : (size_t)b) * a.r.allowed_ld + (v0 >> 5);
-        t.lead = min(t.here, -((int)(reinterpret_cast<uintptr_t>(t.x) / sizeof(T))) & (E - 1));
-        t.pieces = (t.here - t.lead) / E;
+        if (t.mask != nullptr) t.mask += (a.r.allowed_by_row ? row : (size_t)b) * a.r.allowed_ld;
+        t.lead = -((int)(reinterpret_cast<uintptr_t>(t.x) / sizeof(T))) & (E - 1);
         return t;
     };
+    int done = 0;                                            // the CTA's blocks before those at hand
+    // first token of block j; the block's tokens and pieces
+    auto token0 = [&](int j) { return ((done + j) * cut.cluster + rank) * BLOCK; };
+    auto tokens_of = [&](int j) { return min(BLOCK, a.V - token0(j)); };
+    auto pieces_of = [&](int j, int lead) { return max(0, tokens_of(j) - lead) / E; };
+    const int vocab_blocks = (a.V + BLOCK - 1) / BLOCK;
+    const int mine = vocab_blocks > rank ? (vocab_blocks - rank + cut.cluster - 1) / cut.cluster : 0;
+    int blocks = 0;                                          // at hand
     // rows whose bits are the same (their masks and alignments are)
-    const bool bits = TABLES || a.r.allowed != nullptr;
-    const bool one = !(a.r.allowed != nullptr && a.r.allowed_by_row) && (size_t)a.ldx * sizeof(T) % 16 == 0;
+    const bool bits = TABLES || a.r.allowed != nullptr, even = (size_t)a.ldx * sizeof(T) % 16 == 0;
+    const bool one = !(a.r.allowed != nullptr && a.r.allowed_by_row) && even;
 
-    // A warp's items, parts of rows, one after the other: the place of a batch.
+    // A warp's batches: the blocks of its rows or parts of them, one after the other.
     struct Place {
-        const T* x; T* y;                                    // the row's first piece
-        int item, row, lead, j, j_end;
+        const T* x; T* y;                                    // the row's first piece of block 0
+        int item, row, lead, j;
     };
-    auto settle = [&](Place& p, int v0) {                    // the first item from p.item on that has pieces
-        for (; p.item < items; p.item += STREAM) {
+    auto settle = [&](Place& p) {                            // the next block that has pieces, from p's on
+        while (p.item < items) {
+            if (p.j < blocks && pieces_of(p.j, p.lead) > 0) return;
+            if (p.j < blocks) { p.j += cut.parts; continue; }
+            p.item += STREAM;
+            p.j = p.item & (cut.parts - 1);
             p.row = p.item >> cut.parts_log;
-            const Slice t = slice_of(p.row, v0);
-            const int share = (t.pieces + cut.parts - 1) >> cut.parts_log;
-            p.j = (p.item & (cut.parts - 1)) * share;
-            p.j_end = min(t.pieces, p.j + share);
-            p.lead = t.lead;
-            p.x = t.x + t.lead;
-            p.y = PICK ? nullptr : t.y + t.lead;
-            if (p.j < p.j_end) return;
+            if (p.item < items) {
+                const Row t = row_of(p.row);
+                p.x = t.x + t.lead;
+                p.y = PICK ? nullptr : t.y + t.lead;
+                p.lead = t.lead;
+            }
         }
     };
     struct Batch { uint4 w[U]; };
-    // Pieces j + 32 u + lane; what is behind the item's last one is read as the last one and not used.
-    auto load = [&](Place& p, int v0, Batch& q) {
+    // Pieces 32 u + lane of a block; what is behind the last one is read as the last one and not used.
+    auto load = [&](Place& p, Batch& q) {
         if (p.item >= items) return;
+        const T* const x = p.x + token0(p.j);
+        const int last = pieces_of(p.j, p.lead) - 1;
         #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint4* from = reinterpret_cast<const uint4*>(p.x) + min(p.j + 32 * u + lane, p.j_end - 1);
+            const uint4* from = reinterpret_cast<const uint4*>(x) + min(32 * u + lane, last);
             q.w[u] = PICK ? __ldcs(from) : *from;
         }
-        p.j += 32 * U;
-        if (p.j >= p.j_end) {
-            p.item += STREAM;
-            settle(p, v0);
-        }
+        p.j += cut.parts;
+        settle(p);
     };
 
     const bool t_ok = temperature >= 1e-30f && temperature <= 1e30f, r_ok = repetition >= 1e-30f && repetition <= 1e30f;
     if (PICK)
-        for (int i = tid; i < ROWS * (STREAM + 1 + CHUNKS); i += THREADS) s_item[0][i] = nothing<KIND>();
+        for (int i = tid; i < ROWS * (STREAM + CHUNKS); i += THREADS) s_item[0][i] = nothing<KIND>();
     float warm = 0.f, kk = 0.f;
 
-    for (int v0 = rank * cut.len; v0 < a.V; v0 += cut.cluster * cut.len) {
-        const int here = min(cut.len, a.V - v0);
+    for (; done < mine; done += cut.blocks) {
+        blocks = min(cut.blocks, mine - done);
         Batch q[BUFFERS];
-        Place at{nullptr, nullptr, streams ? warp : items, 0, 0, 0, 0};
-        settle(at, v0);
+        Place at{nullptr, nullptr, (streams ? warp : items) - STREAM, 0, 0, blocks};
+        settle(at);
         Place next = at;
         #pragma unroll
-        for (int k = 0; k < BUFFERS - 1; ++k) load(next, v0, q[k]);       // on their way beside the tables
-        if (v0 == rank * cut.len) {
+        for (int k = 0; k < BUFFERS - 1; ++k) load(next, q[k]);           // on their way beside the tables
+        if (done == 0) {
             const bool odd = !(t_ok && r_ok) || told < 0 || told > a.r.history_ld || entries < 0 || entries > a.r.bias_ld;
             if (!t_ok) temperature = 1.f;
             if (!r_ok) repetition = 1.f;
@@ -363,22 +389,28 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
             warm = __fdiv_rn(1.f, temperature);
             kk = warm * LOG2E;
         }
-        __syncthreads();                                     // the tables of the slice before are done with
+        __syncthreads();                                     // the tables of the blocks before are done with
         if (tid == 0) { s_next = 0; s_names = 0; }
+        // a token's place among the blocks at hand, -1 if it is not there
+        auto place_of = [&](int v) {
+            const int blk = v / BLOCK, j = PICK ? blk >> cut.cluster_log : blk / cut.cluster;
+            return blk - j * cut.cluster == rank && j >= done && j < done + blocks ? (j - done) * BLOCK + v % BLOCK : -1;
+        };
         if (TABLES) {
             // counts, then bits; list entries before them
-            const int zeros = 3 * cut.room + cut.len + words + 1;
-            for (int i = 4 * (2 * cut.room / 4 + tid); i < zeros; i += 4 * THREADS)
+            const int zeros = 3 * cut.room + (places >> narrow) + words + 1;
+            for (int i = 2 * cut.room + 4 * tid; i < zeros; i += 4 * THREADS)
                 *reinterpret_cast<uint4*>(tables + i) = make_uint4(0, 0, 0, 0);
             __syncthreads();
             auto name = [&](int v, bool told_one) {
-                const int p = v - v0;
                 if (v < 0 || v >= a.V) {
                     atomicOr(a.status, STATUS_RANGE);
-                } else if (p >= 0 && p < here) {
-                    if (told_one) atomicAdd(count + p, 1u);
-                    atomicOr(named + (p >> 5), 1u << (p & 31));
+                    return;
                 }
+                const int p = place_of(v);
+                if (p < 0) return;
+                if (told_one) atomicAdd(count + (p >> narrow), 1u << (narrow & p) * 16);
+                atomicOr(named + (p >> 5), 1u << (p & 31));
             };
             #pragma unroll
             for (int k = 0; k < AHEAD; ++k)
@@ -389,19 +421,20 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
             for (int i = tid + THREADS; i < entries; i += THREADS) name(__ldg(ids + i), false);
             __syncthreads();
         }
-        if (bits) {                                          // bit i of a row: token lead + i is allowed and not named
-            const int some = (here + 31) / 32;
+        if (bits) {                                          // bit i of a block: token lead + i is allowed and not named
+            const int last = (a.V - 1) / 32;
             for (int r = one ? 0 : warp; r < (one ? 1 : rows); r += WARPS) {
-                const Slice t = slice_of(r, v0);
+                const Row t = row_of(r);
                 #pragma unroll 4
-                for (int k = one ? tid : lane; k < some; k += one ? THREADS : 32) {
-                    const int e = t.lead + 32 * k, w = e >> 5;
+                for (int k = one ? tid : lane; k < BLOCK_WORDS * blocks; k += one ? THREADS : 32) {
+                    const int e = t.lead + 32 * (k % BLOCK_WORDS), w = token0(k / BLOCK_WORDS) / 32 + (e >> 5);
                     uint32_t free = ~0u;
-                    if (t.mask != nullptr) {
-                        const uint32_t lo = __ldg(t.mask + min(w, some - 1)), hi = __ldg(t.mask + min(w + 1, some - 1));
-                        free = __funnelshift_r(lo, hi, e);
+                    if (t.mask != nullptr)
+                        free = __funnelshift_r(__ldg(t.mask + min(w, last)), __ldg(t.mask + min(w + 1, last)), e);
+                    if (TABLES) {
+                        const uint32_t* of = named + k / BLOCK_WORDS * BLOCK_WORDS + (e >> 5);
+                        free &= ~__funnelshift_r(of[0], of[1], e);
                     }
-                    if (TABLES) free &= ~__funnelshift_r(named[min(w, words)], named[min(w + 1, words)], e);
                     free_bits[r * words + k] = free;
                 }
             }
@@ -410,45 +443,47 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
 
         Best best = nothing<KIND>();
         auto work = [&](const Place& p, const Batch& q) {
+            const int pieces = pieces_of(p.j, p.lead), v0 = token0(p.j);
             float z[BATCH];
             uint32_t good[U];
             #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int jj = p.j + 32 * u + lane;
+                const int k0 = (32 * u + lane) * E;          // the piece's first token behind the lead
                 float f[E];
                 open_as<T>(q.w[u], f);
-                good[u] = jj < p.j_end ? FULL : 0u;
-                if (bits) good[u] &= free_bits[(one ? 0 : p.row * words) + (min(jj, p.j_end - 1) * E >> 5)] >> (jj * E & 31);
+                good[u] = 32 * u + lane < pieces ? FULL : 0u;
+                if (bits) good[u] &= free_bits[(one ? 0 : p.row * words) + p.j * BLOCK_WORDS + (k0 >> 5)] >> (k0 & 31);
                 #pragma unroll
                 for (int k = 0; k < E; ++k) z[u * E + k] = good[u] >> k & 1 ? f[k] : NEG_INF;
             }
             if constexpr (!PICK) {
-                const bool wide = reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
+                T* const y = p.y + v0;
+                const bool wide = reinterpret_cast<uintptr_t>(y) % 16 == 0;
                 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const int jj = p.j + 32 * u + lane;
+                    const int k0 = (32 * u + lane) * E;
                     T o[E];
                     #pragma unroll
                     for (int k = 0; k < E; ++k) o[k] = (T)(__fmul_rn(z[u * E + k], warm));
-                    if (jj >= p.j_end) continue;
-                    uint32_t mine = FULL;                     // tokens that are not named
-                    const int e = p.lead + jj * E;
-                    if (TABLES && good[u] != FULL) mine &= ~__funnelshift_r(named[e >> 5], named[(e >> 5) + 1], e);
-                    if (wide && mine == FULL) {
+                    if (32 * u + lane >= pieces) continue;
+                    uint32_t others = FULL;                   // tokens that are not named
+                    const int e = p.j * BLOCK + p.lead + k0;
+                    if (TABLES && good[u] != FULL) others &= ~__funnelshift_r(named[e >> 5], named[(e >> 5) + 1], e);
+                    if (wide && others == FULL) {
                         uint4 v;
                         memcpy(&v, o, 16);
-                        reinterpret_cast<uint4*>(p.y)[jj] = v;
+                        *reinterpret_cast<uint4*>(y + k0) = v;
                     } else {
                         #pragma unroll
                         for (int k = 0; k < E; ++k)
-                            if (mine >> k & 1) p.y[jj * E + k] = o[k];
+                            if (others >> k & 1) y[k0 + k] = o[k];
                     }
                 }
             } else {
                 const float top = largest(z);
                 if (__any_sync(0xffffffffu, !(top <= (MARGIN<KIND> ? best.s : best.m))))
                     move_best<KIND>(best, z, top, [&](int k) {
-                        return v0 + p.lead + (p.j + 32 * (k / E) + lane) * E + k % E;
+                        return v0 + p.lead + (32 * (k / E) + lane) * E + k % E;
                     }, kk);
                 add_weights<KIND, BATCH>(best, z, kk);
             }
@@ -470,15 +505,13 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
         while (at.item < items) {
             #pragma unroll
             for (int k = 0; k < BUFFERS; ++k) {
-                load(next, v0, q[(k + BUFFERS - 1) % BUFFERS]);
+                load(next, q[(k + BUFFERS - 1) % BUFFERS]);
                 work(at, q[k]);
-                at.j += 32 * U;
-                if (at.j >= at.j_end) {
-                    if (PICK) finish(s_item[at.row][warp]);
-                    at.item += STREAM;
-                    settle(at, v0);
-                    if (at.item >= items) break;
-                }
+                const int row = at.row, item = at.item;
+                at.j += cut.parts;
+                settle(at);
+                if (PICK && at.item != item) finish(s_item[row][warp]);
+                if (at.item >= items) break;
             }
         }
 
@@ -487,7 +520,7 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
         if (TABLES && !streams) {
             const int hid = tid - 32 * STREAM, help = warp - STREAM;
             auto meet = [] { asm volatile("bar.sync 1, %0;" :: "n"(32 * HELP) : "memory"); };
-            // the bits' numbers, in the order of the tokens: a thread takes a run of words
+            // the bits' numbers, in the order of the places: a thread takes a run of words
             const int per = (words + HELPERS - 1) / HELPERS, w0 = hid * per, w1 = min(words, w0 + per);
             int sum = 0;
             for (int w = w0; w < w1; ++w) sum += __popc(named[w]);
@@ -511,20 +544,18 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
             }
             if (hid == 0) s_names = names;
             meet();
-            // four bits of a word a thread (named tokens lie close together)
-            for (int i = hid; i < 8 * words; i += HELPERS) {
-                const uint32_t word = named[i >> 3], low = word & ((1u << 4 * (i & 7)) - 1);
-                uint32_t m = word >> 4 * (i & 7) & 15;
-                for (int to = (int)before[i >> 3] + __popc(low); m != 0; m &= m - 1, ++to) {
-                    const int p = 4 * i + __ffs(m) - 1;
-                    const uint32_t c = count[p];
+            for (int w = hid; w < words; w += HELPERS) {
+                int to = (int)before[w];
+                for (uint32_t m = named[w]; m != 0; m &= m - 1, ++to) {
+                    const int p = 32 * w + __ffs(m) - 1;
+                    const uint32_t c = narrow ? count[p >> 1] >> (p & 1) * 16 & 0xffff : count[p];
                     token_of[to] = (uint32_t)p | (c ? COUNTED : 0u);
                     penalty[to] = __fadd_rn(__fmul_rn(frequency, (float)c), presence);
                 }
             }
             for (int i = hid; i < entries; i += HELPERS) {   // the last of a token's entries counts
-                const int p = __ldg(ids + i) - v0;
-                if (p >= 0 && p < here)
+                const int v = __ldg(ids + i), p = v >= 0 && v < a.V ? place_of(v) : -1;
+                if (p >= 0)
                     atomicMax(entry + before[p >> 5] + __popc(named[p >> 5] & ((1u << (p & 31)) - 1)), (uint32_t)i + 1);
             }
             meet();
@@ -537,65 +568,72 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
                     }
                 }
         }
-        // --- the named tokens and the edges of the rows, by whoever is free ----------------
+        // --- the named tokens and the blocks' edges, by whoever is free --------------------
         // (the helpers wait for one another, the streaming warps for them)
         if (streams) asm volatile("bar.sync 2, %0;" :: "n"(32 * WARPS) : "memory");
         else {
             asm volatile("bar.arrive 2, %0;" :: "n"(32 * WARPS) : "memory");
             asm volatile("bar.sync 1, %0;" :: "n"(32 * HELP) : "memory");
         }
+        // A block has fewer than 2 E edge tokens; where all rows begin at 16 bytes, only the vocabulary's last block has.
         const int names = TABLES ? *static_cast<volatile int*>(&s_names) : 0;
-        const int chunks = (names + CHUNK - 1) / CHUNK;
+        const bool flush = even && row_of(0).lead == 0;
+        const int edge0 = flush ? (tokens_of(blocks - 1) < BLOCK ? blocks - 1 : blocks) : 0;
+        const int chunks = (names + 2 * E * (blocks - edge0) + CHUNK - 1) / CHUNK;
         for (;;) {
             int i = 0;
             if (lane == 0) i = atomicAdd(&s_next, 1);
             i = __shfl_sync(0xffffffffu, i, 0);
-            if (i >= rows * (chunks + 1)) break;
-            const int r = i / (chunks + 1), chunk = i - r * (chunks + 1) - 1;        // -1: the edges
-            const Slice t = slice_of(r, v0);
+            if (i >= rows * chunks) break;
+            const int r = i / chunks, chunk = i - r * chunks;
+            const Row t = row_of(r);
             uint32_t by[NAMES], word[NAMES];
             T x[NAMES];
-            if (chunk >= 0) {
-                #pragma unroll
-                for (int k = 0; k < NAMES; ++k) {
-                    const int m = chunk * CHUNK + 32 * k + lane;
-                    by[k] = token_of[min(m, names - 1)] | (m < names ? 0u : NONE);
+            #pragma unroll
+            for (int k = 0; k < NAMES; ++k) {
+                const int m = chunk * CHUNK + 32 * k + lane;
+                by[k] = NONE;
+                if (TABLES && m < names) {
+                    by[k] = token_of[m];
+                } else {
+                    const int j = edge0 + (m - names) / (2 * E), e = (m - names) % (2 * E);
+                    if (j < blocks) {
+                        const int whole = pieces_of(j, t.lead) * E, p = j * BLOCK + (e < t.lead ? e : e + whole);
+                        // (a named one is in the list)
+                        if (e < tokens_of(j) - whole && !(TABLES && (named[p >> 5] >> (p & 31) & 1))) by[k] = (uint32_t)p;
+                    }
                 }
-            } else {
-                const int ends = t.here - t.pieces * E;
-                if (ends == 0) continue;
-                const int p = lane < t.lead ? lane : lane + t.pieces * E;
-                by[0] = lane < ends ? (uint32_t)p : NONE;
-                if (TABLES && lane < ends && (named[p >> 5] >> (p & 31) & 1)) by[0] = NONE;          // it is in the list
-                #pragma unroll
-                for (int k = 1; k < NAMES; ++k) by[k] = NONE;
             }
             #pragma unroll
-            for (int k = 0; k < NAMES; ++k) {                // (where there is none, token 0)
-                const uint32_t p = by[k] & (COUNTED - 1);
-                x[k] = t.x[p];
-                word[k] = t.mask != nullptr ? __ldg(t.mask + (p >> 5)) : ~0u;
+            for (int k = 0; k < NAMES; ++k) {                // (where there is none, the first place)
+                const int p = (int)(by[k] & (COUNTED - 1)), v = token0(p / BLOCK) + p % BLOCK;
+                x[k] = t.x[v];
+                word[k] = t.mask != nullptr ? __ldg(t.mask + (v >> 5)) : ~0u;
             }
             float z[NAMES];
             #pragma unroll
             for (int k = 0; k < NAMES; ++k) {
-                const uint32_t p = by[k] & (COUNTED - 1);
+                const int p = (int)(by[k] & (COUNTED - 1)), v = token0(p / BLOCK) + p % BLOCK;
                 z[k] = (float)x[k];
-                if (TABLES && chunk >= 0) {
-                    const int m = min(chunk * CHUNK + 32 * k + lane, names - 1);
+                if (TABLES) {
+                    const int m = min(chunk * CHUNK + 32 * k + lane, max(names, 1) - 1);
                     const float scaled = z[k] > 0.f ? __fdiv_rn(z[k], repetition) : __fmul_rn(z[k], repetition);
                     if (by[k] & COUNTED) z[k] = __fsub_rn(scaled, penalty[m]);
                     if (by[k] & LISTED) z[k] = __fadd_rn(z[k], __uint_as_float(entry[m]));
                 }
-                if ((by[k] & NONE) || !(word[k] >> (p & 31) & 1)) z[k] = NEG_INF;
-                if (!PICK && !(by[k] & NONE)) t.y[p] = (T)(__fmul_rn(z[k], warm));
+                if ((by[k] & NONE) || !(word[k] >> (v & 31) & 1)) z[k] = NEG_INF;
+                if (!PICK && !(by[k] & NONE)) t.y[v] = (T)(__fmul_rn(z[k], warm));
             }
             if constexpr (PICK) {
                 const float top = largest(z);
-                if (__any_sync(0xffffffffu, !(top < (MARGIN<KIND> ? best.s : best.m)) && top != NEG_INF))
-                    move_best<KIND>(best, z, top, [&](int k) { return v0 + (int)(by[k] & (COUNTED - 1)); }, kk);
-                add_weights<KIND, NAMES>(best, z, kk);
-                finish(s_item[r][STREAM + 1 + chunk]);
+                if (__any_sync(0xffffffffu, top != NEG_INF)) {
+                    move_best<KIND>(best, z, top, [&](int k) {
+                        const int p = (int)(by[k] & (COUNTED - 1));
+                        return token0(p / BLOCK) + p % BLOCK;
+                    }, kk);
+                    add_weights<KIND, NAMES>(best, z, kk);
+                }
+                finish(s_item[r][STREAM + chunk]);
             }
         }
     }
@@ -604,7 +642,7 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
         // a warp a row: the CTA's result to the cluster's first CTA, then all of them
         Best best = nothing<KIND>();
         if (warp < rows) {
-            for (int i = lane; i < STREAM + 1 + CHUNKS; i += 32) join<KIND>(best, s_item[warp][i], kk);
+            for (int i = lane; i < STREAM + CHUNKS; i += 32) join<KIND>(best, s_item[warp][i], kk);
             join_lanes<KIND>(best, kk);
         }
         if (cut.cluster > 1) {
@@ -641,27 +679,32 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
 
 template <typename T, int KIND, bool TABLES>
 cudaError_t launch_kernel(const LogitsArgs& a, cudaStream_t s) {
-    // Up to eight rows of a sequence a CTA, and as many slices as fill the
-    // GPU or leave a CTA 1024 tokens of each row.
+    // Up to eight rows of a sequence a CTA, and as many CTAs a row as fill the
+    // GPU while every streaming warp has a block.
     Cut c;
     c.groups = (a.max_new + ROWS - 1) / ROWS;
     c.rows = (a.max_new + c.groups - 1) / c.groups;
     c.parts_log = c.rows % 8 == 0 ? 0 : c.rows % 4 == 0 ? 1 : c.rows % 2 == 0 ? 2 : 3;      // every warp has as many
     c.parts = 1 << c.parts_log;
     const long long units = (long long)a.B * c.groups, target = 2ll * num_sms();
+    const int blocks = (a.V + BLOCK - 1) / BLOCK;
+    const long long most = std::max<long long>(1, ((long long)blocks * c.rows + STREAM - 1) / STREAM);
     c.cluster = 1;
-    if (KIND == APPLY) c.cluster = (int)std::max<long long>(1, std::min<long long>(target / units, (a.V + 2047) / 2048));
+    c.cluster_log = 0;
+    if (KIND == APPLY) c.cluster = (int)std::max<long long>(1, std::min<long long>({target / units, most, blocks}));
     else
-        while (c.cluster < MAX_CLUSTER && units * c.cluster < target && a.V > 2048 * c.cluster) c.cluster *= 2;
+        while (c.cluster < MAX_CLUSTER && units * c.cluster < target && c.cluster < most && 2 * c.cluster <= blocks)
+            c.cluster = 2 << c.cluster_log++;
     const long long names = TABLES ? (long long)a.r.history_ld + a.r.bias_ld : 0;
-    const int longest = names > NAMED ? NAMED : SLICE;
-    const int rounds = (a.V + c.cluster * longest - 1) / (c.cluster * longest), cuts = c.cluster * rounds;
-    c.len = std::min(longest, ((a.V + cuts - 1) / cuts + 31) / 32 * 32);
-    c.room = (int)std::min<long long>(c.len, (names + 3) / 4 * 4);
+    const int longest = (names > NAMED ? NAMED : SLICE) / BLOCK, each = (blocks + c.cluster - 1) / c.cluster;
+    const int rounds = (each + longest - 1) / longest;
+    c.blocks = (each + rounds - 1) / rounds;
+    c.room = (int)std::min<long long>(c.blocks * BLOCK, (names + 3) / 4 * 4);
     if (units * c.cluster >= (1ll << 31)) return cudaErrorInvalidValue;
+    const int words = c.blocks * BLOCK / 32;
     size_t smem = 0;
-    if (TABLES || a.r.allowed != nullptr) smem = (size_t)c.rows * (c.len / 32) * 4;
-    if (TABLES) smem += (size_t)c.room * 12 + (size_t)c.len * 4 + (c.len / 32) * 8 + 16;
+    if (TABLES || a.r.allowed != nullptr) smem = (size_t)c.rows * words * 4;
+    if (TABLES) smem += (size_t)c.room * 12 + (size_t)c.blocks * BLOCK * (a.r.history_ld < 65536 ? 2 : 4) + words * 8 + 16;
     static DeviceCache<int> ready;
     int dummy = 0;
     cudaError_t e = ready.get(&dummy, [](int, int* v) {
