@@ -48,6 +48,13 @@ struct KvReadArgs {
 };
 cudaError_t launch_kv_read(const KvReadArgs& a, cudaStream_t s);
 
+// How a pass of KV_SPLIT was cut, for whoever joins its runs.
+struct KvCut {
+    int ctas, rows, slot_rows, whole;
+    const long long* prefix;
+    const float* slots;
+};
+
 struct KvAttnArgs {
     starq_kv_cache c;
     const void* Q; int ldq; int dtype; int T;
@@ -67,6 +74,8 @@ struct KvAttnArgs {
     // over its other slots. Nothing is written but sums: of whole units to `sums`, [T][H][D], then the (m, l) of each.
     int prefix; int sequences; int groups; const int32_t* group_start; const int32_t* shared_len;
     float* sums;
+    // The sequences' pass, if its units are whole, joins the groups' pass: how that was cut, its sums and its bounds.
+    int joins; KvCut group_cut; const float* group_sums; int group_rows; int group_len;
 };
 size_t kv_attention_workspace_bytes(int B, int max_new, int H, int Hkv, int D);
 cudaError_t launch_kv_attention(const KvAttnArgs& a, cudaStream_t s);

@@ -168,6 +168,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
     constexpr int DN = D / 8;                // value columns per thread, and column tiles
     constexpr int HELD = NARROW ? 8 : ROWS;  // rows that can be there
     extern __shared__ __align__(128) uint8_t smem[];
+    struct GroupPass { int row0, n, nt; PassTiles of; };
+    __shared__ GroupPass s_group;            // (KV_SPLIT)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
 
     grid_dependency_wait();
@@ -290,6 +292,22 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
                 for (int j = 0; j < OT; ++j)
                     #pragma unroll
                     for (int k = 0; k < 4; ++k) o[j][k] = 0.f;
+                if (FORM == KV_SPLIT && a.joins && tid == 0) {           // read behind the barriers at the unit's end
+                    const int g = cur.s.group;
+                    s_group.nt = 0;
+                    if (g >= 0) {
+                        KvAttnArgs p = a;
+                        p.prefix = 1;
+                        p.max_new = a.group_rows;
+                        p.max_len = a.group_len;
+                        p.whole = a.group_cut.whole;
+                        const SeqShape s = seq_shape<ROWS, TILE, FORM>(p, G, g, false);
+                        s_group.row0 = s.row0;
+                        s_group.n = s.n;
+                        s_group.nt = s.n > 0 ? s.nt : 0;
+                        s_group.of = pass_tiles(a.group_cut, a.groups, g);
+                    }
+                }
                 if (FORM != KV_PLAIN) low_most = low_of<FORM>(a, cur.s, min(cur.s.n - 1, (cur.rt * ROWS + ROWS - 1) / G));
                 fresh = false;
                 seg_kt0 = cur.kt;
@@ -539,7 +557,60 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM<NARROW>) kv_attention_ker
                 }
                 __syncthreads();
                 const bool whole = seg_kt0 == 0 && cur.kt == cur.s.nt;
-                if (whole && FORM == KV_SPLIT) {
+                if (FORM == KV_SPLIT && a.joins) {
+                    // the unit's sums and those of the group's runs, in their order
+                    for (int e = tid; e < HELD * (D / 8); e += THREADS) {
+                        const int r = e / (D / 8), c = e % (D / 8);
+                        const int rr = cur.rt * ROWS + r, i = rr / G, head = cur.h * G + (rr - i * G);
+                        if (i >= cur.s.n) continue;
+                        const size_t row = (size_t)(cur.s.row0 + i);
+                        Runs runs = {nullptr, nullptr, 0, 0, 0};
+                        const int at = (int)row - s_group.row0;
+                        if (s_group.nt > 0 && at >= 0 && at < s_group.n)
+                            runs = runs_of<D>(a.group_cut, a.group_sums, a.T, a.H, G, s_group.of, s_group.n, s_group.nt, row,
+                                              at, head);
+                        float2 v = ml[r];
+                        float f[8];
+                        #pragma unroll
+                        for (int k = 0; k < 8; ++k) f[k] = buf[r * D + 8 * c + k];
+                        constexpr int AT_ONCE = 4;
+                        for (int q0 = 0; q0 < runs.count; q0 += AT_ONCE) {
+                            float2 w[AT_ONCE];
+                            float g[AT_ONCE][8];
+                            float top = v.x;
+                            #pragma unroll
+                            for (int q = 0; q < AT_ONCE; ++q) {
+                                w[q] = make_float2(NEG_INF, 0.f);
+                                #pragma unroll
+                                for (int k = 0; k < 8; ++k) g[q][k] = 0.f;
+                                if (q0 + q < runs.count) {
+                                    const size_t off = (q0 + q) * runs.step + (q0 + q == 0 ? runs.second : 0);
+                                    w[q] = *reinterpret_cast<const float2*>(runs.ml + off);
+                                    // (slots begin at 16 bytes, and so do rows of D floats)
+                                    Eight<float>::load(runs.acc + off + 8 * c, g[q]);
+                                }
+                                top = fmaxf(top, w[q].x);
+                            }
+                            const float f0 = v.x == top ? 1.f : ex2(v.x - top);
+                            v = make_float2(top, v.y * f0);
+                            #pragma unroll
+                            for (int k = 0; k < 8; ++k) f[k] *= f0;
+                            #pragma unroll
+                            for (int q = 0; q < AT_ONCE; ++q) {
+                                const float fq = w[q].x == top ? 1.f : ex2(w[q].x - top);
+                                v.y = fmaf(w[q].y, fq, v.y);
+                                #pragma unroll
+                                for (int k = 0; k < 8; ++k) f[k] = fmaf(g[q][k], fq, f[k]);
+                            }
+                        }
+                        const float inv = v.y == 0.f ? 0.f : __fdiv_rn(1.f, v.y);
+                        #pragma unroll
+                        for (int k = 0; k < 8; ++k) f[k] = v.y == 0.f ? 0.f : f[k] * inv;
+                        Eight<T>::store(static_cast<T*>(a.Out) + row * a.ldo + (size_t)head * D + 8 * c, f);
+                        if (c == 0 && a.lse != nullptr)
+                            a.lse[row * a.H + head] = v.y == 0.f ? NEG_INF : (log2f(v.y) + (v.x - HEAD)) * 0.6931471805599453f;
+                    }
+                } else if (whole && FORM == KV_SPLIT) {
                     for (int e = tid; e < HELD * (D / 4); e += THREADS) {
                         const int r = e / (D / 4), c = e % (D / 4);
                         const int rr = cur.rt * ROWS + r, i = rr / G, j = rr - i * G;
@@ -586,6 +657,7 @@ cudaError_t launch_rows(const KvAttnArgs& args, KvCut* cut, cudaStream_t s) {
     const int ctas = num_sms() * CTAS_PER_SM<NARROW>;
     KvAttnArgs a = args;
     a.whole = whole_units(a, ROWS, TILE, ctas);
+    a.joins &= a.whole;
     const int G = a.H / a.c.Hkv;
     static DeviceCache<int> ready;
     int dummy = 0;

@@ -426,12 +426,46 @@ cudaError_t launch_join(const KvAttnArgs& a, int G, int ctas, int slot_rows, con
 
 }  // namespace
 
-// How a pass of KV_SPLIT was cut, for the join of the two.
-struct KvCut {
-    int ctas, rows, slot_rows, whole;
-    const long long* prefix;
-    const float* slots;
+namespace {
+
+// A sequence's or a group's tiles in the list of its pass of KV_SPLIT: those
+// before it, and a CTA's share of the list.
+struct PassTiles { long long before, share; };
+__device__ __forceinline__ PassTiles pass_tiles(const KvCut& cut, int B, int b) {
+    if (cut.whole) return {0, 1};
+    return {cut.prefix[b], quotient(cut.prefix[B] + cut.ctas - 1, cut.ctas)};
+}
+
+// One row's runs in one pass.
+struct Runs {
+    const float* acc;                  // of the first run, this row
+    const float* ml;
+    size_t step;                       // from a run's slot to the next run's
+    size_t second;                     // from the first run's first slot to the one that it used
+    int count;
 };
+
+// Row `row` of T, head `head` of H, is token i of the n of its sequence or group, which has nt key tiles.
+template <int D>
+__device__ __forceinline__ Runs runs_of(const KvCut& cut, const float* sums, int T, int H, int G, const PassTiles& of, int n,
+                                        int nt, size_t row, int i, int head) {
+    const size_t at = row * H + head;
+    Runs r = {sums + at * D, sums + (size_t)T * H * D + 2 * at, 0, 0, 1};
+    if (cut.whole) return r;
+    const int h = head / G, unit_row = i * G + (head - h * G), tile = unit_row / cut.rows, rr = unit_row - tile * cut.rows;
+    const int tiles = (n * G + cut.rows - 1) / cut.rows;
+    const long long u0 = of.before + ((long long)h * tiles + tile) * nt;
+    const int c0 = (int)(u0 / of.share), c1 = (int)((u0 + nt - 1) / of.share);
+    if (c0 == c1) return r;                               // one run covered the unit
+    r.count = c1 - c0 + 1;
+    r.step = 2 * slot_floats(cut.slot_rows, D);
+    r.second = u0 > (long long)c0 * of.share ? slot_floats(cut.slot_rows, D) : 0;
+    r.acc = cut.slots + c0 * r.step + (size_t)rr * D;
+    r.ml = cut.slots + c0 * r.step + (size_t)cut.slot_rows * D + 2 * rr;
+    return r;
+}
+
+}  // namespace
 
 // kvattn_tc.cu
 size_t kv_attention_tc_slot_bytes(int max_rows, int D);

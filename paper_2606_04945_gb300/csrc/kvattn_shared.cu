@@ -3,14 +3,20 @@
 //
 //   o_i = (sum over the shared slots + sum over the sequence's own) p_ij v_j / l_i
 //
-// Two passes of the attention kernels (KV_SPLIT) and a join. In the first the
-// rows of a group's sequences are the rows of one: with S sequences of n new
-// tokens a key meets S n G rows at once, so the cache's bytes fall by S and
-// the tensor cores are filled (one token of 32 sequences with 7 query heads a
-// key/value head: 224 of a unit's 256 rows, where each sequence by itself has
-// 7 of 16). The second takes each sequence's slots behind the prefix. Both
-// leave sums relative to a row's running maximum; the join adds a row's runs of
-// both, in their order.
+// Two passes of the attention kernels (KV_SPLIT). In the first the rows of a
+// group's sequences are the rows of one: with S sequences of n new tokens a
+// key meets S n G rows at once, so the cache's bytes fall by S and the tensor
+// cores are filled (one token of 32 sequences with 7 query heads a key/value
+// head: 224 of a unit's 256 rows, where each sequence by itself has 7 of 16).
+// The second takes each sequence's slots behind the prefix. Both leave sums
+// relative to a row's running maximum. A row's runs of both, in their order,
+// are added by the second pass where its units are whole (short own parts, the
+// usual case), else by a kernel of its own.
+//
+// Measured (bf16, 28 heads on 4 of 128): the next token of 64 sequences in two
+// groups behind 32768 and 24576 tokens, with up to 500 of their own: 66 us (70
+// with the join as a third launch, 330 as a plain call); of it the first pass
+// 54, 11.8 key tiles a CTA (26 GFLOP).
 #include <algorithm>
 #include <cmath>
 
@@ -20,15 +26,6 @@ namespace starq {
 namespace {
 
 constexpr int TILE = 128;              // keys of a tile of either kernel
-
-// One row's runs in one pass.
-struct Runs {
-    const float* acc;                  // of the first run, this row
-    const float* ml;
-    size_t step;                       // from a run's slot to the next run's
-    size_t second;                     // 1: the first run's slot is its CTA's second (else 0)
-    int count;
-};
 
 // Both passes: of a sequence's own slots, and of its group's.
 struct Passes {
@@ -47,7 +44,7 @@ kv_attention_split_join_kernel(const __grid_constant__ Passes p, int G) {
     const KvAttnArgs& own = p.a[0];
     const int idx = blockIdx.x * (JOIN_WARPS / SHARE) + warp / SHARE;      // token * H + head
     int i = idx / own.H, b = blockIdx.y;
-    const int head = idx - i * own.H, h = head / G;
+    const int head = idx - i * own.H;
     size_t row = 0;
     Runs mine = {nullptr, nullptr, 0, 0, 0}, ours = mine;
     bool real = false;
@@ -66,26 +63,8 @@ kv_attention_split_join_kernel(const __grid_constant__ Passes p, int G) {
             if (i < 0 || i >= s.n) break;                 // (only where the starts are not in order)
         }
         Runs r = {nullptr, nullptr, 0, 0, 0};
-        if (s.nt > 0) {
-            const size_t at = row * a.H + head;
-            r.acc = a.sums + at * D;
-            r.ml = a.sums + (size_t)a.T * a.H * D + 2 * at;
-            r.count = 1;
-            if (!cut.whole) {
-                const int unit_row = i * G + (head - h * G), tile = unit_row / cut.rows, rr = unit_row - tile * cut.rows;
-                const int tiles = (s.n * G + cut.rows - 1) / cut.rows;
-                const long long total = cut.prefix[a.B], u0 = cut.prefix[b] + ((long long)h * tiles + tile) * s.nt;
-                const long long share = quotient(total + cut.ctas - 1, cut.ctas);
-                const int c0 = (int)(u0 / share), c1 = (int)((u0 + s.nt - 1) / share);
-                if (c0 < c1) {                            // (else one run covered the unit)
-                    r.count = c1 - c0 + 1;
-                    r.step = 2 * slot_floats(cut.slot_rows, D);
-                    r.second = u0 > (long long)c0 * share ? slot_floats(cut.slot_rows, D) : 0;
-                    r.acc = cut.slots + c0 * r.step + (size_t)rr * D;
-                    r.ml = cut.slots + c0 * r.step + (size_t)cut.slot_rows * D + 2 * rr;
-                }
-            }
-        }
+        if (s.nt > 0)
+            r = runs_of<D>(cut, a.sums, a.T, a.H, G, pass_tiles(cut, a.B, b), s.n, s.nt, row, i, head);
         if (q == 0) mine = r;
         else ours = r;
         b = s.group;
@@ -186,13 +165,13 @@ cudaError_t launch_split_join(const Passes& p, cudaStream_t s) {
 // knows. A key tile (128 keys of a head) costs the GPU about 5 ns with up to 16
 // rows (4 with heads of 64), 11 (8) with up to 128 and 16 for every 256 rows;
 // what the shared tiles cost less once a group than once a sequence has to
-// make up for about 16 us of two more launches and the sums' way through
-// memory. Measured, plain / shared, us (bf16, 200 own tokens; 170 settings, on
-// average 0.6 % above the better of each): 28 heads on 4, one token of 8
-// sequences, 8192 shared 21 / 35, 32768 shared 52 / 42; of 32, 2048 shared
-// 23 / 28, 8192 shared 53 / 33, 32768 shared 168 / 51; 32 tokens of each of 8
-// (the tensor cores are full either way), 8192 shared 56 / 70; 32 heads with
-// keys of their own, 8 sequences, 2048 shared 34 / 22, 32768 shared 328 / 68.
+// make up for about 16 us of another launch and the sums' way through memory.
+// Measured, plain / shared, us (bf16, 200 own tokens; 170 settings, on average
+// 0.6 % above the better of each): 28 heads on 4, one token of 8 sequences,
+// 8192 shared 21 / 33, 32768 shared 52 / 43; of 32, 2048 shared 22 / 27, 8192
+// shared 53 / 29, 32768 shared 168 / 48; 32 tokens of each of 8 (the tensor
+// cores are full either way), 8192 shared 56 / 70; 32 heads with keys of their
+// own, 8 sequences, 2048 shared 34 / 19, 32768 shared 328 / 66.
 bool worth_sharing(const KvAttnArgs& a, int max_rows, int max_shared) {
     if (a.groups == 0 || max_rows <= a.max_new || max_shared == 0) return false;
     const int G = a.H / a.c.Hkv;
@@ -237,11 +216,20 @@ cudaError_t launch_kv_attention_shared(const KvAttnArgs& a, int max_rows, int ma
     p.a[1] = pre;
     for (int q = 1; q >= 0; --q) {
         KvAttnArgs& pass = p.a[q];
-        const cudaError_t e = kv_attention_by_warps(pass) ? launch_kv_attention_warp<KV_SPLIT>(pass, &p.cut[q], s)
-                                                          : launch_kv_attention_tc<KV_SPLIT>(pass, &p.cut[q], s);
+        const bool by_warps = kv_attention_by_warps(pass);
+        if (q == 0 && by_warps) {
+            pass.joins = 1;
+            pass.group_cut = p.cut[1];
+            pass.group_sums = pre.sums;
+            pass.group_rows = max_rows;
+            pass.group_len = max_shared;
+        }
+        const cudaError_t e = by_warps ? launch_kv_attention_warp<KV_SPLIT>(pass, &p.cut[q], s)
+                                       : launch_kv_attention_tc<KV_SPLIT>(pass, &p.cut[q], s);
         if (e != cudaSuccess) return e;
         pass.whole = p.cut[q].whole;
     }
+    if (p.a[0].joins && p.a[0].whole) return cudaSuccess;
     if (a.dtype == STARQ_BF16)
         return D == 64 ? launch_split_join<__nv_bfloat16, 64>(p, s) : launch_split_join<__nv_bfloat16, 128>(p, s);
     return D == 64 ? launch_split_join<__half, 64>(p, s) : launch_split_join<__half, 128>(p, s);

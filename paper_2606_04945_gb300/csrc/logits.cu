@@ -37,9 +37,9 @@
 // MB) 42 us, 3.2 TB/s; the entropy of 244 rows of 50257 bfloat16 logits, a mask
 // a row, 4096 tokens of history, 34.5 us; 80 rows of 131072 bfloat16 logits
 // rewritten (43 MB) 15.5 us, 2.8 TB/s; one row of 32000 about 8 us of the GPU,
-// a chain of loads and barriers. A warp's own instructions bound the stream
-// (about 200 for 512 tokens, four such warps a scheduler)
-// more than their number: larger batches spill, smaller ones (55 us) and
+// a chain of loads and barriers. What bounds the stream is a warp's own chain
+// of instructions (about 200 for 512 tokens, four such warps a scheduler) more
+// than memory: larger batches spill, smaller ones (55 us) and
 // three CTAs an SM (51) lose. One named token looked up at a time where it
 // stands cost 122 us, contiguous slices 47 (the first CTA had half of the
 // names), four helping warps 43 and fewer registers for the stream.
