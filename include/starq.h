@@ -901,11 +901,9 @@ int kv_cache_attention(const void* Q, int ldq, int dtype, int T, const int32_t* 
  * slots that it would see without a window those with
  *   j > s - window  or  j < sinks
  * (window 1: itself; slots behind s, which a row without `causal` sees too,
- * are never outside). Only blocks with a slot that some row of a sequence's
- * first tokens may see are read, so pages that the window has left for good
- * may be given away: their entries of page_table are not looked up (16 slots
- * at a time; a block of 16 slots that begins outside the first row's window
- * and first slots and ends inside is read).
+ * are never outside). Slots that the windows of all new tokens have left, and
+ * that are not first ones, are not read, 16 at a time: a page with no others
+ * may be given away, and its entry of page_table may be anything.
  *   window >= 1, sinks >= 0; a window of kv_len or more is no window.
  * Other arguments, workspace and result as kv_cache_attention.
  *

@@ -264,9 +264,9 @@ class CachedStack:
         blocks of new tokens; returns [batch][blocks x block]. captured:
         capture()'s result. rules: arguments of abi.LogitsRules (params,
         biases, allowed; the history is the prompt and the answer as fixed in
-        the steps before), confidence: "probability", "margin" or "entropy", by which a step
-        chooses its positions. With either a position for which nothing is allowed stays
-        masked."""
+        the steps before), confidence: "probability", "margin" or "entropy",
+        by which a step chooses its positions. With either, a position for
+        which nothing is allowed stays masked."""
         c = self.cfg
         if prompt.shape[-1] + blocks * c.block > c.capacity:
             raise ValueError(f"prompt and answer are longer than the cache's {c.capacity} tokens")

@@ -379,3 +379,56 @@ def test_shared_graph_and_stream(abi):
             check(pg, q, outs[k], lses[k], [2] * 3, now, 4, torch.float16, see)
         assert torch.equal(outs[1], outs[2])
     abi.check_status()
+
+
+@pytest.mark.parametrize("new", [1, 6, 40])
+def test_rows_behind_the_last_sequence(abi, new):
+    """Rows of Q that no sequence owns stay as they were, in both forms."""
+    rng = np.random.default_rng(new)
+    lens = [200, 190, 210]
+    pg = Shared(abi, rng, [0, 3], [128], lens, 1, 16, 64)
+    T = 3 * new
+    q, _ = randn(rng, (T + 5, 2 * 64), torch.float16)
+    for call in (dict(window=50, sinks=2), dict(group_start=i32([0, 3]), shared_len=i32([128]), max_rows=T, max_shared=APART)):
+        out = torch.full((T + 5, 128), 7.0, dtype=torch.float16, device="cuda")
+        lse = torch.full((T + 5, 2), 7.0, device="cuda")
+        fn = abi.kv_cache_attention_window if "window" in call else abi.kv_cache_attention_shared
+        fn(q, pg.cache, pg.dev_table, i32(lens), starts([new] * 3), out, max_new=new, max_len=210, lse=lse, **call)
+        abi.check_status()
+        assert torch.all(out[T:] == 7.0) and torch.all(lse[T:] == 7.0)
+        see = lambda b: od.window_sees(new, lens[b], call.get("window", 1 << 28), call.get("sinks", 0), False)
+        check(pg, q[:T], out[:T], lse[:T], [new] * 3, lens, 2, torch.float16, see)
+
+
+def test_graphs_without_a_workspace(abi):
+    """Two graphs whose calls make workspaces of their own, replayed in turn
+    and beside eager calls."""
+    rng = np.random.default_rng(11)
+    lens = [1500, 1400, 1300]
+    pg = Shared(abi, rng, [0, 3], [1024], lens, 2, 32, 128)
+    q, _ = randn(rng, (3, 14 * 128), torch.bfloat16)
+    outs = [torch.empty_like(q) for _ in range(4)]
+    args = (q, pg.cache, pg.dev_table, i32(lens), starts([1] * 3))
+    kw = dict(max_new=1, max_len=1500)
+    group = dict(group_start=i32([0, 3]), shared_len=i32([1024]), max_rows=3, max_shared=APART)
+    window = lambda out: abi.kv_cache_attention_window(*args, out, window=700, sinks=1, **kw)
+    shared = lambda out: abi.kv_cache_attention_shared(*args, out, **kw, **group)
+    graphs = []
+    for call, out in ((window, outs[0]), (shared, outs[1])):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call(out)
+    window(outs[2])
+    shared(outs[3])
+    want = [o.clone() for o in outs[2:]]
+    for _ in range(5):
+        for o in outs:
+            o.zero_()
+        graphs[0].replay()
+        window(outs[2])
+        graphs[1].replay()
+        shared(outs[3])
+        graphs[0].replay()
+        for o, w in zip(outs, want + want):
+            assert torch.equal(o, w)
+    abi.check_status()

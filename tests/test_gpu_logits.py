@@ -115,8 +115,8 @@ class Case:
                 m = abs(float(z[r][want]) / t)
                 E = (self.V / 32 + 64) * 2.0 ** -22 + 2.0 ** -21 * (1.4427 * D + 1)
                 top = np.exp(min(0.0, float(z[r][want]) / t - s))     # 1 / l
-                tol = {"probability": E * c, "margin": E * c + 2.0 ** -22 * top,
-                       "entropy": E * (2.9 * D + 2) + 2.0 ** -22 * abs(np.log(top))}[kind]
+                tol = E * c if kind == "probability" else E * c + 2.0 ** -22 * top if kind == "margin" else \
+                    E * (2.9 * D + 2) + 2.0 ** -22 * abs(np.log(top))
                 assert abs(conf[r] - c) <= tol, (kind, r, conf[r], c, tol)
                 assert abs(lse[r] - s) <= E + 2.0 ** -22 * (m + abs(s)), (r, lse[r], s)
         end = self.first[-1]
@@ -296,6 +296,48 @@ def test_a_long_history(abi):
     y = torch.empty_like(c.X)
     abi.logits_apply_rules(c.X, c.start, c.rules(abi), max_new=1, Y=y)
     assert torch.equal(y.cpu(), torch.from_numpy(c.reference()[1]))
+
+
+@pytest.mark.parametrize("kw", [dict(history=300), dict(biases=30), dict(masked=True), dict(history=9000, biases=20),
+                                dict(history=9000, masked=True, by_row=True)])
+def test_a_large_vocabulary(abi, kw):
+    """More tokens than a cluster takes at a time, each rule by itself, more
+    named tokens than a CTA has room for at once."""
+    c = Case(6, torch.bfloat16, 300001, (3,), **kw)
+    z, y = c.reference()
+    c.check_pick(abi, "entropy", z)
+    c.check_pick(abi, "margin", z)
+    out = torch.empty_like(c.X)
+    abi.logits_apply_rules(c.X, c.start, c.rules(abi), max_new=3, Y=out)
+    assert torch.equal(out.cpu(), torch.from_numpy(y).bfloat16())
+
+
+@pytest.mark.parametrize("told", [65535, 65536, 100000])
+def test_counts_beyond_16_bits(abi, told):
+    """One token all along a history, beside its neighbours once."""
+    V = 3000
+    c = Case(7, torch.float32, V, (2, 1), history=told)
+    table = np.full((2, told), 1000, np.int32)
+    table[:, :2] = [999, 1001]
+    lengths = [told, told - 7]
+    c.kw.update(history=i32(table), history_len=i32(lengths))
+    c.history = [table[b, :lengths[b]] for b in range(2)]
+    c.check_pick(abi, "probability")
+    out = torch.empty_like(c.X)
+    abi.logits_apply_rules(c.X, c.start, c.rules(abi), max_new=2, Y=out)
+    assert torch.equal(out.cpu(), torch.from_numpy(c.reference()[1]))
+
+
+def test_empty_tables(abi):
+    """Histories and lists without room for an entry."""
+    c = Case(8, torch.float32, 700, (2,))
+    none = lambda *shape, dtype=torch.int32: torch.zeros(*shape, dtype=dtype, device="cuda")
+    c.kw.update(history=none(1, 0), history_len=none(1), bias_ids=none(1, 0), bias_values=none(1, 0, dtype=torch.float32),
+                bias_len=none(1))
+    c.check_pick(abi, "margin")
+    one = none(1, 8)
+    c.kw.update(history=one, bias_ids=one, bias_values=none(1, 8, dtype=torch.float32))        # room, but no entries
+    c.check_pick(abi, "entropy")
 
 
 def test_graph_and_stream(abi):
