@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
     // row the bits of the tokens that the stream may take
     extern __shared__ __align__(16) uint32_t tables[];
     __shared__ Best s_item[ROWS][STREAM + CHUNKS], s_row[ROWS][MAX_CLUSTER];
-    __shared__ int s_sum[HELP], s_next, s_names;
+    __shared__ int s_sum[HELP], s_next[2], s_names;          // s_next: the next unit, of this time and of the time after
     const int places = cut.blocks * BLOCK, words = places / 32;
     const int narrow = a.r.history_ld < 65536;               // 1: two counts a word
     uint32_t* const token_of = tables;
@@ -369,9 +369,10 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
     const bool t_ok = temperature >= 1e-30f && temperature <= 1e30f, r_ok = repetition >= 1e-30f && repetition <= 1e30f;
     if (PICK)
         for (int i = tid; i < ROWS * (STREAM + CHUNKS); i += THREADS) s_item[0][i] = nothing<KIND>();
+    if (tid < 2) s_next[tid] = 0;
     float warm = 0.f, kk = 0.f;
 
-    for (; done < mine; done += cut.blocks) {
+    for (int time = 0; done < mine; done += cut.blocks, time ^= 1) {
         blocks = min(cut.blocks, mine - done);
         Batch q[BUFFERS];
         Place at{nullptr, nullptr, (streams ? warp : items) - STREAM, 0, 0, blocks};
@@ -390,7 +391,7 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
             kk = warm * LOG2E;
         }
         __syncthreads();                                     // the tables of the blocks before are done with
-        if (tid == 0) { s_next = 0; s_names = 0; }
+        if (tid == 0) s_next[time ^ 1] = 0;                  // (counted up again behind the next such barrier)
         // a token's place among the blocks at hand, -1 if it is not there
         auto place_of = [&](int v) {
             const int blk = v / BLOCK, j = PICK ? blk >> cut.cluster_log : blk / cut.cluster;
@@ -582,7 +583,7 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
         const int chunks = (names + 2 * E * (blocks - edge0) + CHUNK - 1) / CHUNK;
         for (;;) {
             int i = 0;
-            if (lane == 0) i = atomicAdd(&s_next, 1);
+            if (lane == 0) i = atomicAdd(&s_next[time], 1);
             i = __shfl_sync(0xffffffffu, i, 0);
             if (i >= rows * chunks) break;
             const int r = i / chunks, chunk = i - r * chunks;

@@ -369,3 +369,23 @@ def test_graph_and_stream(abi):
     z = c.reference()[0]
     assert out[0].tolist() == [ol.pick(z[r], 1.0, "margin")[0] for r in range(8)]
     abi.check_status()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,lead", [(1021, 1), (20011, 3), (40000, 0)])
+def test_plain_calls_among_ruled_ones(abi, dtype, V, lead):
+    """A row without rules whose largest logit is one of the vocabulary's edge tokens, which are taken up last: the
+    result does not depend on what the kernel before left in shared memory or on which warp comes first."""
+    x = np.random.default_rng(V).standard_normal((12, V)).astype(np.float32)
+    x[::2, V - 1], x[1::2, 0] = 20, 20
+    plain = Case(1, dtype, V, [8, 4], params=False, lead=lead, logits=x)
+    ruled = Case(2, dtype, V, [8, 4], history=40, biases=5, masked=True)
+    first = None
+    for k in range(20):
+        ruled.check_pick(abi, "margin")
+        token, conf = torch.empty(12, dtype=torch.int32, device="cuda"), torch.empty(12, device="cuda")
+        abi.logits_pick(plain.X, plain.start, None, token, conf, max_new=8, kind="margin")
+        assert token.tolist() == [V - 1, 0] * 6
+        first = conf if first is None else first
+        assert torch.equal(conf, first)
+    plain.check_pick(abi, "margin")
