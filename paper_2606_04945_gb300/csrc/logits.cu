@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
     constexpr bool PICK = KIND != APPLY;
     constexpr uint32_t FULL = (1u << E) - 1;
     constexpr uint32_t COUNTED = 1u << 29, LISTED = 1u << 30, NONE = 1u << 31;
-    static_assert(BLOCK == 32 * BATCH, "a block is a batch");
+    static_assert(BLOCK == 32 * BATCH && BUFFERS >= 2, "a block is a batch; one is loaded while one is worked on");
     // by number: the named tokens (their places among the CTA's blocks, and which rules name them), penalties, list
     // entries that become biases [room]; by place: counts, the named tokens' bits, the numbers before a word; for each
     // row the bits of the tokens that the stream may take
@@ -333,37 +333,47 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
 
     // A warp's batches: the blocks of its rows or parts of them, one after the other.
     struct Place {
-        const T* x; T* y;                                    // the row's first piece of block 0
-        int item, row, lead, j;
+        const T* x;                                          // the row's first piece
+        int item, row, lead, j, v0, pieces;                  // block j, its first token and its pieces
     };
-    auto settle = [&](Place& p) {                            // the next block that has pieces, from p's on
+    auto enter = [&](Place& p) {                             // the item's first block
+        if (p.item >= items) return;
+        p.row = p.item >> cut.parts_log;
+        p.j = p.item & (cut.parts - 1);
+        const Row t = row_of(p.row);
+        p.lead = t.lead;
+        p.x = t.x + t.lead;
+        p.v0 = token0(p.j);
+    };
+    auto seek = [&](Place& p) {                              // the next block that has pieces, from p's on
         while (p.item < items) {
-            if (p.j < blocks && pieces_of(p.j, p.lead) > 0) return;
-            if (p.j < blocks) { p.j += cut.parts; continue; }
-            p.item += STREAM;
-            p.j = p.item & (cut.parts - 1);
-            p.row = p.item >> cut.parts_log;
-            if (p.item < items) {
-                const Row t = row_of(p.row);
-                p.x = t.x + t.lead;
-                p.y = PICK ? nullptr : t.y + t.lead;
-                p.lead = t.lead;
+            if (p.j < blocks) {
+                p.pieces = min(BLOCK - p.lead, max(0, a.V - p.v0 - p.lead)) / E;
+                if (p.pieces > 0) return;
             }
+            p.item += STREAM;
+            enter(p);
         }
     };
-    struct Batch { uint4 w[U]; };
+    struct Batch {
+        uint4 w[U];
+        int row, lead, j, v0, pieces, last;                  // row < 0: none; last: of the item
+    };
     // Pieces 32 u + lane of a block; what is behind the last one is read as the last one and not used.
     auto load = [&](Place& p, Batch& q) {
+        q.row = -1;
         if (p.item >= items) return;
-        const T* const x = p.x + token0(p.j);
-        const int last = pieces_of(p.j, p.lead) - 1;
+        q.row = p.row; q.lead = p.lead; q.j = p.j; q.v0 = p.v0; q.pieces = p.pieces;
         #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint4* from = reinterpret_cast<const uint4*>(x) + min(32 * u + lane, last);
+            const uint4* from = reinterpret_cast<const uint4*>(p.x + p.v0) + min(32 * u + lane, p.pieces - 1);
             q.w[u] = PICK ? __ldcs(from) : *from;
         }
+        const int item = p.item;
         p.j += cut.parts;
-        settle(p);
+        p.v0 += cut.parts * cut.cluster * BLOCK;
+        seek(p);
+        q.last = p.item != item;
     };
 
     const bool t_ok = temperature >= 1e-30f && temperature <= 1e30f, r_ok = repetition >= 1e-30f && repetition <= 1e30f;
@@ -375,9 +385,9 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
     for (int time = 0; done < mine; done += cut.blocks, time ^= 1) {
         blocks = min(cut.blocks, mine - done);
         Batch q[BUFFERS];
-        Place at{nullptr, nullptr, (streams ? warp : items) - STREAM, 0, 0, blocks};
-        settle(at);
-        Place next = at;
+        Place next{nullptr, streams ? warp : items, 0, 0, 0, 0, 0};
+        enter(next);
+        seek(next);
         #pragma unroll
         for (int k = 0; k < BUFFERS - 1; ++k) load(next, q[k]);           // on their way beside the tables
         if (done == 0) {
@@ -443,8 +453,7 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
         }
 
         Best best = nothing<KIND>();
-        auto work = [&](const Place& p, const Batch& q) {
-            const int pieces = pieces_of(p.j, p.lead), v0 = token0(p.j);
+        auto work = [&](const Batch& q) {
             float z[BATCH];
             uint32_t good[U];
             #pragma unroll
@@ -452,13 +461,13 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
                 const int k0 = (32 * u + lane) * E;          // the piece's first token behind the lead
                 float f[E];
                 open_as<T>(q.w[u], f);
-                good[u] = 32 * u + lane < pieces ? FULL : 0u;
-                if (bits) good[u] &= free_bits[(one ? 0 : p.row * words) + p.j * BLOCK_WORDS + (k0 >> 5)] >> (k0 & 31);
+                good[u] = 32 * u + lane < q.pieces ? FULL : 0u;
+                if (bits) good[u] &= free_bits[(one ? 0 : q.row * words) + q.j * BLOCK_WORDS + (k0 >> 5)] >> (k0 & 31);
                 #pragma unroll
                 for (int k = 0; k < E; ++k) z[u * E + k] = good[u] >> k & 1 ? f[k] : NEG_INF;
             }
             if constexpr (!PICK) {
-                T* const y = p.y + v0;
+                T* const y = static_cast<T*>(a.Y) + ((size_t)row0 + first + q.row) * a.ldy + (q.lead + q.v0);
                 const bool wide = reinterpret_cast<uintptr_t>(y) % 16 == 0;
                 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -466,9 +475,9 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
                     T o[E];
                     #pragma unroll
                     for (int k = 0; k < E; ++k) o[k] = (T)(__fmul_rn(z[u * E + k], warm));
-                    if (32 * u + lane >= pieces) continue;
+                    if (32 * u + lane >= q.pieces) continue;
                     uint32_t others = FULL;                   // tokens that are not named
-                    const int e = p.j * BLOCK + p.lead + k0;
+                    const int e = q.j * BLOCK + q.lead + k0;
                     if (TABLES && good[u] != FULL) others &= ~__funnelshift_r(named[e >> 5], named[(e >> 5) + 1], e);
                     if (wide && others == FULL) {
                         uint4 v;
@@ -484,7 +493,7 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
                 const float top = largest(z);
                 if (__any_sync(0xffffffffu, !(top <= (MARGIN<KIND> ? best.s : best.m))))
                     move_best<KIND>(best, z, top, [&](int k) {
-                        return v0 + p.lead + (32 * (k / E) + lane) * E + k % E;
+                        return q.v0 + q.lead + (32 * (k / E) + lane) * E + k % E;
                     }, kk);
                 add_weights<KIND, BATCH>(best, z, kk);
             }
@@ -503,16 +512,14 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
             best = nothing<KIND>();
         };
         #pragma unroll 1
-        while (at.item < items) {
+        while (q[0].row >= 0) {
             #pragma unroll
             for (int k = 0; k < BUFFERS; ++k) {
                 load(next, q[(k + BUFFERS - 1) % BUFFERS]);
-                work(at, q[k]);
-                const int row = at.row, item = at.item;
-                at.j += cut.parts;
-                settle(at);
-                if (PICK && at.item != item) finish(s_item[row][warp]);
-                if (at.item >= items) break;
+                if (q[k].row < 0) break;                     // (then so is q[0], or it has been worked on)
+                work(q[k]);
+                if (PICK && q[k].last) finish(s_item[q[k].row][warp]);
+                q[k].row = -1;
             }
         }
 
