@@ -34,15 +34,16 @@
 //
 // Measured (one call after the other): the margin of 256 rows of 131072
 // float32 logits (8 sequences with a mask and 1500 tokens of history each, 134
-// MB) 42 us, 3.2 TB/s; the entropy of 244 rows of 50257 bfloat16 logits, a mask
-// a row, 4096 tokens of history, 34.5 us; 80 rows of 131072 bfloat16 logits
+// MB) 39.3 us, 3.4 TB/s; the entropy of 244 rows of 50257 bfloat16 logits, a mask
+// a row, 4096 tokens of history, 33.7 us; 80 rows of 131072 bfloat16 logits
 // rewritten (43 MB) 15.5 us, 2.8 TB/s; one row of 32000 about 8 us of the GPU,
 // a chain of loads and barriers. What bounds the stream is a warp's own chain
 // of instructions (about 200 for 512 tokens, four such warps a scheduler) more
 // than memory: larger batches spill, smaller ones (55 us) and
 // three CTAs an SM (51) lose. One named token looked up at a time where it
 // stands cost 122 us, contiguous slices 47 (the first CTA had half of the
-// names), four helping warps 43 and fewer registers for the stream.
+// names), four helping warps 43 and fewer registers for the stream, a second
+// walk over the blocks for the work beside that for the loads 42.
 #include <algorithm>
 
 #include "logits.cuh"
