@@ -75,7 +75,6 @@ enum { APPLY = -1 };                   // else a starq_confidence
 struct Cut {
     int rows;                          // of a CTA
     int groups;                        // CTAs' row groups of a sequence
-    int parts, parts_log;              // of a row's blocks: 1, 2, 4 or 8
     int cluster, cluster_log;          // CTAs that share the blocks (the logarithm: of a power of two)
     int blocks;                        // of a CTA at a time
     int room;                          // named tokens among them at most
@@ -301,7 +300,7 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
     }
     if (first >= n) return;
     if (PICK && cut.cluster > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
-    const int rows = min(cut.rows, n - first), items = rows << cut.parts_log;
+    const int rows = min(cut.rows, n - first);
 
     // A row: where it is, and the tokens of each block before its 16-byte pieces (the first block's are at 16 bytes
     // where the others' are, too). The tokens before and behind the pieces are the blocks' edges.
@@ -332,49 +331,47 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
     const bool bits = TABLES || a.r.allowed != nullptr, even = (size_t)a.ldx * sizeof(T) % 16 == 0;
     const bool one = !(a.r.allowed != nullptr && a.r.allowed_by_row) && even;
 
-    // A warp's batches: the blocks of its rows or parts of them, one after the other.
+    // A warp's batches: of all rows' blocks, row by row, its eighth.
     struct Place {
         const T* x;                                          // the row's first piece
-        int item, row, lead, j, v0, pieces;                  // block j, its first token and its pieces
+        int row, lead, j, v0, pieces, left;                  // block j, its first token and its pieces; batches from it on
     };
-    auto enter = [&](Place& p) {                             // the item's first block
-        if (p.item >= items) return;
-        p.row = p.item >> cut.parts_log;
-        p.j = p.item & (cut.parts - 1);
+    auto enter = [&](Place& p) {
         const Row t = row_of(p.row);
         p.lead = t.lead;
         p.x = t.x + t.lead;
         p.v0 = token0(p.j);
     };
     auto seek = [&](Place& p) {                              // the next block that has pieces, from p's on
-        while (p.item < items) {
-            if (p.j < blocks) {
-                p.pieces = min(BLOCK - p.lead, max(0, a.V - p.v0 - p.lead)) / E;
-                if (p.pieces > 0) return;
+        for (; p.left > 0; --p.left, ++p.j, p.v0 += cut.cluster * BLOCK) {
+            if (p.j == blocks) {
+                p.j = 0;
+                ++p.row;
+                enter(p);
             }
-            p.item += STREAM;
-            enter(p);
+            p.pieces = min(BLOCK - p.lead, max(0, a.V - p.v0 - p.lead)) / E;
+            if (p.pieces > 0) return;
         }
     };
     struct Batch {
         uint4 w[U];
-        int row, lead, j, v0, pieces, last;                  // row < 0: none; last: of the item
+        int row, lead, j, v0, pieces, last;                  // row < 0: none; last: the warp's last of the row
     };
     // Pieces 32 u + lane of a block; what is behind the last one is read as the last one and not used.
     auto load = [&](Place& p, Batch& q) {
         q.row = -1;
-        if (p.item >= items) return;
+        if (p.left <= 0) return;
         q.row = p.row; q.lead = p.lead; q.j = p.j; q.v0 = p.v0; q.pieces = p.pieces;
         #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint4* from = reinterpret_cast<const uint4*>(p.x + p.v0) + min(32 * u + lane, p.pieces - 1);
             q.w[u] = PICK ? __ldcs(from) : *from;
         }
-        const int item = p.item;
-        p.j += cut.parts;
-        p.v0 += cut.parts * cut.cluster * BLOCK;
+        ++p.j;
+        p.v0 += cut.cluster * BLOCK;
+        --p.left;
         seek(p);
-        q.last = p.item != item;
+        q.last = p.left <= 0 || p.row != q.row;
     };
 
     const bool t_ok = temperature >= 1e-30f && temperature <= 1e30f, r_ok = repetition >= 1e-30f && repetition <= 1e30f;
@@ -386,9 +383,16 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
     for (int time = 0; done < mine; done += cut.blocks, time ^= 1) {
         blocks = min(cut.blocks, mine - done);
         Batch q[BUFFERS];
-        Place next{nullptr, streams ? warp : items, 0, 0, 0, 0, 0};
-        enter(next);
-        seek(next);
+        Place next;
+        next.left = 0;
+        if (streams) {
+            const int from = rows * blocks * warp / STREAM;
+            next.left = rows * blocks * (warp + 1) / STREAM - from;
+            next.row = min(from / blocks, rows - 1);
+            next.j = from - next.row * blocks;
+            enter(next);
+            seek(next);
+        }
         #pragma unroll
         for (int k = 0; k < BUFFERS - 1; ++k) load(next, q[k]);           // on their way beside the tables
         if (done == 0) {
@@ -693,8 +697,6 @@ cudaError_t launch_kernel(const LogitsArgs& a, cudaStream_t s) {
     Cut c;
     c.groups = (a.max_new + ROWS - 1) / ROWS;
     c.rows = (a.max_new + c.groups - 1) / c.groups;
-    c.parts_log = c.rows % 8 == 0 ? 0 : c.rows % 4 == 0 ? 1 : c.rows % 2 == 0 ? 2 : 3;      // every warp has as many
-    c.parts = 1 << c.parts_log;
     const long long units = (long long)a.B * c.groups, target = 2ll * num_sms();
     const int blocks = (a.V + BLOCK - 1) / BLOCK;
     const long long most = std::max<long long>(1, ((long long)blocks * c.rows + STREAM - 1) / STREAM);
@@ -706,10 +708,17 @@ cudaError_t launch_kernel(const LogitsArgs& a, cudaStream_t s) {
             c.cluster = 2 << c.cluster_log++;
     const long long names = TABLES ? (long long)a.r.history_ld + a.r.bias_ld : 0;
     const int longest = (names > NAMED ? NAMED : SLICE) / BLOCK, each = (blocks + c.cluster - 1) / c.cluster;
+    // Fewer rows a CTA where the GPU takes more CTAs.
+    const long long groups = std::min(target / ((long long)a.B * c.cluster), (long long)a.max_new * each / STREAM);
+    if (groups > c.groups) {
+        c.rows = (int)((a.max_new + groups - 1) / groups);
+        c.groups = (a.max_new + c.rows - 1) / c.rows;
+    }
     const int rounds = (each + longest - 1) / longest;
     c.blocks = (each + rounds - 1) / rounds;
     c.room = (int)std::min<long long>(c.blocks * BLOCK, (names + 3) / 4 * 4);
-    if (units * c.cluster >= (1ll << 31)) return cudaErrorInvalidValue;
+    const long long ctas = (long long)a.B * c.groups * c.cluster;
+    if (ctas >= (1ll << 31)) return cudaErrorInvalidValue;
     const int words = c.blocks * BLOCK / 32;
     size_t smem = 0;
     if (TABLES || a.r.allowed != nullptr) smem = (size_t)c.rows * words * 4;
@@ -723,7 +732,7 @@ cudaError_t launch_kernel(const LogitsArgs& a, cudaStream_t s) {
     });
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(units * c.cluster));
+    cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
