@@ -54,9 +54,9 @@ namespace {
 constexpr int STREAM = 8, HELP = 2;    // warps
 constexpr int WARPS = STREAM + HELP, THREADS = 32 * WARPS;
 // Tokens of a thread that are worked on together (a chain of dependent
-// operations a batch: four batches of 4 took 640 cycles each), and 16-byte
-// loads on their way beside them.
-constexpr int BATCH = 16, FLIGHT = 4;
+// operations a batch: four batches of 4 took 640 cycles each); the next such
+// batch is on its way meanwhile.
+constexpr int BATCH = 16;
 constexpr int BLOCK = 32 * BATCH;      // tokens that are dealt together: a batch of a warp
 constexpr int BLOCK_WORDS = BLOCK / 32;
 constexpr int SLICE = 16384;           // most tokens of a CTA's blocks at a time
@@ -64,6 +64,7 @@ constexpr int NAMED = 8192;            // named tokens that a CTA has room for (
 constexpr int MAX_CLUSTER = 8;
 constexpr int ROWS = 8;                // rows of a CTA
 constexpr int AHEAD = 4;               // tokens of the history that a thread asks for at once
+constexpr int WORDS = 4;               // words of a mask that a thread asks for at once
 constexpr int NAMES = 4;               // named tokens of a thread on their way
 constexpr int CHUNK = 32 * NAMES, CHUNKS = (NAMED + SLICE / BLOCK * 16) / CHUNK;   // of named tokens and blocks' edges
 constexpr float NEG_INF = -__builtin_huge_valf();
@@ -250,7 +251,7 @@ template <typename T> __device__ __forceinline__ void open_as(const uint4& w, fl
 
 template <typename T, int KIND, bool TABLES>
 __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, const Cut cut) {
-    constexpr int E = SE<T>, U = BATCH / E, BUFFERS = FLIGHT / U + 1;
+    constexpr int E = SE<T>, U = BATCH / E, BUFFERS = 2, TURNS = sizeof(T) == 4 ? 2 : 1;
     constexpr bool PICK = KIND != APPLY;
     constexpr uint32_t FULL = (1u << E) - 1;
     constexpr uint32_t COUNTED = 1u << 29, LISTED = 1u << 30, NONE = 1u << 31;
@@ -431,27 +432,45 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
             #pragma unroll
             for (int k = 0; k < AHEAD; ++k)
                 if (tid + k * THREADS < told) name(told0[k], true);
-            #pragma unroll 4
-            for (int i = tid + AHEAD * THREADS; i < told; i += THREADS) name(__ldg(history + i), true);
+            for (int i = tid + AHEAD * THREADS; i < told; i += AHEAD * THREADS) {
+                int v[AHEAD];
+                #pragma unroll
+                for (int k = 0; k < AHEAD; ++k) v[k] = __ldg(history + min(i + k * THREADS, told - 1));
+                #pragma unroll
+                for (int k = 0; k < AHEAD; ++k)
+                    if (i + k * THREADS < told) name(v[k], true);
+            }
             if (tid < entries) name(listed0, false);
             for (int i = tid + THREADS; i < entries; i += THREADS) name(__ldg(ids + i), false);
             __syncthreads();
         }
         if (bits) {                                          // bit i of a block: token lead + i is allowed and not named
             const int last = (a.V - 1) / 32;
-            for (int r = one ? 0 : warp; r < (one ? 1 : rows); r += WARPS) {
+            const int all = one ? 1 : rows, r = warp % all, parts = WARPS / all, upto = BLOCK_WORDS * blocks;
+            if (warp / all < parts) {                        // a row's words by as many warps as there are for it
                 const Row t = row_of(r);
-                #pragma unroll 4
-                for (int k = one ? tid : lane; k < BLOCK_WORDS * blocks; k += one ? THREADS : 32) {
-                    const int e = t.lead + 32 * (k % BLOCK_WORDS), w = token0(k / BLOCK_WORDS) / 32 + (e >> 5);
-                    uint32_t free = ~0u;
-                    if (t.mask != nullptr)
-                        free = __funnelshift_r(__ldg(t.mask + min(w, last)), __ldg(t.mask + min(w + 1, last)), e);
-                    if (TABLES) {
-                        const uint32_t* of = named + k / BLOCK_WORDS * BLOCK_WORDS + (e >> 5);
-                        free &= ~__funnelshift_r(of[0], of[1], e);
+                const int step = 32 * parts;
+                for (int k0 = warp / all * 32 + lane; k0 < upto; k0 += WORDS * step) {
+                    uint32_t free[WORDS];
+                    #pragma unroll
+                    for (int i = 0; i < WORDS; ++i) {
+                        const int k = min(k0 + i * step, upto - 1), e = t.lead + 32 * (k % BLOCK_WORDS);
+                        const int w = token0(k / BLOCK_WORDS) / 32 + (e >> 5);
+                        free[i] = ~0u;
+                        if (t.mask != nullptr)
+                            free[i] = __funnelshift_r(__ldg(t.mask + min(w, last)), __ldg(t.mask + min(w + 1, last)), e);
                     }
-                    free_bits[r * words + k] = free;
+                    #pragma unroll
+                    for (int i = 0; i < WORDS; ++i) {
+                        const int k = k0 + i * step;
+                        if (k >= upto) break;
+                        if (TABLES) {
+                            const int e = t.lead + 32 * (k % BLOCK_WORDS);
+                            const uint32_t* of = named + k / BLOCK_WORDS * BLOCK_WORDS + (e >> 5);
+                            free[i] &= ~__funnelshift_r(of[0], of[1], e);
+                        }
+                        free_bits[r * words + k] = free[i];
+                    }
                 }
             }
             __syncthreads();
@@ -516,16 +535,20 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
             }
             best = nothing<KIND>();
         };
+        // (The loop's body is there once for 16-bit types, whose next batch is 8 registers to move: 244 rows' entropy 28.5
+        // us, 29 with two bodies and 33 with three and two batches on their way, whose instructions come from further
+        // away. For float32, two bodies: 256 rows' margins 40 us, 46.6 with one.)
         #pragma unroll 1
         while (q[0].row >= 0) {
             #pragma unroll
-            for (int k = 0; k < BUFFERS; ++k) {
-                load(next, q[(k + BUFFERS - 1) % BUFFERS]);
-                if (q[k].row < 0) break;                     // (then so is q[0], or it has been worked on)
+            for (int k = 0; k < TURNS; ++k) {
+                load(next, q[k ^ 1]);
+                if (q[k].row < 0) break;
                 work(q[k]);
                 if (PICK && q[k].last) finish(s_item[q[k].row][warp]);
                 q[k].row = -1;
             }
+            if (TURNS == 1) q[0] = q[1];
         }
 
         // --- the other warps: the list of the named tokens --------------------------------
