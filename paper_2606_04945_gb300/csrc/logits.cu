@@ -64,7 +64,7 @@ constexpr int NAMED = 8192;            // named tokens that a CTA has room for (
 constexpr int MAX_CLUSTER = 8;
 constexpr int ROWS = 8;                // rows of a CTA
 constexpr int AHEAD = 4;               // tokens of the history that a thread asks for at once
-constexpr int WORDS = 4;               // words of a mask that a thread asks for at once
+constexpr int WORDS = 2;               // words of a mask that a thread asks for at once
 constexpr int NAMES = 4;               // named tokens of a thread on their way
 constexpr int CHUNK = 32 * NAMES, CHUNKS = (NAMED + SLICE / BLOCK * 16) / CHUNK;   // of named tokens and blocks' edges
 constexpr float NEG_INF = -__builtin_huge_valf();
@@ -251,11 +251,11 @@ template <typename T> __device__ __forceinline__ void open_as(const uint4& w, fl
 
 template <typename T, int KIND, bool TABLES>
 __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, const Cut cut) {
-    constexpr int E = SE<T>, U = BATCH / E, BUFFERS = 2, TURNS = sizeof(T) == 4 ? 2 : 1;
+    constexpr int E = SE<T>, U = BATCH / E, TURNS = sizeof(T) == 4 ? 2 : 1;
     constexpr bool PICK = KIND != APPLY;
     constexpr uint32_t FULL = (1u << E) - 1;
     constexpr uint32_t COUNTED = 1u << 29, LISTED = 1u << 30, NONE = 1u << 31;
-    static_assert(BLOCK == 32 * BATCH && BUFFERS >= 2, "a block is a batch; one is loaded while one is worked on");
+    static_assert(BLOCK == 32 * BATCH, "a block is a batch");
     // by number: the named tokens (their places among the CTA's blocks, and which rules name them), penalties, list
     // entries that become biases [room]; by place: counts, the named tokens' bits, the numbers before a word; for each
     // row the bits of the tokens that the stream may take
@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
 
     for (int time = 0; done < mine; done += cut.blocks, time ^= 1) {
         blocks = min(cut.blocks, mine - done);
-        Batch q[BUFFERS];
+        Batch q[2];                                          // one is on its way while one is worked on
         Place next;
         next.left = 0;
         if (streams) {
@@ -394,8 +394,7 @@ __global__ void __launch_bounds__(THREADS, 2) logits_kernel(const LogitsArgs a, 
             enter(next);
             seek(next);
         }
-        #pragma unroll
-        for (int k = 0; k < BUFFERS - 1; ++k) load(next, q[k]);           // on their way beside the tables
+        load(next, q[0]);                                    // beside the tables
         if (done == 0) {
             const bool odd = !(t_ok && r_ok) || told < 0 || told > a.r.history_ld || entries < 0 || entries > a.r.bias_ld;
             if (!t_ok) temperature = 1.f;
