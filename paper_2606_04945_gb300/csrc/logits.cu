@@ -26,24 +26,27 @@
 // number the bits and list the named tokens with their penalties and biases,
 // and take them one a lane, which the eight join when the stream has ended.
 // (Looked up in the stream itself, a warp met a named token in most of its
-// pieces and spent most of its time on them; before the stream, it stood still
-// for as long.) A CTA takes up to eight rows of a sequence, which share the
-// tables; a warp takes a row or parts of it, its maximum is one number for all
-// lanes and moves only when a batch of tokens passes it. The cluster's first
-// CTA joins the results, in their order.
+// pieces and spent most of its time on them; before the stream, it stood
+// still for as long.) A CTA takes up to eight rows of a sequence, which share
+// the tables; the eight warps take equal runs of these rows' blocks, a warp's
+// maximum is one number for all lanes and moves only when a batch of tokens
+// passes it. The cluster's first CTA joins the results, in their order.
 //
 // Measured (one call after the other): the margin of 256 rows of 131072
-// float32 logits (8 sequences with a mask and 1500 tokens of history each, 134
-// MB) 39.3 us, 3.4 TB/s; the entropy of 244 rows of 50257 bfloat16 logits, a mask
-// a row, 4096 tokens of history, 33.7 us; 80 rows of 131072 bfloat16 logits
-// rewritten (43 MB) 15.5 us, 2.8 TB/s; one row of 32000 about 8 us of the GPU,
-// a chain of loads and barriers. What bounds the stream is a warp's own chain
-// of instructions (about 200 for 512 tokens, four such warps a scheduler) more
-// than memory: larger batches spill, smaller ones (55 us) and
+// float32 logits (8 sequences with a mask and 1500 tokens of history each,
+// 134 MB) 39.1 us, 3.4 TB/s; the entropy of 244 rows of 50257 bfloat16
+// logits, a mask a row, 4096 tokens of history, 28.7 us; 80 rows of 131072
+// bfloat16 logits rewritten (43 MB) 13.7 us, 3.1 TB/s; one row of 32000 about
+// 8 us of the GPU, a chain of loads and barriers. What bounds the stream is a
+// warp's own chain of instructions (for 512 tokens, four such warps a
+// scheduler) more than memory: larger batches spill, smaller ones (55 us) and
 // three CTAs an SM (51) lose. One named token looked up at a time where it
 // stands cost 122 us, contiguous slices 47 (the first CTA had half of the
 // names), four helping warps 43 and fewer registers for the stream, a second
-// walk over the blocks for the work beside that for the loads 42.
+// walk over the blocks for the work beside that for the loads 42. Blocks that
+// begin at each row's own 16 bytes, with fewer edges, cost a lookup more a
+// named token: the entropy 27.7 us, the rest 0.3 to 0.5 us more; clusters of
+// four CTAs 47.6 us for the margins.
 #include <algorithm>
 
 #include "logits.cuh"
